@@ -52,7 +52,9 @@ extern "C" {
 #define FOCUS_MAX_BLOCK 64
 
 enum { FOCUS_OK = 0, FOCUS_EINVAL = -1, FOCUS_ENOMEM = -2, FOCUS_EHIP = -3 };
-enum { FOCUS_F32 = 0, FOCUS_BF16 = 1 };
+enum { FOCUS_F32 = 0, FOCUS_BF16 = 1,
+       FOCUS_MX4 = 2 };     /* microscaled 4-bit floats (see focus_mx): an operand type of the products, not of a model */
+enum { FOCUS_SCORE_SOFTMAX = 0, FOCUS_SCORE_SIGMOID = 1 };
 enum { FOCUS_BUDGET_TOPK = 0, FOCUS_BUDGET_RATIO = 1, FOCUS_BUDGET_DYNAMIC = 2, FOCUS_BUDGET_OVERRIDE = 3 };
 enum { FOCUS_KEEP_AR_CONTEXT = 1, FOCUS_KEEP_PLACEHOLDERS = 2 };
 enum { FOCUS_SELECT_TOP = 0, FOCUS_SELECT_RANDOM = 1, FOCUS_SELECT_BOTTOM = 2 };
@@ -309,6 +311,106 @@ int focus_get_kernel_time(focus_ctx *ctx, int32_t kernel_class, float *total_ms,
 int focus_free(focus_ctx *ctx);
 /* Infrastructure.  Text of the last error of ctx, or of the last failed call without a context when ctx is NULL. */
 const char *focus_last_error(const focus_ctx *ctx);
+
+/* ---------------------------------------------------------------------------------------------------------------------
+ * Expert routing and microscaled 4-bit weights.
+ *
+ * The entries with a stream and no context need none: they enqueue on the stream of the current device, allocate nothing, keep nothing
+ * between calls, never synchronise and may be captured; calls may overlap if their outputs and workspaces do not.  The same call on the
+ * same inputs gives the same bits.  Errors are reported through focus_last_error(NULL), which is kept per host thread.  Operands must not
+ * overlap outputs. */
+
+/* A router: how a row's E logits l become k experts and their mixing weights.
+ *   score   s_e = softmax(l)_e over all E, or 1 / (1 + exp(-l_e))
+ *   choice  c_e = s_e + bias_e (the bias balances the load; it takes part in the choice only)
+ *   groups  the experts are n_groups runs of E / n_groups neighbours; a group is worth the sum of its group_top largest choices, and only
+ *           the groups_kept groups worth most can be chosen from (ties: lower group)
+ *   picks   the k largest choices left, in descending order (ties: lower expert)
+ *   weight  route_scale * s_e, with renormalize divided by the sum of the k scores (0 if that sum is 0)
+ * Scores are compared as exactly as 64-bit arithmetic gives them.  A logit that is not a number has score 0 and is chosen last, as is
+ * an expert whose bias is not a number; -inf has score 0; with softmax, +inf logits share the whole score. */
+typedef struct focus_router {
+  int32_t n_experts;          /* E, 1..512 */
+  int32_t experts_per_token;  /* k, 1..min(32, groups_kept * E / n_groups) */
+  int32_t score;              /* FOCUS_SCORE_* */
+  int32_t n_groups;           /* 1..64, divides E; 1 = no groups */
+  int32_t groups_kept;        /* 1..n_groups */
+  int32_t group_top;          /* 1 or 2; a group of one expert is worth that expert's choice in either case */
+  int32_t renormalize;        /* 0 or 1 */
+  float   route_scale;        /* > 0 */
+} focus_router;
+
+/* The experts and weights of n_rows rows.
+ *   dtype    FOCUS_F32 or FOCUS_BF16, of the logits; scores and weights are fp32
+ *   logits   device [n_rows, ld], E of each row used; ld >= E
+ *   bias     device [E] fp32, or NULL
+ *   experts  device [n_rows, k] int32; weights device [n_rows, k] fp32 */
+int focus_route(const focus_router *router, void *hip_stream, int32_t n_rows, int32_t dtype, const void *logits, int64_t ld,
+                const float *bias, int32_t *experts, float *weights);
+
+/* Microscaled 4-bit floats (MXFP4): 32 neighbours along a row share a scale.  For a matrix [rows, cols]:
+ *   codes   [rows, ceil(cols / 32) * 16] bytes, element 2 i of a row in the low half of byte i: sign, two exponent bits, one mantissa bit
+ *           (magnitudes 0, 0.5, 1, 1.5, 2, 3, 4, 6).  16-byte aligned
+ *   scales  [rows, ceil(cols / 32)] bytes: s stands for 2^(s - 127), 255 makes the block not a number
+ * Rows follow each other without gaps; a matrix per expert is [E * rows, cols]. */
+typedef struct focus_mx {
+  const void *codes;
+  const void *scales;
+} focus_mx;
+
+/* Rows to MXFP4.  The scale of a block is 2^(floor(log2(max |x|)) - 2), within 2^-127 and 2^127 (2^-127 for zeros); x / scale is rounded to
+ * the nearest code, half way to the even mantissa, magnitudes over 6 to 6.  A block with an infinity or a NaN gets scale 255 and zero codes.  Elements
+ * beyond cols in a row's last block are coded as zeros.
+ *   dtype    FOCUS_F32 or FOCUS_BF16;  x device [rows, ldx], ldx >= cols */
+int focus_mx_quantize(void *hip_stream, int32_t dtype, int64_t rows, int32_t cols, const void *x, int64_t ldx, void *codes, void *scales);
+
+/* The values of codes and scales, exact in both dtypes (magnitudes beyond the largest finite number become infinite).  Writes cols elements of each
+ * row of x [rows, ldx]. */
+int focus_mx_dequantize(void *hip_stream, int32_t dtype, int64_t rows, int32_t cols, const focus_mx *mx, void *x, int64_t ldx);
+
+/* C[m, n] = sum_k A[m, k] W[n, k], summed in fp32 and rounded once.
+ *   k            a multiple of 32 (the quantiser fills a row's last block with zeros); 0: C = 0
+ *   a_type       FOCUS_BF16: A device [m, lda] bf16, 16-byte aligned, lda a multiple of 8; a_scales NULL.
+ *                FOCUS_MX4: A the codes [m, k / 2] (lda ignored), a_scales [m, k / 32]
+ *   w            MXFP4 [n, k]
+ *   c_type       FOCUS_F32 or FOCUS_BF16; C device [m, ldc]
+ *   workspace    device, 16-byte aligned: partial sums of launches that cut K, for outputs too small to fill the chip.  With less than
+ *                focus_mx_gemm_bytes() (0 for most sizes), or NULL, K is cut into fewer parts or none: slower, rounded in another order */
+int focus_mx_gemm_bytes(int32_t m, int32_t n, int32_t k, int32_t a_type, size_t *bytes);
+int focus_mx_gemm(void *hip_stream, int32_t m, int32_t n, int32_t k, int32_t a_type, const void *a, const void *a_scales, int64_t lda,
+                  const focus_mx *w, int32_t c_type, void *c, int64_t ldc, void *workspace, size_t workspace_bytes);
+
+/* Routed SwiGLU experts with MXFP4 weights, on bf16 rows:
+ *   out[r] = sum_j weights[r, j] * Down_e( silu(Gate_e x_r) * (Up_e x_r) ),  e = experts[r, j], j < k ascending
+ * in fp32, except that the inner activations silu(..) * (..) are rounded to bf16, the operand type of the second product.  An entry of experts outside 0..E-1
+ * contributes nothing (experts that live elsewhere); a row may name an expert twice.
+ *   hidden, ffn  multiples of 32
+ *   gate_up      MXFP4 [E, 2 ffn, hidden]: per expert ffn gate rows, then ffn up rows;  down  MXFP4 [E, hidden, ffn]
+ *   x            device [n_rows, ldx] bf16, 16-byte aligned, ldx a multiple of 8;  n_rows * ldx below 2^30
+ *   experts      device [n_rows, k] int32;  weights  device [n_rows, k] fp32;  k 1..32, n_rows * k at most 2^24
+ *   out          device [n_rows, ldo], out_type FOCUS_F32 or FOCUS_BF16; add: out += (FOCUS_F32 only)
+ *   workspace    device, 256-byte aligned, focus_mx_experts_bytes() */
+int focus_mx_experts_bytes(int32_t n_experts, int32_t hidden, int32_t ffn, int32_t n_rows, int32_t k, size_t *bytes);
+int focus_mx_experts(void *hip_stream, int32_t n_experts, int32_t hidden, int32_t ffn, const focus_mx *gate_up, const focus_mx *down,
+                     int32_t n_rows, int32_t k, const void *x, int64_t ldx, const int32_t *experts, const float *weights, int32_t out_type,
+                     void *out, int64_t ldo, int32_t add, void *workspace, size_t workspace_bytes);
+
+/* From now on the mixture-of-experts layers of the context choose experts by this router instead of the one focus_config describes
+ * (softmax, no bias, no groups, renormalised).  n_experts and experts_per_token must be the configuration's; the router's route_scale
+ * counts.  Forced experts (focus_set_route_override) get this router's scores as weights.  router NULL: back to the configuration's.
+ *   bias     host array of n_layers device pointers ([E] fp32 each, borrowed until replaced), entries or the array may be NULL */
+int focus_set_router(focus_ctx *ctx, const focus_router *router, const float *const *bias);
+
+/* From now on the feed-forward layers listed here run on MXFP4 weights (bf16 models).  Every member is a host array of n_layers, or NULL; an
+ * entry with NULL codes leaves that layer on the matrices given to focus_init.  A layer's two matrices are given together.  The
+ * device memory is borrowed until replaced; the context copies the arrays.  weights NULL: back to the matrices of focus_init.  Inner widths and
+ * hidden must be multiples of 32. */
+typedef struct focus_mx_weights {
+  const focus_mx *w_gate_up, *w_down;                 /* dense layers: [2 F, hidden], [hidden, F] */
+  const focus_mx *w_expert_gate_up, *w_expert_down;   /* [E, 2 F_e, hidden], [E, hidden, F_e] */
+  const focus_mx *w_shared_gate_up, *w_shared_down;   /* [2 F_s, hidden], [hidden, F_s] */
+} focus_mx_weights;
+int focus_set_mx_weights(focus_ctx *ctx, const focus_mx_weights *weights);
 
 #ifdef __cplusplus
 }

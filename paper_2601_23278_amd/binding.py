@@ -16,7 +16,8 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libfocus.so")
 
 FOCUS_OK, FOCUS_EINVAL, FOCUS_ENOMEM, FOCUS_EHIP = 0, -1, -2, -3
-FOCUS_F32, FOCUS_BF16 = 0, 1
+FOCUS_F32, FOCUS_BF16, FOCUS_MX4 = 0, 1, 2
+FOCUS_SCORE_SOFTMAX, FOCUS_SCORE_SIGMOID = 0, 1
 FOCUS_MAX_BLOCK = 64
 KC_GEMM, KC_ATTENTION, KC_IMPORTANCE, KC_POINTWISE, KC_DECODE, KC_ROUTE, KC_EXPERTS, KC_SELECT, KC_GATHER, KC_KV_WRITE, KC_COUNT = range(11)
 KC_NAMES = ["gemm", "attention", "importance", "pointwise", "decode", "route", "experts", "select", "gather", "kv_write"]
@@ -58,6 +59,22 @@ class focus_seq_state(C.Structure):
                 ("tokens", C.c_int32 * FOCUS_MAX_BLOCK)]
 
 
+class focus_router(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_experts", "experts_per_token", "score", "n_groups", "groups_kept", "group_top", "renormalize")] + \
+               [("route_scale", C.c_float)]
+
+
+class focus_mx(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p)]
+
+
+_MX_FIELDS = ("w_gate_up", "w_down", "w_expert_gate_up", "w_expert_down", "w_shared_gate_up", "w_shared_down")
+
+
+class focus_mx_weights(C.Structure):
+    _fields_ = [(n, C.POINTER(focus_mx)) for n in _MX_FIELDS]
+
+
 class FocusError(RuntimeError):
     def __init__(self, code: int, text: str):
         super().__init__("libfocus error %d: %s" % (code, text))
@@ -88,6 +105,15 @@ def load_library() -> C.CDLL:
         "focus_set_timing": [P, I],
         "focus_get_kernel_time": [P, I, C.POINTER(C.c_float), C.POINTER(I)],
         "focus_free": [P],
+        "focus_route": [C.POINTER(focus_router), P, I, I, P, C.c_int64, P, P, P],
+        "focus_mx_quantize": [P, I, C.c_int64, I, P, C.c_int64, P, P],
+        "focus_mx_dequantize": [P, I, C.c_int64, I, C.POINTER(focus_mx), P, C.c_int64],
+        "focus_mx_gemm_bytes": [I, I, I, I, SZ],
+        "focus_mx_gemm": [P, I, I, I, I, P, P, C.c_int64, C.POINTER(focus_mx), I, P, C.c_int64, P, C.c_size_t],
+        "focus_mx_experts_bytes": [I, I, I, I, I, SZ],
+        "focus_mx_experts": [P, I, I, I, C.POINTER(focus_mx), C.POINTER(focus_mx), I, I, P, C.c_int64, P, P, I, P, C.c_int64, I, P, C.c_size_t],
+        "focus_set_router": [P, C.POINTER(focus_router), C.POINTER(P)],
+        "focus_set_mx_weights": [P, C.POINTER(focus_mx_weights)],
     }
     for name, args in sig.items():
         f = getattr(lib, name)
@@ -99,7 +125,8 @@ def load_library() -> C.CDLL:
 _lib = load_library()
 EXPORTS = ["focus_workspace_bytes", "focus_kv_pool_bytes", "focus_init", "focus_prefill_kv", "focus_step",
            "focus_select_compact", "focus_select_compact_noalloc", "focus_commit", "focus_run_layers", "focus_finalize_blocks", "focus_set_route_override", "focus_set_row_hint", "focus_run_steps", "focus_get_state", "focus_set_state", "focus_set_timing",
-           "focus_get_kernel_time", "focus_free", "focus_last_error"]
+           "focus_get_kernel_time", "focus_free", "focus_last_error", "focus_route", "focus_mx_quantize", "focus_mx_dequantize",
+           "focus_mx_gemm_bytes", "focus_mx_gemm", "focus_mx_experts_bytes", "focus_mx_experts", "focus_set_router", "focus_set_mx_weights"]
 
 
 def _check(rc: int, ctx=None):
@@ -137,6 +164,166 @@ def focus_select_compact_noalloc(cfg: focus_config, n_seq: int, delta_I: torch.T
     _check(_lib.focus_select_compact_noalloc(C.byref(cfg), Focus._stream(stream), n_seq, _ptr(delta_I), _ptr(mask_bits),
                                              _ptr(cached_bits), _ptr(token_sum), _ptr(total_steps), _ptr(k_override),
                                              C.byref(out)))
+
+
+# -- expert routing and MXFP4 (no context) ----------------------------------------------------------
+# A matrix in MXFP4 is a pair (codes, scales) of contiguous uint8 tensors, [..., K / 2] and [..., K / 32].  Tensors are checked here, on the host: the
+# library sees addresses only.  They live on the current device; the work goes to `stream`, or to torch's current one.  Outputs that are not
+# given, and workspaces, are torch tensors made on the call's stream.
+_DTYPES = {torch.float32: FOCUS_F32, torch.bfloat16: FOCUS_BF16}
+
+
+def _bad(text: str, *args):
+    raise FocusError(FOCUS_EINVAL, text % args)
+
+
+def _on_device(device, *tensors):
+    if device.type != "cuda" or device.index != torch.cuda.current_device():
+        _bad("tensors must be on the current device, not on %s", device)
+    for t in tensors:
+        if t is not None and t.device != device:
+            _bad("tensors on %s and %s", device, t.device)
+
+
+def _rows_of(t: torch.Tensor, name: str, dtypes=None):
+    """(rows, columns, distance of rows, dtype code) of a matrix whose rows are contiguous."""
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+        _bad("%s must be a matrix with contiguous rows that do not overlap", name)
+    code = _DTYPES.get(t.dtype)
+    if code is None or (dtypes is not None and t.dtype not in dtypes):
+        _bad("%s has an unsupported dtype", name)
+    return t.shape[0], t.shape[1], t.stride(0) if t.shape[0] > 1 else t.shape[1], code
+
+
+def _plain(t: torch.Tensor, name: str, shape, dtype):
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous():
+        _bad("%s must be a contiguous %s tensor of shape %s", name, dtype, tuple(shape))
+
+
+def _mx_of(mx, name: str, *lead: int) -> tuple:
+    """(focus_mx, K) of a pair of codes [*lead, K / 2] and scales [*lead, K / 32]."""
+    codes, scales = mx
+    if codes.dim() != len(lead) + 1:
+        _bad("%s: codes must have %d dimensions", name, len(lead) + 1)
+    blocks = scales.shape[-1] if scales.dim() else 0
+    _plain(codes, name + " (codes)", (*lead, 16 * blocks), torch.uint8)
+    _plain(scales, name + " (scales)", (*lead, blocks), torch.uint8)
+    return focus_mx(codes.data_ptr(), scales.data_ptr()), 32 * blocks
+
+
+def _scratch(nbytes: int, device, stream):
+    if nbytes == 0:
+        return None
+    if stream is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+def focus_route(router: focus_router, logits: torch.Tensor, bias: Optional[torch.Tensor] = None, experts: Optional[torch.Tensor] = None,
+                weights: Optional[torch.Tensor] = None, stream=None):
+    """(experts [rows, k] int32, weights [rows, k] fp32) of the rows of logits [rows, E], fp32 or bf16."""
+    rows, cols, ld, dtype = _rows_of(logits, "logits")
+    k, dev = router.experts_per_token, logits.device
+    _on_device(dev, bias, experts, weights)
+    if cols != router.n_experts:
+        _bad("logits have %d columns, the router %d experts", cols, router.n_experts)
+    if bias is not None:
+        _plain(bias, "bias", (cols,), torch.float32)
+    if experts is None or weights is None:
+        if k < 1 or k > 32:
+            _bad("experts_per_token must be in 1..32")
+        with torch.cuda.stream(stream):
+            experts = torch.empty(rows, k, dtype=torch.int32, device=dev) if experts is None else experts
+            weights = torch.empty(rows, k, dtype=torch.float32, device=dev) if weights is None else weights
+    _plain(experts, "experts", (rows, k), torch.int32)
+    _plain(weights, "weights", (rows, k), torch.float32)
+    _check(_lib.focus_route(C.byref(router), Focus._stream(stream), rows, dtype, logits.data_ptr(), ld, _ptr(bias), experts.data_ptr(), weights.data_ptr()))
+    return experts, weights
+
+
+def focus_mx_quantize(x: torch.Tensor, codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None, stream=None):
+    """(codes, scales) of the rows of x [rows, cols], fp32 or bf16."""
+    rows, cols, ld, dtype = _rows_of(x, "x")
+    _on_device(x.device, codes, scales)
+    blocks = (cols + 31) // 32
+    with torch.cuda.stream(stream):
+        codes = torch.empty(rows, 16 * blocks, dtype=torch.uint8, device=x.device) if codes is None else codes
+        scales = torch.empty(rows, blocks, dtype=torch.uint8, device=x.device) if scales is None else scales
+    _plain(codes, "codes", (rows, 16 * blocks), torch.uint8)
+    _plain(scales, "scales", (rows, blocks), torch.uint8)
+    _check(_lib.focus_mx_quantize(Focus._stream(stream), dtype, rows, cols, x.data_ptr(), ld, codes.data_ptr(), scales.data_ptr()))
+    return codes, scales
+
+
+def focus_mx_dequantize(codes: torch.Tensor, scales: torch.Tensor, out: torch.Tensor, stream=None):
+    """The values of codes and scales, into out [rows, cols], fp32 or bf16."""
+    rows, cols, ld, dtype = _rows_of(out, "out")
+    _on_device(out.device, codes, scales)
+    mx, k = _mx_of((codes, scales), "mx", rows)
+    if k != (cols + 31) // 32 * 32:
+        _bad("codes have %d elements a row, out %d columns", k, cols)
+    _check(_lib.focus_mx_dequantize(Focus._stream(stream), dtype, rows, cols, C.byref(mx), out.data_ptr(), ld))
+    return out
+
+
+def focus_mx_gemm_bytes(m: int, n: int, k: int, a_type: int) -> int:
+    nbytes = C.c_size_t()
+    _check(_lib.focus_mx_gemm_bytes(m, n, k, a_type, C.byref(nbytes)))
+    return nbytes.value
+
+
+def focus_mx_gemm(a, w, out: torch.Tensor, workspace: Optional[torch.Tensor] = None, stream=None):
+    """out [m, n] (fp32 or bf16) = A W^T; w the pair of an MXFP4 [n, k], a a bf16 matrix [m, k] or the pair of an MXFP4 [m, k]."""
+    m, n, ldc, c_type = _rows_of(out, "out")
+    _on_device(out.device, w[0], w[1])
+    mw, k = _mx_of(w, "w", n)
+    if isinstance(a, torch.Tensor):
+        rows, cols, lda, a_type = _rows_of(a, "a", (torch.bfloat16,))
+        a_ptr, a_scales, dev = a.data_ptr(), None, a.device
+    else:
+        ma, cols = _mx_of(a, "a", m)
+        rows, lda, a_type = m, cols, FOCUS_MX4
+        a_ptr, a_scales, dev = ma.codes, ma.scales, a[0].device
+        _on_device(out.device, a[1])
+    _on_device(out.device, workspace)
+    if dev != out.device or (rows, cols) != (m, k):
+        _bad("a is %d x %d, out %d x %d and w has %d columns", rows, cols, m, n, k)
+    if workspace is None:
+        workspace = _scratch(focus_mx_gemm_bytes(m, n, k, a_type), out.device, stream)
+    _check(_lib.focus_mx_gemm(Focus._stream(stream), m, n, k, a_type, a_ptr, a_scales, lda, C.byref(mw), c_type, out.data_ptr(), ldc, _ptr(workspace),
+                              0 if workspace is None else workspace.numel() * workspace.element_size()))
+    return out
+
+
+def focus_mx_experts_bytes(n_experts: int, hidden: int, ffn: int, n_rows: int, k: int) -> int:
+    nbytes = C.c_size_t()
+    _check(_lib.focus_mx_experts_bytes(n_experts, hidden, ffn, n_rows, k, C.byref(nbytes)))
+    return nbytes.value
+
+
+def focus_mx_experts(gate_up, down, x: torch.Tensor, experts: torch.Tensor, weights: torch.Tensor, out: torch.Tensor, add: bool = False,
+                     workspace: Optional[torch.Tensor] = None, stream=None):
+    """out [rows, hidden] (+)= the routed SwiGLU experts of x [rows, hidden] bf16; gate_up, down the pairs of an MXFP4 [E, 2 ffn, hidden] and
+    [E, hidden, ffn]; experts [rows, k] int32, weights [rows, k] fp32."""
+    rows, hidden, ldx, _ = _rows_of(x, "x", (torch.bfloat16,))
+    out_rows, out_cols, ldo, out_type = _rows_of(out, "out")
+    _on_device(out.device, x, experts, weights, *gate_up, *down, workspace)
+    E, two_ffn = gate_up[0].shape[:2] if gate_up[0].dim() == 3 else _bad("gate_up: codes must have 3 dimensions")
+    mg, hidden_g = _mx_of(gate_up, "gate_up", E, two_ffn)
+    md, ffn = _mx_of(down, "down", E, hidden)
+    if hidden_g != hidden or two_ffn != 2 * ffn or (out_rows, out_cols) != (rows, hidden):
+        _bad("x, out, gate_up and down do not fit together")
+    if experts.dim() != 2:
+        _bad("experts must be a matrix")
+    k = experts.shape[1]
+    _plain(experts, "experts", (rows, k), torch.int32)
+    _plain(weights, "weights", (rows, k), torch.float32)
+    if workspace is None:
+        workspace = _scratch(focus_mx_experts_bytes(E, hidden, ffn, rows, k), out.device, stream)
+    _check(_lib.focus_mx_experts(Focus._stream(stream), E, hidden, ffn, C.byref(mg), C.byref(md), rows, k, x.data_ptr(), ldx, experts.data_ptr(), weights.data_ptr(),
+                                 out_type, out.data_ptr(), ldo, int(add), _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size()))
+    return out
 
 
 def make_step_out(**tensors) -> focus_step_out:
@@ -222,6 +409,41 @@ class Focus:
 
     def focus_set_row_hint(self, packed_rows: int, rows_per_seq: int = 0):
         _check(_lib.focus_set_row_hint(self._ctx, packed_rows, rows_per_seq), self._ctx)
+
+    def focus_set_router(self, router: Optional[focus_router], bias: Optional[Sequence[Optional[torch.Tensor]]] = None):
+        """bias: one fp32 tensor [E], or None, per layer."""
+        E = self.cfg.n_experts
+        for b in bias or ():
+            if b is not None:
+                _plain(b, "bias", (E,), torch.float32)
+        if bias is not None and len(bias) != self.cfg.n_layers:
+            _bad("one bias per layer")
+        arr = None if bias is None else (C.c_void_p * len(bias))(*[None if b is None else b.data_ptr() for b in bias])
+        _check(_lib.focus_set_router(self._ctx, None if router is None else C.byref(router), arr), self._ctx)
+        self._router_bias = bias             # borrowed by the library
+
+    def focus_set_mx_weights(self, layers: Optional[Sequence[Dict[str, tuple]]]):
+        """layers: per layer a dict of matrix name (w_gate_up, w_expert_down, ...) -> pair (codes, scales); {} leaves a layer as it is."""
+        if layers is None:
+            _check(_lib.focus_set_mx_weights(self._ctx, None), self._ctx)
+            self._mx_layers = None
+            return
+        g = self.cfg
+        if len(layers) != g.n_layers:
+            _bad("one entry per layer")
+        shapes = {"w_gate_up": (2 * g.ffn, g.hidden), "w_down": (g.hidden, g.ffn),
+                  "w_expert_gate_up": (g.n_experts, 2 * g.expert_ffn, g.hidden), "w_expert_down": (g.n_experts, g.hidden, g.expert_ffn),
+                  "w_shared_gate_up": (2 * g.shared_ffn, g.hidden), "w_shared_down": (g.hidden, g.shared_ffn)}
+        w, arrays = focus_mx_weights(), []
+        for name in _MX_FIELDS:
+            if any(name in l for l in layers):
+                pairs = [_mx_of(l[name], name, *shapes[name][:-1]) if name in l else (focus_mx(), shapes[name][-1]) for l in layers]
+                if any(k != shapes[name][-1] for _, k in pairs):
+                    _bad("%s has another width", name)
+                arrays.append((focus_mx * len(layers))(*[m for m, _ in pairs]))
+                setattr(w, name, arrays[-1])
+        _check(_lib.focus_set_mx_weights(self._ctx, C.byref(w)), self._ctx)
+        self._mx_layers = layers             # borrowed by the library
 
     def focus_get_state(self, slot: int) -> focus_seq_state:
         st = focus_seq_state()

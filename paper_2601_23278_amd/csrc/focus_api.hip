@@ -8,11 +8,11 @@
 #include <algorithm>
 #include <new>
 
-#include "focus_internal.h"
+#include "focus_mx.h"
 
 namespace {
 
-std::string g_error;   // last error of a call that had no context
+thread_local std::string g_error;   // last error of a call that had no context
 
 // Scratch of focus_select_compact_noalloc: per-sequence retained counts and the packed row total.  One copy per GPU, held
 // until the process ends.  In host code the array's name is only a handle for hipGetSymbolAddress: the device address of
@@ -221,6 +221,11 @@ struct focus_ctx {
   const int32_t *route_override = nullptr;
   int32_t *out_route_experts = nullptr;
   float *out_route_weights = nullptr;
+  // focus_set_router, focus_set_mx_weights: empty vectors (or null codes) where nothing was set
+  bool has_router = false;
+  focus_router router{};
+  std::vector<const float *> router_bias;
+  std::vector<focus_mx> mx_gate_up, mx_down, mx_expert_gate_up, mx_expert_down, mx_shared_gate_up, mx_shared_down;
   bool route_by_row_id = false;         // inside focus_step / focus_run_layers: rows are block positions of the step's batch
   std::string error;
   // timing
@@ -248,6 +253,7 @@ struct focus_ctx {
     const fk::Scratch s = scratch();
     return s.bytes && p.layer_scratch_bytes > s.bytes ? fk::Scratch{ws + p.off_layer_scratch, p.layer_scratch_bytes} : s;
   }
+  static focus_mx mx_of(const std::vector<focus_mx> &v, int l) { return v.empty() ? focus_mx{nullptr, nullptr} : v[l]; }
   bool moe_layer(int l) const { return cfg.n_experts > 0 && l >= cfg.first_moe_layer; }
   fk::KvLayer kv_layer(int l) const {
     size_t layer_bytes = (size_t)cfg.n_pages * 2 * cfg.n_kv_heads * cfg.page_size * cfg.head_dim * esize(cfg.dtype);
@@ -266,6 +272,19 @@ int fail(focus_ctx *ctx, int code, const char *fmt, ...) {
   (ctx ? ctx->error : g_error) = buf;
   return code;
 }
+
+}  // namespace
+
+int fk::fail_call(int code, const char *fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  return fail(nullptr, code, "%s", buf);
+}
+
+namespace {
 
 #define HIP_TRY(ctx, expr)                                                                         \
   do {                                                                                             \
@@ -384,8 +403,8 @@ void layer_qkv(focus_ctx *c, hipStream_t s, int l, const RowSet &rs, const float
     fk::rope_kv_write(s, g.dtype, qkv, g.n_q_heads, rs.rows, rs.ri, rs.pl ? rs.st : c->slots(), c->kv_layer(l), c->at<float2>(pl.off_rope), rs.n_seq, rs.cu); }
 }
 
-void swiglu_ffn(focus_ctx *c, hipStream_t s, const RowSet &rs, const void *norm_w, void *normed, const void *w_gate_up, const void *w_down, int ffn,
-                float *resid);
+void swiglu_ffn(focus_ctx *c, hipStream_t s, const RowSet &rs, const void *norm_w, void *normed, const void *w_gate_up, const void *w_down, focus_mx mx_gate_up,
+                focus_mx mx_down, int ffn, float *resid);
 void moe_ffn(focus_ctx *c, hipStream_t s, int l, const RowSet &rs, float *resid, void *normed);
 
 // attention -> O projection (+residual) -> rmsnorm -> feed-forward (+residual).
@@ -418,15 +437,23 @@ void layer_rest(focus_ctx *c, hipStream_t s, int l, const RowSet &rs, float *res
     moe_ffn(c, s, l, rs, resid, normed);
     return;
   }
-  swiglu_ffn(c, s, rs, c->mlp_norm[l], normed, c->w_gate_up[l], c->w_down[l], g.ffn, resid);
+  swiglu_ffn(c, s, rs, c->mlp_norm[l], normed, c->w_gate_up[l], c->w_down[l], c->mx_of(c->mx_gate_up, l), c->mx_of(c->mx_down, l), g.ffn, resid);
 }
 
 // SwiGLU feed-forward, added to the residual stream: (RMSNorm, where norm_w is given, else `normed` holds its result) -> gate/up -> SiLU*up -> down.
-void swiglu_ffn(focus_ctx *c, hipStream_t s, const RowSet &rs, const void *norm_w, void *normed, const void *w_gate_up, const void *w_down, int ffn,
-                float *resid) {
+// mx_gate_up, mx_down: the matrices to use instead, where their codes are not null.
+void swiglu_ffn(focus_ctx *c, hipStream_t s, const RowSet &rs, const void *norm_w, void *normed, const void *w_gate_up, const void *w_down, focus_mx mx_gate_up,
+                focus_mx mx_down, int ffn, float *resid) {
   const focus_config &g = c->cfg;
   const Plan &pl = rs.pl ? *rs.pl : c->plan;
   void *gate_up = c->at<char>(pl.off_gate_up), *act = c->at<char>(pl.off_act);
+  if (mx_gate_up.codes) {
+    if (norm_w) { Timed t(c, s, FOCUS_KC_POINTWISE); fk::rmsnorm(s, g.dtype, resid, norm_w, normed, g.hidden, g.rms_eps, rs.rows); }
+    Timed t(c, s, FOCUS_KC_GEMM);
+    fk::mx_gemm(s, normed, nullptr, g.hidden, mx_gate_up, 2 * ffn, g.hidden, rs.rows, fk::MX_SILU_MUL, act, ffn, c->layer_scratch(pl));
+    fk::mx_gemm(s, act, nullptr, ffn, mx_down, g.hidden, ffn, rs.rows, fk::MX_ADD_F32, resid, g.hidden, c->layer_scratch(pl));
+    return;
+  }
   if (fk::gemm_fuses_silu_mul(g.dtype, normed, w_gate_up, 2 * ffn, g.hidden, rs.rows.cap)) {
     norm_and_project(c, s, resid, norm_w, normed, w_gate_up, 2 * ffn, rs.rows, fk::EPI_SILU_MUL, act, ffn,
                      c->layer_scratch(pl));
@@ -459,10 +486,25 @@ void moe_ffn(focus_ctx *c, hipStream_t s, int l, const RowSet &rs, float *resid,
   a.out_weights = c->route_by_row_id && c->out_route_weights ? c->out_route_weights + (size_t)l * plane : nullptr;
   { Timed t(c, s, FOCUS_KC_GEMM);
     fk::gemm(s, g.dtype, normed, c->w_router[l], g.n_experts, g.hidden, rs.rows, fk::EPI_STORE_F32, c->at<float>(pl.off_moe_logits), g.n_experts, c->layer_scratch(pl)); }
-  { Timed t(c, s, FOCUS_KC_ROUTE); fk::moe_route(s, a); fk::moe_group(s, a); }
-  { Timed t(c, s, FOCUS_KC_EXPERTS); fk::moe_experts(s, a); }
+  { Timed t(c, s, FOCUS_KC_ROUTE);
+    if (c->has_router) {
+      const float *bias = c->router_bias.empty() ? nullptr : c->router_bias[l];
+      fk::route(s, fk::RouteArgs{c->router, FOCUS_F32, a.logits, g.n_experts, bias, a.rows, a.row_map, a.route_override, a.topk_idx, a.topk_w, a.out_experts, a.out_weights});
+    } else {
+      fk::moe_route(s, a);
+    }
+    fk::moe_group(s, a); }
+  { Timed t(c, s, FOCUS_KC_EXPERTS);
+    static_assert(fk::kMxTileRows == fk::kMoeTileRows, "both grouped products walk the tiles of moe_group()");
+    const focus_mx mx = c->mx_of(c->mx_expert_gate_up, l);
+    if (mx.codes)
+      fk::mx_grouped(s, fk::MxGroups{a.offs, a.count, a.tile_e, a.tile_m0, a.n_tiles, a.n_tile_slots, a.arow}, a.u, g.hidden, a.rows.cap, mx,
+                     c->mx_of(c->mx_expert_down, l), g.hidden, g.expert_ffn, a.act, a.y);
+    else
+      fk::moe_experts(s, a); }
   // the shared expert adds into the residual stream before the routed sum (both orders are the same sum)
-  if (g.shared_ffn > 0) swiglu_ffn(c, s, rs, nullptr, normed, c->w_shared_gate_up[l], c->w_shared_down[l], g.shared_ffn, resid);
+  if (g.shared_ffn > 0) swiglu_ffn(c, s, rs, nullptr, normed, c->w_shared_gate_up[l], c->w_shared_down[l], c->mx_of(c->mx_shared_gate_up, l),
+                                   c->mx_of(c->mx_shared_down, l), g.shared_ffn, resid);
   { Timed t(c, s, FOCUS_KC_ROUTE); fk::moe_combine(s, a); }
 }
 
@@ -1061,6 +1103,66 @@ int focus_set_route_override(focus_ctx *ctx, const int32_t *experts) {
   if (!ctx) return fail(nullptr, FOCUS_EINVAL, "null context");
   if (experts && ctx->cfg.n_experts == 0) return fail(ctx, FOCUS_EINVAL, "the model has no mixture-of-experts layers");
   ctx->route_override = experts;
+  return FOCUS_OK;
+}
+
+int focus_set_router(focus_ctx *ctx, const focus_router *router, const float *const *bias) {
+  if (!ctx) return fail(nullptr, FOCUS_EINVAL, "null context");
+  const focus_config &g = ctx->cfg;
+  if (!router) {
+    ctx->has_router = false;
+    return FOCUS_OK;
+  }
+  if (g.n_experts == 0) return fail(ctx, FOCUS_EINVAL, "the model has no mixture-of-experts layers");
+  if (const char *e = fk::check_router(*router)) return fail(ctx, FOCUS_EINVAL, "%s", e);
+  if (router->n_experts != g.n_experts || router->experts_per_token != g.experts_per_token)
+    return fail(ctx, FOCUS_EINVAL, "the router's n_experts and experts_per_token must be the configuration's");
+  for (int l = 0; bias && l < g.n_layers; ++l)
+    if ((uintptr_t)bias[l] & 3) return fail(ctx, FOCUS_EINVAL, "a bias is not aligned to its elements");
+  try {
+    std::vector<const float *> copy;
+    if (bias) copy.assign(bias, bias + g.n_layers);
+    ctx->router_bias.swap(copy);
+  } catch (...) {
+    return fail(ctx, FOCUS_ENOMEM, "out of host memory");
+  }
+  ctx->router = *router;
+  ctx->has_router = true;
+  return FOCUS_OK;
+}
+
+int focus_set_mx_weights(focus_ctx *ctx, const focus_mx_weights *weights) {
+  if (!ctx) return fail(nullptr, FOCUS_EINVAL, "null context");
+  const focus_config &g = ctx->cfg;
+  std::vector<focus_mx> *const to[6] = {&ctx->mx_gate_up, &ctx->mx_down, &ctx->mx_expert_gate_up, &ctx->mx_expert_down, &ctx->mx_shared_gate_up, &ctx->mx_shared_down};
+  if (!weights) {
+    for (auto *v : to) v->clear();
+    return FOCUS_OK;
+  }
+  if (g.dtype != FOCUS_BF16) return fail(ctx, FOCUS_EINVAL, "MXFP4 weights need a bf16 model");
+  const focus_mx *const from[6] = {weights->w_gate_up, weights->w_down, weights->w_expert_gate_up, weights->w_expert_down, weights->w_shared_gate_up, weights->w_shared_down};
+  const int inner[3] = {g.ffn, g.expert_ffn, g.shared_ffn};
+  for (int p = 0; p < 3; ++p) {
+    const focus_mx *up = from[2 * p], *down = from[2 * p + 1];
+    if (!up != !down) return fail(ctx, FOCUS_EINVAL, "gate/up and down matrices are given together");
+    for (int l = 0; up && l < g.n_layers; ++l) {
+      if (!up[l].codes && !down[l].codes) continue;
+      if (!up[l].codes || !up[l].scales || !down[l].codes || !down[l].scales) return fail(ctx, FOCUS_EINVAL, "layer %d: a matrix or its scales are missing", l);
+      if (((uintptr_t)up[l].codes | (uintptr_t)down[l].codes) & 15) return fail(ctx, FOCUS_EINVAL, "layer %d: codes must be 16-byte aligned", l);
+      if (p == 0 ? ctx->moe_layer(l) : !ctx->moe_layer(l) || inner[p] == 0) return fail(ctx, FOCUS_EINVAL, "layer %d has no such matrix", l);
+      if (g.hidden % 32 || inner[p] % 32) return fail(ctx, FOCUS_EINVAL, "hidden and the inner width must be multiples of 32");
+      if ((int64_t)2 * inner[p] * (g.hidden / 2) >= (1ll << 31) || (int64_t)std::max(ctx->plan.max_rows, kPrefillRows) * g.hidden >= (1ll << 30))
+        return fail(ctx, FOCUS_EINVAL, "the model is too large for MXFP4 weights");
+    }
+  }
+  try {
+    std::vector<focus_mx> copy[6];
+    for (int i = 0; i < 6; ++i)
+      if (from[i]) copy[i].assign(from[i], from[i] + g.n_layers);
+    for (int i = 0; i < 6; ++i) to[i]->swap(copy[i]);
+  } catch (...) {
+    return fail(ctx, FOCUS_ENOMEM, "out of host memory");
+  }
   return FOCUS_OK;
 }
 

@@ -1,0 +1,223 @@
+// Expert router: scores, balance bias, groups, the k best experts of every row and their weights (focus_router in the header).
+//
+// A row's work is a chain (scores -> groups -> k picks, each of which needs the one before), a few hundred instructions on E numbers, so a
+// wavefront takes a row and everything stays in its registers: lane l holds experts l P .. l P + P - 1, P = 1, 2, 4 or 8.  Neighbours in
+// a lane make ties easy: the lowest expert among equals is the lowest lane's lowest element.
+//
+// Picks are whole numbers that have to be those of 64-bit scores.  They are found with fp32 scores, whose errors are bounded below; a row in
+// which two neighbours of the order, or the last kept and the first dropped group, are closer than that bound is done again in 64 bits by the same
+// code.  Equal logits with equal biases are equal in any arithmetic and need no second look.
+#include "focus_mx.h"
+
+namespace fk {
+
+namespace {
+
+constexpr int kRouteWaves = 4;       // rows of a workgroup
+
+__device__ __forceinline__ float lane_of(float v, int l) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), l)); }
+__device__ __forceinline__ double lane_of(double v, int l) { return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), l), __builtin_amdgcn_readlane(__double2loint(v), l)); }
+__device__ __forceinline__ float exp_of(float v) { return expf(v); }
+__device__ __forceinline__ double exp_of(double v) { return exp(v); }
+template <typename R> __device__ __forceinline__ R largest(R v) {
+#pragma unroll
+  for (int d = 32; d >= 1; d >>= 1) { const R o = __shfl_xor(v, d); v = o > v ? o : v; }
+  return v;
+}
+// LDS traffic between the lanes of one wavefront: it runs in order, only the compiler has to keep it so
+__device__ __forceinline__ void wave_lds_order() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+template <typename R> constexpr R kLow = -(R)INFINITY;
+
+// Picks of one row; false (R = float only): fp32 does not decide it.  idx and score of lane j < k are those of the j-th pick.  sh: 64 * P
+// numbers of LDS of this wavefront.
+template <typename R, int P>
+__device__ bool pick(const RouteArgs &a, const float (&l)[P], const float (&bias)[P], R *sh, const int32_t *forced, int &idx, R &score) {
+  constexpr bool F32 = sizeof(R) == 4;
+  const focus_router &r = a.router;
+  const int lane = threadIdx.x & 63, E = r.n_experts, k = r.experts_per_token, G = r.n_groups, first = lane * P;
+  R s[P], c[P];
+  float top_logit = -INFINITY;
+  if (r.score == FOCUS_SCORE_SIGMOID) {
+#pragma unroll
+    for (int i = 0; i < P; ++i) s[i] = l[i] == l[i] ? (R)1 / ((R)1 + exp_of(-(R)l[i])) : (R)0;
+  } else {
+#pragma unroll
+    for (int i = 0; i < P; ++i) top_logit = fmaxf(top_logit, first + i < E && l[i] == l[i] ? l[i] : -INFINITY);
+    top_logit = largest(top_logit);
+    R sum = 0;
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      // equal to the largest: 1, also where both are infinite; a row of -inf alone has no scores
+      s[i] = first + i < E && l[i] == l[i] && top_logit > -INFINITY ? (l[i] == top_logit ? (R)1 : exp_of((R)l[i] - (R)top_logit)) : (R)0;
+      sum += s[i];
+    }
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) sum += __shfl_xor(sum, d);
+#pragma unroll
+    for (int i = 0; i < P; ++i) s[i] = sum > 0 ? s[i] / sum : (R)0;
+  }
+  if (forced) {
+#pragma unroll
+    for (int i = 0; i < P; ++i) sh[first + i] = s[i];
+    wave_lds_order();
+    if (lane < k) {
+      idx = min(max(forced[lane], 0), E - 1);
+      score = sh[idx];
+    }
+    return true;
+  }
+  unsigned alive = 0;
+  R top_score = 0;
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    c[i] = s[i] + (R)bias[i];
+    if (l[i] != l[i] || c[i] != c[i]) c[i] = kLow<R>;
+    if (first + i < E) { alive |= 1u << i; top_score = s[i] > top_score ? s[i] : top_score; }
+  }
+  if (G > 1) {
+    // a group per 64 / ceil2(G) lanes: each lane looks at every such-and-such element, then the lanes' two best are merged
+    const int S = E / G, step = 64 >> (32 - __clz(G - 1)), g = lane / step, sub = lane % step;
+#pragma unroll
+    for (int i = 0; i < P; ++i) sh[first + i] = c[i];
+    wave_lds_order();
+    R t1 = kLow<R>, t2 = kLow<R>;
+    if (g < G)
+      for (int t = sub; t < S; t += step) {
+        const R v = sh[g * S + t];
+        t2 = v > t1 ? t1 : (v > t2 ? v : t2);
+        t1 = v > t1 ? v : t1;
+      }
+    for (int d = 1; d < step; d <<= 1) {
+      const R o1 = __shfl_xor(t1, d), o2 = __shfl_xor(t2, d);
+      const R low = o1 > t1 ? t1 : o1, high = o2 > t2 ? o2 : t2;
+      t2 = low > high ? low : high;
+      t1 = o1 > t1 ? o1 : t1;
+    }
+    R value = r.group_top == 2 && S > 1 ? t1 + t2 : t1;
+    if (value != value) value = kLow<R>;
+    int rank = 0;
+    for (int o = 0; o < G; ++o) {
+      const R v = lane_of(value, o * step);
+      rank += v > value || (v == value && o < g);
+    }
+    const bool lead = sub == 0 && g < G;
+    if (F32 && r.groups_kept < G) {
+      const R in = lane_of(value, __ffsll((unsigned long long)__ballot(lead && rank == r.groups_kept - 1)) - 1);
+      const R out = lane_of(value, __ffsll((unsigned long long)__ballot(lead && rank == r.groups_kept)) - 1);
+      top_score = largest(top_score);
+      // each choice is off by at most 2e-6 of the row's largest score (exp, sum, division) and half an ulp of itself
+      if (in - out <= (R)8e-6 * top_score + (R)1e-6 * (fabs(in) + fabs(out))) return false;
+    }
+    const uint64_t kept = __ballot(lead && rank < r.groups_kept);
+    const unsigned by_s = ((1u << 20) + S - 1) / S;                 // e / S = e * by_s >> 20 for e < 512
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const unsigned group = ((unsigned)(first + i) * by_s) >> 20;
+      if (first + i < E && !((kept >> (group * step)) & 1)) alive &= ~(1u << i);
+    }
+  }
+  R last_c = 0, last_s = 0;
+  float last_l = 0, last_b = 0;
+  for (int j = 0;; ++j) {
+    // best element of the lane, then of the wavefront; the lowest lane and in it the lowest element among equals
+    R hc = kLow<R>, hs = 0;
+    float hl = 0, hb = 0;
+    int hi = -1;
+#pragma unroll
+    for (int i = 0; i < P; ++i)
+      if (((alive >> i) & 1) && (hi < 0 || c[i] > hc)) { hc = c[i]; hs = s[i]; hl = l[i]; hb = bias[i]; hi = i; }
+    const R best = largest(hc);
+    const uint64_t who = __ballot(hi >= 0 && hc == best);
+    if (!who) break;                                                // nothing left (j >= k)
+    const int w = __ffsll((unsigned long long)who) - 1;
+    const R ws = lane_of(hs, w);
+    const int we = __builtin_amdgcn_readlane(first + hi, w);
+    if (F32) {
+      const float wl = lane_of(hl, w), wb = lane_of(hb, w);
+      if (j > 0 && !(wl == last_l && wb == last_b)) {
+        // scores are off by at most 6e-7 of themselves (sigmoid), 1.2e-6 and 1.2e-7 per unit of distance from the largest logit (softmax)
+        const float rel = r.score == FOCUS_SCORE_SIGMOID ? 6e-7f : 1.2e-6f + 1.2e-7f * (top_logit - fminf(wl, last_l));
+        if (last_c - best <= rel * (ws + last_s) + 2e-7f * (fabsf((float)best) + fabsf((float)last_c))) return false;
+        if (j >= k) break;
+      }
+      last_c = best; last_s = ws; last_l = wl; last_b = wb;
+    } else if (j >= k) break;
+    if (lane == j && j < k) { idx = we; score = ws; }
+    if (lane == w) alive &= ~(1u << hi);
+  }
+  return true;
+}
+
+// A row takes longer for its chain of dependent steps than for its bytes.
+template <typename T, int P>
+__global__ __launch_bounds__(kRouteWaves * 64) void k_route(RouteArgs a) {
+  __shared__ double sh[kRouteWaves][64 * P];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = blockIdx.x * kRouteWaves + wave;
+  const int M = a.rows.count ? min(*a.rows.count, a.rows.cap) : a.rows.cap, E = a.router.n_experts, k = a.router.experts_per_token;
+  if (row >= M) return;
+  const T *lg = (const T *)a.logits + (size_t)row * a.ld;
+  float l[P], bias[P];
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    const int e = lane * P + i;
+    l[i] = e < E ? (float)lg[e] : 0.f;
+    bias[i] = a.bias && e < E ? a.bias[e] : 0.f;
+  }
+  const int rid = a.row_map ? a.row_map[row] : row;
+  const int32_t *forced = a.route_override ? a.route_override + (size_t)rid * k : nullptr;
+  int idx = 0;
+  float f = 0.f, sum = 0.f, weight;
+  bool decided = pick<float, P>(a, l, bias, (float *)sh[wave], forced, idx, f);
+  for (int j = 0; j < k; ++j) sum += lane_of(f, j);
+  // scores that fp32 holds with few bits or not at all (sigmoids of logits far below zero) have quotients all the same
+  decided = decided && !(a.router.renormalize && sum < 1e-30f);
+  if (decided) {
+    weight = a.router.renormalize ? a.router.route_scale * f / sum : a.router.route_scale * f;
+  } else {
+    double d = 0.0, total = 0.0;
+    pick<double, P>(a, l, bias, sh[wave], forced, idx, d);
+    for (int j = 0; j < k; ++j) total += lane_of(d, j);
+    weight = (float)(a.router.renormalize ? (total > 0.0 ? a.router.route_scale * d / total : 0.0) : a.router.route_scale * d);
+  }
+  if (lane < k) {
+    a.experts[(size_t)row * k + lane] = idx;
+    a.weights[(size_t)row * k + lane] = weight;
+    if (a.out_experts) a.out_experts[(size_t)rid * k + lane] = idx;
+    if (a.out_weights) a.out_weights[(size_t)rid * k + lane] = weight;
+  }
+}
+
+template <typename T> void launch(hipStream_t s, const RouteArgs &a) {
+  const int groups = (a.rows.cap + kRouteWaves - 1) / kRouteWaves, E = a.router.n_experts;
+  if (E <= 64) k_route<T, 1><<<groups, kRouteWaves * 64, 0, s>>>(a);
+  else if (E <= 128) k_route<T, 2><<<groups, kRouteWaves * 64, 0, s>>>(a);
+  else if (E <= 256) k_route<T, 4><<<groups, kRouteWaves * 64, 0, s>>>(a);
+  else k_route<T, 8><<<groups, kRouteWaves * 64, 0, s>>>(a);
+}
+
+}  // namespace
+
+const char *check_router(const focus_router &r) {
+  if (r.n_experts < 1 || r.n_experts > 512) return "n_experts must be in 1..512";
+  if (r.score != FOCUS_SCORE_SOFTMAX && r.score != FOCUS_SCORE_SIGMOID) return "score must be a FOCUS_SCORE_* value";
+  if (r.n_groups < 1 || r.n_groups > 64 || r.n_experts % r.n_groups) return "n_groups must be in 1..64 and divide n_experts";
+  if (r.groups_kept < 1 || r.groups_kept > r.n_groups) return "groups_kept must be in 1..n_groups";
+  if (r.group_top != 1 && r.group_top != 2) return "group_top must be 1 or 2";
+  if (r.experts_per_token < 1 || r.experts_per_token > 32 || r.experts_per_token > r.n_experts / r.n_groups * r.groups_kept)
+    return "experts_per_token must be in 1..min(32, experts of the kept groups)";
+  if (r.renormalize != 0 && r.renormalize != 1) return "renormalize must be 0 or 1";
+  if (!(r.route_scale > 0.f) || r.route_scale > 3.4e38f) return "route_scale must be > 0 and finite";
+  return nullptr;
+}
+
+void route(hipStream_t s, const RouteArgs &a) {
+  if (a.rows.cap <= 0) return;
+  if (a.dtype == FOCUS_F32) launch<float>(s, a);
+  else launch<bf16_t>(s, a);
+}
+
+}  // namespace fk

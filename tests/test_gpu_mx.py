@@ -1,0 +1,553 @@
+"""The expert router and the MXFP4 operators on the GPU, through the public entry points, against plain 64-bit forms (mx_reference.py)."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import focus_inputs as fi
+import mx_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+
+
+def _pk():
+    import paper_2601_23278_amd as pk
+    from paper_2601_23278_amd import runner
+    return pk, runner
+
+
+def gpu(*ts):
+    return tuple(t.to(DEV) for t in ts)
+
+
+# -- router -----------------------------------------------------------------------------------
+def check_route(logits, bias, kind, groups, kept, top, k, renorm, scale):
+    """logits: a CPU tensor [rows, E], possibly a view of columns."""
+    pk, _ = _pk()
+    r = pk.focus_router(n_experts=logits.shape[1], experts_per_token=k, score=int(kind == "sigmoid"), n_groups=groups, groups_kept=kept, group_top=top,
+                        renormalize=renorm, route_scale=scale)
+    wide = torch.zeros(logits.shape[0], logits.stride(0) if logits.shape[0] > 1 else logits.shape[1], dtype=logits.dtype, device=DEV)
+    wide[:, :logits.shape[1]] = logits
+    experts, weights = pk.focus_route(r, wide[:, :logits.shape[1]], None if bias is None else bias.to(DEV))
+    again = pk.focus_route(r, wide[:, :logits.shape[1]], None if bias is None else bias.to(DEV))
+    assert torch.equal(experts, again[0]) and torch.equal(weights, again[1])
+    l = logits.double().numpy()
+    for i in range(logits.shape[0]):
+        e, w = ref.route_row(l[i], None if bias is None else bias.double().numpy(), kind, groups, kept, top, k, renorm, scale)
+        assert experts[i].tolist() == e, (i, experts[i].tolist(), e)
+        # fp32: exp off by an ulp and by the rounding of its argument (up to 2^-24 of 100), a dozen roundings in sums and quotients
+        got, want = weights[i].double().cpu().numpy(), np.array(w)
+        assert np.all(np.abs(got - want) <= np.abs(want) * (100 + 16 + k) * 2.0 ** -24 + 1e-38), (i, got, want)
+
+
+@pytest.mark.parametrize("kind", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("E,k,groups,kept,top,biased,renorm", [
+    (1, 1, 1, 1, 1, False, 1), (2, 2, 1, 1, 1, True, 0), (7, 3, 1, 1, 1, True, 1), (8, 4, 4, 2, 2, False, 1), (64, 8, 64, 8, 1, True, 1), (65, 6, 5, 3, 2, True, 1),
+    (96, 32, 3, 1, 2, True, 0), (160, 6, 8, 3, 1, False, 0), (256, 8, 8, 4, 2, True, 1), (257, 9, 1, 1, 1, False, 1), (512, 22, 16, 5, 2, True, 1), (512, 1, 1, 1, 1, False, 0)])
+def test_route_shapes(kind, E, k, groups, kept, top, biased, renorm):
+    g = torch.Generator().manual_seed(E * 31 + k)
+    bias = torch.randn(E, generator=g) * 0.1 if biased else None
+    for rows, dtype, pad in [(1, torch.float32, 0), (5, torch.bfloat16, 3), (66, torch.float32, 1)]:
+        wide = (torch.randn(rows, E + pad, generator=g) * 2).to(dtype)
+        check_route(wide[:, :E], bias, kind, groups, kept, top, k, renorm, 2.5)
+
+
+@pytest.mark.parametrize("kind", ["softmax", "sigmoid"])
+def test_route_ties_and_values_that_are_no_numbers(kind):
+    E, k = 48, 8
+    g = torch.Generator().manual_seed(3)
+    l = torch.randn(24, E, generator=g)
+    l[0] = 0.0                                             # all equal
+    l[1] = torch.round(l[1])                               # many equal
+    l[2] = -math.inf
+    l[3] = math.inf
+    l[4] = math.nan
+    l[5, 5:] = -math.inf                                   # fewer than k that count
+    l[6, 3:] = math.nan
+    l[7, 40] = math.inf
+    l[8, 40:44] = math.inf
+    l[9, ::2] = math.nan
+    l[10] = l[10] * 100                                    # sigmoid saturates: equal scores of unequal logits
+    l[11] = 50.0 + l[11]
+    l[12] = -300.0 + l[12]
+    l[13] = 1.0 + torch.arange(E) * 2.0 ** -23             # neighbours in fp32
+    l[14] = torch.finfo(torch.float32).min
+    l[15, :24] = l[15, 24:]                                # equal groups
+    l[16] = 3.0e38
+    bias = torch.randn(E, generator=g) * 0.05
+    odd = bias.clone()
+    odd[[1, 30]], odd[[2, 47]], odd[7] = -math.inf, math.nan, math.inf
+    for b in (None, bias, torch.zeros(E), odd):
+        for groups, kept, top in [(1, 1, 1), (2, 1, 2), (6, 2, 2), (12, 3, 1), (48, 9, 2)]:
+            for renorm in (0, 1):
+                check_route(l, b, kind, groups, kept, top, k, renorm, 1.0)
+
+
+@pytest.mark.parametrize("kind", ["softmax", "sigmoid"])
+def test_route_close_calls_are_those_of_64_bits(kind):
+    """Scores that fp32 cannot tell apart: biases that undo the scores' differences up to 1e-8, and sums of two that differ in the last places."""
+    E, k = 64, 8
+    g = torch.Generator().manual_seed(11)
+    l = torch.randn(40, E, generator=g)
+    for i in range(40):
+        s = torch.from_numpy(ref.scores_of(l[i].double().numpy(), kind))
+        bias = (0.75 - s).float()                          # every choice is 0.75 up to a rounding of the bias
+        check_route(l[i:i + 1], bias, kind, 1, 1, 1, k, 1, 1.0)
+        check_route(l[i:i + 1], bias, kind, 8, 3, 2, k, 1, 1.0)
+
+
+# -- conversion -------------------------------------------------------------------------------
+def special_rows(rows, cols, gen):
+    """Rows of many sizes, exact half-way points, zeros, the largest and smallest numbers."""
+    x = torch.randn(rows, cols, generator=gen) * torch.exp2(torch.randint(-100, 100, (rows, 1), generator=gen).float())
+    half = torch.tensor([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 6.0, 7.0, 0.0, -0.0, 0.5, 1.5, 3.0])
+    for r in range(0, rows, 3):
+        n = min(cols, 96)
+        x[r, :n] = half[torch.randint(0, len(half), (n,), generator=gen)] * torch.where(torch.rand(n, generator=gen) < 0.5, 1.0, -1.0) * 2.0 ** (r - 3)
+    if rows > 4:
+        x[4] = 0.0
+        x[1] = x[1].sign() * 2.0 ** -126 * torch.rand(cols, generator=gen)             # subnormal
+    if rows > 6:
+        x[5] = torch.finfo(torch.bfloat16).max * torch.rand(cols, generator=gen)
+        x[6] = 2.0 ** -127
+    return x
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,cols,pad,shift", [(1, 1, 0, 0), (3, 31, 0, 0), (7, 32, 0, 0), (8, 33, 7, 0), (4, 100, 0, 0), (7, 256, 8, 0), (9, 96, 5, 3), (2, 4096, 0, 0), (70, 64, 0, 1)])
+def test_conversion_is_exact(dtype, rows, cols, pad, shift):
+    pk, _ = _pk()
+    gen = torch.Generator().manual_seed(rows * 1000 + cols)
+    x = special_rows(rows, cols, gen).to(dtype)
+    wide = torch.full((rows, cols + pad + shift), math.nan, dtype=dtype, device=DEV)       # what lies beside the matrix is not read into it
+    view = wide[:, shift:shift + cols]
+    view.copy_(x)
+    codes, scales = pk.focus_mx_quantize(view)
+    want_codes, want_scales = ref.quantize(x.double().numpy())
+    assert np.array_equal(scales.cpu().numpy(), want_scales)
+    assert np.array_equal(codes.cpu().numpy(), ref.pack(want_codes))
+    out = torch.full((rows, cols + pad + shift), 7.0, dtype=dtype, device=DEV)
+    pk.focus_mx_dequantize(codes, scales, out[:, shift:shift + cols])
+    v = ref.values(codes.cpu(), scales.cpu())[:, :cols]
+    assert torch.equal(out[:, shift:shift + cols].cpu().double(), v)
+    assert bool((out[:, :shift] == 7).all()) and bool((out[:, shift + cols:] == 7).all())  # and not written
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_blocks_that_are_no_numbers(dtype):
+    pk, _ = _pk()
+    x = torch.ones(4, 96, dtype=dtype)
+    x[0, 33], x[1, 95], x[2, 0] = math.nan, math.inf, -math.inf
+    codes, scales = pk.focus_mx_quantize(x.to(DEV))
+    assert scales.cpu().tolist() == [[125, 255, 125], [125, 125, 255], [255, 125, 125], [125, 125, 125]]
+    out = pk.focus_mx_dequantize(codes, scales, torch.empty(4, 96, dtype=dtype, device=DEV)).cpu()
+    bad = torch.zeros(4, 96, dtype=torch.bool)
+    bad[0, 32:64], bad[1, 64:], bad[2, :32] = True, True, True
+    assert torch.equal(torch.isnan(out), bad) and bool((out[~bad] == 1).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_every_code_with_every_scale(dtype):
+    pk, _ = _pk()
+    codes = torch.arange(256, dtype=torch.uint8).view(1, 16, 16).expand(256, 16, 16).reshape(256, 256).contiguous()
+    scales = torch.arange(256, dtype=torch.uint8).view(256, 1).expand(256, 16).contiguous()
+    out = pk.focus_mx_dequantize(*gpu(codes, scales), torch.empty(256, 512, dtype=dtype, device=DEV)).cpu()
+    want = ref.values(codes, scales).to(dtype)
+    assert torch.equal(torch.isnan(out), torch.isnan(want)) and torch.equal(out[:255], want[:255])
+
+
+# -- products ---------------------------------------------------------------------------------
+def product_bound(a, w, dtype):
+    """K additions in fp32 of at most half an ulp of the sum of magnitudes, doubled for matrix units that truncate; half a step of the result's type."""
+    return a.shape[1] * 2.0 ** -23 * (a.abs() @ w.abs().t()) + (2.0 ** -8 if dtype == torch.bfloat16 else 2.0 ** -24) * (a @ w.t()).abs() + 1e-40
+
+
+@pytest.mark.parametrize("a_type", ["bf16", "mx4"])
+@pytest.mark.parametrize("m,n,k", [(1, 1, 32), (1, 200, 64), (3, 5, 96), (31, 33, 128), (32, 128, 160), (33, 130, 224), (128, 128, 256), (129, 257, 288), (8, 1000, 4096),
+                                   (200, 300, 1312), (300, 64, 8192), (5, 100, 12256), (260, 520, 544), (2, 3, 0)])
+def test_gemm(a_type, m, n, k):
+    pk, _ = _pk()
+    gen = torch.Generator().manual_seed(m * 7 + n * 3 + k)
+    w = ref.random_mx(gen, n, k)
+    wv = ref.values(*w)
+    if a_type == "bf16":
+        wide = torch.full((m, k + 16), math.nan, dtype=torch.bfloat16)
+        wide[:, :k] = torch.randn(m, k, generator=gen)
+        av, a = wide[:, :k].double(), wide.to(DEV)[:, :k]
+    else:
+        am = ref.random_mx(gen, m, k)
+        av, a = ref.values(*am), gpu(*am)
+    for dtype in (torch.float32, torch.bfloat16):
+        outs = []
+        for ws in (None, torch.empty(0, dtype=torch.uint8, device=DEV)):                  # with K cut into parts where that fits, and without
+            wide_c = torch.full((m + 1, n + 3), 7.0, dtype=dtype, device=DEV)
+            c = wide_c[:m, :n]
+            pk.focus_mx_gemm(a, gpu(*w), c, workspace=ws)
+            err = (c.cpu().double() - av @ wv.t()).abs()
+            assert bool((err <= product_bound(av, wv, dtype)).all()), (dtype, float((err / product_bound(av, wv, dtype)).max()))
+            assert bool((wide_c[:m, n:] == 7).all()) and bool((wide_c[m:] == 7).all())     # rows and columns beyond C stay as they were
+            again = torch.empty_like(c.contiguous())
+            pk.focus_mx_gemm(a, gpu(*w), again, workspace=ws)
+            assert torch.equal(again, c.contiguous())
+            outs.append(c.clone())
+
+
+@pytest.mark.parametrize("a_type", ["bf16", "mx4"])
+@pytest.mark.parametrize("k", [96, 512])
+def test_gemm_extreme_scales_and_values_that_are_no_numbers(a_type, k):
+    """Each spoils its own row or column and nothing else; scales down to 2^-127 and up to 2^127 count."""
+    pk, _ = _pk()
+    m, n = 70, 140
+    gen = torch.Generator().manual_seed(k)
+    codes, scales = ref.random_mx(gen, n, k)
+    scales[0], scales[1], scales[129] = 0, 254 - 20, 1
+    scales[7, 1] = 255
+    wv = ref.values(codes, scales)
+    if a_type == "bf16":
+        a = torch.randn(m, k, generator=gen).to(torch.bfloat16)
+        a[3, k - 1], a[40, 0] = math.inf, math.nan
+        av, ga = a.double(), a.to(DEV)
+    else:
+        ac, asc = ref.random_mx(gen, m, k)
+        asc[3, k // 32 - 1], asc[40, 0] = 255, 255
+        asc[5], asc[69] = 127 + 100, 20
+        av, ga = ref.values(ac, asc), gpu(ac, asc)
+    c = pk.focus_mx_gemm(ga, gpu(codes, scales), torch.empty(m, n, device=DEV)).cpu().double()
+    bad = torch.zeros(m, n, dtype=torch.bool)
+    bad[[3, 40]], bad[:, 7] = True, True
+    assert bool((~torch.isfinite(c[bad])).all())
+    av, want = torch.nan_to_num(av, nan=0.0, posinf=0.0), None
+    wv = torch.nan_to_num(wv, nan=0.0)
+    want = av @ wv.t()
+    ok = ~bad & (want.abs() < 3e38)
+    # a sum or a product of scales below the smallest normal number may come out as zero
+    assert bool(((c - want).abs()[ok] <= product_bound(av, wv, torch.float32)[ok] + k * 2.0 ** -126).all())
+
+
+def test_large_products_agree_with_sampled_entries():
+    """The launches with 256 x 256 tiles and several tiles of rows, at odd sizes: sampled rows and columns in 64 bits."""
+    pk, _ = _pk()
+    for a_type, m, n, k in [("mx4", 3001, 4100, 1056), ("mx4", 2048, 8192, 768), ("bf16", 1300, 2500, 1056)]:
+        gen = torch.Generator().manual_seed(m)
+        w = ref.random_mx(gen, n, k)
+        am = ref.random_mx(gen, m, k)
+        av = ref.values(*am)
+        a = gpu(*am)
+        if a_type == "bf16":
+            a = torch.randn(m, k, generator=gen).to(torch.bfloat16)
+            av, a = a.double(), a.to(DEV)
+        c = pk.focus_mx_gemm(a, gpu(*w), torch.empty(m, n, device=DEV)).cpu().double()
+        rows = torch.cat([torch.tensor([0, m - 1]), torch.randint(0, m, (60,), generator=gen)])
+        wv = ref.values(*w)
+        assert bool(((c[rows] - av[rows] @ wv.t()).abs() <= product_bound(av[rows], wv, torch.float32)).all())
+        cols = torch.cat([torch.tensor([0, n - 1]), torch.randint(0, n, (60,), generator=gen)])
+        assert bool(((c[:, cols] - av @ wv[cols].t()).abs() <= product_bound(av, wv[cols], torch.float32)).all())
+
+
+# -- experts ----------------------------------------------------------------------------------
+def experts_case(seed, rows, E, k, hidden, ffn, pad=0):
+    gen = torch.Generator().manual_seed(seed)
+    wide = torch.full((rows, hidden + pad), math.nan, dtype=torch.bfloat16)
+    wide[:, :hidden] = torch.randn(rows, hidden, generator=gen)
+    gate_up, down = ref.random_mx(gen, E, 2 * ffn, hidden, spread=1), ref.random_mx(gen, E, hidden, ffn, spread=1)
+    # down to about the size of trained weights
+    gate_up[1].sub_(3), down[1].sub_(3)
+    picks = torch.stack([torch.randperm(max(E, k), generator=gen)[:k] for _ in range(rows)]).to(torch.int32) if rows else torch.zeros(0, k, dtype=torch.int32)
+    return wide, gate_up, down, picks, torch.rand(rows, k, generator=gen)
+
+
+@pytest.mark.parametrize("rows,E,k,hidden,ffn,pad", [(1, 1, 1, 32, 32, 0), (1, 8, 2, 64, 96, 8), (5, 9, 3, 160, 64, 0), (40, 4, 2, 96, 160, 24), (130, 3, 1, 128, 128, 0),
+                                                     (300, 4, 3, 256, 32, 0), (33, 64, 8, 288, 352, 0), (7, 300, 32, 64, 64, 0), (20, 16, 4, 2048, 512, 0)])
+def test_experts(rows, E, k, hidden, ffn, pad):
+    pk, _ = _pk()
+    wide, gate_up, down, picks, weights = experts_case(rows + E, rows, E, k, hidden, ffn, pad)
+    x = wide.to(DEV)[:, :hidden]
+    args = (gpu(*gate_up), gpu(*down), x, *gpu(picks, weights))
+    want, bound = ref.experts(wide[:, :hidden].double(), ref.values(*gate_up), ref.values(*down), picks, weights.double())
+    for dtype in (torch.float32, torch.bfloat16):
+        out = torch.full((rows + 1, hidden + 5), 7.0, dtype=dtype, device=DEV)
+        pk.focus_mx_experts(*args, out[:rows, :hidden])
+        got = out[:rows, :hidden].cpu().double()
+        tol = bound + (2.0 ** -8 if dtype == torch.bfloat16 else 2.0 ** -24) * want.abs()
+        assert bool(((got - want).abs() <= tol).all()), float(((got - want).abs() / tol).max())
+        assert bool((out[:rows, hidden:] == 7).all()) and bool((out[rows:] == 7).all())
+        again = torch.empty(rows, hidden, dtype=dtype, device=DEV)
+        pk.focus_mx_experts(*args, again)
+        assert torch.equal(again, out[:rows, :hidden].contiguous())
+    out = torch.full((rows, hidden), 3.0, device=DEV)
+    pk.focus_mx_experts(*args, out, add=True)
+    assert bool(((out.cpu().double() - 3.0 - want).abs() <= bound + 2.0 ** -23 * (want.abs() + 3.0)).all())
+
+
+def test_experts_elsewhere_named_twice_or_not_at_all():
+    pk, _ = _pk()
+    rows, E, k, hidden, ffn = 200, 6, 4, 96, 64
+    wide, gate_up, down, picks, weights = experts_case(5, rows, E, k, hidden, ffn)
+    picks[0] = -1
+    picks[1], picks[2, 1], picks[3, 2] = 2, E, -2 ** 31
+    picks[4] = 2 ** 31 - 1
+    picks[10:190] = 5                                           # one expert has most rows, each of them four times
+    weights[7] = 0.0
+    want, bound = ref.experts(wide.double(), ref.values(*gate_up), ref.values(*down), picks, weights.double())
+    out = pk.focus_mx_experts(gpu(*gate_up), gpu(*down), wide.to(DEV), *gpu(picks, weights), torch.full((rows, hidden), 7.0, device=DEV)).cpu().double()
+    assert bool((out[0] == 0).all()) and bool((out[4] == 0).all()) and bool((out[7] == 0).all())
+    assert bool(((out - want).abs() <= bound + 2.0 ** -24 * want.abs()).all())
+    none = torch.full_like(picks, -1)
+    out = pk.focus_mx_experts(gpu(*gate_up), gpu(*down), wide.to(DEV), *gpu(none, weights), torch.full((rows, hidden), 7.0, device=DEV))
+    assert bool((out == 0).all())
+
+
+def test_a_rows_result_does_not_depend_on_the_other_rows():
+    pk, _ = _pk()
+    rows, E, k, hidden, ffn = 500, 5, 2, 128, 96
+    wide, gate_up, down, picks, weights = experts_case(9, rows, E, k, hidden, ffn)
+    x, picks, weights = gpu(wide, picks, weights)
+    gu, dn = gpu(*gate_up), gpu(*down)
+    whole = pk.focus_mx_experts(gu, dn, x, picks, weights, torch.empty(rows, hidden, device=DEV))
+    order = torch.randperm(rows, generator=torch.Generator().manual_seed(1)).to(DEV)
+    other = pk.focus_mx_experts(gu, dn, x[order].contiguous(), picks[order].contiguous(), weights[order].contiguous(), torch.empty(rows, hidden, device=DEV))
+    assert torch.equal(other, whole[order])
+    poisoned = x.clone()
+    poisoned[17] = math.nan
+    other = pk.focus_mx_experts(gu, dn, poisoned, picks, weights, torch.empty(rows, hidden, device=DEV))
+    keep = torch.arange(rows, device=DEV) != 17
+    assert torch.equal(other[keep], whole[keep]) and bool(torch.isnan(other[17]).all())
+
+
+# -- as they are used -------------------------------------------------------------------------
+def layer(pk, x, w_router, router, bias, gate_up, down, out, stream=None):
+    """Router logits in MXFP4 -> picks -> experts."""
+    with torch.cuda.stream(stream):
+        logits = torch.empty(x.shape[0], router.n_experts, device=x.device)
+    pk.focus_mx_gemm(pk.focus_mx_quantize(x, stream=stream), w_router, logits, stream=stream)
+    experts, weights = pk.focus_route(router, logits, bias, stream=stream)
+    pk.focus_mx_experts(gate_up, down, x, experts, weights, out, stream=stream)
+    return logits, experts, weights
+
+
+def layer_inputs(pk, rows, E=24, k=3, hidden=256, ffn=96, seed=2):
+    gen = torch.Generator().manual_seed(seed)
+    x = torch.randn(rows, hidden, generator=gen).to(torch.bfloat16).to(DEV)
+    w_router = pk.focus_mx_quantize((torch.randn(E, hidden, generator=gen) * 0.05).to(DEV))
+    gate_up = tuple(t.view(E, 2 * ffn, -1) for t in pk.focus_mx_quantize((torch.randn(E * 2 * ffn, hidden, generator=gen) * 0.05).to(DEV)))
+    down = tuple(t.view(E, hidden, -1) for t in pk.focus_mx_quantize((torch.randn(E * hidden, ffn, generator=gen) * 0.05).to(DEV)))
+    router = pk.focus_router(n_experts=E, experts_per_token=k, score=pk.FOCUS_SCORE_SIGMOID, n_groups=4, groups_kept=2, group_top=2, renormalize=1, route_scale=2.5)
+    return x, w_router, router, (torch.randn(E, generator=gen) * 0.05).to(DEV), gate_up, down
+
+
+def test_quantized_layer_from_rows_to_rows():
+    pk, _ = _pk()
+    rows = 77
+    x, w_router, router, bias, gate_up, down = layer_inputs(pk, rows)
+    out = torch.empty_like(x)
+    logits, experts, weights = layer(pk, x, w_router, router, bias, gate_up, down, out)
+    c, s = ref.quantize(x.cpu().double().numpy())
+    xq = ref.values(torch.from_numpy(ref.pack(c)), torch.from_numpy(s))
+    rv = ref.values(w_router[0].cpu(), w_router[1].cpu())
+    assert bool(((logits.cpu().double() - xq @ rv.t()).abs() <= product_bound(xq, rv, torch.float32)).all())
+    for i in range(rows):
+        e, w = ref.route_row(logits[i].cpu().double().numpy(), bias.cpu().double().numpy(), "sigmoid", 4, 2, 2, 3, True, 2.5)
+        assert experts[i].tolist() == e
+    want, bound = ref.experts(x.cpu().double(), ref.values(*(t.cpu() for t in gate_up)), ref.values(*(t.cpu() for t in down)), experts.cpu(), weights.cpu().double())
+    assert bool(((out.cpu().double() - want).abs() <= bound + 2.0 ** -8 * want.abs()).all())
+
+
+def test_captured_layers_replay_and_share_nothing():
+    """Two captured layers of different sizes, replayed in turn with eager calls between, on a stream of their own."""
+    pk, _ = _pk()
+    side = torch.cuda.Stream()
+    graphs = []
+    for rows, seed in [(70, 2), (9, 4)]:
+        ins = layer_inputs(pk, rows, seed=seed)
+        out = torch.zeros_like(ins[0])
+        layer(pk, *ins, out)
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            layer(pk, *ins, out, stream=side)
+        graphs.append((g, ins, out))
+    gen = torch.Generator().manual_seed(8)
+    for _ in range(3):
+        for g, ins, out in graphs:
+            ins[0].copy_(torch.randn(ins[0].shape, generator=gen))
+            out.fill_(7.0)
+            torch.cuda.synchronize()
+            g.replay()
+            torch.cuda.synchronize()
+            eager = torch.empty_like(out)
+            layer(pk, *ins, eager)
+            assert torch.equal(out, eager)
+
+
+def test_calls_on_two_streams_at_once():
+    pk, _ = _pk()
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    ins = [layer_inputs(pk, 40 + 30 * i, seed=20 + i) for i in range(3)]
+    want = []
+    for i in ins:
+        want.append(torch.empty_like(i[0]))
+        layer(pk, *i, want[-1])
+    torch.cuda.synchronize()
+    outs = [[torch.empty_like(i[0]) for _ in range(4)] for i in ins]
+    for n in range(4):
+        for s, i, o in zip(streams, ins, outs):
+            layer(pk, *i, o[n], stream=s)
+    torch.cuda.synchronize()
+    for w, o in zip(want, outs):
+        assert all(torch.equal(w, t) for t in o)
+
+
+# -- inside a context -------------------------------------------------------------------------
+def small(**over):
+    base = dict(n_layers=3, hidden=512, n_q_heads=8, n_kv_heads=2, ffn=1024, vocab=4096, mask_token_id=4095, batch=5, prefix_lo=70, prefix_hi=200,
+                prefix_dist="uniform", block_size=32, budget_mode=1, keep_ratio=0.25, steps=3, shuffle_pages=True, n_experts=16, experts_per_token=4,
+                expert_ffn=128, shared_ffn=96, route_scale=1.5, first_moe_layer=1)
+    base.update(over)
+    return fi.workload("c3_llada36", **base)
+
+
+MATRICES = ("w_gate_up", "w_down", "w_expert_gate_up", "w_expert_down", "w_shared_gate_up", "w_shared_down")
+
+
+def run_steps(pk, sess, n, steps, forced=None):
+    wl = sess.wl
+    logits = torch.zeros(n * wl.block_size, wl.vocab, device=DEV)
+    tokens = torch.zeros(n, wl.block_size, dtype=torch.int32, device=DEV)
+    keep = torch.zeros(n, dtype=torch.int64, device=DEV)
+    cu = torch.zeros(n + 1, dtype=torch.int32, device=DEV)
+    got = []
+    for _ in range(steps):
+        sess.focus.focus_step(n, out=pk.make_step_out(logits=logits, tokens=tokens, keep_bits=keep, cu_seqlens=cu), keep_override=forced)
+        torch.cuda.synchronize()
+        got.append(logits[:int(cu[n])].cpu().clone())
+    return got
+
+
+@pytest.mark.parametrize("which", ["all", "experts", "dense"])
+def test_context_on_mx_weights_equals_the_same_values_in_bf16(which):
+    """A context whose matrices were replaced by the values of the MXFP4 ones, against one that is given the codes: the same products, summed in
+    another order and rounded to bf16 between kernels, so the tolerance of the bf16 model's parity tests."""
+    pk, runner = _pk()
+    wl = small()
+    n, B = wl.batch, wl.block_size
+    names = MATRICES if which == "all" else MATRICES[2:4] if which == "experts" else MATRICES[:2]
+    forced = torch.tensor([(0x0F0F3311 * (b + 1)) & 0xFFFFFFFF for b in range(n)], dtype=torch.int64, device=DEV)
+    routes = torch.tensor(wl.route_override(n), dtype=torch.int32, device=DEV)
+    results = []
+    for mx in (False, True):
+        sess = runner.open_session(wl, DEV)
+        layers = []
+        for l, w in enumerate(sess.weights[3]):
+            pairs = {}
+            for name in names:
+                if name in w:
+                    t = w[name]
+                    c, s = pk.focus_mx_quantize(t.reshape(-1, t.shape[-1]))
+                    if not mx:
+                        pk.focus_mx_dequantize(c, s, t.view(-1, t.shape[-1]))
+                    pairs[name] = (c.view(*t.shape[:-1], -1), s.view(*t.shape[:-1], -1))
+            layers.append(pairs)
+        if mx:
+            sess.focus.focus_set_mx_weights(layers)
+        sess.focus.focus_set_route_override(routes)
+        results.append(run_steps(pk, sess, n, 2, forced))
+        if mx:                                                      # and back
+            sess.focus.focus_set_mx_weights(None)
+            sess.focus.focus_prefill_kv(sess.prefix_lens, sess.page_tables, None)
+            plain = run_steps(pk, sess, n, 1, forced)[0]
+            assert not torch.equal(plain, results[1][0])
+        sess.focus.focus_free()
+    for a, b in zip(*results):
+        assert float((a - b).abs().max() / a.abs().max()) <= 2e-2
+
+
+def test_context_with_the_configurations_own_router_written_out():
+    """softmax, no bias, no groups, renormalised: the picks of the built-in router."""
+    pk, runner = _pk()
+    wl = small(first_moe_layer=0)
+    n, B, k = wl.batch, wl.block_size, wl.experts_per_token
+    got = []
+    for own in (False, True):
+        sess = runner.open_session(wl, DEV)
+        if own:
+            sess.focus.focus_set_router(pk.focus_router(n_experts=wl.n_experts, experts_per_token=k, score=0, n_groups=1, groups_kept=1, group_top=1, renormalize=1,
+                                                        route_scale=wl.route_scale))
+        e = torch.full((wl.n_layers, n * B, k), -1, dtype=torch.int32, device=DEV)
+        w = torch.zeros(wl.n_layers, n * B, k, device=DEV)
+        sess.focus.focus_step(n, out=pk.make_step_out(route_experts=e, route_weights=w))
+        torch.cuda.synchronize()
+        got.append((e.cpu(), w.cpu()))
+        sess.focus.focus_free()
+    assert torch.equal(got[0][0][0], got[1][0][0])                  # the first layer's rows are the same rows
+    assert float((got[0][1][0] - got[1][1][0]).abs().max()) <= 1e-5 * wl.route_scale
+
+
+def test_context_with_a_grouped_sigmoid_router():
+    """fp32 model: the picks of the first layer against the plain router on the oracle's logits, where 1e-4 decides them; forced experts get this
+    router's weights."""
+    from oracle import focus_oracle as fo
+    from oracle.harness import oracle_batch
+    pk, runner = _pk()
+    wl = fi.workload("c1_tiny", n_layers=3, first_moe_layer=0, steps=1, n_experts=16, experts_per_token=4, expert_ffn=64, shared_ffn=32, route_scale=2.5)
+    cfg, W, pool, states, lens, tables, n_pages = oracle_batch(wl)
+    n, B, k, E = len(states), wl.block_size, 4, 16
+    gen = torch.Generator().manual_seed(1)
+    bias = (torch.randn(E, generator=gen) * 0.02).to(DEV)
+    r = pk.focus_router(n_experts=E, experts_per_token=k, score=1, n_groups=4, groups_kept=2, group_top=2, renormalize=1, route_scale=2.5)
+    for forced in (None, torch.tensor(wl.route_override(n), dtype=torch.int32, device=DEV)):
+        sess = runner.open_session(wl, DEV)
+        sess.focus.focus_set_router(r, [bias] * wl.n_layers)
+        sess.focus.focus_set_route_override(forced)
+        e = torch.full((wl.n_layers, n * B, k), -1, dtype=torch.int32, device=DEV)
+        w = torch.zeros(wl.n_layers, n * B, k, device=DEV)
+        sess.focus.focus_step(n, out=pk.make_step_out(route_experts=e, route_weights=w))
+        torch.cuda.synchronize()
+        routes = [[[int(x) for x in e[l, i]] if int(e[l, i, 0]) >= 0 else list(range(k)) for i in range(n * B)] for l in range(wl.n_layers)]
+        states_now = oracle_batch(wl)[3]
+        tr = fo.focus_step(cfg, W, pool, states_now, route_override=routes)
+        decided = 0
+        for rid, (experts, weights, logits) in tr.route[0].items():
+            chosen = e[0, rid].tolist()
+            given = None if forced is None else forced[0, rid].tolist()
+            want, wt = ref.route_row(logits, bias.cpu().double().numpy(), "sigmoid", 4, 2, 2, k, True, 2.5, given)
+            near = [ref.route_row(np.asarray(logits) + 1e-4 * s, bias.cpu().double().numpy(), "sigmoid", 4, 2, 2, k, True, 2.5, given)[0]
+                    for s in np.random.default_rng(rid).choice([-1.0, 1.0], (6, E))]
+            if all(v == want for v in near):
+                decided += 1
+                assert chosen == want, rid
+                assert np.max(np.abs(w[0, rid].cpu().numpy() - np.array(wt))) <= 1e-3
+        assert decided > n * B // 2
+        sess.focus.focus_free()
+
+
+def test_context_setters_refuse():
+    pk, runner = _pk()
+    wl = small()
+    sess = runner.open_session(wl, DEV)
+    f = sess.focus
+    ok = dict(n_experts=16, experts_per_token=4, score=1, n_groups=4, groups_kept=2, group_top=2, renormalize=1, route_scale=1.0)
+    for bad in (dict(n_experts=8), dict(experts_per_token=3), dict(n_groups=3), dict(route_scale=-1.0)):
+        with pytest.raises(pk.FocusError):
+            f.focus_set_router(pk.focus_router(**{**ok, **bad}))
+    with pytest.raises(pk.FocusError):
+        f.focus_set_router(pk.focus_router(**ok), [None])
+    up = tuple(t.view(16, 256, -1) for t in pk.focus_mx_quantize(torch.zeros(16 * 256, 512, device=DEV)))
+    down = tuple(t.view(16, 512, -1) for t in pk.focus_mx_quantize(torch.zeros(16 * 512, 128, device=DEV)))
+    pair = dict(w_expert_gate_up=up, w_expert_down=down)
+    for bad in ([pair, {}, {}], [{}, dict(w_expert_gate_up=up), {}], [{}, pair], [{}, dict(w_expert_gate_up=up, w_expert_down=up), {}]):
+        with pytest.raises(pk.FocusError):
+            f.focus_set_mx_weights(bad)
+    f.focus_set_mx_weights([{}, pair, {}])
+    f.focus_set_mx_weights(None)
+    f.focus_free()
+    sess = runner.open_session(fi.workload("c1_tiny"), DEV)
+    with pytest.raises(pk.FocusError):
+        sess.focus.focus_set_router(pk.focus_router(**ok))
+    z = pk.focus_mx_quantize(torch.zeros(2048, 256, device=DEV))
+    zd = pk.focus_mx_quantize(torch.zeros(256, 1024, device=DEV))
+    with pytest.raises(pk.FocusError):                              # an fp32 model
+        sess.focus.focus_set_mx_weights([dict(w_gate_up=z, w_down=zd)] * 2)
+    sess.focus.focus_free()
