@@ -3,6 +3,7 @@
 // Two forms.  bf16 rows: codes become bf16 in registers (a 4-bit float times a power of two is exact in bf16) and go through
 // v_mfma_f32_32x32x16_bf16.  MXFP4 rows: codes and scales go as they are through v_mfma_scale_f32_32x32x64_f8f6f4, four times the rate.
 #include <algorithm>
+#include <type_traits>
 
 #include "focus_mx.h"
 
@@ -39,20 +40,32 @@ struct RowsArgs {
 };
 enum { RM_STORE, RM_STORE_F32, RM_ADD_F32, RM_SILU, RM_PARTIAL };
 
-// A workgroup (4 wavefronts) takes up to BM rows and 128 rows of W; the wavefronts lie side by side, each BM x 32, so that every code is
-// converted once, and tile rows of 32 that hold no rows are skipped.  K goes in steps of 64 of the rows (128 bytes a row) and slabs of 128 of the
-// codes (64 bytes a row), straight into LDS.  Lane l multiplies elements 32 h .. 32 h + 31 of a step, h = l / 32: one block of its weight
-// row, so one scale; the order of the elements within a step is the same for both operands and does not matter otherwise.
-constexpr int ahead_of(int bm) { return bm > 32 ? 2 : 6; }      // steps between asking for data and using it (even)
-constexpr int rows_lds(int bm) { return (ahead_of(bm) + 1) * bm * 128 + (ahead_of(bm) / 2 + 2) * (8192 + 1024); }
+// the 8 scales of blocks b0 .. b0 + 7 of a row of `blocks`; those beyond the row are 0 (2^-127: their codes are zeros)
+__device__ __forceinline__ uint64_t eight_scales(const unsigned char *row, int b0, int blocks) {
+  uint64_t v = 0;
+  if (blocks >= 8) {
+    const int over = max(0, b0 + 8 - blocks);
+    __builtin_memcpy(&v, row + (b0 - over), 8);
+    return over >= 8 ? 0 : v >> (8 * over);
+  }
+  for (int j = 0; j < 8; ++j)
+    if (b0 + j < blocks) v |= (uint64_t)row[b0 + j] << (8 * j);
+  return v;
+}
 
-template <int BM, int MODE, bool GROUPED, bool WHOLE>      // WHOLE: K is a multiple of 128
+// A workgroup (4 wavefronts) takes up to BM rows and 128 CT rows of W; the wavefronts lie side by side, each BM x 32 CT, so that every code is
+// read and converted by one wavefront; tile rows of 32 that hold no rows are skipped.  K goes in steps of 64 (128 bytes of a row of A, through LDS,
+// DA steps ahead) and slabs of 256 (128 bytes of a row of W: a whole line, straight into registers, a slab ahead).  Lane l multiplies elements
+// 32 h .. 32 h + 31 of a step, h = l / 32: one block of its weight row, so one scale; the order of the elements within a step is the same for
+// both operands and does not matter otherwise.
+constexpr int kAhead = 4;      // steps between asking for rows and using them: those of a slab
+
+template <int BM, int CT, int MODE, bool GROUPED, bool WHOLE>      // WHOLE: K is a multiple of 256
 __global__ __launch_bounds__(256, 2) void k_mx_rows(RowsArgs g) {
 #if defined(__HIP_DEVICE_COMPILE__)   // buffer-resource builtins exist in the device pass only
-  constexpr int TM = BM / 32, IA = BM / 32, DA = ahead_of(BM), SA = DA + 1, DW = DA / 2 + 1, SW = DW + 1;
-  constexpr int ASTAGE = BM * 128, WSTAGE = 8192, SSTAGE = 1024, WBASE = SA * ASTAGE, SBASE = WBASE + SW * WSTAGE;
+  constexpr int TM = BM / 32, DA = kAhead, SA = DA + 1, ASTAGE = BM * 128;
   constexpr bool SILU = MODE == RM_SILU;
-  __shared__ __attribute__((aligned(1024))) unsigned char lds[rows_lds(BM)];
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[SA * ASTAGE];
   const int splits = GROUPED ? 1 : g.splits;
   const int M = GROUPED ? 0 : g.rows.count ? min(*g.rows.count, g.rows.cap) : g.rows.cap;
   const int tiles_m = GROUPED ? *g.n_tiles : (M + BM - 1) / BM, total = tiles_m * g.tiles_n * splits, per_xcd = (total + 7) / 8;
@@ -69,9 +82,10 @@ __global__ __launch_bounds__(256, 2) void k_mx_rows(RowsArgs g) {
   } else {
     valid = min(BM, M - row0);
   }
-  const int N = g.N, K = g.K, n0 = nt * (SILU ? 64 : 128), blocks = K / 32;
-  const int slabs = (blocks + 3) / 4, per_split = (slabs + splits - 1) / splits, slab0 = split * per_split;
-  const int my_slabs = min(slabs - slab0, per_split), steps = 2 * my_slabs;          // slabs of this workgroup (0 or less: zeros)
+  const int N = g.N, K = g.K, n0 = nt * (SILU ? 64 * CT : 128 * CT), blocks = K / 32;
+  const int slabs = (blocks + 7) / 8, per_split = (slabs + splits - 1) / splits, slab0 = split * per_split;
+  const int my_slabs = min(slabs - slab0, per_split);                                // slabs of this workgroup (0 or less: zeros)
+  const int my_steps = (min(K, (slab0 + my_slabs) * 256) - slab0 * 256 + 63) / 64;   // steps that hold anything
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int frow = lane & 31, h = lane >> 5, live = (valid + 31) / 32;
   const unsigned char *const codes = g.codes + (size_t)e * N * (size_t)(K / 2), *const scales = g.scales + (size_t)e * N * (size_t)blocks;
@@ -80,161 +94,183 @@ __global__ __launch_bounds__(256, 2) void k_mx_rows(RowsArgs g) {
   __amdgpu_buffer_rsrc_t rs_a = __builtin_amdgcn_make_buffer_rsrc((void *)A, 0, gather ? g.a_bytes : (unsigned)(((int64_t)(valid - 1) * g.lda + K) * 2), 0x00020000);
   __amdgpu_buffer_rsrc_t rs_w = __builtin_amdgcn_make_buffer_rsrc((void *)codes, 0, (unsigned)N * (unsigned)(K / 2), 0x00020000);
   __amdgpu_buffer_rsrc_t rs_s = __builtin_amdgcn_make_buffer_rsrc((void *)scales, 0, (unsigned)N * (unsigned)blocks, 0x00020000);
-  // chunk (8 elements) of a step that this lane fetches for row r of the tile: swizzled so that LDS reads spread over the banks
-  unsigned voa[IA];
-  int ca[IA];
+  // chunk (8 elements) of a step that this lane fetches for row 32 q + 8 wave + lane / 8 of the tile: swizzled so that LDS reads spread over
+  // the banks (16 q + 4 wave + lane / 16 is half the row)
+  const int ca = (lane & 7) ^ ((4 * (wave & 1) + (lane >> 4)) & 7);
+  unsigned voa[TM];
 #pragma unroll
-  for (int q = 0; q < IA; ++q) {
-    const int r = (wave * IA + q) * 8 + (lane >> 3);
-    ca[q] = (lane & 7) ^ ((r >> 1) & 7);
-    const int srow = r < valid ? (gather ? g.src[row0 + r] : r) : -1;
-    voa[q] = srow < 0 ? kOutside : (unsigned)srow * (unsigned)g.lda * 2u + ca[q] * 16;
+  for (int q = 0; q < TM; ++q) {
+    const int r = q * 32 + wave * 8 + (lane >> 3), srow = r < valid ? (gather ? g.src[row0 + r] : r) : -1;
+    voa[q] = srow < 0 ? kOutside : (unsigned)srow * (unsigned)g.lda * 2u + ca * 16;
   }
-  // the matrix row of row r (0..31) of this wavefront's columns: with SiLU*up 16 gate rows, then the 16 matching up rows
-  auto weight_row = [&](int r) {
+  // the matrix row of this lane's column in column tile j.  SiLU*up: with two tiles a wavefront gate and up of the same 32 columns; with
+  // one 16 gate rows, then the 16 matching up rows
+  unsigned vow[CT], vos[CT];
+#pragma unroll
+  for (int j = 0; j < CT; ++j) {
+    int row;
     if (SILU) {
-      const int c = n0 + wave * 16 + (r & 15);
-      return c < N / 2 ? (r >> 4) * (N / 2) + c : -1;
+      const int c = CT == 2 ? n0 + wave * 32 + frow : n0 + wave * 16 + (frow & 15);
+      row = c < N / 2 ? (CT == 2 ? j : frow >> 4) * (N / 2) + c : -1;
+    } else {
+      const int c = n0 + (wave * CT + j) * 32 + frow;
+      row = c < N ? c : -1;
     }
-    const int c = n0 + wave * 32 + r;
-    return c < N ? c : -1;
-  };
-  unsigned vow[2];
-  const int cw[2] = {(lane & 3) ^ ((lane >> 4) & 3), (lane & 3) ^ ((lane >> 4) & 3)};
-#pragma unroll
-  for (int p = 0; p < 2; ++p) {
-    const int wr = weight_row(p * 16 + (lane >> 2));
-    vow[p] = wr < 0 ? kOutside : (unsigned)wr * (unsigned)(K / 2) + cw[p] * 16;
+    vow[j] = row < 0 ? kOutside : (unsigned)row * (unsigned)(K / 2) + h * 16;
+    vos[j] = (unsigned)max(row, 0) * (unsigned)blocks;
   }
-  const int srow = weight_row(frow);
-  const unsigned vos = srow < 0 || h ? kOutside : (unsigned)srow * (unsigned)blocks;
 
-  auto issue_a = [&](int step, int stage) {
-    const int k0 = slab0 * 128 + step * 64;
-    const unsigned so = step < steps && k0 < K ? (unsigned)k0 * 2u : kOutside;
-    const bool half = !WHOLE && k0 + 32 >= K;           // the second block of the step does not exist
+  u32x4 w[CT][4];
+  uint64_t sc[CT];
+  // two chunks of a slab's codes, q and q + 1
+  auto load_w = [&](int slab, int q0) __attribute__((always_inline)) {
+    const unsigned so = slab < my_slabs ? (unsigned)(slab0 + slab) * 128u : kOutside;
 #pragma unroll
-    for (int q = 0; q < IA; ++q)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs_a, FK_LDS_PTR(lds + stage * ASTAGE + (wave * IA + q) * 1024), 16, half && ca[q] >= 4 ? kOutside : voa[q], so, 0, 0);
-  };
-  auto issue_w = [&](int slab, int stage, int part) {
-    const unsigned so = slab < my_slabs ? (unsigned)(slab0 + slab) * 64u : kOutside;
-    const unsigned v = !WHOLE && (slab0 + slab) * 4 + cw[part] >= blocks ? kOutside : vow[part];
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(rs_w, FK_LDS_PTR(lds + WBASE + stage * WSTAGE + (wave * 2 + part) * 1024), 16, v, so, 0, 0);
-  };
-  auto issue_s = [&](int slab, int stage) {
-    unsigned char *to = lds + SBASE + stage * SSTAGE + wave * 256;
-    if (WHOLE) {
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs_s, FK_LDS_PTR(to), 4, vos, slab < my_slabs ? (unsigned)(slab0 + slab) * 4u : kOutside, 0, 0);
-    } else if (slab < my_slabs && h == 0) {              // rows of scales are not aligned: byte by byte
-      unsigned s = 0;
+    for (int j = 0; j < CT; ++j)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int b = (slab0 + slab) * 4 + j;
-        s |= (unsigned)__builtin_amdgcn_raw_buffer_load_b8(rs_s, b < blocks && vos != kOutside ? vos + b : kOutside, 0, 0) << (8 * j);
-      }
-      *(unsigned *)(to + frow * 4) = s;
+      for (int q = q0; q < q0 + 2; ++q)
+        w[j][q] = __builtin_amdgcn_raw_buffer_load_b128(rs_w, !WHOLE && (slab0 + slab) * 8 + 2 * q + h >= blocks ? kOutside : vow[j] + q * 32, so, 0);
+  };
+  auto load_scales = [&](int slab) __attribute__((always_inline)) {
+    const int b0 = (slab0 + min(slab, my_slabs - 1)) * 8;
+#pragma unroll
+    for (int j = 0; j < CT; ++j) {
+      if (WHOLE) sc[j] = __builtin_bit_cast(uint64_t, __builtin_amdgcn_raw_buffer_load_b64(rs_s, vos[j], b0, 0));
+      else sc[j] = eight_scales(scales + vos[j], b0, blocks);
     }
   };
 
-  f32x16 acc[TM];
+  f32x16 acc[TM][CT];
 #pragma unroll
   for (int i = 0; i < TM; ++i)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) acc[i][r] = 0.f;
+    for (int j = 0; j < CT; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
 
-  // step s asks for the rows of step s + DA and half of the codes of slab s / 2 + DW; even steps also for that slab's scales.  So a step's codes
-  // and scales were asked for before its rows.
-  issue_w(0, 0, 0);
-  issue_w(0, 0, 1);
-  issue_s(0, 0);
+  const int swz_a = (frow >> 1) & 7;
+  // L: tile rows of 32 that hold rows.  The loop exists once for each, since a branch around each tile row kept the fragments' LDS reads
+  // from being asked for ahead.
+  auto multiply = [&](auto rows_live) __attribute__((always_inline)) {
+    constexpr int L = decltype(rows_live)::value;
+    auto issue_a = [&](int step, int stage) __attribute__((always_inline)) {
+      const int k0 = slab0 * 256 + step * 64;
+      const unsigned so = step < my_steps ? (unsigned)k0 * 2u : kOutside;
+      const bool half = !WHOLE && k0 + 32 >= K;           // the second block of the step does not exist
 #pragma unroll
-  for (int s = 0; s < DA; ++s) {
-    issue_a(s, s);
-    issue_w(s / 2 + 1, s / 2 + 1, s & 1);
-    if (!(s & 1)) issue_s(s / 2 + 1, s / 2 + 1);
-  }
-  constexpr int FLY = WHOLE ? DA / 2 * (IA + 1) + (DA / 2 - 1) * (IA + 2) + 2 : DA / 2 * (IA + 1) + (DA / 2 - 1) * (IA + 1) + 1;
-  int sa = 0, sw = 0, la = DA % SA, lw = DW % SW;       // stages of this step's data and of the loads it makes
-  const int swz_a = (frow >> 1) & 7, swz_w = (frow >> 2) & 3;
-  for (int slab = 0; slab < my_slabs; ++slab) {
+      for (int q = 0; q < L; ++q)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rs_a, FK_LDS_PTR(lds + stage * ASTAGE + (q * 4 + wave) * 1024), 16, half && ca >= 4 ? kOutside : voa[q], so, 0, 0);
+    };
+    // in the order in which the loop asks for them, so that its count of younger loads holds from the first step on
 #pragma unroll
-    for (int q = 0; q < 2; ++q) {
-      // all but the youngest FLY loads have landed: the rows of this step, and older ones; everyone has finished the step before
-      __builtin_amdgcn_s_waitcnt(vmcnt_imm(FLY));
-      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-      issue_a(2 * slab + q + DA, la);
-      issue_w(slab + DW, lw, q);
-      if (q == 0) issue_s(slab + DW, lw);
-      const unsigned char *pa = lds + sa * ASTAGE, *pw = lds + WBASE + sw * WSTAGE + (wave * 32 + frow) * 64;
-      const unsigned sc = *(const unsigned *)(lds + SBASE + sw * SSTAGE + wave * 256 + frow * 4);
-      const u32x4 wv = *(const u32x4 *)(pw + (((2 * q + h) ^ swz_w) << 4));
-      const float scale = __uint_as_float(((sc >> (8 * (2 * q + h))) & 255u) << 23);
-#pragma unroll
-      for (int ks = 0; ks < 4; ++ks) {
-        const bf16x2 b0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(wv[ks], scale, 0), b1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(wv[ks], scale, 1);
-        const bf16x2 b2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(wv[ks], scale, 2), b3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(wv[ks], scale, 3);
-        const bf16x8 fb = {b0[0], b0[1], b1[0], b1[1], b2[0], b2[1], b3[0], b3[1]};
-#pragma unroll
-        for (int i = 0; i < TM; ++i)
-          if (i < live) {
-            const bf16x8 fa = *(const bf16x8 *)(pa + (i * 32 + frow) * 128 + (((4 * h + ks) ^ swz_a) << 4));
-            acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa, fb, acc[i], 0, 0, 0);
-          }
-      }
-      sa = sa == SA - 1 ? 0 : sa + 1;
-      la = la == SA - 1 ? 0 : la + 1;
+    for (int s = 0; s < DA; ++s) {
+      issue_a(s, s);
+      if (s & 1) load_w(0, s - 1);
+      if (s == 3) load_scales(0);
     }
-    sw = sw == SW - 1 ? 0 : sw + 1;
-    lw = lw == SW - 1 ? 0 : lw + 1;
-  }
+    int sa = 0, la = DA % SA;       // stages of this step's rows and of the loads it makes
+    for (int slab = 0; slab < my_slabs; ++slab) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        // younger than the rows of this step: those of the three steps after it, four chunks of codes and a slab's scales
+        __builtin_amdgcn_s_waitcnt(vmcnt_imm((DA - 1) * L + (WHOLE ? 5 : 4) * CT));
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");      // everyone has finished the step before
+        issue_a(4 * slab + q + DA, la);
+        const unsigned char *pa = lds + sa * ASTAGE;
+        if (WHOLE || 4 * slab + q < my_steps) {
+          float scale[CT];
+#pragma unroll
+          for (int j = 0; j < CT; ++j) {
+            const unsigned x = (unsigned)((sc[j] >> (8 * h)) >> (32 * (q >> 1)));       // byte 2 (q & 1) is the scale of block 2 q + h
+            scale[j] = __uint_as_float(((q & 1) ? x << 7 : x << 23) & 0x7F800000u);
+          }
+#pragma unroll
+          for (int ks = 0; ks < 4; ++ks) {
+            bf16x8 fb[CT], fa[L];
+#pragma unroll
+            for (int i = 0; i < L; ++i) fa[i] = *(const bf16x8 *)(pa + (i * 32 + frow) * 128 + (((4 * h + ks) ^ swz_a) << 4));
+#pragma unroll
+            for (int j = 0; j < CT; ++j) {
+              const unsigned c = w[j][q][ks];
+              const bf16x2 b0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale[j], 0), b1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale[j], 1);
+              const bf16x2 b2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale[j], 2), b3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale[j], 3);
+              fb[j] = bf16x8{b0[0], b0[1], b1[0], b1[1], b2[0], b2[1], b3[0], b3[1]};
+            }
+#pragma unroll
+            for (int i = 0; i < L; ++i)
+#pragma unroll
+              for (int j = 0; j < CT; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[i], fb[j], acc[i][j], 0, 0, 0);
+          }
+        }
+        // into the registers just used
+        if (q & 1) load_w(slab + 1, q - 1);
+        if (q == 3) load_scales(slab + 1);
+        sa = sa == SA - 1 ? 0 : sa + 1;
+        la = la == SA - 1 ? 0 : la + 1;
+      }
+    }
+  };
+  if (my_slabs <= 0) {}
+  else if (TM == 1 || live == 1) multiply(std::integral_constant<int, 1>());
+  else if (live == 2) multiply(std::integral_constant<int, TM < 2 ? 1 : 2>());
+  else if (live == 3) multiply(std::integral_constant<int, TM < 3 ? 1 : 3>());
+  else multiply(std::integral_constant<int, TM>());
   __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
   // register r of lane l is C[8 (r / 4) + 4 (l / 32) + r % 4][l % 32] of its 32 x 32 tile
   if (SILU) {
-    // lanes 0..15 of a half hold gate columns, 16..31 the matching up columns: exchanging halves between two registers gives the lower
-    // lanes both numbers of register r and the upper lanes both of register r + 1
-    const int gn = n0 + wave * 16 + (lane & 15);
+    // one column tile: lanes 0..15 of a half hold gate columns, 16..31 the matching up columns; exchanging halves between two registers gives
+    // the lower lanes both numbers of register r and the upper lanes both of register r + 1
+    const int gn = CT == 2 ? n0 + wave * 32 + frow : n0 + wave * 16 + (lane & 15);
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
-      for (int r = 0; r < 16; r += 2) {
-        const u32x2 x = __builtin_amdgcn_permlane16_swap(__float_as_uint(acc[i][r]), __float_as_uint(acc[i][r + 1]), false, false);
-        const float ga = __uint_as_float(x[0]), up = __uint_as_float(x[1]);
-        const int rr = r + ((lane >> 4) & 1), gm = i * 32 + 8 * (rr >> 2) + 4 * h + (rr & 3);
+      for (int r = 0; r < 16; r += CT == 2 ? 1 : 2) {
+        float ga = acc[i][0][r], up = acc[i][CT - 1][r];
+        int rr = r;
+        if (CT == 1) {
+          const u32x2 x = __builtin_amdgcn_permlane16_swap(__float_as_uint(acc[i][0][r]), __float_as_uint(acc[i][0][(r + 1) & 15]), false, false);
+          ga = __uint_as_float(x[0]); up = __uint_as_float(x[1]);
+          rr = r + ((lane >> 4) & 1);
+        }
+        const int gm = i * 32 + 8 * (rr >> 2) + 4 * h + (rr & 3);
         // exp overflows to infinity and the quotient to 0 for a large negative gate
         if (gm < valid && gn < N / 2) ((bf16_t *)g.out)[(size_t)(row0 + gm) * g.ldo + gn] = (bf16_t)(ga / (1.0f + __expf(-ga)) * up);
       }
     return;
   }
-  const int gn = n0 + wave * 32 + frow;
 #pragma unroll
   for (int i = 0; i < TM; ++i)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int gm = i * 32 + 8 * (r >> 2) + 4 * h + (r & 3);
-      if (gm < valid && gn < N) {
-        const size_t at = (size_t)(row0 + gm) * g.ldo + gn;
-        if (MODE == RM_STORE) ((bf16_t *)g.out)[at] = (bf16_t)acc[i][r];
-        else if (MODE == RM_ADD_F32) ((float *)g.out)[at] += acc[i][r];
-        else (MODE == RM_PARTIAL ? (float *)g.out + (size_t)split * g.split_stride : (float *)g.out)[at] = acc[i][r];
+    for (int j = 0; j < CT; ++j) {
+      const int gn = n0 + (wave * CT + j) * 32 + frow;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int gm = i * 32 + 8 * (r >> 2) + 4 * h + (r & 3);
+        if (gm < valid && gn < N) {
+          const size_t at = (size_t)(row0 + gm) * g.ldo + gn;
+          if (MODE == RM_STORE) ((bf16_t *)g.out)[at] = (bf16_t)acc[i][j][r];
+          else if (MODE == RM_ADD_F32) ((float *)g.out)[at] += acc[i][j][r];
+          else (MODE == RM_PARTIAL ? (float *)g.out + (size_t)split * g.split_stride : (float *)g.out)[at] = acc[i][j][r];
+        }
       }
     }
 #endif
 }
 
-template <int BM, int MODE, bool GROUPED>
-void launch_rows(hipStream_t s, const RowsArgs &g, int tile_slots) {
+template <int BM, int CT, int MODE, bool GROUPED>
+void launch_rows(hipStream_t s, RowsArgs g, int tile_slots) {
+  g.tiles_n = MODE == RM_SILU ? (g.N / 2 + 64 * CT - 1) / (64 * CT) : (g.N + 128 * CT - 1) / (128 * CT);
   const int grid = (tile_slots * g.tiles_n * (GROUPED ? 1 : g.splits) + 7) / 8 * 8;
-  if (g.K % 128 == 0) k_mx_rows<BM, MODE, GROUPED, true><<<grid, 256, 0, s>>>(g);
-  else k_mx_rows<BM, MODE, GROUPED, false><<<grid, 256, 0, s>>>(g);
+  if (g.K % 256 == 0) k_mx_rows<BM, CT, MODE, GROUPED, true><<<grid, 256, 0, s>>>(g);
+  else k_mx_rows<BM, CT, MODE, GROUPED, false><<<grid, 256, 0, s>>>(g);
 }
-template <int BM>
+template <int BM, int CT>
 void launch_rows(hipStream_t s, int mode, const RowsArgs &g, int tile_slots) {
-  if (mode == RM_STORE) launch_rows<BM, RM_STORE, false>(s, g, tile_slots);
-  else if (mode == RM_STORE_F32) launch_rows<BM, RM_STORE_F32, false>(s, g, tile_slots);
-  else if (mode == RM_ADD_F32) launch_rows<BM, RM_ADD_F32, false>(s, g, tile_slots);
-  else if (mode == RM_SILU) launch_rows<BM, RM_SILU, false>(s, g, tile_slots);
-  else launch_rows<BM, RM_PARTIAL, false>(s, g, tile_slots);
+  if (mode == RM_STORE) launch_rows<BM, CT, RM_STORE, false>(s, g, tile_slots);
+  else if (mode == RM_STORE_F32) launch_rows<BM, CT, RM_STORE_F32, false>(s, g, tile_slots);
+  else if (mode == RM_ADD_F32) launch_rows<BM, CT, RM_ADD_F32, false>(s, g, tile_slots);
+  else if (mode == RM_SILU) launch_rows<BM, CT, RM_SILU, false>(s, g, tile_slots);
+  else launch_rows<BM, CT, RM_PARTIAL, false>(s, g, tile_slots);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -249,19 +285,6 @@ struct MxArgs {
   size_t split_stride;
 };
 enum { XM_STORE, XM_STORE_F32, XM_PARTIAL };
-
-// the 8 scales of blocks b0 .. b0 + 7 of a row of `blocks`; those beyond the row are 0 (2^-127: their codes are zeros)
-__device__ __forceinline__ uint64_t eight_scales(const unsigned char *row, int b0, int blocks) {
-  uint64_t v = 0;
-  if (blocks >= 8) {
-    const int over = max(0, b0 + 8 - blocks);
-    __builtin_memcpy(&v, row + (b0 - over), 8);
-    return over >= 8 ? 0 : v >> (8 * over);
-  }
-  for (int j = 0; j < 8; ++j)
-    if (b0 + j < blocks) v |= (uint64_t)row[b0 + j] << (8 * j);
-  return v;
-}
 
 template <int BM, int BN, int MODE>
 __global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void k_mx_mx(MxArgs g) {
@@ -420,8 +443,8 @@ void launch_reduce(hipStream_t s, int epi, const float *part, int splits, size_t
   else k_mx_reduce<MX_SILU_MUL><<<grid, 256, 0, s>>>(part, splits, stride, rows, n, out, ldo);
 }
 
-// Parts of K for `tiles` workgroups of which `resident` run at once: as many as fill the chip, each with 4 slabs at least.
-int parts_of(int tiles, int resident, int slabs) { return std::max(1, std::min(resident / std::max(1, tiles), slabs / 4)); }
+// Parts of K for `tiles` workgroups of which `resident` run at once: as many as fill the chip, each with 2 slabs at least.
+int parts_of(int tiles, int resident, int slabs) { return std::max(1, std::min(resident / std::max(1, tiles), slabs / 2)); }
 // parts with no slab left over are dropped
 int whole_parts(int parts, int slabs) { const int per = (slabs + parts - 1) / parts; return (slabs + per - 1) / per; }
 
@@ -433,8 +456,9 @@ Shape shape_of(int rows, int n, int k, bool a_mx) {
     const int tiles = ((rows + 127) / 128) * ((n + 127) / 128);
     return {128, 128, whole_parts(parts_of(tiles, 512, slabs), std::max(1, slabs))};
   }
-  const int bm = rows <= 32 ? 32 : 128, slabs = (k / 32 + 3) / 4, tiles = ((rows + bm - 1) / bm) * ((n + 127) / 128);
-  return {bm, 128, whole_parts(parts_of(tiles, 512, slabs), std::max(1, slabs))};
+  const int bm = rows <= 32 ? 32 : 128, slabs = (k / 32 + 7) / 8, tiles_m = (rows + bm - 1) / bm, wide = tiles_m * ((n + 255) / 256);
+  if (bm == 128 && wide >= 256) return {bm, 256, 1};
+  return {bm, 128, whole_parts(parts_of(tiles_m * ((n + 127) / 128), 512, slabs), std::max(1, slabs))};
 }
 
 }  // namespace
@@ -449,7 +473,7 @@ void mx_gemm(hipStream_t s, const void *a, const void *a_scales, int64_t lda, fo
   const bool a_mx = a_scales != nullptr;
   Shape p = shape_of(rows.cap, n, k, a_mx);
   const size_t stride = (size_t)rows.cap * n;
-  const int slabs = (k / 32 + (a_mx ? 7 : 3)) / (a_mx ? 8 : 4);
+  const int slabs = (k / 32 + 7) / 8;
   if (p.splits > 1) p.splits = whole_parts((int)std::max<size_t>(1, std::min<size_t>(p.splits, scratch.ptr ? scratch.bytes / (stride * 4) : 0)), slabs);
   const bool parts = p.splits > 1;
   if (a_mx) {
@@ -462,11 +486,10 @@ void mx_gemm(hipStream_t s, const void *a, const void *a_scales, int64_t lda, fo
     RowsArgs g{};
     g.A = (const bf16_t *)a; g.lda = lda; g.codes = (const unsigned char *)w.codes; g.scales = (const unsigned char *)w.scales; g.N = n; g.K = k; g.rows = rows;
     g.splits = p.splits; g.split_stride = stride; g.out = parts ? scratch.ptr : out; g.ldo = parts ? n : ldo;
-    const bool silu = epilogue == MX_SILU_MUL && !parts;
-    g.tiles_n = silu ? (n / 2 + 63) / 64 : (n + 127) / 128;
     const int mode = parts ? RM_PARTIAL : epilogue == MX_STORE ? RM_STORE : epilogue == MX_STORE_F32 ? RM_STORE_F32 : epilogue == MX_ADD_F32 ? RM_ADD_F32 : RM_SILU;
-    if (p.bm == 32) launch_rows<32>(s, mode, g, (rows.cap + 31) / 32);
-    else launch_rows<128>(s, mode, g, (rows.cap + 127) / 128);
+    if (p.bm == 32) launch_rows<32, 1>(s, mode, g, (rows.cap + 31) / 32);
+    else if (p.bn == 256) launch_rows<128, 2>(s, mode, g, (rows.cap + 127) / 128);
+    else launch_rows<128, 1>(s, mode, g, (rows.cap + 127) / 128);
   }
   if (parts) launch_reduce(s, epilogue, (const float *)scratch.ptr, p.splits, stride, rows, n, out, ldo);
 }
@@ -476,12 +499,12 @@ void mx_grouped(hipStream_t s, const MxGroups &g, const void *x, int64_t ldx, in
   a.A = (const bf16_t *)x; a.lda = ldx; a.src = g.src; a.a_bytes = (unsigned)(((int64_t)(n_rows - 1) * ldx + hidden) * 2);
   a.codes = (const unsigned char *)gate_up.codes; a.scales = (const unsigned char *)gate_up.scales;
   a.N = 2 * ffn; a.K = hidden; a.offs = g.offs; a.count = g.count; a.tile_e = g.tile_e; a.tile_m0 = g.tile_m0; a.n_tiles = g.n_tiles;
-  a.tiles_n = (ffn + 63) / 64; a.splits = 1; a.out = act; a.ldo = ffn;
-  launch_rows<128, RM_SILU, true>(s, a, g.n_tile_slots);
+  a.splits = 1; a.out = act; a.ldo = ffn;
+  launch_rows<128, 2, RM_SILU, true>(s, a, g.n_tile_slots);
   a.A = (const bf16_t *)act; a.lda = ffn; a.src = nullptr; a.a_bytes = 0;
   a.codes = (const unsigned char *)down.codes; a.scales = (const unsigned char *)down.scales;
-  a.N = hidden; a.K = ffn; a.tiles_n = (hidden + 127) / 128; a.out = y; a.ldo = hidden;
-  launch_rows<128, RM_STORE_F32, true>(s, a, g.n_tile_slots);
+  a.N = hidden; a.K = ffn; a.out = y; a.ldo = hidden;
+  launch_rows<128, 2, RM_STORE_F32, true>(s, a, g.n_tile_slots);
 }
 
 // ---------------------------------------------------------------------------------------------
