@@ -486,6 +486,10 @@ void moe_ffn(focus_ctx *c, hipStream_t s, int l, const RowSet &rs, float *resid,
   a.out_weights = c->route_by_row_id && c->out_route_weights ? c->out_route_weights + (size_t)l * plane : nullptr;
   { Timed t(c, s, FOCUS_KC_GEMM);
     fk::gemm(s, g.dtype, normed, c->w_router[l], g.n_experts, g.hidden, rs.rows, fk::EPI_STORE_F32, c->at<float>(pl.off_moe_logits), g.n_experts, c->layer_scratch(pl)); }
+  // MXFP4 experts work in the same buffers: the counts where the lists of entries would be, the tiles over the two arrays of tiles (one behind the other)
+  const focus_mx mx = c->mx_of(c->mx_expert_gate_up, l);
+  fk::MxExperts m{g.n_experts, g.hidden, g.expert_ffn, g.experts_per_token, mx, c->mx_of(c->mx_expert_down, l), a.rows, a.u, g.hidden, a.topk_idx, a.topk_w,
+                  FOCUS_F32, resid, g.hidden, true, a.list, (int2 *)a.tile_e, a.n_tiles, a.pos, a.arow, a.act, a.y};
   { Timed t(c, s, FOCUS_KC_ROUTE);
     if (c->has_router) {
       const float *bias = c->router_bias.empty() ? nullptr : c->router_bias[l];
@@ -493,19 +497,17 @@ void moe_ffn(focus_ctx *c, hipStream_t s, int l, const RowSet &rs, float *resid,
     } else {
       fk::moe_route(s, a);
     }
-    fk::moe_group(s, a); }
+    if (mx.codes) fk::mx_group(s, m);
+    else fk::moe_group(s, a); }
   { Timed t(c, s, FOCUS_KC_EXPERTS);
-    static_assert(fk::kMxTileRows == fk::kMoeTileRows, "both grouped products walk the tiles of moe_group()");
-    const focus_mx mx = c->mx_of(c->mx_expert_gate_up, l);
-    if (mx.codes)
-      fk::mx_grouped(s, fk::MxGroups{a.offs, a.count, a.tile_e, a.tile_m0, a.n_tiles, a.n_tile_slots, a.arow}, a.u, g.hidden, a.rows.cap, mx,
-                     c->mx_of(c->mx_expert_down, l), g.hidden, g.expert_ffn, a.act, a.y);
-    else
-      fk::moe_experts(s, a); }
+    if (mx.codes) fk::mx_grouped(s, m);
+    else fk::moe_experts(s, a); }
   // the shared expert adds into the residual stream before the routed sum (both orders are the same sum)
   if (g.shared_ffn > 0) swiglu_ffn(c, s, rs, nullptr, normed, c->w_shared_gate_up[l], c->w_shared_down[l], c->mx_of(c->mx_shared_gate_up, l),
                                    c->mx_of(c->mx_shared_down, l), g.shared_ffn, resid);
-  { Timed t(c, s, FOCUS_KC_ROUTE); fk::moe_combine(s, a); }
+  { Timed t(c, s, FOCUS_KC_ROUTE);
+    if (mx.codes) fk::mx_combine(s, m);
+    else fk::moe_combine(s, a); }
 }
 
 // Launch order and splits of the attention over a row set of its own.

@@ -45,7 +45,7 @@ void mx_gemm(hipStream_t s, const void *a, const void *a_scales, int64_t lda, fo
 
 // Routed experts.  Entries (row, choice) are sorted by expert into tiles of kMxTileRows rows, multiplied expert by expert, and
 // added up row by row.
-constexpr int kMxTileRows = 128;
+constexpr int kMxTileRows = 128, kMxMaxExperts = 512;
 struct MxExperts {
   int n_experts, hidden, ffn, k;
   focus_mx gate_up, down;
@@ -58,25 +58,21 @@ struct MxExperts {
   void *out;
   int64_t ldo;
   bool add;
-  // work buffers: mx_experts_bytes() / lay_mx_experts()
-  int32_t *hist;                  // [entry chunks, E]
-  int32_t *offs, *count;          // [E + 1], [E]: first sorted row and rows of every expert
-  int32_t *tile_e, *tile_m0;      // [tile slots] expert and first row inside it
+  // work buffers
+  int32_t *hist;                  // [mx_chunks(), E] entries of every expert in every 1024 entries
+  int2 *tiles;                    // [mx_tile_slots()] first sorted row; expert and rows << 16
   int32_t *n_tiles;               // [1]
   int32_t *pos;                   // [rows * k] entry -> sorted row, -1: no such expert
   int32_t *arow;                  // [rows * k] sorted row -> row of x
   void *act;                      // [rows * k, ffn] bf16
   float *y;                       // [rows * k, hidden]
 };
+int mx_tile_slots(int rows, int k, int n_experts);
+int mx_chunks(int rows, int k);
 size_t mx_experts_bytes(int n_experts, int hidden, int ffn, int n_rows, int k);
 void lay_mx_experts(MxExperts &a, void *workspace);
-void mx_experts(hipStream_t s, const MxExperts &a);
-// The two grouped products alone, on entries that moe_group() sorted.
-struct MxGroups {
-  const int32_t *offs, *count, *tile_e, *tile_m0, *n_tiles;
-  int n_tile_slots;
-  const int32_t *src;             // sorted row -> row of x
-};
-void mx_grouped(hipStream_t s, const MxGroups &g, const void *x, int64_t ldx, int n_rows, focus_mx gate_up, focus_mx down, int hidden, int ffn, void *act, float *y);
+void mx_group(hipStream_t s, const MxExperts &a);     // entries sorted by expert, tiles
+void mx_grouped(hipStream_t s, const MxExperts &a);   // the two products
+void mx_combine(hipStream_t s, const MxExperts &a);   // weighted sum
 
 }  // namespace fk

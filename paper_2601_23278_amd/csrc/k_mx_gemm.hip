@@ -32,7 +32,8 @@ struct RowsArgs {
   const unsigned char *codes, *scales;
   int N, K;                           // of one expert's matrix
   Rows rows;                          // dense
-  const int32_t *offs, *count, *tile_e, *tile_m0, *n_tiles;   // grouped
+  const int2 *tiles;                  // grouped: first sorted row; expert and rows << 16
+  const int32_t *n_tiles;
   int tiles_m, tiles_n, splits;
   void *out;
   int64_t ldo;
@@ -54,34 +55,37 @@ __device__ __forceinline__ uint64_t eight_scales(const unsigned char *row, int b
 }
 
 // A workgroup (4 wavefronts) takes up to BM rows and 128 CT rows of W; the wavefronts lie side by side, each BM x 32 CT, so that every code is
-// read and converted by one wavefront; tile rows of 32 that hold no rows are skipped.  K goes in steps of 64 (128 bytes of a row of A, through LDS,
-// DA steps ahead) and slabs of 256 (128 bytes of a row of W: a whole line, straight into registers, a slab ahead).  Lane l multiplies elements
-// 32 h .. 32 h + 31 of a step, h = l / 32: one block of its weight row, so one scale; the order of the elements within a step is the same for
-// both operands and does not matter otherwise.
-constexpr int kAhead = 4;      // steps between asking for rows and using them: those of a slab
+// read and converted by one wavefront; tile rows of 32 that hold no rows are skipped.  K goes in steps of 64 (128 bytes of a row of A) and slabs
+// of four steps (128 bytes of a row of W), whole lines of both, straight into LDS: the rows three steps ahead, the codes kCodeStages slabs ahead of the
+// registers that hold the slab in work.  (Codes read from memory into registers, a row per lane, cost the vector caches 64 lookups an instruction instead of
+// 16: 2048 rows through 256 experts 134 us instead of 100.)  Lane l multiplies elements 32 h .. 32 h + 31 of a step, h = l / 32: one
+// block of its weight row, so one scale; the order of the elements within a step is the same for both operands and does not matter otherwise.
+// Pipelined by hand: behind the MFMAs of 16 elements of K go the LDS reads of the rows' next fragments, the conversions of the next codes and the
+// loads.  A step's last quarter begins with the only barrier: by then everyone has read all of the step's rows, whose stage is filled again right
+// behind it, and the next step's rows have landed.  Codes are read and written by their own wavefront alone.
+constexpr int kRowStages = 3;
+constexpr int code_stages(int bm) { return bm > 32 ? 1 : 2; }
+constexpr int rows_lds(int bm, int ct) { return kRowStages * bm * 128 + code_stages(bm) * ct * 16384; }
 
 template <int BM, int CT, int MODE, bool GROUPED, bool WHOLE>      // WHOLE: K is a multiple of 256
 __global__ __launch_bounds__(256, 2) void k_mx_rows(RowsArgs g) {
 #if defined(__HIP_DEVICE_COMPILE__)   // buffer-resource builtins exist in the device pass only
-  constexpr int TM = BM / 32, DA = kAhead, SA = DA + 1, ASTAGE = BM * 128;
+  constexpr int TM = BM / 32, SA = kRowStages, ASTAGE = BM * 128, SW = code_stages(BM), WSTAGE = CT * 4096, WBASE = SA * ASTAGE;
   constexpr bool SILU = MODE == RM_SILU;
-  __shared__ __attribute__((aligned(1024))) unsigned char lds[SA * ASTAGE];
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[rows_lds(BM, CT)];
   const int splits = GROUPED ? 1 : g.splits;
   const int M = GROUPED ? 0 : g.rows.count ? min(*g.rows.count, g.rows.cap) : g.rows.cap;
+  const int tile_at = blockIdx.x / 8 / g.tiles_n * 8 + blockIdx.x % 8;
+  const int2 tile = GROUPED ? g.tiles[tile_at] : make_int2(0, 0);       // asked for together with the number of tiles: the list has room for every workgroup
   const int tiles_m = GROUPED ? *g.n_tiles : (M + BM - 1) / BM, total = tiles_m * g.tiles_n * splits, per_xcd = (total + 7) / 8;
-  // XCD x (workgroups x, x + 8, ...) takes a contiguous range of the work: workgroups that read the same rows share an L2
-  const int item = (blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
-  if ((int)(blockIdx.x / 8) >= per_xcd || item >= total) return;
-  const int split = item % splits, t = item / splits / g.tiles_n, nt = item / splits % g.tiles_n;
-  int e = 0, row0 = t * BM, valid;
-  if (GROUPED) {
-    e = g.tile_e[t];
-    const int m0 = g.tile_m0[t];
-    row0 = g.offs[e] + m0;
-    valid = min(BM, g.count[e] - m0);
-  } else {
-    valid = min(BM, M - row0);
-  }
+  // XCD x has the workgroups x, x + 8, ...  Dense: it takes a contiguous range of the work, so that workgroups that read the same rows share an
+  // L2.  Grouped: it takes the row tiles x, x + 8, ..., each with all its columns; the fullest tiles come first in the list, so that the
+  // launch ends with short ones on every XCD.
+  const int local = blockIdx.x / 8, item = (blockIdx.x % 8) * per_xcd + local;
+  if (GROUPED ? tile_at >= tiles_m : local >= per_xcd || item >= total) return;
+  const int split = item % splits, t = item / splits / g.tiles_n;
+  const int nt = GROUPED ? local % g.tiles_n : item / splits % g.tiles_n;
+  const int e = GROUPED ? tile.y & 0xFFFF : 0, row0 = GROUPED ? tile.x : t * BM, valid = GROUPED ? tile.y >> 16 : min(BM, M - row0);
   const int N = g.N, K = g.K, n0 = nt * (SILU ? 64 * CT : 128 * CT), blocks = K / 32;
   const int slabs = (blocks + 7) / 8, per_split = (slabs + splits - 1) / splits, slab0 = split * per_split;
   const int my_slabs = min(slabs - slab0, per_split);                                // slabs of this workgroup (0 or less: zeros)
@@ -103,43 +107,27 @@ __global__ __launch_bounds__(256, 2) void k_mx_rows(RowsArgs g) {
     const int r = q * 32 + wave * 8 + (lane >> 3), srow = r < valid ? (gather ? g.src[row0 + r] : r) : -1;
     voa[q] = srow < 0 ? kOutside : (unsigned)srow * (unsigned)g.lda * 2u + ca * 16;
   }
-  // the matrix row of this lane's column in column tile j.  SiLU*up: with two tiles a wavefront gate and up of the same 32 columns; with
-  // one 16 gate rows, then the 16 matching up rows
-  unsigned vow[CT], vos[CT];
-#pragma unroll
-  for (int j = 0; j < CT; ++j) {
-    int row;
+  // the matrix row of column r (0 .. 32 CT - 1) of this wavefront.  SiLU*up: with two column tiles gate and up of the same 32 columns; with one 16
+  // gate rows, then the 16 matching up rows
+  auto weight_row = [&](int r) __attribute__((always_inline)) {
     if (SILU) {
-      const int c = CT == 2 ? n0 + wave * 32 + frow : n0 + wave * 16 + (frow & 15);
-      row = c < N / 2 ? (CT == 2 ? j : frow >> 4) * (N / 2) + c : -1;
-    } else {
-      const int c = n0 + (wave * CT + j) * 32 + frow;
-      row = c < N ? c : -1;
+      const int c = CT == 2 ? n0 + wave * 32 + (r & 31) : n0 + wave * 16 + (r & 15);
+      return c < N / 2 ? (CT == 2 ? r >> 5 : r >> 4) * (N / 2) + c : -1;
     }
-    vow[j] = row < 0 ? kOutside : (unsigned)row * (unsigned)(K / 2) + h * 16;
-    vos[j] = (unsigned)max(row, 0) * (unsigned)blocks;
+    const int c = n0 + wave * 32 * CT + r;
+    return c < N ? c : -1;
+  };
+  // chunk (block of 32) of a slab that this lane fetches for columns 8 q + lane / 8, q even and odd: swizzled like the rows' chunks
+  const int cw = (lane & 7) ^ (lane >> 4);
+  unsigned vow[4 * CT];
+#pragma unroll
+  for (int q = 0; q < 4 * CT; ++q) {
+    const int row = weight_row(q * 8 + (lane >> 3));
+    vow[q] = row < 0 ? kOutside : (unsigned)row * (unsigned)(K / 2) + (cw ^ (4 * (q & 1))) * 16;
   }
-
-  u32x4 w[CT][4];
-  uint64_t sc[CT];
-  // two chunks of a slab's codes, q and q + 1
-  auto load_w = [&](int slab, int q0) __attribute__((always_inline)) {
-    const unsigned so = slab < my_slabs ? (unsigned)(slab0 + slab) * 128u : kOutside;
-#pragma unroll
-    for (int j = 0; j < CT; ++j)
-#pragma unroll
-      for (int q = q0; q < q0 + 2; ++q)
-        w[j][q] = __builtin_amdgcn_raw_buffer_load_b128(rs_w, !WHOLE && (slab0 + slab) * 8 + 2 * q + h >= blocks ? kOutside : vow[j] + q * 32, so, 0);
-  };
-  auto load_scales = [&](int slab) __attribute__((always_inline)) {
-    const int b0 = (slab0 + min(slab, my_slabs - 1)) * 8;
-#pragma unroll
-    for (int j = 0; j < CT; ++j) {
-      if (WHOLE) sc[j] = __builtin_bit_cast(uint64_t, __builtin_amdgcn_raw_buffer_load_b64(rs_s, vos[j], b0, 0));
-      else sc[j] = eight_scales(scales + vos[j], b0, blocks);
-    }
-  };
-
+  // scales: with two column tiles the lower lanes fetch those of the first, the upper ones of the second
+  const int srow = weight_row(CT == 2 ? lane : frow);
+  const unsigned vos = (unsigned)max(srow, 0) * (unsigned)blocks;
   f32x16 acc[TM][CT];
 #pragma unroll
   for (int i = 0; i < TM; ++i)
@@ -148,74 +136,171 @@ __global__ __launch_bounds__(256, 2) void k_mx_rows(RowsArgs g) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
 
-  const int swz_a = (frow >> 1) & 7;
-  // L: tile rows of 32 that hold rows.  The loop exists once for each, since a branch around each tile row kept the fragments' LDS reads
-  // from being asked for ahead.
+  // L: tile rows of 32 that hold rows.  The loop exists once for each, since a branch around each tile row would part the pipeline.
   auto multiply = [&](auto rows_live) __attribute__((always_inline)) {
-    constexpr int L = decltype(rows_live)::value;
-    auto issue_a = [&](int step, int stage) __attribute__((always_inline)) {
+    constexpr int L = decltype(rows_live)::value, NMF = L * CT, PER = (3 + L) / L;      // PER: conversions behind an MFMA, four in L of them
+    u32x4 w[CT][4];             // codes of the slab: chunk of each step
+    u32x2 sc[CT];               // its scales, and those of the next slab as they were fetched
+    u32x2 next_sc;
+    u32x4 fb[2];                // CT = 2: of the two column tiles; CT = 1: of this quarter and the next
+    // Fragments of this quarter and the next; with two column tiles and three or four tile rows a fragment's successor goes where it was, behind its
+    // last MFMA: as many MFMAs as there are tile rows lie between, and 16 registers more did not fit.
+    constexpr bool TWO = CT == 1 || L < 3;
+    bf16x8 fa[TWO ? 2 : 1][L];
+    float scale[CT];
+    auto load_codes = [&](int slab, int stage, int q) __attribute__((always_inline)) {
+      const unsigned so = slab < my_slabs ? (unsigned)(slab0 + slab) * 128u : kOutside;
+      const unsigned v = !WHOLE && (slab0 + slab) * 8 + (cw ^ (4 * (q & 1))) >= blocks ? kOutside : vow[q];
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs_w, FK_LDS_PTR(lds + WBASE + stage * 4 * WSTAGE + wave * WSTAGE + q * 1024), 16, v, so, 0, 0);
+    };
+    auto load_scales = [&](int slab) __attribute__((always_inline)) {
+      const int b0 = (slab0 + min(slab, my_slabs - 1)) * 8;
+      if (WHOLE) next_sc = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rs_s, vos, b0, 0));
+      else next_sc = __builtin_bit_cast(u32x2, eight_scales(scales + vos, b0, blocks));
+    };
+    auto take_scales = [&]() __attribute__((always_inline)) {
+#pragma unroll
+      for (int d = 0; d < 2; ++d) {
+        if (CT == 2) {
+          const u32x2 both = __builtin_amdgcn_permlane32_swap(next_sc[d], next_sc[d], false, false);      // the lower lanes' everywhere, the upper lanes' everywhere
+          sc[0][d] = both[0];
+          sc[CT - 1][d] = both[1];
+        } else {
+          sc[0][d] = next_sc[d];
+        }
+      }
+    };
+    const int swz = (frow >> 1) & 7;
+    auto read_codes = [&](int stage, int j, int q) __attribute__((always_inline)) {
+      w[j][q] = *(const u32x4 *)(lds + WBASE + stage * 4 * WSTAGE + wave * WSTAGE + (j * 32 + frow) * 128 + (((2 * q + h) ^ swz) << 4));
+    };
+    auto load_rows = [&](int step, int stage, int q) __attribute__((always_inline)) {
       const int k0 = slab0 * 256 + step * 64;
       const unsigned so = step < my_steps ? (unsigned)k0 * 2u : kOutside;
       const bool half = !WHOLE && k0 + 32 >= K;           // the second block of the step does not exist
-#pragma unroll
-      for (int q = 0; q < L; ++q)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rs_a, FK_LDS_PTR(lds + stage * ASTAGE + (q * 4 + wave) * 1024), 16, half && ca >= 4 ? kOutside : voa[q], so, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs_a, FK_LDS_PTR(lds + stage * ASTAGE + (q * 4 + wave) * 1024), 16, half && ca >= 4 ? kOutside : voa[q], so, 0, 0);
     };
-    // in the order in which the loop asks for them, so that its count of younger loads holds from the first step on
+    // the scale of block 2 q + h of a slab, as a float
+    auto scale_of = [&](u32x2 eight, int q) __attribute__((always_inline)) {
+      const unsigned x = eight[q >> 1] >> (8 * h);
+      return __uint_as_float(((q & 1) ? x << 7 : x << 23) & 0x7F800000u);
+    };
+    auto convert = [&](unsigned c, float by, int part) __attribute__((always_inline)) {
+      return __builtin_bit_cast(unsigned, part == 0 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, by, 0) : part == 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, by, 1)
+                                                    : part == 2 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, by, 2) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, by, 3));
+    };
+    unsigned first[4];          // this lane's fragment of each quarter of a step
 #pragma unroll
-    for (int s = 0; s < DA; ++s) {
-      issue_a(s, s);
-      if (s & 1) load_w(0, s - 1);
-      if (s == 3) load_scales(0);
+    for (int ks = 0; ks < 4; ++ks) first[ks] = frow * 128 + (((4 * h + ks) ^ ((frow >> 1) & 7)) << 4);
+
+    // in an order in which the loop's count of younger loads holds from its first step on
+    auto in_order = []() __attribute__((always_inline)) { loads_asked_for(); __builtin_amdgcn_sched_barrier(0); };
+#pragma unroll
+    for (int i = 0; i < SW; ++i)
+#pragma unroll
+      for (int q = 0; q < 4 * CT; ++q) load_codes(i, i, q);
+    load_scales(0);
+    in_order();
+#pragma unroll
+    for (int s = 0; s < SA; ++s) {
+#pragma unroll
+      for (int q = 0; q < L; ++q) load_rows(s, s, q);
+      in_order();
     }
-    int sa = 0, la = DA % SA;       // stages of this step's rows and of the loads it makes
-    for (int slab = 0; slab < my_slabs; ++slab) {
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm((SA - 1) * L));
+    asm volatile("s_barrier" ::: "memory");
+    take_scales();
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        // younger than the rows of this step: those of the three steps after it, four chunks of codes and a slab's scales
-        __builtin_amdgcn_s_waitcnt(vmcnt_imm((DA - 1) * L + (WHOLE ? 5 : 4) * CT));
-        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");      // everyone has finished the step before
-        issue_a(4 * slab + q + DA, la);
-        const unsigned char *pa = lds + sa * ASTAGE;
-        if (WHOLE || 4 * slab + q < my_steps) {
-          float scale[CT];
+    for (int i = 0; i < L; ++i) fa[0][i] = *(const bf16x8 *)(lds + first[0] + i * 4096);
 #pragma unroll
-          for (int j = 0; j < CT; ++j) {
-            const unsigned x = (unsigned)((sc[j] >> (8 * h)) >> (32 * (q >> 1)));       // byte 2 (q & 1) is the scale of block 2 q + h
-            scale[j] = __uint_as_float(((q & 1) ? x << 7 : x << 23) & 0x7F800000u);
-          }
+    for (int j = 0; j < CT; ++j) read_codes(0, j, 0);
 #pragma unroll
-          for (int ks = 0; ks < 4; ++ks) {
-            bf16x8 fb[CT], fa[L];
+    for (int j = 0; j < CT; ++j) scale[j] = scale_of(sc[j], 0);
 #pragma unroll
-            for (int i = 0; i < L; ++i) fa[i] = *(const bf16x8 *)(pa + (i * 32 + frow) * 128 + (((4 * h + ks) ^ swz_a) << 4));
+    for (int part = 0; part < 4; ++part) fb[0][part] = convert(w[0][0][0], scale[0], part);
+    int stage = 0, code_stage = 0;              // of this step's rows, of this slab's codes
+    // STEP: step of its slab.  A slab's first step reads the rest of its codes from LDS and, behind the barrier, asks for those that take their place.
+    auto step_of = [&](auto which, int slab) __attribute__((always_inline)) {
+      constexpr int STEP = decltype(which)::value;
+      const int after = stage == SA - 1 ? 0 : stage + 1, next_code = code_stage == SW - 1 ? 0 : code_stage + 1;
 #pragma unroll
-            for (int j = 0; j < CT; ++j) {
-              const unsigned c = w[j][q][ks];
-              const bf16x2 b0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale[j], 0), b1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale[j], 1);
-              const bf16x2 b2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale[j], 2), b3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale[j], 3);
-              fb[j] = bf16x8{b0[0], b0[1], b1[0], b1[1], b2[0], b2[1], b3[0], b3[1]};
-            }
-#pragma unroll
-            for (int i = 0; i < L; ++i)
-#pragma unroll
-              for (int j = 0; j < CT; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[i], fb[j], acc[i][j], 0, 0, 0);
-          }
+      for (int ks = 0; ks < 4; ++ks) {
+        if (ks == 3) {
+          // younger than the next step's rows: those of the step behind it, and, where they were asked for in the two steps before this
+          // one, codes and scales
+          __builtin_amdgcn_s_waitcnt(vmcnt_imm((SA - 2) * L + (STEP == 1 ? 4 * CT + (WHOLE ? 1 : 0) : 0)));
+          asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
         }
-        // into the registers just used
-        if (q & 1) load_w(slab + 1, q - 1);
-        if (q == 3) load_scales(slab + 1);
-        sa = sa == SA - 1 ? 0 : sa + 1;
-        la = la == SA - 1 ? 0 : la + 1;
+        // what is converted next: the other column tile's codes of this quarter, then this one's of the next
+        const int word = (ks + 1) & 3;
+        const unsigned char *const from = lds + first[word] + (ks == 3 ? after : stage) * ASTAGE;
+#pragma unroll
+        for (int s = 0; s < NMF; ++s) {
+          const int j = s / L, i = s % L;
+          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[TWO ? ks & 1 : 0][i], __builtin_bit_cast(bf16x8, fb[CT == 2 ? j : ks & 1]), acc[i][j], 0, 0, 0);
+          if (TWO ? s < L : j == 1) fa[TWO ? (ks & 1) ^ 1 : 0][i] = *(const bf16x8 *)(from + i * 4096);
+#pragma unroll
+          for (int part = i * PER; part < i * PER + PER && part < 4; ++part) {
+            if (CT == 2 && j == 0) {
+              if (ks == 0 && part == 0) scale[CT - 1] = scale_of(sc[CT - 1], STEP);
+              fb[1][part] = convert(w[CT - 1][STEP][ks], scale[CT - 1], part);
+            } else {
+              if (ks == 3 && part == 0) {
+                if (STEP == 3) take_scales();
+                scale[0] = scale_of(sc[0], (STEP + 1) & 3);
+              }
+              fb[CT == 2 ? 0 : (ks & 1) ^ 1][part] = convert(ks < 3 ? w[0][STEP][word] : w[0][(STEP + 1) & 3][0], scale[0], part);
+            }
+          }
+          if (s == NMF - 1) {
+            if (STEP == 0 && ks < 3) {
+#pragma unroll
+              for (int c = 0; c < CT; ++c) read_codes(code_stage, c, ks + 1);
+            }
+            if (STEP == 3 && ks == 2) {
+#pragma unroll
+              for (int c = 0; c < CT; ++c) read_codes(next_code, c, 0);
+            }
+          }
+          if (STEP == 0 && ks == 3) {
+#pragma unroll
+            for (int q = s * 4 * CT / NMF; q < (s + 1) * 4 * CT / NMF; ++q) load_codes(slab + SW, code_stage, q);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        if (ks == 3) {
+          if (STEP == 0) load_scales(slab + 1);
+#pragma unroll
+          for (int q = 0; q < L; ++q) load_rows(4 * slab + STEP + SA, stage, q);
+          __builtin_amdgcn_sched_barrier(0);
+        }
       }
+      stage = after;
+      if (STEP == 3) code_stage = next_code;
+    };
+    constexpr std::integral_constant<int, 0> s0;
+    constexpr std::integral_constant<int, 1> s1;
+    constexpr std::integral_constant<int, 2> s2;
+    constexpr std::integral_constant<int, 3> s3;
+    int slab = 0;
+    for (; 4 * slab + 4 <= my_steps; ++slab) {
+      step_of(s0, slab);
+      step_of(s1, slab);
+      step_of(s2, slab);
+      step_of(s3, slab);
     }
+    if (!WHOLE && 4 * slab < my_steps) {
+      step_of(s0, slab);
+      if (4 * slab + 1 < my_steps) step_of(s1, slab);
+      if (4 * slab + 2 < my_steps) step_of(s2, slab);
+    }
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
   };
   if (my_slabs <= 0) {}
   else if (TM == 1 || live == 1) multiply(std::integral_constant<int, 1>());
   else if (live == 2) multiply(std::integral_constant<int, TM < 2 ? 1 : 2>());
   else if (live == 3) multiply(std::integral_constant<int, TM < 3 ? 1 : 3>());
   else multiply(std::integral_constant<int, TM>());
-  __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
   // register r of lane l is C[8 (r / 4) + 4 (l / 32) + r % 4][l % 32] of its 32 x 32 tile
   if (SILU) {
     // one column tile: lanes 0..15 of a half hold gate columns, 16..31 the matching up columns; exchanging halves between two registers gives
@@ -260,7 +345,7 @@ __global__ __launch_bounds__(256, 2) void k_mx_rows(RowsArgs g) {
 template <int BM, int CT, int MODE, bool GROUPED>
 void launch_rows(hipStream_t s, RowsArgs g, int tile_slots) {
   g.tiles_n = MODE == RM_SILU ? (g.N / 2 + 64 * CT - 1) / (64 * CT) : (g.N + 128 * CT - 1) / (128 * CT);
-  const int grid = (tile_slots * g.tiles_n * (GROUPED ? 1 : g.splits) + 7) / 8 * 8;
+  const int grid = GROUPED ? tile_slots * g.tiles_n : (tile_slots * g.tiles_n * g.splits + 7) / 8 * 8;
   if (g.K % 256 == 0) k_mx_rows<BM, CT, MODE, GROUPED, true><<<grid, 256, 0, s>>>(g);
   else k_mx_rows<BM, CT, MODE, GROUPED, false><<<grid, 256, 0, s>>>(g);
 }
@@ -494,29 +579,32 @@ void mx_gemm(hipStream_t s, const void *a, const void *a_scales, int64_t lda, fo
   if (parts) launch_reduce(s, epilogue, (const float *)scratch.ptr, p.splits, stride, rows, n, out, ldo);
 }
 
-void mx_grouped(hipStream_t s, const MxGroups &g, const void *x, int64_t ldx, int n_rows, focus_mx gate_up, focus_mx down, int hidden, int ffn, void *act, float *y) {
+void mx_grouped(hipStream_t s, const MxExperts &m) {
   RowsArgs a{};
-  a.A = (const bf16_t *)x; a.lda = ldx; a.src = g.src; a.a_bytes = (unsigned)(((int64_t)(n_rows - 1) * ldx + hidden) * 2);
-  a.codes = (const unsigned char *)gate_up.codes; a.scales = (const unsigned char *)gate_up.scales;
-  a.N = 2 * ffn; a.K = hidden; a.offs = g.offs; a.count = g.count; a.tile_e = g.tile_e; a.tile_m0 = g.tile_m0; a.n_tiles = g.n_tiles;
-  a.splits = 1; a.out = act; a.ldo = ffn;
-  launch_rows<128, 2, RM_SILU, true>(s, a, g.n_tile_slots);
-  a.A = (const bf16_t *)act; a.lda = ffn; a.src = nullptr; a.a_bytes = 0;
-  a.codes = (const unsigned char *)down.codes; a.scales = (const unsigned char *)down.scales;
-  a.N = hidden; a.K = ffn; a.out = y; a.ldo = hidden;
-  launch_rows<128, 2, RM_STORE_F32, true>(s, a, g.n_tile_slots);
+  a.A = (const bf16_t *)m.x; a.lda = m.ldx; a.src = m.arow; a.a_bytes = (unsigned)(((int64_t)(m.rows.cap - 1) * m.ldx + m.hidden) * 2);
+  a.codes = (const unsigned char *)m.gate_up.codes; a.scales = (const unsigned char *)m.gate_up.scales;
+  a.N = 2 * m.ffn; a.K = m.hidden; a.tiles = m.tiles; a.n_tiles = m.n_tiles; a.splits = 1; a.out = m.act; a.ldo = m.ffn;
+  const int slots = mx_tile_slots(m.rows.cap, m.k, m.n_experts);
+  launch_rows<128, 2, RM_SILU, true>(s, a, slots);
+  a.A = (const bf16_t *)m.act; a.lda = m.ffn; a.src = nullptr; a.a_bytes = 0;
+  a.codes = (const unsigned char *)m.down.codes; a.scales = (const unsigned char *)m.down.scales;
+  a.N = m.hidden; a.K = m.ffn; a.out = m.y; a.ldo = m.hidden;
+  launch_rows<128, 2, RM_STORE_F32, true>(s, a, slots);
 }
 
 // ---------------------------------------------------------------------------------------------
-// Entries sorted by expert.  A workgroup counts 1024 entries per expert; a second launch adds up the counts and places the entries.  Which of a
-// workgroup's entries of one expert comes first is left to the order of its LDS atomics: a row's sums do not depend on its place in a tile.
+// Entries sorted by expert.  Which of a workgroup's entries of one expert comes first is left to the order of its LDS atomics: a row's sums do
+// not depend on its place in a tile.
 namespace {
-constexpr int kChunk = 1024;
+constexpr int kChunk = 1024;      // entries of a workgroup; at least kMxMaxExperts
+// Up to so many chunks every workgroup of the one launch counts all entries; from there on a launch of its own counts them chunk by chunk first
+// (the quadratic counting of 16 chunks takes 3 us, the second launch 5).
+constexpr int kCountAll = 16;
 
 __global__ __launch_bounds__(kChunk) void k_mx_count(MxExperts a) {
-  extern __shared__ int cnt[];
+  __shared__ int cnt[kMxMaxExperts];
   const int E = a.n_experts, tid = threadIdx.x, M = a.rows.count ? min(*a.rows.count, a.rows.cap) : a.rows.cap, n = M * a.k;
-  for (int e = tid; e < E; e += kChunk) cnt[e] = 0;
+  if (tid < E) cnt[tid] = 0;
   __syncthreads();
   const int i = blockIdx.x * kChunk + tid;
   if (i < n) {
@@ -524,55 +612,101 @@ __global__ __launch_bounds__(kChunk) void k_mx_count(MxExperts a) {
     if (e >= 0 && e < E) atomicAdd(&cnt[e], 1);
   }
   __syncthreads();
-  for (int e = tid; e < E; e += kChunk) a.hist[(size_t)blockIdx.x * E + e] = cnt[e];
+  if (tid < E) a.hist[(size_t)blockIdx.x * E + tid] = cnt[tid];
 }
 
-// all[e]: rows of expert e; mine[e]: of the chunks before this one.  Exclusive sums over the experts of rows and of tiles, in LDS.
+// Thread e < E knows how many entries of expert e there are, in all and in the chunks before this workgroup's.  The tiles are listed by falling
+// number of tile rows of 32: full ones, then those of three, two and one, each in the order of the experts.
+template <bool COUNTED>
 __global__ __launch_bounds__(kChunk) void k_mx_place(MxExperts a, int chunks, int tile_slots) {
-  extern __shared__ int lds_place[];
-  const int E = a.n_experts, tid = threadIdx.x, M = a.rows.count ? min(*a.rows.count, a.rows.cap) : a.rows.cap, n = M * a.k;
-  int *all = lds_place, *next = all + E, *rows_lt = next + E, *tiles_lt = rows_lt + E;
-  for (int e = tid; e < E; e += kChunk) {
-    int before = 0, sum = 0;
-    for (int c = 0; c < chunks; ++c) {
-      const int v = a.hist[(size_t)c * E + e];
-      before += c < (int)blockIdx.x ? v : 0;
-      sum += v;
-    }
-    all[e] = sum;
-    next[e] = before;
-  }
-  __syncthreads();
-  if (tid < 64) {                       // one wavefront scans, 64 experts at a time
-    int rows = 0, tiles = 0;
-    for (int e0 = 0; e0 < E; e0 += 64) {
-      const int e = e0 + tid, c = e < E ? all[e] : 0, t = (c + kMxTileRows - 1) / kMxTileRows;
-      int r = c, q = t;
-      for (int d = 1; d < 64; d <<= 1) {
-        const int ro = __shfl_up(r, d), qo = __shfl_up(q, d);
-        if (tid >= d) { r += ro; q += qo; }
+  __shared__ int next[kMxMaxExperts];
+  __shared__ uint64_t wide[kChunk / 64];
+  __shared__ unsigned narrow[kChunk / 64];
+  const int E = a.n_experts, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, me = blockIdx.x;
+  const int M = a.rows.count ? min(*a.rows.count, a.rows.cap) : a.rows.cap, n = M * a.k;
+  int before = 0, all = 0, own = -1;
+  constexpr int U = 16;
+  static_assert(kCountAll <= U, "one round of loads when nothing was counted");
+  if (COUNTED) {
+    if (tid < E)
+      for (int c0 = 0; c0 < chunks; c0 += U) {
+        int v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) v[u] = c0 + u < chunks ? a.hist[(size_t)(c0 + u) * E + tid] : 0;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          before += c0 + u < me ? v[u] : 0;
+          all += v[u];
+        }
       }
-      if (e < E) { rows_lt[e] = rows + r - c; tiles_lt[e] = tiles + q - t; }
-      rows += __shfl(r, 63);
-      tiles += __shfl(q, 63);
+    if (me * kChunk + tid < n) own = a.experts[me * kChunk + tid];
+  } else {
+    int v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) v[u] = u < chunks && u * kChunk + tid < n ? a.experts[u * kChunk + tid] : -1;
+    if (tid < E) next[tid] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (u == me) {
+        own = v[u];
+        __syncthreads();
+        if (tid < E) before = next[tid];
+        __syncthreads();
+      }
+      if (v[u] >= 0 && v[u] < E) atomicAdd(&next[v[u]], 1);
     }
-    if (blockIdx.x == 0 && tid == 0) { a.offs[E] = rows; *a.n_tiles = min(tiles, tile_slots); }
+    __syncthreads();
+    if (tid < E) all = next[tid];
+  }
+  // exclusive sums over the experts of rows and full tiles, and of tiles of three, two and one tile rows (10 bits each)
+  const int full = all / kMxTileRows, rest = (all % kMxTileRows + 31) / 32 % 4, whole = full + (all % kMxTileRows > 96);
+  const uint64_t w0 = ((uint64_t)whole << 32) | (unsigned)all;
+  const unsigned n0 = rest ? 1u << (10 * (3 - rest)) : 0u;
+  uint64_t w = w0;
+  unsigned q = n0;
+  for (int d = 1; d < 64; d <<= 1) {
+    const uint64_t wo = __shfl_up((unsigned long long)w, d);
+    const unsigned qo = __shfl_up(q, d);
+    if (lane >= d) { w += wo; q += qo; }
+  }
+  if (lane == 63) { wide[wave] = w; narrow[wave] = q; }
+  __syncthreads();
+  uint64_t w_all = 0;
+  unsigned q_all = 0;
+  w -= w0;
+  q -= n0;
+  for (int i = 0; i < kMxMaxExperts / 64; ++i) {       // experts are the first threads
+    if (i < wave) { w += wide[i]; q += narrow[i]; }
+    w_all += wide[i];
+    q_all += narrow[i];
+  }
+  const int first = (int)(unsigned)w;
+  if (tid < E) {
+    next[tid] = first + before;
+    if (me == 0) {
+      int t = (int)(w >> 32);
+      for (int m = 0; m < whole; ++m, ++t)
+        if (t < tile_slots) a.tiles[t] = make_int2(first + m * kMxTileRows, tid | min(kMxTileRows, all - m * kMxTileRows) << 16);
+      if (rest) {
+        t = (int)(w_all >> 32);
+        for (int r = 3; r > rest; --r) t += q_all >> (10 * (3 - r)) & 1023;
+        t += q >> (10 * (3 - rest)) & 1023;
+        if (t < tile_slots) a.tiles[t] = make_int2(first + full * kMxTileRows, tid | (all - full * kMxTileRows) << 16);
+      }
+    }
+  }
+  if (me == 0 && tid == 0) {
+    int t = (int)(w_all >> 32);
+    for (int r = 0; r < 3; ++r) t += q_all >> (10 * r) & 1023;
+    *a.n_tiles = min(t, tile_slots);
   }
   __syncthreads();
-  for (int e = tid; e < E; e += kChunk) next[e] += rows_lt[e];
-  if (blockIdx.x == 0)
-    for (int e = tid; e < E; e += kChunk) {
-      a.offs[e] = rows_lt[e];
-      a.count[e] = all[e];
-      for (int m = 0; m * kMxTileRows < all[e] && tiles_lt[e] + m < tile_slots; ++m) { a.tile_e[tiles_lt[e] + m] = e; a.tile_m0[tiles_lt[e] + m] = m * kMxTileRows; }
-    }
-  __syncthreads();
-  const int i = blockIdx.x * kChunk + tid;
+  const int i = me * kChunk + tid;
   if (i < n) {
-    const int e = a.experts[i];
     int p = -1;
-    if (e >= 0 && e < E) {
-      p = atomicAdd(&next[e], 1);
+    if (own >= 0 && own < E) {
+      p = atomicAdd(&next[own], 1);
       a.arow[p] = i / a.k;
     }
     a.pos[i] = p;
@@ -599,20 +733,19 @@ __global__ __launch_bounds__(256) void k_mx_combine(MxExperts a) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) o[i] = ADD ? (T)((float)o[i] + v[i]) : (T)v[i];
 }
-
-int tile_slots_of(int entries, int E) { return entries / kMxTileRows + std::min(entries, E); }
 }  // namespace
+
+// Row tiles there can be, rounded up to the eight XCDs that take them in turn.
+int mx_tile_slots(int rows, int k, int n_experts) { return (rows * k / kMxTileRows + std::min(rows * k, n_experts) + 7) / 8 * 8; }
+int mx_chunks(int rows, int k) { return (rows * k + kChunk - 1) / kChunk; }
 
 // Lays the work buffers out from `base`; returns their size.
 static size_t lay(MxExperts &a, char *base, int rows) {
-  const size_t ent = (size_t)rows * a.k, E = a.n_experts, chunks = (ent + kChunk - 1) / kChunk, tiles = tile_slots_of((int)ent, a.n_experts);
+  const size_t ent = (size_t)rows * a.k;
   size_t at = 0;
   auto take = [&](size_t bytes) { char *p = base + at; at += (bytes + 255) & ~(size_t)255; return p; };
-  a.hist = (int32_t *)take(chunks * E * 4);
-  a.offs = (int32_t *)take((E + 1) * 4);
-  a.count = (int32_t *)take(E * 4);
-  a.tile_e = (int32_t *)take(tiles * 4);
-  a.tile_m0 = (int32_t *)take(tiles * 4);
+  a.hist = (int32_t *)take((size_t)mx_chunks(rows, a.k) * a.n_experts * 4);
+  a.tiles = (int2 *)take((size_t)mx_tile_slots(rows, a.k, a.n_experts) * 8);
   a.n_tiles = (int32_t *)take(4);
   a.pos = (int32_t *)take(ent * 4);
   a.arow = (int32_t *)take(ent * 4);
@@ -627,12 +760,19 @@ size_t mx_experts_bytes(int n_experts, int hidden, int ffn, int n_rows, int k) {
 }
 void lay_mx_experts(MxExperts &a, void *workspace) { lay(a, (char *)workspace, a.rows.cap); }
 
-void mx_experts(hipStream_t s, const MxExperts &a) {
+void mx_group(hipStream_t s, const MxExperts &a) {
   if (a.rows.cap <= 0) return;
-  const int ent = a.rows.cap * a.k, chunks = (ent + kChunk - 1) / kChunk, slots = tile_slots_of(ent, a.n_experts);
-  k_mx_count<<<chunks, kChunk, a.n_experts * 4, s>>>(a);
-  k_mx_place<<<chunks, kChunk, a.n_experts * 16, s>>>(a, chunks, slots);
-  mx_grouped(s, MxGroups{a.offs, a.count, a.tile_e, a.tile_m0, a.n_tiles, slots, a.arow}, a.x, a.ldx, a.rows.cap, a.gate_up, a.down, a.hidden, a.ffn, a.act, a.y);
+  const int chunks = mx_chunks(a.rows.cap, a.k), slots = mx_tile_slots(a.rows.cap, a.k, a.n_experts);
+  if (chunks <= kCountAll) {
+    k_mx_place<false><<<chunks, kChunk, 0, s>>>(a, chunks, slots);
+  } else {
+    k_mx_count<<<chunks, kChunk, 0, s>>>(a);
+    k_mx_place<true><<<chunks, kChunk, 0, s>>>(a, chunks, slots);
+  }
+}
+
+void mx_combine(hipStream_t s, const MxExperts &a) {
+  if (a.rows.cap <= 0) return;
   const dim3 grid(a.rows.cap, (a.hidden + 1023) / 1024);
   if (a.out_type == FOCUS_BF16) k_mx_combine<bf16_t, false><<<grid, 256, 0, s>>>(a);
   else if (a.add) k_mx_combine<float, true><<<grid, 256, 0, s>>>(a);

@@ -24,12 +24,12 @@ const char *check_product(int32_t m, int32_t n, int32_t k, int32_t a_type) {
 }
 
 const char *check_experts(int32_t n_experts, int32_t hidden, int32_t ffn, int32_t n_rows, int32_t k) {
-  if (n_experts < 1 || n_experts > 512) return "n_experts must be in 1..512";
+  if (n_experts < 1 || n_experts > fk::kMxMaxExperts) return "n_experts must be in 1..512";
   if (hidden < 32 || hidden % 32 || ffn < 32 || ffn % 32) return "hidden and ffn must be positive multiples of 32";
   if (hidden > (1 << 20) || ffn > (1 << 20) || (int64_t)hidden * ffn >= (1ll << 31)) return "hidden and ffn too large";
   if (n_rows < 0 || k < 1 || k > 32 || (int64_t)n_rows * k > (1 << 24)) return "n_rows must not be negative, k in 1..32 and n_rows * k at most 2^24";
   // the launches have a workgroup per 128 columns and tile of rows
-  const int64_t tiles = (int64_t)n_rows * k / fk::kMxTileRows + n_experts;
+  const int64_t tiles = (int64_t)n_rows * k / fk::kMxTileRows + n_experts + 8;
   if (tiles * ((std::max(hidden, 2 * ffn) + 127) / 128) >= (1ll << 31)) return "hidden, ffn and n_rows too large";
   return nullptr;
 }
@@ -131,7 +131,9 @@ int focus_mx_experts(void *hip_stream, int32_t n_experts, int32_t hidden, int32_
   a.n_experts = n_experts; a.hidden = hidden; a.ffn = ffn; a.k = k; a.gate_up = *gate_up; a.down = *down; a.rows = fk::Rows{n_rows, nullptr};
   a.x = x; a.ldx = ldx; a.experts = experts; a.weights = weights; a.out_type = out_type; a.out = out; a.ldo = ldo; a.add = add != 0;
   fk::lay_mx_experts(a, workspace);
-  fk::mx_experts((hipStream_t)hip_stream, a);
+  fk::mx_group((hipStream_t)hip_stream, a);
+  fk::mx_grouped((hipStream_t)hip_stream, a);
+  fk::mx_combine((hipStream_t)hip_stream, a);
   return launched();
 }
 
