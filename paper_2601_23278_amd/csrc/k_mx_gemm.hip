@@ -359,8 +359,11 @@ void launch_rows(hipStream_t s, int mode, const RowsArgs &g, int tile_slots) {
 }
 
 // ---------------------------------------------------------------------------------------------
-// MXFP4 rows x MXFP4 weights: 2 x 2 wavefronts, slabs of 256 elements (128 bytes a row).  Lane l supplies row l % 32 and block 2 j + l / 32 of the j-th
-// quarter of a slab: 16 bytes of codes and one scale.
+// MXFP4 rows x MXFP4 weights: 2 x 2 wavefronts.  K goes in slabs of 128, 64 bytes of codes a row, through four LDS stages: a slab is asked for three
+// slabs before it is used.  Lane l supplies row l % 32 and, of the two halves of 64 elements of a slab, block 2 ks + l / 32: 16 bytes of codes and one
+// scale.  Scales are fetched 16 bytes a row, for four slabs at once (a row per lane costs the vector caches a lookup per lane whatever its size), a
+// quad of slabs ahead, and handed on through LDS.  Pipelined by hand like k_mx_rows: behind each MFMA one fragment read of the next half or one load; the
+// only barrier of a slab stands before its second half.
 struct MxArgs {
   const unsigned char *A, *a_scales, *W, *w_scales;
   int M, N, K;
@@ -370,13 +373,16 @@ struct MxArgs {
   size_t split_stride;
 };
 enum { XM_STORE, XM_STORE_F32, XM_PARTIAL };
+constexpr int kMxStages = 4;
+constexpr int mx_lds(int bm, int bn) { return kMxStages * (bm + bn) * 64 + 2 * (bm + bn) * 16; }
 
-template <int BM, int BN, int MODE>
+template <int BM, int BN, int MODE, bool WHOLE>      // WHOLE: K is a multiple of 512
 __global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void k_mx_mx(MxArgs g) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  constexpr int WM = BM / 2, WN = BN / 2, TM = WM / 32, TN = WN / 32, IA = BM / 32, IB = BN / 32;
-  constexpr int ASTAGE = BM * 128, WSTAGE = BN * 128, WBASE = 2 * ASTAGE;
-  __shared__ __attribute__((aligned(1024))) unsigned char lds[2 * (BM + BN) * 128];
+  constexpr int WM = BM / 2, WN = BN / 2, TM = WM / 32, TN = WN / 32, NMF = TM * TN, NF = TM + TN, IA = BM / 64, IB = BN / 64, ROWS = BM + BN, SI = ROWS / 256;
+  constexpr int ASTAGE = BM * 64, WSTAGE = BN * 64, WBASE = kMxStages * ASTAGE, SBASE = WBASE + kMxStages * WSTAGE;
+  static_assert(NF <= NMF && IA + IB <= NMF, "one fragment read and one load per MFMA at most");
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[mx_lds(BM, BN)];
   const int splits = g.splits, tiles_n = g.tiles_n, total = g.tiles_m * tiles_n * splits, per_xcd = (total + 7) / 8;
   const int item = (blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
   if ((int)(blockIdx.x / 8) >= per_xcd || item >= total) return;
@@ -386,40 +392,47 @@ __global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void k_mx_mx(MxArgs g) {
   const int in_group = tile % (GROUP * tiles_n), first_m = tile / (GROUP * tiles_n) * GROUP, gsz = min(g.tiles_m - first_m, GROUP);
   const int m0 = (first_m + in_group % gsz) * BM, n0 = in_group / gsz * BN;
   const int M = g.M, N = g.N, K = g.K, blocks = K / 32, valid_m = min(BM, M - m0), valid_n = min(BN, N - n0);
-  const int slabs = (blocks + 7) / 8, per_split = (slabs + splits - 1) / splits, slab0 = split * per_split, mine = min(slabs - slab0, per_split);
+  const int quads = (blocks + 15) / 16, per_split = (quads + splits - 1) / splits, slab0 = split * per_split * 4;
+  const int slabs = min((blocks + 3) / 4 - slab0, per_split * 4);                    // of this workgroup
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = (wave >> 1) * WM, wn = (wave & 1) * WN, frow = lane & 31, h = lane >> 5;
-  const unsigned char *const A = g.A + (size_t)m0 * (K / 2), *const W = g.W + (size_t)n0 * (K / 2);
-  __amdgpu_buffer_rsrc_t rs_a = __builtin_amdgcn_make_buffer_rsrc((void *)A, 0, (unsigned)valid_m * (unsigned)(K / 2), 0x00020000);
-  __amdgpu_buffer_rsrc_t rs_w = __builtin_amdgcn_make_buffer_rsrc((void *)W, 0, (unsigned)valid_n * (unsigned)(K / 2), 0x00020000);
-  // chunk = block of 32 elements; rows beyond the matrix lie outside the descriptors
-  const int chunk = (lane & 7) ^ ((lane >> 4) & 3);       // r = 8 q' + lane / 8: (r >> 1) & 7 = 4 (q' & 1) + (lane >> 4)
-  auto issue = [&](int slab, int stage) {
-    const unsigned so = slab < mine ? (unsigned)(slab0 + slab) * 128u : kOutside;
-    const int left = blocks - (slab0 + slab) * 8;          // blocks of this slab that exist
+  __amdgpu_buffer_rsrc_t rs_a = __builtin_amdgcn_make_buffer_rsrc((void *)(g.A + (size_t)m0 * (K / 2)), 0, (unsigned)valid_m * (unsigned)(K / 2), 0x00020000);
+  __amdgpu_buffer_rsrc_t rs_w = __builtin_amdgcn_make_buffer_rsrc((void *)(g.W + (size_t)n0 * (K / 2)), 0, (unsigned)valid_n * (unsigned)(K / 2), 0x00020000);
+  // An instruction fills 16 rows; lane l fetches chunk (block) (l % 4) ^ ((row / 4) % 4) of row l / 4, so that LDS reads spread over the banks.
+  // Rows beyond the matrix lie outside the descriptors.
+  const int chunk = (lane & 3) ^ ((lane >> 4) & 3);
+  const unsigned vo = (unsigned)(wave * 16 + (lane >> 2)) * (unsigned)(K / 2) + chunk * 16, row_step = 64u * (unsigned)(K / 2);
+  auto load = [&](int slab, int stage, int q) __attribute__((always_inline)) {          // q: 0 .. IA - 1 the rows, then the weights
+    const unsigned so = slab < slabs ? (unsigned)(slab0 + slab) * 64u : kOutside;
+    const bool gone = !WHOLE && (slab0 + slab) * 4 + chunk >= blocks;
+    const int r = q < IA ? q : q - IA;
+    const unsigned v = gone ? kOutside : vo + r * row_step;
+    if (q < IA) __builtin_amdgcn_raw_ptr_buffer_load_lds(rs_a, FK_LDS_PTR(lds + stage * ASTAGE + (r * 4 + wave) * 1024), 16, v, so, 0, 0);
+    else __builtin_amdgcn_raw_ptr_buffer_load_lds(rs_w, FK_LDS_PTR(lds + WBASE + stage * WSTAGE + (r * 4 + wave) * 1024), 16, v, so, 0, 0);
+  };
+  // scales of four slabs of SI rows per lane: rows of the tile, then of the weights; rows that do not exist take the last one's
+  const unsigned char *srow[SI];
 #pragma unroll
-    for (int q = 0; q < IA; ++q) {
-      const int r = (wave * IA + q) * 8 + (lane >> 3), c = chunk ^ (4 * ((wave * IA + q) & 1));
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs_a, FK_LDS_PTR(lds + stage * ASTAGE + (wave * IA + q) * 1024), 16, c < left ? (unsigned)r * (unsigned)(K / 2) + c * 16 : kOutside, so, 0, 0);
-    }
+  for (int u = 0; u < SI; ++u) {
+    const int r = (u * 4 + wave) * 64 + lane;
+    srow[u] = r < BM ? g.a_scales + (size_t)(m0 + min(r, valid_m - 1)) * blocks : g.w_scales + (size_t)(n0 + min(r - BM, valid_n - 1)) * blocks;
+  }
+  u32x4 fetched[SI];
+  auto fetch_scales = [&](int quad) __attribute__((always_inline)) {
+    const int b0 = slab0 * 4 + quad * 16;
 #pragma unroll
-    for (int q = 0; q < IB; ++q) {
-      const int r = (wave * IB + q) * 8 + (lane >> 3), c = chunk ^ (4 * ((wave * IB + q) & 1));
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs_w, FK_LDS_PTR(lds + WBASE + stage * WSTAGE + (wave * IB + q) * 1024), 16, c < left ? (unsigned)r * (unsigned)(K / 2) + c * 16 : kOutside, so, 0, 0);
+    for (int u = 0; u < SI; ++u) {
+      if (WHOLE) {
+        fetched[u] = *(const u32x4 *)(srow[u] + min(b0, blocks - 16));
+      } else {
+        const uint64_t lo = eight_scales(srow[u], b0, blocks), hi = eight_scales(srow[u], b0 + 8, blocks);
+        fetched[u] = u32x4{(unsigned)lo, (unsigned)(lo >> 32), (unsigned)hi, (unsigned)(hi >> 32)};
+      }
     }
   };
-  const unsigned char *sa[TM], *sb[TN];
+  auto hand_on_scales = [&](int quad) __attribute__((always_inline)) {
 #pragma unroll
-  for (int i = 0; i < TM; ++i) sa[i] = g.a_scales + (size_t)(m0 + min(wm + i * 32 + frow, valid_m - 1)) * blocks;
-#pragma unroll
-  for (int j = 0; j < TN; ++j) sb[j] = g.w_scales + (size_t)(n0 + min(wn + j * 32 + frow, valid_n - 1)) * blocks;
-  uint64_t ca[TM], cb[TN];
-  auto scales = [&](int slab) {
-    const int b0 = (slab0 + min(slab, mine - 1)) * 8;
-#pragma unroll
-    for (int i = 0; i < TM; ++i) ca[i] = eight_scales(sa[i], b0, blocks);
-#pragma unroll
-    for (int j = 0; j < TN; ++j) cb[j] = eight_scales(sb[j], b0, blocks);
+    for (int u = 0; u < SI; ++u) *(u32x4 *)(lds + SBASE + (quad & 1) * ROWS * 16 + ((u * 4 + wave) * 64 + lane) * 16) = fetched[u];
   };
   f32x16 acc[TM][TN];
 #pragma unroll
@@ -428,44 +441,93 @@ __global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void k_mx_mx(MxArgs g) {
     for (int j = 0; j < TN; ++j)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-  const int swz = (frow >> 1) & 7;
-  if (mine > 0) {
-    issue(0, 0);
-    scales(0);
+  // fragment s of a half of a slab in the order in which its MFMAs need them: W0, A0, W1 .. , A1 ..; the halves differ in one bit of the chunk
+  unsigned at_a[2], at_w[2];
+#pragma unroll
+  for (int ks = 0; ks < 2; ++ks) {
+    const unsigned c = (unsigned)((2 * ks + h) ^ ((frow >> 2) & 3)) << 4;
+    at_a[ks] = (wm + frow) * 64 + c;
+    at_w[ks] = WBASE + (wn + frow) * 64 + c;
   }
-  for (int slab = 0; slab < mine; ++slab) {
-    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+  u32x4 fa[2][TM], fw[2][TN];
+  auto read = [&](int s, int ks, int stage, int slot) __attribute__((always_inline)) {
+    const int f = s == 0 ? TM : s == 1 ? 0 : s <= TN ? TM + s - 1 : s - TN;
+    if (f < TM) fa[slot][f < TM ? f : 0] = *(const u32x4 *)(lds + at_a[ks] + stage * ASTAGE + (f < TM ? f : 0) * 2048);
+    else fw[slot][f < TM ? 0 : f - TM] = *(const u32x4 *)(lds + at_w[ks] + stage * WSTAGE + (f < TM ? 0 : f - TM) * 2048);
+  };
+  // the four scales of a slab of every row, in two sets: byte 2 ks belongs to half ks once the upper lanes' are moved down by one
+  unsigned ca[2][TM], cw[2][TN];
+  auto read_scales = [&](int quad, int of_quad, int slot) __attribute__((always_inline)) {
+    const unsigned char *from = lds + SBASE + (quad & 1) * ROWS * 16 + of_quad * 4;
+#pragma unroll
+    for (int i = 0; i < TM; ++i) ca[slot][i] = *(const unsigned *)(from + (wm + i * 32 + frow) * 16);
+#pragma unroll
+    for (int j = 0; j < TN; ++j) cw[slot][j] = *(const unsigned *)(from + (BM + wn + j * 32 + frow) * 16);
+  };
+  auto shift_scales = [&](int slot) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < TM; ++i) ca[slot][i] >>= 8 * h;
+#pragma unroll
+    for (int j = 0; j < TN; ++j) cw[slot][j] >>= 8 * h;
+  };
+  auto in_order = []() __attribute__((always_inline)) { loads_asked_for(); __builtin_amdgcn_sched_barrier(0); };
+  if (slabs > 0) {
+    fetch_scales(0);
+    in_order();
+#pragma unroll
+    for (int s = 0; s < kMxStages; ++s) {
+#pragma unroll
+      for (int q = 0; q < IA + IB; ++q) load(s, s, q);
+      in_order();
+    }
+    hand_on_scales(0);
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm((kMxStages - 1) * (IA + IB)));
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    uint64_t na[TM], nb[TN];
+    read_scales(0, 0, 0);
 #pragma unroll
-    for (int i = 0; i < TM; ++i) na[i] = ca[i] >> (8 * h);       // byte 2 j of the shifted scales belongs to this lane's half
+    for (int s = 0; s < NF; ++s) read(s, 0, 0, 0);
+    // OF: slab of its quad (its LDS stage), FETCH: whether another quad may follow
+    auto slab_of = [&](auto which, int quad) __attribute__((always_inline)) {
+      constexpr int OF = decltype(which)::value, SLOT = OF & 1, NEXT = (OF + 1) & 3;
+      shift_scales(SLOT);
 #pragma unroll
-    for (int j = 0; j < TN; ++j) nb[j] = cb[j] >> (8 * h);
-    issue(slab + 1, (slab + 1) & 1);
-    scales(slab + 1);
-    const unsigned char *pa = lds + (slab & 1) * ASTAGE, *pw = lds + WBASE + (slab & 1) * WSTAGE;
-#pragma unroll
-    for (int ks = 0; ks < 4; ++ks) {
-      i32x8 fa[TM], fb[TN];
-      const int ch = ((2 * ks + h) ^ swz) << 4;
-#pragma unroll
-      for (int i = 0; i < TM; ++i) {
-        const u32x4 v = *(const u32x4 *)(pa + (wm + i * 32 + frow) * 128 + ch);
-        fa[i] = i32x8{(int)v[0], (int)v[1], (int)v[2], (int)v[3], 0, 0, 0, 0};
-      }
-#pragma unroll
-      for (int j = 0; j < TN; ++j) {
-        const u32x4 v = *(const u32x4 *)(pw + (wn + j * 32 + frow) * 128 + ch);
-        fb[j] = i32x8{(int)v[0], (int)v[1], (int)v[2], (int)v[3], 0, 0, 0, 0};
-      }
-#pragma unroll
-      for (int i = 0; i < TM; ++i)
-#pragma unroll
-        for (int j = 0; j < TN; ++j) {
-          const int xa = (int)(na[i] >> (32 * (ks >> 1))), xb = (int)(nb[j] >> (32 * (ks >> 1)));
-          if (ks & 1) acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fa[i], fb[j], acc[i][j], 4, 4, 2, xa, 2, xb);
-          else acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fa[i], fb[j], acc[i][j], 4, 4, 0, xa, 0, xb);
+      for (int ks = 0; ks < 2; ++ks) {
+        if (ks == 1) {
+          if (OF == 3) hand_on_scales(quad + 1);
+          // the next slab has landed: younger are those of the two slabs behind it (and scales, which are not counted)
+          __builtin_amdgcn_s_waitcnt(vmcnt_imm((kMxStages - 2) * (IA + IB)));
+          asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+          if (OF == 0) { fetch_scales(quad + 1); in_order(); }
+          read_scales(OF == 3 ? quad + 1 : quad, NEXT, SLOT ^ 1);
         }
+#pragma unroll
+        for (int s = 0; s < NMF; ++s) {
+          const int i = s / TN, j = s % TN;
+          const i32x8 a = {(int)fa[ks][i][0], (int)fa[ks][i][1], (int)fa[ks][i][2], (int)fa[ks][i][3], 0, 0, 0, 0};
+          const i32x8 b = {(int)fw[ks][j][0], (int)fw[ks][j][1], (int)fw[ks][j][2], (int)fw[ks][j][3], 0, 0, 0, 0};
+          if (ks == 0) acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, acc[i][j], 4, 4, 0, (int)ca[SLOT][i], 0, (int)cw[SLOT][j]);
+          else acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, acc[i][j], 4, 4, 2, (int)ca[SLOT][i], 2, (int)cw[SLOT][j]);
+          if (s < NF) read(s, ks ^ 1, ks == 0 ? OF : NEXT, ks ^ 1);
+          if (ks == 1 && s < IA + IB) load(4 * quad + OF + kMxStages, OF, s);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+    };
+    constexpr std::integral_constant<int, 0> s0;
+    constexpr std::integral_constant<int, 1> s1;
+    constexpr std::integral_constant<int, 2> s2;
+    constexpr std::integral_constant<int, 3> s3;
+    int quad = 0;
+    for (; 4 * quad + 4 <= slabs; ++quad) {
+      slab_of(s0, quad);
+      slab_of(s1, quad);
+      slab_of(s2, quad);
+      slab_of(s3, quad);
+    }
+    if (!WHOLE && 4 * quad < slabs) {
+      slab_of(s0, quad);
+      if (4 * quad + 1 < slabs) slab_of(s1, quad);
+      if (4 * quad + 2 < slabs) slab_of(s2, quad);
     }
   }
   __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
@@ -487,14 +549,19 @@ __global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void k_mx_mx(MxArgs g) {
 #endif
 }
 
+template <int BM, int BN, int MODE>
+void launch_mx(hipStream_t s, const MxArgs &g) {
+  const int grid = (g.tiles_m * g.tiles_n * g.splits + 7) / 8 * 8;
+  if (g.K % 512 == 0 && g.K > 0) k_mx_mx<BM, BN, MODE, true><<<grid, 256, 0, s>>>(g);
+  else k_mx_mx<BM, BN, MODE, false><<<grid, 256, 0, s>>>(g);
+}
 template <int BM, int BN>
 void launch_mx(hipStream_t s, int mode, MxArgs g) {
   g.tiles_m = (g.M + BM - 1) / BM;
   g.tiles_n = (g.N + BN - 1) / BN;
-  const int grid = (g.tiles_m * g.tiles_n * g.splits + 7) / 8 * 8;
-  if (mode == XM_STORE) k_mx_mx<BM, BN, XM_STORE><<<grid, 256, 0, s>>>(g);
-  else if (mode == XM_STORE_F32) k_mx_mx<BM, BN, XM_STORE_F32><<<grid, 256, 0, s>>>(g);
-  else k_mx_mx<BM, BN, XM_PARTIAL><<<grid, 256, 0, s>>>(g);
+  if (mode == XM_STORE) launch_mx<BM, BN, XM_STORE>(s, g);
+  else if (mode == XM_STORE_F32) launch_mx<BM, BN, XM_STORE_F32>(s, g);
+  else launch_mx<BM, BN, XM_PARTIAL>(s, g);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -536,10 +603,10 @@ int whole_parts(int parts, int slabs) { const int per = (slabs + parts - 1) / pa
 struct Shape { int bm, bn, splits; };
 Shape shape_of(int rows, int n, int k, bool a_mx) {
   if (a_mx) {
-    const int t256 = ((rows + 255) / 256) * ((n + 255) / 256), slabs = (k / 32 + 7) / 8;
+    const int t256 = ((rows + 255) / 256) * ((n + 255) / 256), slabs = (k / 32 + 15) / 16;      // what is cut are quads of slabs
     if (t256 >= 192) return {256, 256, 1};
     const int tiles = ((rows + 127) / 128) * ((n + 127) / 128);
-    return {128, 128, whole_parts(parts_of(tiles, 512, slabs), std::max(1, slabs))};
+    return {128, 128, whole_parts(std::max(1, std::min(512 / tiles, slabs / 2)), std::max(1, slabs))};
   }
   const int bm = rows <= 32 ? 32 : 128, slabs = (k / 32 + 7) / 8, tiles_m = (rows + bm - 1) / bm, wide = tiles_m * ((n + 255) / 256);
   if (bm == 128 && wide >= 256) return {bm, 256, 1};
@@ -558,7 +625,7 @@ void mx_gemm(hipStream_t s, const void *a, const void *a_scales, int64_t lda, fo
   const bool a_mx = a_scales != nullptr;
   Shape p = shape_of(rows.cap, n, k, a_mx);
   const size_t stride = (size_t)rows.cap * n;
-  const int slabs = (k / 32 + 7) / 8;
+  const int slabs = a_mx ? (k / 32 + 15) / 16 : (k / 32 + 7) / 8;
   if (p.splits > 1) p.splits = whole_parts((int)std::max<size_t>(1, std::min<size_t>(p.splits, scratch.ptr ? scratch.bytes / (stride * 4) : 0)), slabs);
   const bool parts = p.splits > 1;
   if (a_mx) {
