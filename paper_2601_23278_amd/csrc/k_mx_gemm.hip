@@ -360,7 +360,7 @@ void launch_rows(hipStream_t s, int mode, const RowsArgs &g, int tile_slots) {
 
 // ---------------------------------------------------------------------------------------------
 // MXFP4 rows x MXFP4 weights: 2 x 2 wavefronts.  K goes in slabs of 128, 64 bytes of codes a row, through four LDS stages: a slab is asked for three
-// slabs before it is used.  Lane l supplies row l % 32 and, of the two halves of 64 elements of a slab, block 2 ks + l / 32: 16 bytes of codes and one
+// slabs before it is used, half of it in each half of a slab.  Lane l supplies row l % 32 and, of the two halves of 64 elements of a slab, block 2 ks + l / 32: 16 bytes of codes and one
 // scale.  Scales are fetched 16 bytes a row, for four slabs at once (a row per lane costs the vector caches a lookup per lane whatever its size), a
 // quad of slabs ahead, and handed on through LDS.  Pipelined by hand like k_mx_rows: behind each MFMA one fragment read of the next half or one load; the
 // only barrier of a slab stands before its second half.
@@ -379,9 +379,9 @@ constexpr int mx_lds(int bm, int bn) { return kMxStages * (bm + bn) * 64 + 2 * (
 template <int BM, int BN, int MODE, bool WHOLE>      // WHOLE: K is a multiple of 512
 __global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void k_mx_mx(MxArgs g) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  constexpr int WM = BM / 2, WN = BN / 2, TM = WM / 32, TN = WN / 32, NMF = TM * TN, NF = TM + TN, IA = BM / 64, IB = BN / 64, ROWS = BM + BN, SI = ROWS / 256;
+  constexpr int WM = BM / 2, WN = BN / 2, TM = WM / 32, TN = WN / 32, NMF = TM * TN, NF = TM + TN, IA = BM / 64, IB = BN / 64, ROWS = BM + BN, SI = ROWS / 256, HALF = (IA + IB) / 2, EVERY = NMF / HALF;
   constexpr int ASTAGE = BM * 64, WSTAGE = BN * 64, WBASE = kMxStages * ASTAGE, SBASE = WBASE + kMxStages * WSTAGE;
-  static_assert(NF <= NMF && IA + IB <= NMF, "one fragment read and one load per MFMA at most");
+  static_assert(NF <= NMF && HALF <= NMF, "one fragment read and one load per MFMA at most");
   __shared__ __attribute__((aligned(1024))) unsigned char lds[mx_lds(BM, BN)];
   const int splits = g.splits, tiles_n = g.tiles_n, total = g.tiles_m * tiles_n * splits, per_xcd = (total + 7) / 8;
   const int item = (blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
@@ -477,11 +477,11 @@ __global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void k_mx_mx(MxArgs g) {
 #pragma unroll
     for (int s = 0; s < kMxStages; ++s) {
 #pragma unroll
-      for (int q = 0; q < IA + IB; ++q) load(s, s, q);
+      for (int q = 0; q < (s < kMxStages - 1 ? 2 : 1) * HALF; ++q) load(s, s, q);
       in_order();
     }
     hand_on_scales(0);
-    __builtin_amdgcn_s_waitcnt(vmcnt_imm((kMxStages - 1) * (IA + IB)));
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm((2 * kMxStages - 3) * HALF));
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     read_scales(0, 0, 0);
 #pragma unroll
@@ -495,7 +495,7 @@ __global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void k_mx_mx(MxArgs g) {
         if (ks == 1) {
           if (OF == 3) hand_on_scales(quad + 1);
           // the next slab has landed: younger are those of the two slabs behind it (and scales, which are not counted)
-          __builtin_amdgcn_s_waitcnt(vmcnt_imm((kMxStages - 2) * (IA + IB)));
+          __builtin_amdgcn_s_waitcnt(vmcnt_imm((kMxStages - 2) * 2 * HALF));
           asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
           if (OF == 0) { fetch_scales(quad + 1); in_order(); }
           read_scales(OF == 3 ? quad + 1 : quad, NEXT, SLOT ^ 1);
@@ -508,7 +508,11 @@ __global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void k_mx_mx(MxArgs g) {
           if (ks == 0) acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, acc[i][j], 4, 4, 0, (int)ca[SLOT][i], 0, (int)cw[SLOT][j]);
           else acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, acc[i][j], 4, 4, 2, (int)ca[SLOT][i], 2, (int)cw[SLOT][j]);
           if (s < NF) read(s, ks ^ 1, ks == 0 ? OF : NEXT, ks ^ 1);
-          if (ks == 1 && s < IA + IB) load(4 * quad + OF + kMxStages, OF, s);
+          // spread: in a burst the loads hold up the MFMAs behind them for as long as the address unit takes
+          if (s % EVERY == EVERY - 1) {
+            if (ks == 0) load(4 * quad + OF + kMxStages - 1, (OF + 3) & 3, HALF + s / EVERY);
+            else load(4 * quad + OF + kMxStages, OF, s / EVERY);
+          }
           __builtin_amdgcn_sched_barrier(0);
         }
       }
