@@ -177,93 +177,111 @@ def _bad(text: str, *args):
     raise FocusError(FOCUS_EINVAL, text % args)
 
 
-def _on_device(device, *tensors):
+def _begin(device, stream) -> int:
+    """Address of the stream that a call's work goes to; its tensors live on `device`, which has to be the current one."""
     if device.type != "cuda" or device.index != torch.cuda.current_device():
         _bad("tensors must be on the current device, not on %s", device)
-    for t in tensors:
-        if t is not None and t.device != device:
-            _bad("tensors on %s and %s", device, t.device)
+    return torch._C._cuda_getCurrentRawStream(device.index) if stream is None else stream.cuda_stream
 
 
-def _rows_of(t: torch.Tensor, name: str, dtypes=None):
+def _new(shape, dtype, device, stream):
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _rows_of(t: torch.Tensor, name: str):
     """(rows, columns, distance of rows, dtype code) of a matrix whose rows are contiguous."""
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+    if t.dim() != 2:
+        _bad("%s must be a matrix", name)
+    (rows, cols), (ld, step) = t.shape, t.stride()
+    if (cols > 1 and step != 1) or (rows > 1 and ld < cols):
         _bad("%s must be a matrix with contiguous rows that do not overlap", name)
     code = _DTYPES.get(t.dtype)
-    if code is None or (dtypes is not None and t.dtype not in dtypes):
+    if code is None:
         _bad("%s has an unsupported dtype", name)
-    return t.shape[0], t.shape[1], t.stride(0) if t.shape[0] > 1 else t.shape[1], code
+    return rows, cols, ld if rows > 1 else cols, code
 
 
-def _plain(t: torch.Tensor, name: str, shape, dtype):
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous():
-        _bad("%s must be a contiguous %s tensor of shape %s", name, dtype, tuple(shape))
+def _plain(t: torch.Tensor, name: str, shape, dtype, device=None):
+    if t.shape != shape or t.dtype != dtype or not t.is_contiguous() or (device is not None and t.device != device):
+        _bad("%s must be a contiguous %s tensor of shape %s%s", name, dtype, tuple(shape), "" if device is None else " on %s" % device)
 
 
-def _mx_of(mx, name: str, *lead: int) -> tuple:
+def _mx_of(mx, name: str, *lead: int, device=None) -> tuple:
     """(focus_mx, K) of a pair of codes [*lead, K / 2] and scales [*lead, K / 32]."""
     codes, scales = mx
-    if codes.dim() != len(lead) + 1:
-        _bad("%s: codes must have %d dimensions", name, len(lead) + 1)
     blocks = scales.shape[-1] if scales.dim() else 0
-    _plain(codes, name + " (codes)", (*lead, 16 * blocks), torch.uint8)
-    _plain(scales, name + " (scales)", (*lead, blocks), torch.uint8)
+    _plain(codes, name + " (codes)", (*lead, 16 * blocks), torch.uint8, device)
+    _plain(scales, name + " (scales)", (*lead, blocks), torch.uint8, device)
     return focus_mx(codes.data_ptr(), scales.data_ptr()), 32 * blocks
 
 
-def _scratch(nbytes: int, device, stream):
-    if nbytes == 0:
-        return None
-    if stream is None:
-        return torch.empty(nbytes, dtype=torch.uint8, device=device)
-    with torch.cuda.stream(stream):
-        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+def _scratch(workspace, nbytes: int, device, stream):
+    """(address, bytes) of the caller's workspace, or of one made for the call, and the tensor that keeps it alive."""
+    if workspace is None:
+        if nbytes == 0:
+            return None, 0, None
+        workspace = _new(nbytes, torch.uint8, device, stream)
+    elif workspace.device != device or not workspace.is_contiguous():
+        _bad("the workspace must be a contiguous tensor on %s", device)
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
 
 
 def focus_route(router: focus_router, logits: torch.Tensor, bias: Optional[torch.Tensor] = None, experts: Optional[torch.Tensor] = None,
                 weights: Optional[torch.Tensor] = None, stream=None):
     """(experts [rows, k] int32, weights [rows, k] fp32) of the rows of logits [rows, E], fp32 or bf16."""
     rows, cols, ld, dtype = _rows_of(logits, "logits")
-    k, dev = router.experts_per_token, logits.device
-    _on_device(dev, bias, experts, weights)
-    if cols != router.n_experts:
-        _bad("logits have %d columns, the router %d experts", cols, router.n_experts)
+    dev, k = logits.device, router.experts_per_token
+    to = _begin(dev, stream)
+    if cols != router.n_experts or not 1 <= k <= 32:
+        _bad("logits have %d columns; the router has %d experts, %d of them for a row", cols, router.n_experts, k)
     if bias is not None:
-        _plain(bias, "bias", (cols,), torch.float32)
-    if experts is None or weights is None:
-        if k < 1 or k > 32:
-            _bad("experts_per_token must be in 1..32")
-        with torch.cuda.stream(stream):
-            experts = torch.empty(rows, k, dtype=torch.int32, device=dev) if experts is None else experts
-            weights = torch.empty(rows, k, dtype=torch.float32, device=dev) if weights is None else weights
-    _plain(experts, "experts", (rows, k), torch.int32)
-    _plain(weights, "weights", (rows, k), torch.float32)
-    _check(_lib.focus_route(C.byref(router), Focus._stream(stream), rows, dtype, logits.data_ptr(), ld, _ptr(bias), experts.data_ptr(), weights.data_ptr()))
+        _plain(bias, "bias", (cols,), torch.float32, dev)
+    if experts is None:
+        experts = _new((rows, k), torch.int32, dev, stream)
+    else:
+        _plain(experts, "experts", (rows, k), torch.int32, dev)
+    if weights is None:
+        weights = _new((rows, k), torch.float32, dev, stream)
+    else:
+        _plain(weights, "weights", (rows, k), torch.float32, dev)
+    rc = _lib.focus_route(router, to, rows, dtype, logits.data_ptr(), ld, None if bias is None else bias.data_ptr(), experts.data_ptr(), weights.data_ptr())
+    if rc:
+        _check(rc)
     return experts, weights
 
 
 def focus_mx_quantize(x: torch.Tensor, codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None, stream=None):
     """(codes, scales) of the rows of x [rows, cols], fp32 or bf16."""
     rows, cols, ld, dtype = _rows_of(x, "x")
-    _on_device(x.device, codes, scales)
-    blocks = (cols + 31) // 32
-    with torch.cuda.stream(stream):
-        codes = torch.empty(rows, 16 * blocks, dtype=torch.uint8, device=x.device) if codes is None else codes
-        scales = torch.empty(rows, blocks, dtype=torch.uint8, device=x.device) if scales is None else scales
-    _plain(codes, "codes", (rows, 16 * blocks), torch.uint8)
-    _plain(scales, "scales", (rows, blocks), torch.uint8)
-    _check(_lib.focus_mx_quantize(Focus._stream(stream), dtype, rows, cols, x.data_ptr(), ld, codes.data_ptr(), scales.data_ptr()))
+    dev, blocks = x.device, (cols + 31) // 32
+    to = _begin(dev, stream)
+    if codes is None:
+        codes = _new((rows, 16 * blocks), torch.uint8, dev, stream)
+    else:
+        _plain(codes, "codes", (rows, 16 * blocks), torch.uint8, dev)
+    if scales is None:
+        scales = _new((rows, blocks), torch.uint8, dev, stream)
+    else:
+        _plain(scales, "scales", (rows, blocks), torch.uint8, dev)
+    rc = _lib.focus_mx_quantize(to, dtype, rows, cols, x.data_ptr(), ld, codes.data_ptr(), scales.data_ptr())
+    if rc:
+        _check(rc)
     return codes, scales
 
 
 def focus_mx_dequantize(codes: torch.Tensor, scales: torch.Tensor, out: torch.Tensor, stream=None):
     """The values of codes and scales, into out [rows, cols], fp32 or bf16."""
     rows, cols, ld, dtype = _rows_of(out, "out")
-    _on_device(out.device, codes, scales)
-    mx, k = _mx_of((codes, scales), "mx", rows)
+    to = _begin(out.device, stream)
+    mx, k = _mx_of((codes, scales), "mx", rows, device=out.device)
     if k != (cols + 31) // 32 * 32:
         _bad("codes have %d elements a row, out %d columns", k, cols)
-    _check(_lib.focus_mx_dequantize(Focus._stream(stream), dtype, rows, cols, C.byref(mx), out.data_ptr(), ld))
+    rc = _lib.focus_mx_dequantize(to, dtype, rows, cols, mx, out.data_ptr(), ld)
+    if rc:
+        _check(rc)
     return out
 
 
@@ -276,23 +294,23 @@ def focus_mx_gemm_bytes(m: int, n: int, k: int, a_type: int) -> int:
 def focus_mx_gemm(a, w, out: torch.Tensor, workspace: Optional[torch.Tensor] = None, stream=None):
     """out [m, n] (fp32 or bf16) = A W^T; w the pair of an MXFP4 [n, k], a a bf16 matrix [m, k] or the pair of an MXFP4 [m, k]."""
     m, n, ldc, c_type = _rows_of(out, "out")
-    _on_device(out.device, w[0], w[1])
-    mw, k = _mx_of(w, "w", n)
+    dev = out.device
+    to = _begin(dev, stream)
+    mw, k = _mx_of(w, "w", n, device=dev)
     if isinstance(a, torch.Tensor):
-        rows, cols, lda, a_type = _rows_of(a, "a", (torch.bfloat16,))
-        a_ptr, a_scales, dev = a.data_ptr(), None, a.device
+        rows, cols, lda, a_type = _rows_of(a, "a")
+        if a_type != FOCUS_BF16 or a.device != dev:
+            _bad("a must be bf16 and on %s", dev)
+        a_ptr, a_scales = a.data_ptr(), None
     else:
-        ma, cols = _mx_of(a, "a", m)
-        rows, lda, a_type = m, cols, FOCUS_MX4
-        a_ptr, a_scales, dev = ma.codes, ma.scales, a[0].device
-        _on_device(out.device, a[1])
-    _on_device(out.device, workspace)
-    if dev != out.device or (rows, cols) != (m, k):
+        ma, cols = _mx_of(a, "a", m, device=dev)
+        rows, lda, a_type, a_ptr, a_scales = m, cols, FOCUS_MX4, ma.codes, ma.scales
+    if rows != m or cols != k:
         _bad("a is %d x %d, out %d x %d and w has %d columns", rows, cols, m, n, k)
-    if workspace is None:
-        workspace = _scratch(focus_mx_gemm_bytes(m, n, k, a_type), out.device, stream)
-    _check(_lib.focus_mx_gemm(Focus._stream(stream), m, n, k, a_type, a_ptr, a_scales, lda, C.byref(mw), c_type, out.data_ptr(), ldc, _ptr(workspace),
-                              0 if workspace is None else workspace.numel() * workspace.element_size()))
+    ws, ws_bytes, keep = _scratch(workspace, focus_mx_gemm_bytes(m, n, k, a_type) if workspace is None else 0, dev, stream)
+    rc = _lib.focus_mx_gemm(to, m, n, k, a_type, a_ptr, a_scales, lda, mw, c_type, out.data_ptr(), ldc, ws, ws_bytes)
+    if rc:
+        _check(rc)
     return out
 
 
@@ -306,23 +324,26 @@ def focus_mx_experts(gate_up, down, x: torch.Tensor, experts: torch.Tensor, weig
                      workspace: Optional[torch.Tensor] = None, stream=None):
     """out [rows, hidden] (+)= the routed SwiGLU experts of x [rows, hidden] bf16; gate_up, down the pairs of an MXFP4 [E, 2 ffn, hidden] and
     [E, hidden, ffn]; experts [rows, k] int32, weights [rows, k] fp32."""
-    rows, hidden, ldx, _ = _rows_of(x, "x", (torch.bfloat16,))
+    rows, hidden, ldx, x_type = _rows_of(x, "x")
     out_rows, out_cols, ldo, out_type = _rows_of(out, "out")
-    _on_device(out.device, x, experts, weights, *gate_up, *down, workspace)
-    E, two_ffn = gate_up[0].shape[:2] if gate_up[0].dim() == 3 else _bad("gate_up: codes must have 3 dimensions")
-    mg, hidden_g = _mx_of(gate_up, "gate_up", E, two_ffn)
-    md, ffn = _mx_of(down, "down", E, hidden)
-    if hidden_g != hidden or two_ffn != 2 * ffn or (out_rows, out_cols) != (rows, hidden):
+    dev = out.device
+    to = _begin(dev, stream)
+    if x_type != FOCUS_BF16 or x.device != dev:
+        _bad("x must be bf16 and on %s", dev)
+    if gate_up[0].dim() != 3 or experts.dim() != 2:
+        _bad("gate_up has three dimensions, experts two")
+    (E, two_ffn, _), k = gate_up[0].shape, experts.shape[1]
+    mg, hidden_g = _mx_of(gate_up, "gate_up", E, two_ffn, device=dev)
+    md, ffn = _mx_of(down, "down", E, hidden, device=dev)
+    if hidden_g != hidden or two_ffn != 2 * ffn or out_rows != rows or out_cols != hidden:
         _bad("x, out, gate_up and down do not fit together")
-    if experts.dim() != 2:
-        _bad("experts must be a matrix")
-    k = experts.shape[1]
-    _plain(experts, "experts", (rows, k), torch.int32)
-    _plain(weights, "weights", (rows, k), torch.float32)
-    if workspace is None:
-        workspace = _scratch(focus_mx_experts_bytes(E, hidden, ffn, rows, k), out.device, stream)
-    _check(_lib.focus_mx_experts(Focus._stream(stream), E, hidden, ffn, C.byref(mg), C.byref(md), rows, k, x.data_ptr(), ldx, experts.data_ptr(), weights.data_ptr(),
-                                 out_type, out.data_ptr(), ldo, int(add), _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size()))
+    _plain(experts, "experts", (rows, k), torch.int32, dev)
+    _plain(weights, "weights", (rows, k), torch.float32, dev)
+    ws, ws_bytes, keep = _scratch(workspace, focus_mx_experts_bytes(E, hidden, ffn, rows, k) if workspace is None else 0, dev, stream)
+    rc = _lib.focus_mx_experts(to, E, hidden, ffn, mg, md, rows, k, x.data_ptr(), ldx, experts.data_ptr(), weights.data_ptr(), out_type, out.data_ptr(), ldo,
+                               int(add), ws, ws_bytes)
+    if rc:
+        _check(rc)
     return out
 
 

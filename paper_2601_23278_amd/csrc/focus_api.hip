@@ -486,10 +486,17 @@ void moe_ffn(focus_ctx *c, hipStream_t s, int l, const RowSet &rs, float *resid,
   a.out_weights = c->route_by_row_id && c->out_route_weights ? c->out_route_weights + (size_t)l * plane : nullptr;
   { Timed t(c, s, FOCUS_KC_GEMM);
     fk::gemm(s, g.dtype, normed, c->w_router[l], g.n_experts, g.hidden, rs.rows, fk::EPI_STORE_F32, c->at<float>(pl.off_moe_logits), g.n_experts, c->layer_scratch(pl)); }
-  // MXFP4 experts work in the same buffers: the counts where the lists of entries would be, the tiles over the two arrays of tiles (one behind the other)
+  // MXFP4 experts work in the same buffers: the counts where the lists of entries would be, with the tiles behind them if they fit, else over the two
+  // arrays of tiles (one behind the other), which tiles of 128 rows do
   const focus_mx mx = c->mx_of(c->mx_expert_gate_up, l);
   fk::MxExperts m{g.n_experts, g.hidden, g.expert_ffn, g.experts_per_token, mx, c->mx_of(c->mx_expert_down, l), a.rows, a.u, g.hidden, a.topk_idx, a.topk_w,
-                  FOCUS_F32, resid, g.hidden, true, a.list, (int2 *)a.tile_e, a.n_tiles, a.pos, a.arow, a.act, a.y};
+                  FOCUS_F32, resid, g.hidden, true, a.list, 128, (int2 *)a.tile_e, a.n_tiles, a.pos, a.arow, a.act, a.y};
+  const int cap = a.rows.cap, few = fk::mx_tile_rows(a.rows.expected(), m.k, m.n_experts);
+  const size_t counts = ((size_t)fk::mx_chunks(cap, m.k) * m.n_experts * 4 + 255) & ~(size_t)255;
+  if (counts + (size_t)fk::mx_tile_slots(cap, m.k, m.n_experts, few) * 8 <= (size_t)m.n_experts * cap * 4) {
+    m.tile_rows = few;
+    m.tiles = (int2 *)((char *)a.list + counts);
+  }
   { Timed t(c, s, FOCUS_KC_ROUTE);
     if (c->has_router) {
       const float *bias = c->router_bias.empty() ? nullptr : c->router_bias[l];

@@ -43,9 +43,8 @@ size_t mx_gemm_scratch(int rows, int n, int k, bool a_mx);
 void mx_gemm(hipStream_t s, const void *a, const void *a_scales, int64_t lda, focus_mx w, int n, int k, Rows rows, int epilogue, void *out, int64_t ldo,
              Scratch scratch);
 
-// Routed experts.  Entries (row, choice) are sorted by expert into tiles of kMxTileRows rows, multiplied expert by expert, and
-// added up row by row.
-constexpr int kMxTileRows = 128, kMxMaxExperts = 512;
+// Routed experts.  Entries (row, choice) are sorted by expert into tiles of 32 or 128 rows, multiplied expert by expert, and added up row by row.
+constexpr int kMxMaxExperts = 512, kMxFewRows = 32;
 struct MxExperts {
   int n_experts, hidden, ffn, k;
   focus_mx gate_up, down;
@@ -60,6 +59,7 @@ struct MxExperts {
   bool add;
   // work buffers
   int32_t *hist;                  // [mx_chunks(), E] entries of every expert in every 1024 entries
+  int tile_rows;                  // 32 or 128
   int2 *tiles;                    // [mx_tile_slots()] first sorted row; expert and rows << 16
   int32_t *n_tiles;               // [1]
   int32_t *pos;                   // [rows * k] entry -> sorted row, -1: no such expert
@@ -67,7 +67,8 @@ struct MxExperts {
   void *act;                      // [rows * k, ffn] bf16
   float *y;                       // [rows * k, hidden]
 };
-int mx_tile_slots(int rows, int k, int n_experts);
+int mx_tile_rows(int rows, int k, int n_experts);     // the height for so many rows: what is expected, where only the device knows
+int mx_tile_slots(int rows, int k, int n_experts, int tile_rows);
 int mx_chunks(int rows, int k);
 size_t mx_experts_bytes(int n_experts, int hidden, int ffn, int n_rows, int k);
 void lay_mx_experts(MxExperts &a, void *workspace);

@@ -3,6 +3,7 @@
 // Two forms.  bf16 rows: codes become bf16 in registers (a 4-bit float times a power of two is exact in bf16) and go through
 // v_mfma_f32_32x32x16_bf16.  MXFP4 rows: codes and scales go as they are through v_mfma_scale_f32_32x32x64_f8f6f4, four times the rate.
 #include <algorithm>
+#include <iterator>
 #include <type_traits>
 
 #include "focus_mx.h"
@@ -569,52 +570,84 @@ void launch_mx(hipStream_t s, int mode, MxArgs g) {
 }
 
 // ---------------------------------------------------------------------------------------------
-// Adds the parts of a cut K in part order and does the epilogue.
-template <int EPI>
+// Adds the parts of a cut K in part order and does the epilogue.  A thread takes V neighbouring columns of a row (four where the rows of all operands
+// are 16-byte aligned), and all its parts are asked for before the first is added, four at a time.
+template <int EPI, int V>
 __global__ __launch_bounds__(256) void k_mx_reduce(const float *__restrict__ part, int splits, size_t stride, Rows rows, int n, void *out, int64_t ldo) {
+  typedef float fv __attribute__((ext_vector_type(V)));
   const int M = rows.count ? min(*rows.count, rows.cap) : rows.cap, cols = EPI == MX_SILU_MUL ? n / 2 : n;
-  const int64_t total = (int64_t)M * cols;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-    const int64_t row = i / cols, col = i - row * cols;
-    const float *p = part + row * n + col;
-    float v = 0.f, u = 0.f;
-    for (int k = 0; k < splits; ++k) {
-      v += p[(size_t)k * stride];
-      if (EPI == MX_SILU_MUL) u += p[(size_t)k * stride + n / 2];
+  const int col = (blockIdx.x * 256 + threadIdx.x) * V;
+  if (col >= cols) return;
+  for (int row = blockIdx.y; row < M; row += gridDim.y) {
+    const float *p = part + (size_t)row * n + col;
+    fv v = 0.f, u = 0.f;
+    for (int k0 = 0; k0 < splits; k0 += 4) {
+      fv a[4], b[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        a[k] = k0 + k < splits ? *(const fv *)(p + (size_t)(k0 + k) * stride) : (fv)0.f;
+        if (EPI == MX_SILU_MUL) b[k] = k0 + k < splits ? *(const fv *)(p + (size_t)(k0 + k) * stride + n / 2) : (fv)0.f;
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        v += a[k];
+        if (EPI == MX_SILU_MUL) u += b[k];
+      }
     }
     const size_t at = (size_t)row * ldo + col;
-    if (EPI == MX_STORE) ((bf16_t *)out)[at] = (bf16_t)v;
-    else if (EPI == MX_STORE_F32) ((float *)out)[at] = v;
-    else if (EPI == MX_ADD_F32) ((float *)out)[at] += v;
-    else ((bf16_t *)out)[at] = (bf16_t)(v / (1.0f + __expf(-v)) * u);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      if (EPI == MX_STORE) ((bf16_t *)out)[at + i] = (bf16_t)v[i];
+      else if (EPI == MX_STORE_F32) ((float *)out)[at + i] = v[i];
+      else if (EPI == MX_ADD_F32) ((float *)out)[at + i] += v[i];
+      else ((bf16_t *)out)[at + i] = (bf16_t)(v[i] / (1.0f + __expf(-v[i])) * u[i]);
+    }
   }
 }
 
+template <int V> void launch_reduce(hipStream_t s, int epi, const float *part, int splits, size_t stride, Rows rows, int n, void *out, int64_t ldo) {
+  const int cols = epi == MX_SILU_MUL ? n / 2 : n;
+  const dim3 grid((cols + 256 * V - 1) / (256 * V), std::min(rows.cap, 32768));
+  if (epi == MX_STORE) k_mx_reduce<MX_STORE, V><<<grid, 256, 0, s>>>(part, splits, stride, rows, n, out, ldo);
+  else if (epi == MX_STORE_F32) k_mx_reduce<MX_STORE_F32, V><<<grid, 256, 0, s>>>(part, splits, stride, rows, n, out, ldo);
+  else if (epi == MX_ADD_F32) k_mx_reduce<MX_ADD_F32, V><<<grid, 256, 0, s>>>(part, splits, stride, rows, n, out, ldo);
+  else k_mx_reduce<MX_SILU_MUL, V><<<grid, 256, 0, s>>>(part, splits, stride, rows, n, out, ldo);
+}
 void launch_reduce(hipStream_t s, int epi, const float *part, int splits, size_t stride, Rows rows, int n, void *out, int64_t ldo) {
-  const int64_t total = (int64_t)rows.cap * (epi == MX_SILU_MUL ? n / 2 : n);
-  const int grid = (int)std::min<int64_t>((total + 255) / 256, 4096);
-  if (epi == MX_STORE) k_mx_reduce<MX_STORE><<<grid, 256, 0, s>>>(part, splits, stride, rows, n, out, ldo);
-  else if (epi == MX_STORE_F32) k_mx_reduce<MX_STORE_F32><<<grid, 256, 0, s>>>(part, splits, stride, rows, n, out, ldo);
-  else if (epi == MX_ADD_F32) k_mx_reduce<MX_ADD_F32><<<grid, 256, 0, s>>>(part, splits, stride, rows, n, out, ldo);
-  else k_mx_reduce<MX_SILU_MUL><<<grid, 256, 0, s>>>(part, splits, stride, rows, n, out, ldo);
+  // the parts' rows are n apart, and so are the parts' starts rows.cap * n: both multiples of four where n (with SiLU*up half of it) is
+  if (n % (epi == MX_SILU_MUL ? 8 : 4) == 0 && ((uintptr_t)part & 15) == 0) launch_reduce<4>(s, epi, part, splits, stride, rows, n, out, ldo);
+  else launch_reduce<1>(s, epi, part, splits, stride, rows, n, out, ldo);
 }
 
-// Parts of K for `tiles` workgroups of which `resident` run at once: as many as fill the chip, each with 2 slabs at least.
-int parts_of(int tiles, int resident, int slabs) { return std::max(1, std::min(resident / std::max(1, tiles), slabs / 2)); }
-// parts with no slab left over are dropped
-int whole_parts(int parts, int slabs) { const int per = (slabs + parts - 1) / parts; return (slabs + per - 1) / per; }
+// parts with no unit of K left over are dropped
+int whole_parts(int parts, int units) { const int per = (units + parts - 1) / parts; return (units + per - 1) / per; }
 
+// Tile and parts of K with the least estimated time.  Measured on 15 problems of 8 to 2048 rows, 2048 to 24576 columns and K of 2048 to 12288, every
+// tile with up to 16 parts; the estimate picks the best or one within 12 % of it.  us for one unit of K (256; both operands in MXFP4: 512) of n
+// workgroups = base + first min(n, 256) / 256 + more max(n - 256, 0) / 256; a launch costs 3 us, adding parts 2.5 us and 8 bytes an output and part at
+// 4.5 TB/s.  (333 rows x 4096, K = 4096, MXFP4 rows: 13.8 us in one part, 22.8 in five, which fill the chip; K = 12288: 30.7 in one, 24.9 in two.  1024 rows: 128 x 128
+// 17.9, 256 x 256 34.3; 2048 rows x 6144: 45.1 and 40.7.  bf16 rows: 8 x 24576 32 x 128 17, 128 x 128 18.5; 1024 x 4096 128 x 128 41.4, 128 x 256 55.)
+struct Variant { int bm, bn; float base, first, more; };
+constexpr Variant kRowVariants[] = {{32, 128, 0.8f, 0.45f, 0.6f}, {128, 128, 1.4f, 1.0f, 1.7f}, {128, 256, 2.6f, 1.1f, 3.0f}};
+constexpr Variant kMxVariants[] = {{128, 128, 0.95f, 0.6f, 2.15f}, {256, 256, 2.0f, 3.2f, 5.3f}};
 struct Shape { int bm, bn, splits; };
 Shape shape_of(int rows, int n, int k, bool a_mx) {
-  if (a_mx) {
-    const int t256 = ((rows + 255) / 256) * ((n + 255) / 256), slabs = (k / 32 + 15) / 16;      // what is cut are quads of slabs
-    if (t256 >= 192) return {256, 256, 1};
-    const int tiles = ((rows + 127) / 128) * ((n + 127) / 128);
-    return {128, 128, whole_parts(std::max(1, std::min(512 / tiles, slabs / 2)), std::max(1, slabs))};
+  const int units = std::max(1, a_mx ? (k / 32 + 15) / 16 : (k / 32 + 7) / 8);
+  Shape best{0, 0, 1};
+  float least = 0.f;
+  for (const Variant *v = a_mx ? kMxVariants : kRowVariants, *end = a_mx ? std::end(kMxVariants) : std::end(kRowVariants); v != end; ++v) {
+    const int tiles_m = (rows + v->bm - 1) / v->bm;
+    const int64_t tiles = (int64_t)tiles_m * ((n + v->bn - 1) / v->bn);
+    // tile rows of 32 that hold no rows are skipped
+    const float live = a_mx || v->bm == 32 ? 1.f : 0.4f + 0.6f * (float)((rows + 31) / 32) / (float)(tiles_m * v->bm / 32);
+    for (int parts = 1; parts <= std::min(units, 16); ++parts) {
+      if (whole_parts(parts, units) != parts || (parts > 1 && tiles * parts > 1024)) continue;
+      const float wg = (float)(tiles * parts), unit_us = v->base + v->first * std::min(wg, 256.f) / 256.f + v->more * std::max(wg - 256.f, 0.f) / 256.f;
+      const float us = 3.f + live * unit_us * (float)((units + parts - 1) / parts) + (parts > 1 ? 2.5f + (float)parts * (float)rows * (float)n * (8.f / 4.5e6f) : 0.f);
+      if (!best.bm || us < least) { best = {v->bm, v->bn, parts}; least = us; }
+    }
   }
-  const int bm = rows <= 32 ? 32 : 128, slabs = (k / 32 + 7) / 8, tiles_m = (rows + bm - 1) / bm, wide = tiles_m * ((n + 255) / 256);
-  if (bm == 128 && wide >= 256) return {bm, 256, 1};
-  return {bm, 128, whole_parts(parts_of(tiles_m * ((n + 127) / 128), 512, slabs), std::max(1, slabs))};
+  return best;
 }
 
 }  // namespace
@@ -627,10 +660,10 @@ size_t mx_gemm_scratch(int rows, int n, int k, bool a_mx) {
 void mx_gemm(hipStream_t s, const void *a, const void *a_scales, int64_t lda, focus_mx w, int n, int k, Rows rows, int epilogue, void *out, int64_t ldo, Scratch scratch) {
   if (rows.cap <= 0 || n <= 0) return;
   const bool a_mx = a_scales != nullptr;
-  Shape p = shape_of(rows.cap, n, k, a_mx);
+  Shape p = shape_of(rows.expected(), n, k, a_mx);
   const size_t stride = (size_t)rows.cap * n;
-  const int slabs = a_mx ? (k / 32 + 15) / 16 : (k / 32 + 7) / 8;
-  if (p.splits > 1) p.splits = whole_parts((int)std::max<size_t>(1, std::min<size_t>(p.splits, scratch.ptr ? scratch.bytes / (stride * 4) : 0)), slabs);
+  const int units = a_mx ? (k / 32 + 15) / 16 : (k / 32 + 7) / 8;
+  if (p.splits > 1) p.splits = whole_parts((int)std::max<size_t>(1, std::min<size_t>(p.splits, scratch.ptr ? scratch.bytes / (stride * 4) : 0)), units);
   const bool parts = p.splits > 1;
   if (a_mx) {
     MxArgs g{(const unsigned char *)a, (const unsigned char *)a_scales, (const unsigned char *)w.codes, (const unsigned char *)w.scales, rows.cap, n, k, 0, 0, p.splits,
@@ -650,17 +683,28 @@ void mx_gemm(hipStream_t s, const void *a, const void *a_scales, int64_t lda, fo
   if (parts) launch_reduce(s, epilogue, (const float *)scratch.ptr, p.splits, stride, rows, n, out, ldo);
 }
 
+// Tiles of 32 x 128 for up to kMxFewRows rows per expert on average (256 experts, 2048 -> 512, whole operator in us, 32-row tiles / 128-row ones: 4 rows an expert 107 / 116, 16 129 /
+// 140, 32 170 / 170, 64 262 / 220; 8 experts, 2560 -> 1408, 16 rows 33 / 35, 64 47 / 48, 128 72 / 61).  Above, 128 x 256 where there may be kMxWide of them, 128 x 128 where
+// the wide ones would leave compute units idle (128 x 256 / 128 x 128: 8 experts, 256 rows each 90 / 84, 1024 rows each 218 / 229; 32 experts, 1024 -> 768, 128 rows each 60 / 50).
+constexpr int kMxWide = 512;
+template <int MODE>
+static void launch_grouped(hipStream_t s, const RowsArgs &a, const MxExperts &m) {
+  const int slots = mx_tile_slots(m.rows.cap, m.k, m.n_experts, m.tile_rows);
+  if (m.tile_rows == 32) launch_rows<32, 1, MODE, true>(s, a, slots);
+  else if ((int64_t)mx_tile_slots(m.rows.expected(), m.k, m.n_experts, 128) * ((a.N + 255) / 256) >= kMxWide) launch_rows<128, 2, MODE, true>(s, a, slots);
+  else launch_rows<128, 1, MODE, true>(s, a, slots);
+}
+
 void mx_grouped(hipStream_t s, const MxExperts &m) {
   RowsArgs a{};
   a.A = (const bf16_t *)m.x; a.lda = m.ldx; a.src = m.arow; a.a_bytes = (unsigned)(((int64_t)(m.rows.cap - 1) * m.ldx + m.hidden) * 2);
   a.codes = (const unsigned char *)m.gate_up.codes; a.scales = (const unsigned char *)m.gate_up.scales;
   a.N = 2 * m.ffn; a.K = m.hidden; a.tiles = m.tiles; a.n_tiles = m.n_tiles; a.splits = 1; a.out = m.act; a.ldo = m.ffn;
-  const int slots = mx_tile_slots(m.rows.cap, m.k, m.n_experts);
-  launch_rows<128, 2, RM_SILU, true>(s, a, slots);
+  launch_grouped<RM_SILU>(s, a, m);
   a.A = (const bf16_t *)m.act; a.lda = m.ffn; a.src = nullptr; a.a_bytes = 0;
   a.codes = (const unsigned char *)m.down.codes; a.scales = (const unsigned char *)m.down.scales;
   a.N = m.hidden; a.K = m.ffn; a.out = m.y; a.ldo = m.hidden;
-  launch_rows<128, 2, RM_STORE_F32, true>(s, a, slots);
+  launch_grouped<RM_STORE_F32>(s, a, m);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -731,7 +775,7 @@ __global__ __launch_bounds__(kChunk) void k_mx_place(MxExperts a, int chunks, in
     if (tid < E) all = next[tid];
   }
   // exclusive sums over the experts of rows and full tiles, and of tiles of three, two and one tile rows (10 bits each)
-  const int full = all / kMxTileRows, rest = (all % kMxTileRows + 31) / 32 % 4, whole = full + (all % kMxTileRows > 96);
+  const int T = a.tile_rows, full = all / T, rest = (all % T + 31) / 32 % (T / 32), whole = full + (all % T > T - 32);
   const uint64_t w0 = ((uint64_t)whole << 32) | (unsigned)all;
   const unsigned n0 = rest ? 1u << (10 * (3 - rest)) : 0u;
   uint64_t w = w0;
@@ -758,12 +802,12 @@ __global__ __launch_bounds__(kChunk) void k_mx_place(MxExperts a, int chunks, in
     if (me == 0) {
       int t = (int)(w >> 32);
       for (int m = 0; m < whole; ++m, ++t)
-        if (t < tile_slots) a.tiles[t] = make_int2(first + m * kMxTileRows, tid | min(kMxTileRows, all - m * kMxTileRows) << 16);
+        if (t < tile_slots) a.tiles[t] = make_int2(first + m * T, tid | min(T, all - m * T) << 16);
       if (rest) {
         t = (int)(w_all >> 32);
         for (int r = 3; r > rest; --r) t += q_all >> (10 * (3 - r)) & 1023;
         t += q >> (10 * (3 - rest)) & 1023;
-        if (t < tile_slots) a.tiles[t] = make_int2(first + full * kMxTileRows, tid | (all - full * kMxTileRows) << 16);
+        if (t < tile_slots) a.tiles[t] = make_int2(first + full * T, tid | (all - full * T) << 16);
       }
     }
   }
@@ -806,8 +850,9 @@ __global__ __launch_bounds__(256) void k_mx_combine(MxExperts a) {
 }
 }  // namespace
 
+int mx_tile_rows(int rows, int k, int n_experts) { return rows * k <= kMxFewRows * std::min(rows * k, n_experts) ? 32 : 128; }
 // Row tiles there can be, rounded up to the eight XCDs that take them in turn.
-int mx_tile_slots(int rows, int k, int n_experts) { return (rows * k / kMxTileRows + std::min(rows * k, n_experts) + 7) / 8 * 8; }
+int mx_tile_slots(int rows, int k, int n_experts, int tile_rows) { return (rows * k / tile_rows + std::min(rows * k, n_experts) + 7) / 8 * 8; }
 int mx_chunks(int rows, int k) { return (rows * k + kChunk - 1) / kChunk; }
 
 // Lays the work buffers out from `base`; returns their size.
@@ -816,7 +861,8 @@ static size_t lay(MxExperts &a, char *base, int rows) {
   size_t at = 0;
   auto take = [&](size_t bytes) { char *p = base + at; at += (bytes + 255) & ~(size_t)255; return p; };
   a.hist = (int32_t *)take((size_t)mx_chunks(rows, a.k) * a.n_experts * 4);
-  a.tiles = (int2 *)take((size_t)mx_tile_slots(rows, a.k, a.n_experts) * 8);
+  a.tile_rows = mx_tile_rows(rows, a.k, a.n_experts);
+  a.tiles = (int2 *)take((size_t)mx_tile_slots(rows, a.k, a.n_experts, a.tile_rows) * 8);
   a.n_tiles = (int32_t *)take(4);
   a.pos = (int32_t *)take(ent * 4);
   a.arow = (int32_t *)take(ent * 4);
@@ -833,7 +879,7 @@ void lay_mx_experts(MxExperts &a, void *workspace) { lay(a, (char *)workspace, a
 
 void mx_group(hipStream_t s, const MxExperts &a) {
   if (a.rows.cap <= 0) return;
-  const int chunks = mx_chunks(a.rows.cap, a.k), slots = mx_tile_slots(a.rows.cap, a.k, a.n_experts);
+  const int chunks = mx_chunks(a.rows.cap, a.k), slots = mx_tile_slots(a.rows.cap, a.k, a.n_experts, a.tile_rows);
   if (chunks <= kCountAll) {
     k_mx_place<false><<<chunks, kChunk, 0, s>>>(a, chunks, slots);
   } else {

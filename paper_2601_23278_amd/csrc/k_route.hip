@@ -19,10 +19,36 @@ __device__ __forceinline__ float lane_of(float v, int l) { return __int_as_float
 __device__ __forceinline__ double lane_of(double v, int l) { return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), l), __builtin_amdgcn_readlane(__double2loint(v), l)); }
 __device__ __forceinline__ float exp_of(float v) { return expf(v); }
 __device__ __forceinline__ double exp_of(double v) { return exp(v); }
+// Over the wavefront, by lane exchanges in the vector unit: rows of 16 lanes by 1, 2, 4 and 8, then a row's last lane to the next row, then the lower
+// half's to the upper; the result is in the last lane.  Six exchanges through LDS, of which every pick waits for one after the other, took ten times as
+// long (a whole call of 2048 rows 10.3 us instead of 7.2).  Lanes without a source keep `other`.
+template <int CTRL, int ROWS> __device__ __forceinline__ float moved(float other, float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(other), __float_as_int(v), CTRL, ROWS, 0xF, false));
+}
+template <int CTRL, int ROWS> __device__ __forceinline__ double moved(double other, double v) {
+  return __hiloint2double(__builtin_amdgcn_update_dpp(__double2hiint(other), __double2hiint(v), CTRL, ROWS, 0xF, false),
+                          __builtin_amdgcn_update_dpp(__double2loint(other), __double2loint(v), CTRL, ROWS, 0xF, false));
+}
+__device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }
+__device__ __forceinline__ double larger(double a, double b) { return fmax(a, b); }
 template <typename R> __device__ __forceinline__ R largest(R v) {
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) { const R o = __shfl_xor(v, d); v = o > v ? o : v; }
-  return v;
+  v = larger(v, moved<0x111, 0xF>(v, v));
+  v = larger(v, moved<0x112, 0xF>(v, v));
+  v = larger(v, moved<0x114, 0xF>(v, v));
+  v = larger(v, moved<0x118, 0xF>(v, v));
+  v = larger(v, moved<0x142, 0xA>(v, v));
+  v = larger(v, moved<0x143, 0xC>(v, v));
+  return lane_of(v, 63);
+}
+template <typename R> __device__ __forceinline__ R total(R v) {
+  const R none = 0;
+  v += moved<0x111, 0xF>(none, v);
+  v += moved<0x112, 0xF>(none, v);
+  v += moved<0x114, 0xF>(none, v);
+  v += moved<0x118, 0xF>(none, v);
+  v += moved<0x142, 0xA>(none, v);
+  v += moved<0x143, 0xC>(none, v);
+  return lane_of(v, 63);
 }
 // LDS traffic between the lanes of one wavefront: it runs in order, only the compiler has to keep it so
 __device__ __forceinline__ void wave_lds_order() {
@@ -32,10 +58,10 @@ __device__ __forceinline__ void wave_lds_order() {
 
 template <typename R> constexpr R kLow = -(R)INFINITY;
 
-// Picks of one row; false (R = float only): fp32 does not decide it.  idx and score of lane j < k are those of the j-th pick.  sh: 64 * P
-// numbers of LDS of this wavefront.
+// Picks of one row; false (R = float only): fp32 does not decide it.  idx and score of lane j < k are those of the j-th pick.  sh: LDS of this
+// wavefront, 64 * P numbers and, with fp32, twice as many more.
 template <typename R, int P>
-__device__ bool pick(const RouteArgs &a, const float (&l)[P], const float (&bias)[P], R *sh, const int32_t *forced, int &idx, R &score) {
+__device__ __forceinline__ bool pick(const RouteArgs &a, const float (&l)[P], const float (&bias)[P], R *sh, const int32_t *forced, int &idx, R &score) {
   constexpr bool F32 = sizeof(R) == 4;
   const focus_router &r = a.router;
   const int lane = threadIdx.x & 63, E = r.n_experts, k = r.experts_per_token, G = r.n_groups, first = lane * P;
@@ -55,8 +81,7 @@ __device__ bool pick(const RouteArgs &a, const float (&l)[P], const float (&bias
       s[i] = first + i < E && l[i] == l[i] && top_logit > -INFINITY ? (l[i] == top_logit ? (R)1 : exp_of((R)l[i] - (R)top_logit)) : (R)0;
       sum += s[i];
     }
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) sum += __shfl_xor(sum, d);
+    sum = total(sum);
 #pragma unroll
     for (int i = 0; i < P; ++i) s[i] = sum > 0 ? s[i] / sum : (R)0;
   }
@@ -120,34 +145,79 @@ __device__ bool pick(const RouteArgs &a, const float (&l)[P], const float (&bias
       if (first + i < E && !((kept >> (group * step)) & 1)) alive &= ~(1u << i);
     }
   }
-  R last_c = 0, last_s = 0;
-  float last_l = 0, last_b = 0;
-  for (int j = 0;; ++j) {
-    // best element of the lane, then of the wavefront; the lowest lane and in it the lowest element among equals
-    R hc = kLow<R>, hs = 0;
-    float hl = 0, hb = 0;
-    int hi = -1;
+  // each lane's elements by falling choice, ties by the lower element; those that cannot be chosen come last
+  constexpr int kNone = 0x7FFFFFFF;
+  int order[P];
 #pragma unroll
-    for (int i = 0; i < P; ++i)
-      if (((alive >> i) & 1) && (hi < 0 || c[i] > hc)) { hc = c[i]; hs = s[i]; hl = l[i]; hb = bias[i]; hi = i; }
-    const R best = largest(hc);
-    const uint64_t who = __ballot(hi >= 0 && hc == best);
-    if (!who) break;                                                // nothing left (j >= k)
-    const int w = __ffsll((unsigned long long)who) - 1;
-    const R ws = lane_of(hs, w);
-    const int we = __builtin_amdgcn_readlane(first + hi, w);
-    if (F32) {
-      const float wl = lane_of(hl, w), wb = lane_of(hb, w);
-      if (j > 0 && !(wl == last_l && wb == last_b)) {
-        // scores are off by at most 6e-7 of themselves (sigmoid), 1.2e-6 and 1.2e-7 per unit of distance from the largest logit (softmax)
-        const float rel = r.score == FOCUS_SCORE_SIGMOID ? 6e-7f : 1.2e-6f + 1.2e-7f * (top_logit - fminf(wl, last_l));
-        if (last_c - best <= rel * (ws + last_s) + 2e-7f * (fabsf((float)best) + fabsf((float)last_c))) return false;
-        if (j >= k) break;
-      }
-      last_c = best; last_s = ws; last_l = wl; last_b = wb;
-    } else if (j >= k) break;
-    if (lane == j && j < k) { idx = we; score = ws; }
-    if (lane == w) alive &= ~(1u << hi);
+  for (int i = 0; i < P; ++i) {
+    order[i] = (alive >> i) & 1 ? first + i : kNone;
+    if (!((alive >> i) & 1)) c[i] = kLow<R>;
+  }
+#pragma unroll
+  for (int n = 0; n < P; ++n)
+#pragma unroll
+    for (int i = n & 1; i + 1 < P; i += 2) {
+      const bool swap = c[i + 1] > c[i] || (c[i + 1] == c[i] && order[i + 1] < order[i]);
+      const R hc = swap ? c[i + 1] : c[i], lc = swap ? c[i] : c[i + 1];
+      const int ho = swap ? order[i + 1] : order[i], lo = swap ? order[i] : order[i + 1];
+      c[i] = hc; c[i + 1] = lc; order[i] = ho; order[i + 1] = lo;
+    }
+  // scores, and logits and biases for the comparison of neighbours, by expert
+  float *const sh_l = (float *)(sh + 64 * P), *const sh_b = sh_l + 64 * P;
+  wave_lds_order();
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    sh[first + i] = s[i];
+    if (F32) { sh_l[first + i] = l[i]; sh_b[first + i] = bias[i]; }
+  }
+  wave_lds_order();
+  R choice = 0;
+  int found = 0;
+  // the next best of the wavefront: the lowest lane among equals; its expert, or -1
+  auto next_best = [&](R &best) {
+    best = largest(c[0]);
+    const uint64_t who = __ballot(order[0] != kNone && c[0] == best);
+    if (!who) return -1;
+    const int w = __ffsll((unsigned long long)who) - 1, e = __builtin_amdgcn_readlane(order[0], w);
+    if (lane == w) {
+#pragma unroll
+      for (int i = 0; i + 1 < P; ++i) { c[i] = c[i + 1]; order[i] = order[i + 1]; }
+      c[P - 1] = kLow<R>;
+      order[P - 1] = kNone;
+    }
+    return e;
+  };
+  for (int j = 0; j < (F32 ? k + 1 : k); ++j) {
+    R best;
+    const int e = next_best(best);
+    if (e < 0) break;                                               // as many as there are (j = k)
+    if (lane == j) { idx = e; choice = best; }
+    found = j + 1;
+  }
+  if (lane < found) score = sh[idx];
+  if (!F32) return true;
+  // Neighbours of the order that fp32 does not tell apart: closer than their errors, and not equal in logit and bias (those are equal, whatever the
+  // arithmetic, and ordered by their index).  Scores are off by at most 6e-7 of themselves (sigmoid), 1.2e-6 and 1.2e-7 per unit of distance from the
+  // largest logit (softmax).
+  auto too_close = [&](R above, R s_above, float l_above, R below, R s_below, float l_below) {
+    const float rel = r.score == FOCUS_SCORE_SIGMOID ? 6e-7f : 1.2e-6f + 1.2e-7f * (top_logit - fminf(l_above, l_below));
+    return above - below <= rel * (s_above + s_below) + 2e-7f * (fabsf((float)above) + fabsf((float)below));
+  };
+  const float ml = lane < found ? sh_l[idx] : 0.f, mb = lane < found ? sh_b[idx] : 0.f;
+  const R below = __shfl_down(choice, 1), s_below = __shfl_down(score, 1);
+  const float l_below = __shfl_down(ml, 1), b_below = __shfl_down(mb, 1);
+  const bool same = ml == l_below && mb == b_below;
+  if (__ballot(lane + 1 < found && !same && too_close(choice, score, ml, below, s_below, l_below))) return false;
+  // equals of the last pick may go on behind it, and what follows them has to be far enough too
+  bool equal = found > k && (__ballot(same) >> (k - 1) & 1);
+  const R end_c = lane_of(choice, k - 1), end_s = lane_of(score, k - 1);
+  const float end_l = lane_of(ml, k - 1), end_b = lane_of(mb, k - 1);
+  while (equal) {
+    R best;
+    const int e = next_best(best);
+    if (e < 0) break;
+    equal = sh_l[e] == end_l && sh_b[e] == end_b;
+    if (!equal && too_close(end_c, end_s, end_l, best, sh[e], sh_l[e])) return false;
   }
   return true;
 }
@@ -155,7 +225,7 @@ __device__ bool pick(const RouteArgs &a, const float (&l)[P], const float (&bias
 // A row takes longer for its chain of dependent steps than for its bytes.
 template <typename T, int P>
 __global__ __launch_bounds__(kRouteWaves * 64) void k_route(RouteArgs a) {
-  __shared__ double sh[kRouteWaves][64 * P];
+  __shared__ double sh[kRouteWaves][64 * P * 3 / 2];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = blockIdx.x * kRouteWaves + wave;
   const int M = a.rows.count ? min(*a.rows.count, a.rows.cap) : a.rows.cap, E = a.router.n_experts, k = a.router.experts_per_token;
   if (row >= M) return;

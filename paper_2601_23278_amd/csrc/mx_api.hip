@@ -29,7 +29,7 @@ const char *check_experts(int32_t n_experts, int32_t hidden, int32_t ffn, int32_
   if (hidden > (1 << 20) || ffn > (1 << 20) || (int64_t)hidden * ffn >= (1ll << 31)) return "hidden and ffn too large";
   if (n_rows < 0 || k < 1 || k > 32 || (int64_t)n_rows * k > (1 << 24)) return "n_rows must not be negative, k in 1..32 and n_rows * k at most 2^24";
   // the launches have a workgroup per 128 columns and tile of rows
-  const int64_t tiles = (int64_t)n_rows * k / fk::kMxTileRows + n_experts + 8;
+  const int64_t tiles = (int64_t)n_rows * k / 32 + n_experts + 8;
   if (tiles * ((std::max(hidden, 2 * ffn) + 127) / 128) >= (1ll << 31)) return "hidden, ffn and n_rows too large";
   return nullptr;
 }
