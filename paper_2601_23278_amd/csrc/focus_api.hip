@@ -507,13 +507,13 @@ void moe_ffn(focus_ctx *c, hipStream_t s, int l, const RowSet &rs, float *resid,
     if (mx.codes) fk::mx_group(s, m);
     else fk::moe_group(s, a); }
   { Timed t(c, s, FOCUS_KC_EXPERTS);
-    if (mx.codes) fk::mx_grouped(s, m);
+    if (mx.codes) fk::mx_up(s, m);
     else fk::moe_experts(s, a); }
   // the shared expert adds into the residual stream before the routed sum (both orders are the same sum)
   if (g.shared_ffn > 0) swiglu_ffn(c, s, rs, nullptr, normed, c->w_shared_gate_up[l], c->w_shared_down[l], c->mx_of(c->mx_shared_gate_up, l),
                                    c->mx_of(c->mx_shared_down, l), g.shared_ffn, resid);
-  { Timed t(c, s, FOCUS_KC_ROUTE);
-    if (mx.codes) fk::mx_combine(s, m);
+  { Timed t(c, s, mx.codes ? FOCUS_KC_EXPERTS : FOCUS_KC_ROUTE);
+    if (mx.codes) fk::mx_down(s, m);
     else fk::moe_combine(s, a); }
 }
 

@@ -65,7 +65,7 @@ struct MxExperts {
   int32_t *pos;                   // [rows * k] entry -> sorted row, -1: no such expert
   int32_t *arow;                  // [rows * k] sorted row -> row of x
   void *act;                      // [rows * k, ffn] bf16
-  float *y;                       // [rows * k, hidden]
+  float *y;                       // [rows * k, columns of a slice]
 };
 int mx_tile_rows(int rows, int k, int n_experts);     // the height for so many rows: what is expected, where only the device knows
 int mx_tile_slots(int rows, int k, int n_experts, int tile_rows);
@@ -73,7 +73,7 @@ int mx_chunks(int rows, int k);
 size_t mx_experts_bytes(int n_experts, int hidden, int ffn, int n_rows, int k);
 void lay_mx_experts(MxExperts &a, void *workspace);
 void mx_group(hipStream_t s, const MxExperts &a);     // entries sorted by expert, tiles
-void mx_grouped(hipStream_t s, const MxExperts &a);   // the two products
-void mx_combine(hipStream_t s, const MxExperts &a);   // weighted sum
+void mx_up(hipStream_t s, const MxExperts &a);        // act
+void mx_down(hipStream_t s, const MxExperts &a);      // second product and weighted sum
 
 }  // namespace fk

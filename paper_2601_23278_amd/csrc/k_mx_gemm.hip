@@ -19,6 +19,7 @@ typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
+constexpr int64_t kMxSliceBytes = 136ll << 20;
 #define FK_LDS_PTR(p) ((__attribute__((address_space(3))) void *)(p))
 constexpr int vmcnt_imm(int n) { return 0x0F70 | (n & 15) | ((n >> 4) << 14); }   // s_waitcnt vmcnt(n) only
 constexpr unsigned kOutside = 0x80000000u;   // an offset beyond every descriptor: the load returns zeros
@@ -32,6 +33,7 @@ struct RowsArgs {
   unsigned a_bytes;                   // with src: size of A
   const unsigned char *codes, *scales;
   int N, K;                           // of one expert's matrix
+  int n_begin, n_end;                 // columns of C wanted; column n_begin is the first one written
   Rows rows;                          // dense
   const int2 *tiles;                  // grouped: first sorted row; expert and rows << 16
   const int32_t *n_tiles;
@@ -87,7 +89,7 @@ __global__ __launch_bounds__(256, 2) void k_mx_rows(RowsArgs g) {
   const int split = item % splits, t = item / splits / g.tiles_n;
   const int nt = GROUPED ? local % g.tiles_n : item / splits % g.tiles_n;
   const int e = GROUPED ? tile.y & 0xFFFF : 0, row0 = GROUPED ? tile.x : t * BM, valid = GROUPED ? tile.y >> 16 : min(BM, M - row0);
-  const int N = g.N, K = g.K, n0 = nt * (SILU ? 64 * CT : 128 * CT), blocks = K / 32;
+  const int N = g.N, K = g.K, n0 = g.n_begin + nt * (SILU ? 64 * CT : 128 * CT), n_end = g.n_end, blocks = K / 32;
   const int slabs = (blocks + 7) / 8, per_split = (slabs + splits - 1) / splits, slab0 = split * per_split;
   const int my_slabs = min(slabs - slab0, per_split);                                // slabs of this workgroup (0 or less: zeros)
   const int my_steps = (min(K, (slab0 + my_slabs) * 256) - slab0 * 256 + 63) / 64;   // steps that hold anything
@@ -113,10 +115,10 @@ __global__ __launch_bounds__(256, 2) void k_mx_rows(RowsArgs g) {
   auto weight_row = [&](int r) __attribute__((always_inline)) {
     if (SILU) {
       const int c = CT == 2 ? n0 + wave * 32 + (r & 31) : n0 + wave * 16 + (r & 15);
-      return c < N / 2 ? (CT == 2 ? r >> 5 : r >> 4) * (N / 2) + c : -1;
+      return c < n_end ? (CT == 2 ? r >> 5 : r >> 4) * (N / 2) + c : -1;
     }
     const int c = n0 + wave * 32 * CT + r;
-    return c < N ? c : -1;
+    return c < n_end ? c : -1;
   };
   // chunk (block of 32) of a slab that this lane fetches for columns 8 q + lane / 8, q even and odd: swizzled like the rows' chunks
   const int cw = (lane & 7) ^ (lane >> 4);
@@ -320,7 +322,7 @@ __global__ __launch_bounds__(256, 2) void k_mx_rows(RowsArgs g) {
         }
         const int gm = i * 32 + 8 * (rr >> 2) + 4 * h + (rr & 3);
         // exp overflows to infinity and the quotient to 0 for a large negative gate
-        if (gm < valid && gn < N / 2) ((bf16_t *)g.out)[(size_t)(row0 + gm) * g.ldo + gn] = (bf16_t)(ga / (1.0f + __expf(-ga)) * up);
+        if (gm < valid && gn < n_end) ((bf16_t *)g.out)[(size_t)(row0 + gm) * g.ldo + gn - g.n_begin] = (bf16_t)(ga / (1.0f + __expf(-ga)) * up);
       }
     return;
   }
@@ -332,8 +334,8 @@ __global__ __launch_bounds__(256, 2) void k_mx_rows(RowsArgs g) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const int gm = i * 32 + 8 * (r >> 2) + 4 * h + (r & 3);
-        if (gm < valid && gn < N) {
-          const size_t at = (size_t)(row0 + gm) * g.ldo + gn;
+        if (gm < valid && gn < n_end) {
+          const size_t at = (size_t)(row0 + gm) * g.ldo + gn - g.n_begin;
           if (MODE == RM_STORE) ((bf16_t *)g.out)[at] = (bf16_t)acc[i][j][r];
           else if (MODE == RM_ADD_F32) ((float *)g.out)[at] += acc[i][j][r];
           else (MODE == RM_PARTIAL ? (float *)g.out + (size_t)split * g.split_stride : (float *)g.out)[at] = acc[i][j][r];
@@ -345,7 +347,7 @@ __global__ __launch_bounds__(256, 2) void k_mx_rows(RowsArgs g) {
 
 template <int BM, int CT, int MODE, bool GROUPED>
 void launch_rows(hipStream_t s, RowsArgs g, int tile_slots) {
-  g.tiles_n = MODE == RM_SILU ? (g.N / 2 + 64 * CT - 1) / (64 * CT) : (g.N + 128 * CT - 1) / (128 * CT);
+  g.tiles_n = MODE == RM_SILU ? (g.n_end - g.n_begin + 64 * CT - 1) / (64 * CT) : (g.n_end - g.n_begin + 128 * CT - 1) / (128 * CT);
   const int grid = GROUPED ? tile_slots * g.tiles_n : (tile_slots * g.tiles_n * g.splits + 7) / 8 * 8;
   if (g.K % 256 == 0) k_mx_rows<BM, CT, MODE, GROUPED, true><<<grid, 256, 0, s>>>(g);
   else k_mx_rows<BM, CT, MODE, GROUPED, false><<<grid, 256, 0, s>>>(g);
@@ -623,13 +625,19 @@ void launch_reduce(hipStream_t s, int epi, const float *part, int splits, size_t
 int whole_parts(int parts, int units) { const int per = (units + parts - 1) / parts; return (units + per - 1) / per; }
 
 // Tile and parts of K with the least estimated time.  Measured on 15 problems of 8 to 2048 rows, 2048 to 24576 columns and K of 2048 to 12288, every
-// tile with up to 16 parts; the estimate picks the best or one within 12 % of it.  us for one unit of K (256; both operands in MXFP4: 512) of n
-// workgroups = base + first min(n, 256) / 256 + more max(n - 256, 0) / 256; a launch costs 3 us, adding parts 2.5 us and 8 bytes an output and part at
-// 4.5 TB/s.  (333 rows x 4096, K = 4096, MXFP4 rows: 13.8 us in one part, 22.8 in five, which fill the chip; K = 12288: 30.7 in one, 24.9 in two.  1024 rows: 128 x 128
-// 17.9, 256 x 256 34.3; 2048 rows x 6144: 45.1 and 40.7.  bf16 rows: 8 x 24576 32 x 128 17, 128 x 128 18.5; 1024 x 4096 128 x 128 41.4, 128 x 256 55.)
-struct Variant { int bm, bn; float base, first, more; };
-constexpr Variant kRowVariants[] = {{32, 128, 0.8f, 0.45f, 0.6f}, {128, 128, 1.4f, 1.0f, 1.7f}, {128, 256, 2.6f, 1.1f, 3.0f}};
-constexpr Variant kMxVariants[] = {{128, 128, 0.95f, 0.6f, 2.15f}, {256, 256, 2.0f, 3.2f, 5.3f}};
+// tile with up to 16 parts.  A unit of K (256; with both operands in MXFP4 512) takes a workgroup `base` us alone and `first` more when all 256 compute
+// units have one; a second on some of them makes it `second`, and `more` for each further 256; beyond per_cu of them rounds follow one another.  A launch
+// costs 3 us, adding parts 2.5 us and 8 bytes an output and part at 4.5 TB/s.  (333 rows x 4096, K = 4096, MXFP4 rows: 13.8 us in one part, 22.8 in
+// five, which fill the chip; K = 12288: 30.7 in one, 24.9 in two, 30.1 in three.  1024 rows: 128 x 128 17.9, 256 x 256 34.3; 2048 rows x 6144: 45.1 and 40.7.
+// bf16 rows: 8 x 24576 32 x 128 17, 128 x 128 18.5; 1024 x 4096 128 x 128 41.4, 128 x 256 55; 333 x 4096, K = 12288, 128 x 128: 83 in one part, 54 in two, 59 in three, 50 in five.)
+struct Variant { int bm, bn, per_cu; float base, first, second, more; };
+constexpr Variant kRowVariants[] = {{32, 128, 3, 0.8f, 0.45f, 1.3f, 0.7f}, {128, 128, 2, 1.4f, 0.9f, 3.0f, 0.8f}, {128, 256, 2, 2.6f, 1.0f, 5.2f, 1.5f}};
+constexpr Variant kMxVariants[] = {{128, 128, 2, 0.95f, 0.6f, 2.2f, 0.6f}, {256, 256, 1, 2.0f, 3.2f, 0.f, 0.f}};
+float unit_us(const Variant &v, int64_t groups) {
+  const int64_t round = 256 * v.per_cu, rounds = (groups - 1) / round, left = groups - rounds * round;
+  auto one = [&](int64_t n) { return n <= 256 ? v.base + v.first * (float)n / 256.f : v.second + v.more * (float)(n - 256) / 256.f; };
+  return (float)rounds * one(round) + one(left);
+}
 struct Shape { int bm, bn, splits; };
 Shape shape_of(int rows, int n, int k, bool a_mx) {
   const int units = std::max(1, a_mx ? (k / 32 + 15) / 16 : (k / 32 + 7) / 8);
@@ -642,8 +650,7 @@ Shape shape_of(int rows, int n, int k, bool a_mx) {
     const float live = a_mx || v->bm == 32 ? 1.f : 0.4f + 0.6f * (float)((rows + 31) / 32) / (float)(tiles_m * v->bm / 32);
     for (int parts = 1; parts <= std::min(units, 16); ++parts) {
       if (whole_parts(parts, units) != parts || (parts > 1 && tiles * parts > 1024)) continue;
-      const float wg = (float)(tiles * parts), unit_us = v->base + v->first * std::min(wg, 256.f) / 256.f + v->more * std::max(wg - 256.f, 0.f) / 256.f;
-      const float us = 3.f + live * unit_us * (float)((units + parts - 1) / parts) + (parts > 1 ? 2.5f + (float)parts * (float)rows * (float)n * (8.f / 4.5e6f) : 0.f);
+      const float us = 3.f + live * unit_us(*v, tiles * parts) * (float)((units + parts - 1) / parts) + (parts > 1 ? 2.5f + (float)parts * (float)rows * (float)n * (8.f / 4.5e6f) : 0.f);
       if (!best.bm || us < least) { best = {v->bm, v->bn, parts}; least = us; }
     }
   }
@@ -673,7 +680,7 @@ void mx_gemm(hipStream_t s, const void *a, const void *a_scales, int64_t lda, fo
     else launch_mx<128, 128>(s, mode, g);
   } else {
     RowsArgs g{};
-    g.A = (const bf16_t *)a; g.lda = lda; g.codes = (const unsigned char *)w.codes; g.scales = (const unsigned char *)w.scales; g.N = n; g.K = k; g.rows = rows;
+    g.A = (const bf16_t *)a; g.lda = lda; g.codes = (const unsigned char *)w.codes; g.scales = (const unsigned char *)w.scales; g.N = n; g.K = k; g.rows = rows; g.n_end = epilogue == MX_SILU_MUL && !parts ? n / 2 : n;
     g.splits = p.splits; g.split_stride = stride; g.out = parts ? scratch.ptr : out; g.ldo = parts ? n : ldo;
     const int mode = parts ? RM_PARTIAL : epilogue == MX_STORE ? RM_STORE : epilogue == MX_STORE_F32 ? RM_STORE_F32 : epilogue == MX_ADD_F32 ? RM_ADD_F32 : RM_SILU;
     if (p.bm == 32) launch_rows<32, 1>(s, mode, g, (rows.cap + 31) / 32);
@@ -691,20 +698,17 @@ template <int MODE>
 static void launch_grouped(hipStream_t s, const RowsArgs &a, const MxExperts &m) {
   const int slots = mx_tile_slots(m.rows.cap, m.k, m.n_experts, m.tile_rows);
   if (m.tile_rows == 32) launch_rows<32, 1, MODE, true>(s, a, slots);
-  else if ((int64_t)mx_tile_slots(m.rows.expected(), m.k, m.n_experts, 128) * ((a.N + 255) / 256) >= kMxWide) launch_rows<128, 2, MODE, true>(s, a, slots);
+  else if ((int64_t)mx_tile_slots(m.rows.expected(), m.k, m.n_experts, 128) * (((MODE == RM_SILU ? 2 : 1) * (a.n_end - a.n_begin) + 255) / 256) >= kMxWide) launch_rows<128, 2, MODE, true>(s, a, slots);
   else launch_rows<128, 1, MODE, true>(s, a, slots);
 }
 
-void mx_grouped(hipStream_t s, const MxExperts &m) {
+void mx_up(hipStream_t s, const MxExperts &m) {
+  if (m.rows.cap <= 0) return;
   RowsArgs a{};
   a.A = (const bf16_t *)m.x; a.lda = m.ldx; a.src = m.arow; a.a_bytes = (unsigned)(((int64_t)(m.rows.cap - 1) * m.ldx + m.hidden) * 2);
   a.codes = (const unsigned char *)m.gate_up.codes; a.scales = (const unsigned char *)m.gate_up.scales;
-  a.N = 2 * m.ffn; a.K = m.hidden; a.tiles = m.tiles; a.n_tiles = m.n_tiles; a.splits = 1; a.out = m.act; a.ldo = m.ffn;
+  a.N = 2 * m.ffn; a.n_end = m.ffn; a.K = m.hidden; a.tiles = m.tiles; a.n_tiles = m.n_tiles; a.splits = 1; a.out = m.act; a.ldo = m.ffn;
   launch_grouped<RM_SILU>(s, a, m);
-  a.A = (const bf16_t *)m.act; a.lda = m.ffn; a.src = nullptr; a.a_bytes = 0;
-  a.codes = (const unsigned char *)m.down.codes; a.scales = (const unsigned char *)m.down.scales;
-  a.N = m.hidden; a.K = m.ffn; a.out = m.y; a.ldo = m.hidden;
-  launch_grouped<RM_STORE_F32>(s, a, m);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -828,31 +832,46 @@ __global__ __launch_bounds__(kChunk) void k_mx_place(MxExperts a, int chunks, in
   }
 }
 
-// out[row] (+)= sum_j weight_j y[pos_j], j ascending; a workgroup takes 1024 columns of a row
+// out[row] (+)= sum_j weight_j y[pos_j], j ascending, for the columns from c0 on that y holds (cols of them), four to a thread.  Eight products are asked
+// for at once (one after the other, each behind its place in the list, 16384 entries of 2048 columns took 22 us).
 template <typename T, bool ADD>
-__global__ __launch_bounds__(256) void k_mx_combine(MxExperts a) {
-  const int row = blockIdx.x, k = a.k, H = a.hidden;
+__global__ __launch_bounds__(256) void k_mx_combine(MxExperts a, int c0, int cols) {
+  const int row = blockIdx.x, k = a.k;
   if (a.rows.count && row >= *a.rows.count) return;
-  const int c = (blockIdx.y * 256 + threadIdx.x) * 4;
-  if (c >= H) return;
-  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int j = 0; j < k; ++j) {
-    const int p = a.pos[(size_t)row * k + j];
-    if (p < 0) continue;
-    const float w = a.weights[(size_t)row * k + j];
-    const float4 v = *(const float4 *)(a.y + (size_t)p * H + c);
-    acc.x += w * v.x; acc.y += w * v.y; acc.z += w * v.z; acc.w += w * v.w;
-  }
-  T *o = (T *)a.out + (size_t)row * a.ldo + c;
-  const float v[4] = {acc.x, acc.y, acc.z, acc.w};
+  const int c = (blockIdx.y * blockDim.x + threadIdx.x) * 4;
+  if (c >= cols) return;
+  const int32_t *const pos = a.pos + (size_t)row * k;
+  const float *const weights = a.weights + (size_t)row * k;
+  float acc[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int j0 = 0; j0 < k; j0 += 8) {
+    int p[8];
+    float w[8];
+    float4 v[8];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) o[i] = ADD ? (T)((float)o[i] + v[i]) : (T)v[i];
+    for (int j = 0; j < 8; ++j) {
+      p[j] = j0 + j < k ? pos[j0 + j] : -1;
+      w[j] = j0 + j < k ? weights[j0 + j] : 0.f;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = *(const float4 *)(a.y + (size_t)max(p[j], 0) * cols + c);
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (p[j] >= 0) { acc[0] += w[j] * v[j].x; acc[1] += w[j] * v[j].y; acc[2] += w[j] * v[j].z; acc[3] += w[j] * v[j].w; }
+  }
+  T *o = (T *)a.out + (size_t)row * a.ldo + c0 + c;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) o[i] = ADD ? (T)((float)o[i] + acc[i]) : (T)acc[i];
 }
 }  // namespace
 
 int mx_tile_rows(int rows, int k, int n_experts) { return rows * k <= kMxFewRows * std::min(rows * k, n_experts) ? 32 : 128; }
 // Row tiles there can be, rounded up to the eight XCDs that take them in turn.
 int mx_tile_slots(int rows, int k, int n_experts, int tile_rows) { return (rows * k / tile_rows + std::min(rows * k, n_experts) + 7) / 8 * 8; }
+// Columns of a slice of the second product: a multiple of 256.
+static int mx_slice(int rows, int k, int hidden) {
+  const int64_t fit = kMxSliceBytes / ((int64_t)rows * k * 4) / 256 * 256;
+  return fit >= hidden ? hidden : (int)std::max<int64_t>(fit, 256);
+}
 int mx_chunks(int rows, int k) { return (rows * k + kChunk - 1) / kChunk; }
 
 // Lays the work buffers out from `base`; returns their size.
@@ -867,7 +886,7 @@ static size_t lay(MxExperts &a, char *base, int rows) {
   a.pos = (int32_t *)take(ent * 4);
   a.arow = (int32_t *)take(ent * 4);
   a.act = take(ent * a.ffn * 2);
-  a.y = (float *)take(ent * a.hidden * 4);
+  a.y = (float *)take(ent * std::min(a.hidden, mx_slice(std::max(1, rows), a.k, a.hidden)) * 4);
   return at;
 }
 size_t mx_experts_bytes(int n_experts, int hidden, int ffn, int n_rows, int k) {
@@ -888,12 +907,25 @@ void mx_group(hipStream_t s, const MxExperts &a) {
   }
 }
 
-void mx_combine(hipStream_t s, const MxExperts &a) {
-  if (a.rows.cap <= 0) return;
-  const dim3 grid(a.rows.cap, (a.hidden + 1023) / 1024);
-  if (a.out_type == FOCUS_BF16) k_mx_combine<bf16_t, false><<<grid, 256, 0, s>>>(a);
-  else if (a.add) k_mx_combine<float, true><<<grid, 256, 0, s>>>(a);
-  else k_mx_combine<float, false><<<grid, 256, 0, s>>>(a);
+// The second product and the weighted sums, so many columns at a time that the fp32 products of a slice stay in the memory-side cache (256 MB) between the
+// two launches, and the next slice's go where they were: 8192 rows through 8 experts each, 2048 columns, 537 MB of products.
+void mx_down(hipStream_t s, const MxExperts &m) {
+  if (m.rows.cap <= 0) return;
+  RowsArgs a{};
+  a.A = (const bf16_t *)m.act; a.lda = m.ffn;
+  a.codes = (const unsigned char *)m.down.codes; a.scales = (const unsigned char *)m.down.scales;
+  a.N = m.hidden; a.K = m.ffn; a.tiles = m.tiles; a.n_tiles = m.n_tiles; a.splits = 1; a.out = m.y;
+  const int slice = mx_slice(m.rows.cap, m.k, m.hidden);
+  for (int c0 = 0; c0 < m.hidden; c0 += slice) {
+    const int cols = std::min(slice, m.hidden - c0);
+    a.n_begin = c0; a.n_end = c0 + cols; a.ldo = cols;
+    launch_grouped<RM_STORE_F32>(s, a, m);
+    const int threads = std::min(256, (cols / 4 + 63) / 64 * 64);
+    const dim3 grid(m.rows.cap, (cols / 4 + threads - 1) / threads);
+    if (m.out_type == FOCUS_BF16) k_mx_combine<bf16_t, false><<<grid, threads, 0, s>>>(m, c0, cols);
+    else if (m.add) k_mx_combine<float, true><<<grid, threads, 0, s>>>(m, c0, cols);
+    else k_mx_combine<float, false><<<grid, threads, 0, s>>>(m, c0, cols);
+  }
 }
 
 }  // namespace fk

@@ -132,8 +132,8 @@ int focus_mx_experts(void *hip_stream, int32_t n_experts, int32_t hidden, int32_
   a.x = x; a.ldx = ldx; a.experts = experts; a.weights = weights; a.out_type = out_type; a.out = out; a.ldo = ldo; a.add = add != 0;
   fk::lay_mx_experts(a, workspace);
   fk::mx_group((hipStream_t)hip_stream, a);
-  fk::mx_grouped((hipStream_t)hip_stream, a);
-  fk::mx_combine((hipStream_t)hip_stream, a);
+  fk::mx_up((hipStream_t)hip_stream, a);
+  fk::mx_down((hipStream_t)hip_stream, a);
   return launched();
 }
 
