@@ -342,7 +342,7 @@ typedef struct focus_router {
 
 /* The experts and weights of n_rows rows.
  *   dtype    FOCUS_F32 or FOCUS_BF16, of the logits; scores and weights are fp32
- *   logits   device [n_rows, ld], E of each row used; ld >= E
+ *   logits   device [n_rows, ld], E of each row used; ld >= E;  n_rows below 2^26
  *   bias     device [E] fp32, or NULL
  *   experts  device [n_rows, k] int32; weights device [n_rows, k] fp32 */
 int focus_route(const focus_router *router, void *hip_stream, int32_t n_rows, int32_t dtype, const void *logits, int64_t ld,
@@ -361,7 +361,7 @@ typedef struct focus_mx {
 /* Rows to MXFP4.  The scale of a block is 2^(floor(log2(max |x|)) - 2), within 2^-127 and 2^127 (2^-127 for zeros); x / scale is rounded to
  * the nearest code, half way to the even mantissa, magnitudes over 6 to 6.  A block with an infinity or a NaN gets scale 255 and zero codes.  Elements
  * beyond cols in a row's last block are coded as zeros.
- *   dtype    FOCUS_F32 or FOCUS_BF16;  x device [rows, ldx], ldx >= cols */
+ *   dtype    FOCUS_F32 or FOCUS_BF16;  x device [rows, ldx], ldx >= cols;  rows * ceil(cols / 32) below 2^30 */
 int focus_mx_quantize(void *hip_stream, int32_t dtype, int64_t rows, int32_t cols, const void *x, int64_t ldx, void *codes, void *scales);
 
 /* The values of codes and scales, exact in both dtypes (magnitudes beyond the largest finite number become infinite).  Writes cols elements of each
@@ -369,7 +369,8 @@ int focus_mx_quantize(void *hip_stream, int32_t dtype, int64_t rows, int32_t col
 int focus_mx_dequantize(void *hip_stream, int32_t dtype, int64_t rows, int32_t cols, const focus_mx *mx, void *x, int64_t ldx);
 
 /* C[m, n] = sum_k A[m, k] W[n, k], summed in fp32 and rounded once.
- *   k            a multiple of 32 (the quantiser fills a row's last block with zeros); 0: C = 0
+ *   k            a multiple of 32 (the quantiser fills a row's last block with zeros), at most 2^22; 0: C = 0.  n * k below 2^32, and C at most
+ *                2^24 tiles of 128 x 128
  *   a_type       FOCUS_BF16: A device [m, lda] bf16, 16-byte aligned, lda a multiple of 8; a_scales NULL.
  *                FOCUS_MX4: A the codes [m, k / 2] (lda ignored), a_scales [m, k / 32]
  *   w            MXFP4 [n, k]
@@ -387,7 +388,7 @@ int focus_mx_gemm(void *hip_stream, int32_t m, int32_t n, int32_t k, int32_t a_t
  *   hidden, ffn  multiples of 32
  *   gate_up      MXFP4 [E, 2 ffn, hidden]: per expert ffn gate rows, then ffn up rows;  down  MXFP4 [E, hidden, ffn]
  *   x            device [n_rows, ldx] bf16, 16-byte aligned, ldx a multiple of 8;  n_rows * ldx below 2^30
- *   experts      device [n_rows, k] int32;  weights  device [n_rows, k] fp32;  k 1..32, n_rows * k at most 2^24
+ *   experts      device [n_rows, k] int32;  weights  device [n_rows, k] fp32;  k 1..32, n_rows * k below 2^24
  *   out          device [n_rows, ldo], out_type FOCUS_F32 or FOCUS_BF16; add: out += (FOCUS_F32 only)
  *   workspace    device, 256-byte aligned, focus_mx_experts_bytes() */
 int focus_mx_experts_bytes(int32_t n_experts, int32_t hidden, int32_t ffn, int32_t n_rows, int32_t k, size_t *bytes);

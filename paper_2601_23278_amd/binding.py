@@ -181,7 +181,11 @@ def _begin(device, stream) -> int:
     """Address of the stream that a call's work goes to; its tensors live on `device`, which has to be the current one."""
     if device.type != "cuda" or device.index != torch.cuda.current_device():
         _bad("tensors must be on the current device, not on %s", device)
-    return torch._C._cuda_getCurrentRawStream(device.index) if stream is None else stream.cuda_stream
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(device.index)
+    if stream.device_index != device.index:
+        _bad("the stream belongs to another device than %s", device)
+    return stream.cuda_stream
 
 
 def _new(shape, dtype, device, stream):
@@ -436,7 +440,7 @@ class Focus:
         E = self.cfg.n_experts
         for b in bias or ():
             if b is not None:
-                _plain(b, "bias", (E,), torch.float32)
+                _plain(b, "bias", (E,), torch.float32, self.workspace.device)
         if bias is not None and len(bias) != self.cfg.n_layers:
             _bad("one bias per layer")
         arr = None if bias is None else (C.c_void_p * len(bias))(*[None if b is None else b.data_ptr() for b in bias])
@@ -458,7 +462,7 @@ class Focus:
         w, arrays = focus_mx_weights(), []
         for name in _MX_FIELDS:
             if any(name in l for l in layers):
-                pairs = [_mx_of(l[name], name, *shapes[name][:-1]) if name in l else (focus_mx(), shapes[name][-1]) for l in layers]
+                pairs = [_mx_of(l[name], name, *shapes[name][:-1], device=self.workspace.device) if name in l else (focus_mx(), shapes[name][-1]) for l in layers]
                 if any(k != shapes[name][-1] for _, k in pairs):
                     _bad("%s has another width", name)
                 arrays.append((focus_mx * len(layers))(*[m for m, _ in pairs]))

@@ -135,7 +135,8 @@ __device__ __forceinline__ bool pick(const RouteArgs &a, const float (&l)[P], co
       const R out = lane_of(value, __ffsll((unsigned long long)__ballot(lead && rank == r.groups_kept)) - 1);
       top_score = largest(top_score);
       // each choice is off by at most 2e-6 of the row's largest score (exp, sum, division) and half an ulp of itself
-      if (in - out <= (R)8e-6 * top_score + (R)1e-6 * (fabs(in) + fabs(out))) return false;
+      // (neither holds where a sum of two large biases overflowed)
+      if (!(in - out > (R)8e-6 * top_score + (R)1e-6 * (fabs(in) + fabs(out)))) return false;
     }
     const uint64_t kept = __ballot(lead && rank < r.groups_kept);
     const unsigned by_s = ((1u << 20) + S - 1) / S;                 // e / S = e * by_s >> 20 for e < 512

@@ -551,3 +551,330 @@ def test_context_setters_refuse():
     with pytest.raises(pk.FocusError):                              # an fp32 model
         sess.focus.focus_set_mx_weights([dict(w_gate_up=z, w_down=zd)] * 2)
     sess.focus.focus_free()
+
+
+# -- sizes at which the launches differ -------------------------------------------------------
+def sampled(n, gen, count=40):
+    return torch.cat([torch.tensor([0, n - 1]), torch.randint(0, n, (count,), generator=gen)])
+
+
+@pytest.mark.parametrize("a_type,m,n,k", [
+    ("bf16", 40, 40, 1056), ("bf16", 40, 40, 2048), ("bf16", 5, 40, 1056), ("bf16", 5, 40, 2048),                                  # tiles of 32 and 128 rows, K cut
+    ("bf16", 290, 6150, 224), ("bf16", 290, 6150, 256), ("bf16", 200, 8200, 224), ("bf16", 200, 8200, 256), ("bf16", 1000, 2050, 224),  # two to four tile rows in the last tile
+    ("bf16", 40, 2050, 2080), ("bf16", 40, 2050, 2048), ("bf16", 70, 2050, 4128), ("bf16", 70, 4100, 2048), ("bf16", 1000, 130, 2080),
+    ("bf16", 1300, 4100, 224), ("bf16", 1300, 4100, 256), ("bf16", 700, 8200, 224), ("bf16", 700, 8200, 256), ("bf16", 730, 8200, 224), ("bf16", 730, 8200, 256),
+    ("bf16", 1000, 6150, 224), ("bf16", 1000, 6150, 256), ("bf16", 130, 8200, 4128), ("bf16", 1000, 40, 4096),
+    ("mx4", 5, 40, 2080), ("mx4", 5, 40, 2048), ("mx4", 1000, 8200, 224), ("mx4", 1000, 8200, 512), ("mx4", 130, 1030, 1024)])
+def test_gemm_tiles(a_type, m, n, k):
+    """Sampled rows and columns in 64 bits."""
+    pk, _ = _pk()
+    gen = torch.Generator().manual_seed(m + n + k)
+    w = ref.random_mx(gen, n, k)
+    if a_type == "bf16":
+        a = torch.randn(m, k, generator=gen).to(torch.bfloat16)
+        av, a = a.double(), a.to(DEV)
+    else:
+        am = ref.random_mx(gen, m, k)
+        av, a = ref.values(*am), gpu(*am)
+    c = pk.focus_mx_gemm(a, gpu(*w), torch.empty(m, n, device=DEV)).cpu().double()
+    wv, rows, cols = ref.values(*w), sampled(m, gen), sampled(n, gen)
+    for got, x, y in ((c[rows], av[rows], wv), (c[:, cols], av, wv[cols])):
+        assert bool(((got - x @ y.t()).abs() <= product_bound(x, y, torch.float32)).all())
+
+
+@pytest.mark.parametrize("parts", [1, 2, 3, 5])
+@pytest.mark.parametrize("a_type", ["bf16", "mx4"])
+def test_gemm_with_less_workspace_than_it_asks_for(a_type, parts):
+    pk, _ = _pk()
+    m, n, k = 40, 160, 8224
+    gen = torch.Generator().manual_seed(parts)
+    w, am = ref.random_mx(gen, n, k), ref.random_mx(gen, m, k)
+    av, a = (ref.values(*am), gpu(*am)) if a_type == "mx4" else (lambda t: (t.double(), t.to(DEV)))(torch.randn(m, k, generator=gen).to(torch.bfloat16))
+    size = parts * m * n * 4
+    assert pk.focus_mx_gemm_bytes(m, n, k, pk.FOCUS_MX4 if a_type == "mx4" else pk.FOCUS_BF16) > size
+    ws = torch.full((size + 512,), 77, dtype=torch.uint8, device=DEV)
+    c = pk.focus_mx_gemm(a, gpu(*w), torch.empty(m, n, device=DEV), workspace=ws[:size]).cpu().double()
+    wv = ref.values(*w)
+    assert bool(((c - av @ wv.t()).abs() <= product_bound(av, wv, torch.float32)).all())
+    assert bool((ws[size:] == 77).all())
+
+
+def test_scales_may_lie_at_any_address():
+    pk, _ = _pk()
+    gen = torch.Generator().manual_seed(6)
+
+    def odd(t, by):
+        room = torch.zeros(t.numel() + by, dtype=torch.uint8, device=DEV)
+        room[by:] = t.reshape(-1).to(DEV)
+        return room[by:].view(t.shape)
+    for k in (96, 512, 1024):
+        w, am = ref.random_mx(gen, 150, k), ref.random_mx(gen, 70, k)
+        x = torch.randn(70, k, generator=gen).to(torch.bfloat16).to(DEV)
+        want = [pk.focus_mx_gemm(a, gpu(*w), torch.empty(70, 150, device=DEV)) for a in (x, gpu(*am))]
+        for by in (1, 2, 7, 13):
+            w_odd, a_odd = (w[0].to(DEV), odd(w[1], by)), (am[0].to(DEV), odd(am[1], by))
+            got = [pk.focus_mx_gemm(a, w_odd, torch.empty(70, 150, device=DEV)) for a in (x, a_odd)]
+            assert all(torch.equal(g, v) for g, v in zip(got, want))
+            codes, scales = pk.focus_mx_quantize(x, scales=odd(torch.zeros(70, k // 32, dtype=torch.uint8), by))
+            plain = pk.focus_mx_quantize(x)
+            assert torch.equal(codes, plain[0]) and torch.equal(scales, plain[1])
+            assert torch.equal(pk.focus_mx_dequantize(codes, scales, torch.empty_like(x)), pk.focus_mx_dequantize(*plain, torch.empty_like(x)))
+
+
+def test_nothing_to_do():
+    pk, _ = _pk()
+    gen = torch.Generator().manual_seed(1)
+    w = gpu(*ref.random_mx(gen, 40, 64))
+    none = torch.empty(0, 64, dtype=torch.bfloat16, device=DEV)
+    assert pk.focus_mx_gemm(none, w, torch.empty(0, 40, device=DEV)).shape == (0, 40)
+    assert pk.focus_mx_gemm(pk.focus_mx_quantize(none), w, torch.empty(0, 40, device=DEV)).shape == (0, 40)
+    assert pk.focus_mx_gemm(torch.empty(3, 64, dtype=torch.bfloat16, device=DEV), (w[0][:0], w[1][:0]), torch.empty(3, 0, device=DEV)).shape == (3, 0)
+    r = pk.focus_router(n_experts=8, experts_per_token=2, score=0, n_groups=1, groups_kept=1, group_top=1, renormalize=1, route_scale=1.0)
+    experts, weights = pk.focus_route(r, torch.empty(0, 8, device=DEV))
+    gate_up, down = gpu(*ref.random_mx(gen, 8, 64, 64)), gpu(*ref.random_mx(gen, 8, 64, 32))
+    assert pk.focus_mx_experts(gate_up, down, none, experts, weights, torch.empty(0, 64, device=DEV)).shape == (0, 64)
+
+
+def test_more_than_32_bits_of_elements():
+    """Rows whose offsets pass 2^31 elements and 2^32 bytes on either side: the last ones against a call on them alone."""
+    pk, _ = _pk()
+    rows, cols = 70001, 32768
+    gen = torch.Generator().manual_seed(3)
+    tail = torch.randn(5, cols, generator=gen).to(torch.bfloat16).to(DEV)
+    x = torch.zeros(rows, cols, dtype=torch.bfloat16, device=DEV)
+    x[-5:] = tail
+    codes, scales = pk.focus_mx_quantize(x)
+    want = pk.focus_mx_quantize(tail)
+    assert torch.equal(codes[-5:], want[0]) and torch.equal(scales[-5:], want[1]) and not bool(codes[:-5].any()) and not bool(scales[:-5].any())
+    pk.focus_mx_dequantize(codes, scales, x)
+    assert torch.equal(x[-5:], pk.focus_mx_dequantize(*want, torch.empty_like(tail))) and not bool(x[:-5].any())
+    w = gpu(*ref.random_mx(gen, 64, cols))
+    for a, t in (((codes, scales), want), (x, x[-5:].clone())):
+        c = pk.focus_mx_gemm(a, w, torch.empty(rows, 64, device=DEV))
+        few = pk.focus_mx_gemm(t, w, torch.empty(5, 64, device=DEV))
+        v = ref.values(want[0].cpu(), want[1].cpu())
+        bound = product_bound(v, ref.values(w[0].cpu(), w[1].cpu()), torch.float32)
+        assert bool(((c[-5:] - few).abs().cpu() <= 2 * bound).all()) and not bool(c[:-5].any())
+    del x, codes, scales
+    n = 65536
+    a = torch.randn(70001, 32, generator=gen).to(torch.bfloat16)
+    w = ref.random_mx(gen, n, 32)
+    out = torch.empty(70001, n, device=DEV)
+    for given in (a.to(DEV), pk.focus_mx_quantize(a.to(DEV))):
+        out.zero_()
+        pk.focus_mx_gemm(given, gpu(*w), out)
+        av = a.double() if isinstance(given, torch.Tensor) else ref.values(given[0].cpu(), given[1].cpu())
+        r = torch.tensor([0, 33000, 65535, 65536, 70000])
+        wv = ref.values(*w)
+        assert bool(((out[r.to(DEV)].cpu().double() - av[r] @ wv.t()).abs() <= product_bound(av[r], wv, torch.float32)).all())
+
+
+@pytest.mark.parametrize("rows,E,k,hidden,ffn,add", [
+    (1500, 20, 8, 64, 32, False),          # 12 chunks of entries, all counted by everyone
+    (2049, 20, 8, 64, 32, False),          # 17 chunks, counted by a launch of their own
+    (3000, 6, 8, 1024, 384, False),        # wide tiles
+    (3000, 16, 8, 2048, 64, True),         # the second product in two slices of columns, 1280 and 768
+    (3000, 512, 8, 96, 64, False),         # every expert: a few full tiles and the rest
+    (1, 40, 32, 4096, 1024, False)])
+def test_experts_of_many_rows(rows, E, k, hidden, ffn, add):
+    """Sampled rows in 64 bits, all of them against a call on the rows in another order."""
+    pk, _ = _pk()
+    wide, gate_up, down, picks, weights = experts_case(rows * 3 + E, rows, E, k, hidden, ffn)
+    if rows > 1000:
+        picks[5:600] = picks[5]            # experts of many rows
+        picks[700] = -1
+    gu, dn, x, p, w = gpu(*gate_up), gpu(*down), wide.to(DEV), picks.to(DEV), weights.to(DEV)
+    gu, dn = gu[:2], dn[:2]
+    start = torch.full((rows + 1, hidden), 2.0, device=DEV)
+    out = start.clone()
+    pk.focus_mx_experts(gu, dn, x, p, w, out[:rows], add=add)
+    assert bool((out[rows] == 2).all())
+    gen = torch.Generator().manual_seed(rows)
+    some = sampled(rows, gen, 12)
+    if rows > 1000:
+        some = torch.cat([some, torch.tensor([5, 300, 599, 700])])
+    used = sorted({int(e) for e in picks[some].flatten() if 0 <= e < E})
+    index = {e: i for i, e in enumerate(used)}
+    local = torch.tensor([[index.get(int(e), -1) for e in row] for row in picks[some]], dtype=torch.int32)
+    want, bound = ref.experts(wide[some].double(), ref.values(gate_up[0][used], gate_up[1][used]), ref.values(down[0][used], down[1][used]), local, weights[some].double())
+    base = 2.0 if add else 0.0
+    got = out[:rows].cpu().double()[some] - base
+    assert bool(((got - want).abs() <= bound + 2.0 ** -23 * (want.abs() + base)).all())
+    order = torch.randperm(rows, generator=gen).to(DEV)
+    other = start.clone()
+    pk.focus_mx_experts(gu, dn, x[order].contiguous(), p[order].contiguous(), w[order].contiguous(), other[:rows], add=add)
+    assert torch.equal(other[:rows], out[:rows][order])
+
+
+def test_groups_whose_sums_overflow_32_bits():
+    """Biases near the largest fp32 number: two groups' sums are infinite in 32 bits, not in 64."""
+    logits = torch.zeros(3, 8)
+    logits[1, 0] = 1.0
+    bias = torch.tensor([3.0e38, 3.0e38, 3.1e38, 3.1e38, 1.0, 1.0, 2.9e38, 3.3e38])
+    for kept in (1, 2, 3):
+        check_route(logits, bias, "sigmoid", 4, kept, 2, 2, True, 1.0)
+
+
+# -- calls at the same time, other places -----------------------------------------------------
+def test_calls_from_two_host_threads():
+    """Each thread on a stream of its own; a thread's errors are its own."""
+    import threading
+    pk, _ = _pk()
+    ins = [layer_inputs(pk, 60 + 50 * i, seed=40 + i) for i in range(2)]
+    want = [torch.empty_like(i[0]) for i in ins]
+    for i, w in zip(ins, want):
+        layer(pk, *i, w)
+    torch.cuda.synchronize()
+    failures, start = [], threading.Barrier(2)
+
+    def work(t):
+        try:
+            torch.cuda.set_device(0)
+            stream = torch.cuda.Stream()
+            start.wait()
+            for n in range(10):
+                out = torch.empty_like(ins[t][0])
+                layer(pk, *ins[t], out, stream=stream)
+                with pytest.raises(pk.FocusError, match="a_type" if t else "multiple"):
+                    pk.focus_mx_gemm_bytes(1, 1, 32 if t else 33, 7 if t else 1)
+                stream.synchronize()
+                assert torch.equal(out, want[t])
+        except BaseException as e:                                  # noqa: B902  reported by the test's own thread
+            failures.append(e)
+    threads = [threading.Thread(target=work, args=(t,)) for t in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failures, failures
+
+
+def test_python_refuses_tensors_of_the_host():
+    pk, _ = _pk()
+    gen = torch.Generator().manual_seed(1)
+    w, x = ref.random_mx(gen, 40, 64), torch.randn(3, 64, generator=gen).to(torch.bfloat16)
+    out = torch.empty(3, 40, device=DEV)
+    r = pk.focus_router(n_experts=64, experts_per_token=2, score=0, n_groups=1, groups_kept=1, group_top=1, renormalize=1, route_scale=1.0)
+    logits = torch.zeros(3, 64, device=DEV)
+    e, g = torch.zeros(3, 2, dtype=torch.int32), torch.zeros(3, 2)
+    gu, dn = ref.random_mx(gen, 2, 64, 64), ref.random_mx(gen, 2, 64, 32)
+    o = torch.empty(3, 64, device=DEV)
+    for call in (lambda: pk.focus_mx_gemm(x, gpu(*w), out), lambda: pk.focus_mx_gemm(x.to(DEV), w, out), lambda: pk.focus_mx_gemm(x.to(DEV), (w[0].to(DEV), w[1]), out),
+                 lambda: pk.focus_mx_gemm(ref.random_mx(gen, 3, 64), gpu(*w), out), lambda: pk.focus_mx_gemm(x.to(DEV), gpu(*w), out, workspace=torch.empty(64)),
+                 lambda: pk.focus_route(r, logits, torch.zeros(64)), lambda: pk.focus_route(r, logits, experts=e), lambda: pk.focus_route(r, logits, weights=g),
+                 lambda: pk.focus_mx_quantize(x.to(DEV), codes=torch.empty(3, 32, dtype=torch.uint8)), lambda: pk.focus_mx_dequantize(*w, torch.empty(40, 64, device=DEV)),
+                 lambda: pk.focus_mx_experts(gu, gpu(*dn), x.to(DEV), *gpu(e, g), o), lambda: pk.focus_mx_experts(*map(lambda t: gpu(*t), (gu, dn)), x, *gpu(e, g), o),
+                 lambda: pk.focus_mx_experts(*map(lambda t: gpu(*t), (gu, dn)), x.to(DEV), e, g.to(DEV), o)):
+        with pytest.raises(pk.FocusError):
+            call()
+
+
+# -- a context in use -------------------------------------------------------------------------
+def mx_session(pk, runner, wl, router=False):
+    sess = runner.open_session(wl, DEV)
+    layers = []
+    for w in sess.weights[3]:
+        pairs = {}
+        for name in MATRICES:
+            if name in w:
+                c, s = pk.focus_mx_quantize(w[name].reshape(-1, w[name].shape[-1]))
+                pairs[name] = (c.view(*w[name].shape[:-1], -1), s.view(*w[name].shape[:-1], -1))
+        layers.append(pairs)
+    sess.focus.focus_set_mx_weights(layers)
+    if router:
+        gen = torch.Generator().manual_seed(4)
+        sess.focus.focus_set_router(pk.focus_router(n_experts=wl.n_experts, experts_per_token=wl.experts_per_token, score=1, n_groups=4, groups_kept=2, group_top=2,
+                                                    renormalize=1, route_scale=wl.route_scale), [(torch.randn(wl.n_experts, generator=gen) * 0.02).to(DEV) for _ in range(wl.n_layers)])
+    return sess
+
+
+def test_captured_context_on_mx_weights():
+    """A captured step, replayed, against the same steps launched one by one on another context; wide and narrow inner widths, with and without a
+    hint of few rows."""
+    pk, runner = _pk()
+    for over, hint in ((dict(), 0), (dict(ffn=3104, expert_ffn=160, shared_ffn=416), 40)):
+        wl = small(**over)
+        n, B = wl.batch, wl.block_size
+        got = []
+        for captured in (False, True):
+            sess = mx_session(pk, runner, wl, router=True)
+            if hint:
+                sess.focus.focus_set_row_hint(hint, B)
+            tokens = torch.zeros(n, B, dtype=torch.int32, device=DEV)
+            out = pk.make_step_out(tokens=tokens)
+            side = torch.cuda.Stream()
+            sess.focus.focus_step(n, out=out)
+            torch.cuda.synchronize()
+            steps = [tokens.cpu().clone()]
+            if captured:
+                g = torch.cuda.CUDAGraph()
+                with torch.cuda.graph(g, stream=side):
+                    sess.focus.focus_step(n, out=out, stream=side)
+            for _ in range(3):
+                g.replay() if captured else sess.focus.focus_step(n, out=out)
+                torch.cuda.synchronize()
+                steps.append(tokens.cpu().clone())
+            got.append(steps)
+            sess.focus.focus_free()
+        assert all(torch.equal(a, b) for a, b in zip(*got))
+        assert bool((got[0][-1] != wl.mask_token_id).any())
+
+
+@pytest.mark.parametrize("experts", [0, 4])
+def test_prefill_and_looped_steps_on_mx_weights(experts):
+    """Prompts go through the MXFP4 layers as well: their keys and values against a context on the same values in bf16 (every row takes all of the
+    experts, so that a rounding changes no pick; the tolerance of the bf16 model's parity tests); and a loop of steps against the steps one by one."""
+    pk, runner = _pk()
+    moe = dict(n_experts=4, experts_per_token=4) if experts else dict(n_experts=0, experts_per_token=0, expert_ffn=0, shared_ffn=0, first_moe_layer=0)
+    wl = small(prefill="prompt", **moe)
+    n, B = wl.batch, wl.block_size
+    prompts = wl.prompt_tokens(wl.prefix_lens())
+    pools = []
+    for mx in (False, True):
+        sess = runner.open_session(wl, DEV)
+        layers = []
+        for w in sess.weights[3]:
+            pairs = {}
+            for name in MATRICES:
+                if name in w:
+                    t = w[name]
+                    c, s = pk.focus_mx_quantize(t.reshape(-1, t.shape[-1]))
+                    pk.focus_mx_dequantize(c, s, t.view(-1, t.shape[-1]))
+                    pairs[name] = (c.view(*t.shape[:-1], -1), s.view(*t.shape[:-1], -1))
+            layers.append(pairs)
+        if mx:
+            sess.focus.focus_set_mx_weights(layers)
+        ids = [prompts[b] for b in sess.seq_ids]
+        sess.kv_pool.zero_()
+        sess.focus.focus_prefill_kv(sess.prefix_lens, sess.page_tables, ids)
+        torch.cuda.synchronize()
+        pools.append(sess.kv_pool.view(torch.bfloat16).float().cpu())
+        if mx:
+            tokens = torch.zeros(n, B, dtype=torch.int32, device=DEV)
+            out = pk.make_step_out(tokens=tokens)
+            for _ in range(4):
+                sess.focus.focus_step(n, out=out)
+            torch.cuda.synchronize()
+            one_by_one = tokens.cpu().clone()
+            sess.focus.focus_prefill_kv(sess.prefix_lens, sess.page_tables, ids)
+            sess.focus.focus_run_steps(n, 4, finalize=False, out=out)
+            torch.cuda.synchronize()
+            assert torch.equal(tokens.cpu(), one_by_one)
+        sess.focus.focus_free()
+    a, b = pools
+    assert float(a.abs().max()) > 0 and not torch.equal(a, b)
+    assert float((a - b).abs().max() / a.abs().max()) <= 2e-2
+
+
+def test_setters_refuse_tensors_of_the_host():
+    pk, runner = _pk()
+    wl = small()
+    sess = runner.open_session(wl, DEV)
+    r = pk.focus_router(n_experts=16, experts_per_token=4, score=1, n_groups=4, groups_kept=2, group_top=2, renormalize=1, route_scale=1.0)
+    with pytest.raises(pk.FocusError):
+        sess.focus.focus_set_router(r, [torch.zeros(16)] * wl.n_layers)
+    up, down = pk.focus_mx_quantize(torch.zeros(16 * 256, 512, device=DEV)), pk.focus_mx_quantize(torch.zeros(16 * 512, 128, device=DEV))
+    pair = dict(w_expert_gate_up=tuple(t.view(16, 256, -1).cpu() for t in up), w_expert_down=tuple(t.view(16, 512, -1) for t in down))
+    with pytest.raises(pk.FocusError):
+        sess.focus.focus_set_mx_weights([{}, pair, {}])
+    sess.focus.focus_free()

@@ -63,6 +63,7 @@ def test_route_refuses_arguments():
     r = router()
     refused(lib.focus_route(None, None, 1, 0, P, 16, None, P, P), "router")
     refused(lib.focus_route(C.byref(r), None, -1, 0, P, 16, None, P, P), "n_rows")
+    refused(lib.focus_route(C.byref(r), None, 1 << 26, 0, P, 16, None, P, P), "n_rows")
     refused(lib.focus_route(C.byref(r), None, 1, binding.FOCUS_MX4, P, 16, None, P, P), "dtype")
     refused(lib.focus_route(C.byref(r), None, 1, 0, P, 15, None, P, P), "ld")
     refused(lib.focus_route(C.byref(r), None, 1, 0, None, 16, None, P, P), "null")
@@ -84,6 +85,8 @@ def test_conversions_refuse():
         refused(q(0, 1, 33, P, 32, P, P), "ldx")
         refused(q(0, 1 << 39, 1, P, 32, P, P), "large")
         refused(q(0, 1 << 36, 32, P, 32, P, P), "large")
+        refused(q(0, 1 << 30, 32, P, 32, P, P), "large")
+        refused(q(0, 1 << 20, 1 << 15, P, 1 << 15, P, P), "large")
         refused(q(0, 1, 32, None, 32, P, P), "null")
         refused(q(0, 1, 32, P, 32, None, P), "null")
         refused(q(0, 1, 32, P, 32, P, None), "null")
@@ -103,7 +106,8 @@ def test_gemm_refuses():
                       (dict(mw=None), "null"), (dict(ldc=7), "ldc"), (dict(lda=56), "lda"), (dict(lda=68), "lda"), (dict(lda=(1 << 22) + 8), "lda"), (dict(a=None), "null"), (dict(c=None), "null"),
                       (dict(mw=binding.focus_mx(None, P)), "null"), (dict(mw=binding.focus_mx(P, None)), "null"), (dict(at=2), "a_scales"), (dict(sc=P), "a_scales"),
                       (dict(a=P + 8), "aligned"), (dict(mw=binding.focus_mx(P + 8, P)), "aligned"), (dict(ws=P + 8, wb=64), "aligned"), (dict(c=P + 2), "aligned"),
-                      (dict(n=1 << 20, k=1 << 13, lda=1 << 13, ldc=1 << 20), "large"), (dict(k=(1 << 22) + 32), "k")]:
+                      (dict(n=1 << 20, k=1 << 13, lda=1 << 13, ldc=1 << 20), "large"),
+                      (dict(m=2 ** 31 - 1, n=129, ldc=129), "large"), (dict(m=2 ** 31 - 1, n=129, ldc=129, at=2, sc=P), "large"), (dict(k=(1 << 22) + 32), "k")]:
         refused(call(**bad), text)
     assert call(m=0, a=None, c=None) == 0 and call(n=0, ldc=0, c=None) == 0
     refused(lib.focus_mx_gemm_bytes(4, 8, 64, 1, None))
@@ -118,7 +122,7 @@ def test_experts_refuse():
     def call(E=8, h=64, f=32, gu=w, dn=w, rows=4, k=2, x=P, ldx=64, e=P, g=P, ot=0, out=P, ldo=64, add=0, ws=P, wb=1 << 30):
         return lib.focus_mx_experts(None, E, h, f, None if gu is None else C.byref(gu), None if dn is None else C.byref(dn), rows, k, x, ldx, e, g, ot, out, ldo, add, ws, wb)
     for bad, text in [(dict(E=0), "n_experts"), (dict(E=513), "n_experts"), (dict(h=48, ldx=48), "multiples"), (dict(f=16), "multiples"), (dict(h=0), "multiples"),
-                      (dict(rows=-1), "n_rows"), (dict(k=0), "k in"), (dict(k=33), "k in"), (dict(rows=(1 << 24) + 1, k=1), "n_rows"), (dict(h=1 << 20, f=1 << 11, ldx=1 << 20, ldo=1 << 20), "large"),
+                      (dict(rows=-1), "n_rows"), (dict(k=0), "k in"), (dict(k=33), "k in"), (dict(rows=1 << 24, k=1), "n_rows"), (dict(rows=1 << 18, k=32, h=1 << 14, f=1 << 15, ldx=1 << 14, ldo=1 << 14), "large"), (dict(h=1 << 20, f=1 << 11, ldx=1 << 20, ldo=1 << 20), "large"),
                       (dict(ot=2), "out_type"), (dict(add=2), "add"), (dict(add=1, ot=1), "add"), (dict(ldx=56), "ldx"), (dict(ldx=68), "ldx"), (dict(ldo=63), "ldo"),
                       (dict(rows=1 << 20, ldx=1024), "2^30"), (dict(gu=None), "null"), (dict(dn=binding.focus_mx(P, None)), "null"), (dict(x=None), "null"), (dict(e=None), "null"),
                       (dict(g=None), "null"), (dict(out=None), "null"), (dict(ws=None), "null"), (dict(x=P + 8), "aligned"), (dict(gu=binding.focus_mx(P + 4, P)), "aligned"),
