@@ -362,11 +362,12 @@ void launch_rows(hipStream_t s, int mode, const RowsArgs &g, int tile_slots) {
 }
 
 // ---------------------------------------------------------------------------------------------
-// MXFP4 rows x MXFP4 weights: 2 x 2 wavefronts.  K goes in slabs of 128, 64 bytes of codes a row, through four LDS stages: a slab is asked for three
-// slabs before it is used, half of it in each half of a slab.  Lane l supplies row l % 32 and, of the two halves of 64 elements of a slab, block 2 ks + l / 32: 16 bytes of codes and one
-// scale.  Scales are fetched 16 bytes a row, for four slabs at once (a row per lane costs the vector caches a lookup per lane whatever its size), a
-// quad of slabs ahead, and handed on through LDS.  Pipelined by hand like k_mx_rows: behind each MFMA one fragment read of the next half or one load; the
-// only barrier of a slab stands before its second half.
+// MXFP4 rows x MXFP4 weights: 2 x 2 wavefronts.  K goes in pairs of slabs of 128: whole lines of 128 bytes of codes a row, straight into LDS, through
+// a ring of mx_pairs() pairs (from the caches, lines of 128 bytes come at 34 TB/s over all compute units, pieces of 64 at 17).  Lane l supplies row l % 32 and, of the four quarters of 64 elements of a pair, block 2 q + l / 32: 16 bytes of codes and one
+// scale.  Scales are fetched 16 bytes a row, for two pairs at once (a row per lane costs the vector caches a lookup per lane whatever its size), two
+// pairs ahead, and handed on through LDS.  Pipelined by hand like k_mx_rows: behind each MFMA one fragment read of the next quarter or one load.  The
+// only barrier of a pair stands before its last quarter: by then everyone has read all of it, its place is filled again over the next quarters, and the
+// next pair has landed.
 struct MxArgs {
   const unsigned char *A, *a_scales, *W, *w_scales;
   int M, N, K;
@@ -376,15 +377,17 @@ struct MxArgs {
   size_t split_stride;
 };
 enum { XM_STORE, XM_STORE_F32, XM_PARTIAL };
-constexpr int kMxStages = 4;
-constexpr int mx_lds(int bm, int bn) { return kMxStages * (bm + bn) * 64 + 2 * (bm + bn) * 16; }
+constexpr int mx_pairs(int bm) { return bm == 256 ? 2 : 4; }
+constexpr int mx_lds(int bm, int bn) { return mx_pairs(bm) * (bm + bn) * 128 + 2 * (bm + bn) * 16; }
 
 template <int BM, int BN, int MODE, bool WHOLE>      // WHOLE: K is a multiple of 512
-__global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void k_mx_mx(MxArgs g) {
+__global__ __launch_bounds__(256, mx_lds(BM, BN) > 80 * 1024 ? 1 : 2) void k_mx_mx(MxArgs g) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  constexpr int WM = BM / 2, WN = BN / 2, TM = WM / 32, TN = WN / 32, NMF = TM * TN, NF = TM + TN, IA = BM / 64, IB = BN / 64, ROWS = BM + BN, SI = ROWS / 256, HALF = (IA + IB) / 2, EVERY = NMF / HALF;
-  constexpr int ASTAGE = BM * 64, WSTAGE = BN * 64, WBASE = kMxStages * ASTAGE, SBASE = WBASE + kMxStages * WSTAGE;
-  static_assert(NF <= NMF && HALF <= NMF, "one fragment read and one load per MFMA at most");
+  constexpr int WM = BM / 2, WN = BN / 2, TM = WM / 32, TN = WN / 32, NMF = TM * TN, NF = TM + TN, IA = BM / 32, IB = BN / 32, ROWS = BM + BN, SI = ROWS / 256;
+  // the loads of a pair are spread over SPREAD quarters, PART of them in each: the fewer pairs there are, the sooner they have to be asked for
+  constexpr int R = mx_pairs(BM), L = IA + IB, SPREAD = R == 2 ? 2 : 4, PART = L / SPREAD, EVERY = NMF / PART;
+  constexpr int ASTAGE = BM * 128, WSTAGE = BN * 128, WBASE = R * ASTAGE, SBASE = WBASE + R * WSTAGE;
+  static_assert(NF <= NMF && PART <= NMF && NMF % PART == 0, "one fragment read and one load per MFMA at most");
   __shared__ __attribute__((aligned(1024))) unsigned char lds[mx_lds(BM, BN)];
   const int splits = g.splits, tiles_n = g.tiles_n, total = g.tiles_m * tiles_n * splits, per_xcd = (total + 7) / 8;
   const int item = (blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
@@ -401,13 +404,13 @@ __global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void k_mx_mx(MxArgs g) {
   const int wm = (wave >> 1) * WM, wn = (wave & 1) * WN, frow = lane & 31, h = lane >> 5;
   __amdgpu_buffer_rsrc_t rs_a = __builtin_amdgcn_make_buffer_rsrc((void *)(g.A + (size_t)m0 * (K / 2)), 0, (unsigned)valid_m * (unsigned)(K / 2), 0x00020000);
   __amdgpu_buffer_rsrc_t rs_w = __builtin_amdgcn_make_buffer_rsrc((void *)(g.W + (size_t)n0 * (K / 2)), 0, (unsigned)valid_n * (unsigned)(K / 2), 0x00020000);
-  // An instruction fills 16 rows; lane l fetches chunk (block) (l % 4) ^ ((row / 4) % 4) of row l / 4, so that LDS reads spread over the banks.
+  // An instruction fills 8 rows; lane l fetches chunk (block) (l % 8) ^ ((row / 2) % 8) of row l / 8, so that LDS reads spread over the banks.
   // Rows beyond the matrix lie outside the descriptors.
-  const int chunk = (lane & 3) ^ ((lane >> 4) & 3);
-  const unsigned vo = (unsigned)(wave * 16 + (lane >> 2)) * (unsigned)(K / 2) + chunk * 16, row_step = 64u * (unsigned)(K / 2);
-  auto load = [&](int slab, int stage, int q) __attribute__((always_inline)) {          // q: 0 .. IA - 1 the rows, then the weights
-    const unsigned so = slab < slabs ? (unsigned)(slab0 + slab) * 64u : kOutside;
-    const bool gone = !WHOLE && (slab0 + slab) * 4 + chunk >= blocks;
+  const int chunk = (lane & 7) ^ ((4 * (wave & 1) + (lane >> 4)) & 7);
+  const unsigned vo = (unsigned)(wave * 8 + (lane >> 3)) * (unsigned)(K / 2) + chunk * 16, row_step = 32u * (unsigned)(K / 2);
+  auto load = [&](int pair, int stage, int q) __attribute__((always_inline)) {          // q: 0 .. IA - 1 the rows, then the weights
+    const unsigned so = 2 * pair < slabs ? (unsigned)(slab0 + 2 * pair) * 64u : kOutside;
+    const bool gone = !WHOLE && (slab0 + 2 * pair) * 4 + chunk >= blocks;
     const int r = q < IA ? q : q - IA;
     const unsigned v = gone ? kOutside : vo + r * row_step;
     if (q < IA) __builtin_amdgcn_raw_ptr_buffer_load_lds(rs_a, FK_LDS_PTR(lds + stage * ASTAGE + (r * 4 + wave) * 1024), 16, v, so, 0, 0);
@@ -444,19 +447,19 @@ __global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void k_mx_mx(MxArgs g) {
     for (int j = 0; j < TN; ++j)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-  // fragment s of a half of a slab in the order in which its MFMAs need them: W0, A0, W1 .. , A1 ..; the halves differ in one bit of the chunk
-  unsigned at_a[2], at_w[2];
+  // fragment s of a quarter in the order in which its MFMAs need them: W0, A0, W1 .. , A1 ..; the quarters differ in the chunk
+  unsigned at_a[4], at_w[4];
 #pragma unroll
-  for (int ks = 0; ks < 2; ++ks) {
-    const unsigned c = (unsigned)((2 * ks + h) ^ ((frow >> 2) & 3)) << 4;
-    at_a[ks] = (wm + frow) * 64 + c;
-    at_w[ks] = WBASE + (wn + frow) * 64 + c;
+  for (int q = 0; q < 4; ++q) {
+    const unsigned c = (unsigned)((2 * q + h) ^ ((frow >> 1) & 7)) << 4;
+    at_a[q] = (wm + frow) * 128 + c;
+    at_w[q] = WBASE + (wn + frow) * 128 + c;
   }
   u32x4 fa[2][TM], fw[2][TN];
-  auto read = [&](int s, int ks, int stage, int slot) __attribute__((always_inline)) {
+  auto read = [&](int s, int q, int stage) __attribute__((always_inline)) {
     const int f = s == 0 ? TM : s == 1 ? 0 : s <= TN ? TM + s - 1 : s - TN;
-    if (f < TM) fa[slot][f < TM ? f : 0] = *(const u32x4 *)(lds + at_a[ks] + stage * ASTAGE + (f < TM ? f : 0) * 2048);
-    else fw[slot][f < TM ? 0 : f - TM] = *(const u32x4 *)(lds + at_w[ks] + stage * WSTAGE + (f < TM ? 0 : f - TM) * 2048);
+    if (f < TM) fa[q & 1][f < TM ? f : 0] = *(const u32x4 *)(lds + at_a[q] + stage * ASTAGE + (f < TM ? f : 0) * 4096);
+    else fw[q & 1][f < TM ? 0 : f - TM] = *(const u32x4 *)(lds + at_w[q] + stage * WSTAGE + (f < TM ? 0 : f - TM) * 4096);
   };
   // the four scales of a slab of every row, in two sets: byte 2 ks belongs to half ks once the upper lanes' are moved down by one
   unsigned ca[2][TM], cw[2][TN];
@@ -478,31 +481,34 @@ __global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void k_mx_mx(MxArgs g) {
     fetch_scales(0);
     in_order();
 #pragma unroll
-    for (int s = 0; s < kMxStages; ++s) {
+    for (int p = 0; p < R; ++p) {
 #pragma unroll
-      for (int q = 0; q < (s < kMxStages - 1 ? 2 : 1) * HALF; ++q) load(s, s, q);
+      for (int q = 0; q < (p < R - 1 ? L : PART); ++q) load(p, p, q);
       in_order();
     }
     hand_on_scales(0);
-    __builtin_amdgcn_s_waitcnt(vmcnt_imm((2 * kMxStages - 3) * HALF));
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm((R - 2) * L + PART));
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     read_scales(0, 0, 0);
 #pragma unroll
-    for (int s = 0; s < NF; ++s) read(s, 0, 0, 0);
-    // OF: slab of its quad (its LDS stage), FETCH: whether another quad may follow
+    for (int s = 0; s < NF; ++s) read(s, 0, 0);
+    // OF: slab of its quad of slabs, whose pairs lie at `stage` and behind it
     auto slab_of = [&](auto which, int quad) __attribute__((always_inline)) {
       constexpr int OF = decltype(which)::value, SLOT = OF & 1, NEXT = (OF + 1) & 3;
+      const int pair = 2 * quad + OF / 2, stage = R == 2 ? OF / 2 : (2 * quad & (R - 1)) + OF / 2, after = OF < 2 ? stage + 1 : R == 2 ? 0 : (stage + 1) & (R - 1);
       shift_scales(SLOT);
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks) {
-        if (ks == 1) {
+        constexpr int FIRST = 2 * (OF & 1);
+        const int q = FIRST + ks;              // of the pair
+        if (q == 3) {
           if (OF == 3) hand_on_scales(quad + 1);
-          // the next slab has landed: younger are those of the two slabs behind it (and scales, which are not counted)
-          __builtin_amdgcn_s_waitcnt(vmcnt_imm((kMxStages - 2) * 2 * HALF));
+          // the next pair has landed: younger are those of the pairs behind it (and scales, which are not counted)
+          __builtin_amdgcn_s_waitcnt(vmcnt_imm((R - 2) * L));
           asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-          if (OF == 0) { fetch_scales(quad + 1); in_order(); }
-          read_scales(OF == 3 ? quad + 1 : quad, NEXT, SLOT ^ 1);
+          if (OF == 1) { fetch_scales(quad + 1); in_order(); }
         }
+        if (ks == 1) read_scales(OF == 3 ? quad + 1 : quad, NEXT, SLOT ^ 1);
 #pragma unroll
         for (int s = 0; s < NMF; ++s) {
           const int i = s / TN, j = s % TN;
@@ -510,11 +516,11 @@ __global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void k_mx_mx(MxArgs g) {
           const i32x8 b = {(int)fw[ks][j][0], (int)fw[ks][j][1], (int)fw[ks][j][2], (int)fw[ks][j][3], 0, 0, 0, 0};
           if (ks == 0) acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, acc[i][j], 4, 4, 0, (int)ca[SLOT][i], 0, (int)cw[SLOT][j]);
           else acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, acc[i][j], 4, 4, 2, (int)ca[SLOT][i], 2, (int)cw[SLOT][j]);
-          if (s < NF) read(s, ks ^ 1, ks == 0 ? OF : NEXT, ks ^ 1);
+          if (s < NF) read(s, (q + 1) & 3, q == 3 ? after : stage);
           // spread: in a burst the loads hold up the MFMAs behind them for as long as the address unit takes
           if (s % EVERY == EVERY - 1) {
-            if (ks == 0) load(4 * quad + OF + kMxStages - 1, (OF + 3) & 3, HALF + s / EVERY);
-            else load(4 * quad + OF + kMxStages, OF, s / EVERY);
+            if (q == 3) load(pair + R, stage, s / EVERY);
+            else if (q + 1 < SPREAD) load(pair + R - 1, R == 2 ? stage ^ 1 : (stage + R - 1) & (R - 1), (q + 1) * PART + s / EVERY);
           }
           __builtin_amdgcn_sched_barrier(0);
         }
