@@ -24,6 +24,52 @@ constexpr int64_t kMxSliceBytes = 136ll << 20;
 constexpr int vmcnt_imm(int n) { return 0x0F70 | (n & 15) | ((n >> 4) << 14); }   // s_waitcnt vmcnt(n) only
 constexpr unsigned kOutside = 0x80000000u;   // an offset beyond every descriptor: the load returns zeros
 
+// A wavefront's 32 x 32 TN results into C, through LDS of its own (tile_lds() bytes): register r of lane l of acc[j] is C[l % 32][32 j + 8 (r / 4) + 4 (l / 32) + r % 4]
+// (the product of transposed operands), so four neighbours go into LDS at once, and whole pieces of rows come out, 16 bytes a lane.  Stored straight from
+// the registers, an element per lane and instruction, with an address and two comparisons for each, the results of 2048 x 24576 x 4096 took 17 of 125 us.
+// rows, cols: of the tile that exist; wide: the rows of C are 16-byte aligned.
+#if defined(__HIP_DEVICE_COMPILE__)
+__device__ __forceinline__ void wave_lds_order() {      // the lanes' traffic runs in order, only the compiler has to keep it so
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+#endif
+template <typename T> constexpr int tile_pitch(int tn) { return tn * 32 * (int)sizeof(T) + 16; }      // rows four banks apart
+template <typename T, bool ADD, int TN>
+__device__ __forceinline__ void store_tile(unsigned char *mine, const f32x16 (&acc)[TN], T *out, int64_t ldo, int rows, int cols, bool wide) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  constexpr int P = tile_pitch<T>(TN), PER = 16 / sizeof(T), LANES = TN * 32 / PER, ROWS = 64 / LANES;      // elements a lane, lanes a row, rows an instruction
+  typedef float f32x4 __attribute__((ext_vector_type(4)));
+  typedef T tx4 __attribute__((ext_vector_type(4)));
+  const int lane = threadIdx.x & 63, frow = lane & 31, h = lane >> 5;
+#pragma unroll
+  for (int j = 0; j < TN; ++j)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const f32x4 v = {acc[j][4 * g], acc[j][4 * g + 1], acc[j][4 * g + 2], acc[j][4 * g + 3]};
+      *(tx4 *)(mine + frow * P + (j * 32 + 8 * g + 4 * h) * (int)sizeof(T)) = __builtin_convertvector(v, tx4);
+    }
+  wave_lds_order();
+  const int row0 = lane / LANES, col = lane % LANES * PER;
+  T *o = out + (int64_t)row0 * ldo + col;
+#pragma unroll
+  for (int it = 0; it < 32 / ROWS; ++it, o += ROWS * ldo) {
+    typedef T txp __attribute__((ext_vector_type(PER)));
+    txp v = *(const txp *)(mine + (it * ROWS + row0) * P + col * (int)sizeof(T));
+    if (it * ROWS + row0 >= rows || col >= cols) continue;
+    if (wide && col + PER <= cols) {
+      if (ADD) v += *(const txp *)o;
+      *(txp *)o = v;
+    } else {
+#pragma unroll
+      for (int e = 0; e < PER; ++e)
+        if (col + e < cols) o[e] = ADD ? (T)(o[e] + v[e]) : v[e];
+    }
+  }
+  wave_lds_order();
+#endif
+}
+
 // ---------------------------------------------------------------------------------------------
 // bf16 rows x MXFP4 weights.
 struct RowsArgs {
@@ -514,8 +560,8 @@ __global__ __launch_bounds__(256, mx_lds(BM, BN) > 80 * 1024 ? 1 : 2) void k_mx_
           const int i = s / TN, j = s % TN;
           const i32x8 a = {(int)fa[ks][i][0], (int)fa[ks][i][1], (int)fa[ks][i][2], (int)fa[ks][i][3], 0, 0, 0, 0};
           const i32x8 b = {(int)fw[ks][j][0], (int)fw[ks][j][1], (int)fw[ks][j][2], (int)fw[ks][j][3], 0, 0, 0, 0};
-          if (ks == 0) acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, acc[i][j], 4, 4, 0, (int)ca[SLOT][i], 0, (int)cw[SLOT][j]);
-          else acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, acc[i][j], 4, 4, 2, (int)ca[SLOT][i], 2, (int)cw[SLOT][j]);
+          if (ks == 0) acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(b, a, acc[i][j], 4, 4, 0, (int)cw[SLOT][j], 0, (int)ca[SLOT][i]);
+          else acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(b, a, acc[i][j], 4, 4, 2, (int)cw[SLOT][j], 2, (int)ca[SLOT][i]);
           if (s < NF) read(s, (q + 1) & 3, q == 3 ? after : stage);
           // spread: in a burst the loads hold up the MFMAs behind them for as long as the address unit takes
           if (s % EVERY == EVERY - 1) {
@@ -544,21 +590,14 @@ __global__ __launch_bounds__(256, mx_lds(BM, BN) > 80 * 1024 ? 1 : 2) void k_mx_
     }
   }
   __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");                   // LDS is free
+  using T = std::conditional_t<MODE == XM_STORE, bf16_t, float>;
+  static_assert(4 * 32 * tile_pitch<T>(TN) <= (int)sizeof(lds), "results of 32 rows of each wavefront");
+  unsigned char *const mine = lds + wave * 32 * tile_pitch<T>(TN);
+  T *const out = (T *)g.out + (MODE == XM_PARTIAL ? (size_t)split * g.split_stride : 0) + (size_t)(m0 + wm) * g.ldo + n0 + wn;
+  const bool wide = (((uintptr_t)g.out | ((MODE == XM_PARTIAL ? g.split_stride : 0) | (uint64_t)g.ldo) * sizeof(T)) & 15) == 0;
 #pragma unroll
-  for (int i = 0; i < TM; ++i)
-#pragma unroll
-    for (int j = 0; j < TN; ++j) {
-      const int gn = wn + j * 32 + frow;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int gm = wm + i * 32 + 8 * (r >> 2) + 4 * h + (r & 3);
-        if (gm < valid_m && gn < valid_n) {
-          const size_t at = (size_t)(m0 + gm) * g.ldo + n0 + gn;
-          if (MODE == XM_STORE) ((bf16_t *)g.out)[at] = (bf16_t)acc[i][j][r];
-          else (MODE == XM_PARTIAL ? (float *)g.out + (size_t)split * g.split_stride : (float *)g.out)[at] = acc[i][j][r];
-        }
-      }
-    }
+  for (int i = 0; i < TM; ++i) store_tile<T, false>(mine, acc[i], out + (int64_t)(i * 32) * g.ldo, g.ldo, valid_m - wm - i * 32, valid_n - wn, wide);
 #endif
 }
 
