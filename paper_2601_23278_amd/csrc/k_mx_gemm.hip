@@ -24,9 +24,10 @@ constexpr int64_t kMxSliceBytes = 136ll << 20;
 constexpr int vmcnt_imm(int n) { return 0x0F70 | (n & 15) | ((n >> 4) << 14); }   // s_waitcnt vmcnt(n) only
 constexpr unsigned kOutside = 0x80000000u;   // an offset beyond every descriptor: the load returns zeros
 
-// A wavefront's 32 x 32 TN results into C, through LDS of its own (tile_lds() bytes): register r of lane l of acc[j] is C[l % 32][32 j + 8 (r / 4) + 4 (l / 32) + r % 4]
-// (the product of transposed operands), so four neighbours go into LDS at once, and whole pieces of rows come out, 16 bytes a lane.  Stored straight from
-// the registers, an element per lane and instruction, with an address and two comparisons for each, the results of 2048 x 24576 x 4096 took 17 of 125 us.
+// A wavefront's results of 32 rows and 8 G columns into C, through LDS of its own (32 tile_pitch() bytes): value(g) of lane l are C[l % 32][8 g + 4 (l / 32) + 0 .. 3]
+// (four registers of the product of transposed operands), so four neighbours go into LDS at once, and whole pieces of rows come out, 16 bytes a lane.
+// Stored straight from the registers, an element per lane and instruction, with an address and two comparisons for each, 2048 x 24576 x 4096 with both
+// operands in MXFP4 took 125 us instead of 104.
 // rows, cols: of the tile that exist; wide: the rows of C are 16-byte aligned.
 #if defined(__HIP_DEVICE_COMPILE__)
 __device__ __forceinline__ void wave_lds_order() {      // the lanes' traffic runs in order, only the compiler has to keep it so
@@ -34,21 +35,16 @@ __device__ __forceinline__ void wave_lds_order() {      // the lanes' traffic ru
   __builtin_amdgcn_wave_barrier();
 }
 #endif
-template <typename T> constexpr int tile_pitch(int tn) { return tn * 32 * (int)sizeof(T) + 16; }      // rows four banks apart
-template <typename T, bool ADD, int TN>
-__device__ __forceinline__ void store_tile(unsigned char *mine, const f32x16 (&acc)[TN], T *out, int64_t ldo, int rows, int cols, bool wide) {
+template <typename T> constexpr int tile_pitch(int groups) { return groups * 8 * (int)sizeof(T) + 16; }      // rows of 128 bytes and more lie four banks apart
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+template <typename T, bool ADD, int G, typename V>
+__device__ __forceinline__ void store_tile(unsigned char *mine, const V &value, T *out, int64_t ldo, int rows, int cols, bool wide) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  constexpr int P = tile_pitch<T>(TN), PER = 16 / sizeof(T), LANES = TN * 32 / PER, ROWS = 64 / LANES;      // elements a lane, lanes a row, rows an instruction
-  typedef float f32x4 __attribute__((ext_vector_type(4)));
+  constexpr int P = tile_pitch<T>(G), PER = 16 / sizeof(T), LANES = G * 8 / PER, ROWS = 64 / LANES;      // elements a lane, lanes a row, rows an instruction
   typedef T tx4 __attribute__((ext_vector_type(4)));
   const int lane = threadIdx.x & 63, frow = lane & 31, h = lane >> 5;
 #pragma unroll
-  for (int j = 0; j < TN; ++j)
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const f32x4 v = {acc[j][4 * g], acc[j][4 * g + 1], acc[j][4 * g + 2], acc[j][4 * g + 3]};
-      *(tx4 *)(mine + frow * P + (j * 32 + 8 * g + 4 * h) * (int)sizeof(T)) = __builtin_convertvector(v, tx4);
-    }
+  for (int g = 0; g < G; ++g) *(tx4 *)(mine + frow * P + (8 * g + 4 * h) * (int)sizeof(T)) = __builtin_convertvector(value(g), tx4);
   wave_lds_order();
   const int row0 = lane / LANES, col = lane % LANES * PER;
   T *o = out + (int64_t)row0 * ldo + col;
@@ -286,7 +282,7 @@ __global__ __launch_bounds__(256, 2) void k_mx_rows(RowsArgs g) {
 #pragma unroll
         for (int s = 0; s < NMF; ++s) {
           const int j = s / L, i = s % L;
-          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[TWO ? ks & 1 : 0][i], __builtin_bit_cast(bf16x8, fb[CT == 2 ? j : ks & 1]), acc[i][j], 0, 0, 0);
+          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fb[CT == 2 ? j : ks & 1]), fa[TWO ? ks & 1 : 0][i], acc[i][j], 0, 0, 0);
           if (TWO ? s < L : j == 1) fa[TWO ? (ks & 1) ^ 1 : 0][i] = *(const bf16x8 *)(from + i * 4096);
 #pragma unroll
           for (int part = i * PER; part < i * PER + PER && part < 4; ++part) {
@@ -350,44 +346,32 @@ __global__ __launch_bounds__(256, 2) void k_mx_rows(RowsArgs g) {
   else if (live == 2) multiply(std::integral_constant<int, TM < 2 ? 1 : 2>());
   else if (live == 3) multiply(std::integral_constant<int, TM < 3 ? 1 : 3>());
   else multiply(std::integral_constant<int, TM>());
-  // register r of lane l is C[8 (r / 4) + 4 (l / 32) + r % 4][l % 32] of its 32 x 32 tile
-  if (SILU) {
-    // one column tile: lanes 0..15 of a half hold gate columns, 16..31 the matching up columns; exchanging halves between two registers gives
-    // the lower lanes both numbers of register r and the upper lanes both of register r + 1
-    const int gn = CT == 2 ? n0 + wave * 32 + frow : n0 + wave * 16 + (lane & 15);
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");                   // LDS is free
+  using T = std::conditional_t<MODE == RM_STORE || SILU, bf16_t, float>;
+  constexpr int G = SILU ? 2 * CT : 4 * CT;                                          // groups of 8 columns of this wavefront
+  static_assert(4 * 32 * tile_pitch<T>(G) <= (int)sizeof(lds), "results of 32 rows of each wavefront");
+  unsigned char *const mine = lds + wave * 32 * tile_pitch<T>(G);
+  const int first = n0 + wave * 8 * G;
+  T *const out = (T *)g.out + (MODE == RM_PARTIAL ? (size_t)split * g.split_stride : 0) + (size_t)row0 * g.ldo + first - g.n_begin;
+  const bool wide = (((uintptr_t)g.out | ((MODE == RM_PARTIAL ? g.split_stride : 0) | (uint64_t)g.ldo) * sizeof(T)) & 15) == 0;
 #pragma unroll
-    for (int i = 0; i < TM; ++i)
-#pragma unroll
-      for (int r = 0; r < 16; r += CT == 2 ? 1 : 2) {
-        float ga = acc[i][0][r], up = acc[i][CT - 1][r];
-        int rr = r;
-        if (CT == 1) {
-          const u32x2 x = __builtin_amdgcn_permlane16_swap(__float_as_uint(acc[i][0][r]), __float_as_uint(acc[i][0][(r + 1) & 15]), false, false);
-          ga = __uint_as_float(x[0]); up = __uint_as_float(x[1]);
-          rr = r + ((lane >> 4) & 1);
-        }
-        const int gm = i * 32 + 8 * (rr >> 2) + 4 * h + (rr & 3);
+  for (int i = 0; i < TM; ++i) {
+    if (i * 32 >= valid) break;
+    // SiLU*up: gate and up of a column are the same register of two tiles, or registers r and r + 8 of one
+    auto value = [&](int v) __attribute__((always_inline)) {
+      const f32x16 &t = acc[i][SILU ? 0 : v / 4];
+      f32x4 x = {t[4 * (v % 4)], t[4 * (v % 4) + 1], t[4 * (v % 4) + 2], t[4 * (v % 4) + 3]};
+      if (SILU) {
+        const f32x16 &u = acc[i][CT - 1];
+        const int at = CT == 2 ? 4 * v : 4 * (v & 1) + 8;
         // exp overflows to infinity and the quotient to 0 for a large negative gate
-        if (gm < valid && gn < n_end) ((bf16_t *)g.out)[(size_t)(row0 + gm) * g.ldo + gn - g.n_begin] = (bf16_t)(ga / (1.0f + __expf(-ga)) * up);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = x[e] / (1.0f + __expf(-x[e])) * u[at + e];
       }
-    return;
+      return x;
+    };
+    store_tile<T, MODE == RM_ADD_F32, G>(mine, value, out + (int64_t)(i * 32) * g.ldo, g.ldo, valid - i * 32, n_end - first, wide);
   }
-#pragma unroll
-  for (int i = 0; i < TM; ++i)
-#pragma unroll
-    for (int j = 0; j < CT; ++j) {
-      const int gn = n0 + (wave * CT + j) * 32 + frow;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int gm = i * 32 + 8 * (r >> 2) + 4 * h + (r & 3);
-        if (gm < valid && gn < n_end) {
-          const size_t at = (size_t)(row0 + gm) * g.ldo + gn - g.n_begin;
-          if (MODE == RM_STORE) ((bf16_t *)g.out)[at] = (bf16_t)acc[i][j][r];
-          else if (MODE == RM_ADD_F32) ((float *)g.out)[at] += acc[i][j][r];
-          else (MODE == RM_PARTIAL ? (float *)g.out + (size_t)split * g.split_stride : (float *)g.out)[at] = acc[i][j][r];
-        }
-      }
-    }
 #endif
 }
 
@@ -592,12 +576,13 @@ __global__ __launch_bounds__(256, mx_lds(BM, BN) > 80 * 1024 ? 1 : 2) void k_mx_
   __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");                   // LDS is free
   using T = std::conditional_t<MODE == XM_STORE, bf16_t, float>;
-  static_assert(4 * 32 * tile_pitch<T>(TN) <= (int)sizeof(lds), "results of 32 rows of each wavefront");
-  unsigned char *const mine = lds + wave * 32 * tile_pitch<T>(TN);
+  static_assert(4 * 32 * tile_pitch<T>(4 * TN) <= (int)sizeof(lds), "results of 32 rows of each wavefront");
+  unsigned char *const mine = lds + wave * 32 * tile_pitch<T>(4 * TN);
   T *const out = (T *)g.out + (MODE == XM_PARTIAL ? (size_t)split * g.split_stride : 0) + (size_t)(m0 + wm) * g.ldo + n0 + wn;
   const bool wide = (((uintptr_t)g.out | ((MODE == XM_PARTIAL ? g.split_stride : 0) | (uint64_t)g.ldo) * sizeof(T)) & 15) == 0;
 #pragma unroll
-  for (int i = 0; i < TM; ++i) store_tile<T, false>(mine, acc[i], out + (int64_t)(i * 32) * g.ldo, g.ldo, valid_m - wm - i * 32, valid_n - wn, wide);
+  for (int i = 0; i < TM; ++i)
+    store_tile<T, false, 4 * TN>(mine, [&](int v) __attribute__((always_inline)) { const f32x16 &t = acc[i][v / 4]; return f32x4{t[4 * (v % 4)], t[4 * (v % 4) + 1], t[4 * (v % 4) + 2], t[4 * (v % 4) + 3]}; }, out + (int64_t)(i * 32) * g.ldo, g.ldo, valid_m - wm - i * 32, valid_n - wn, wide);
 #endif
 }
 
