@@ -657,12 +657,13 @@ int whole_parts(int parts, int units) { const int per = (units + parts - 1) / pa
 // Tile and parts of K with the least estimated time.  Measured on 15 problems of 8 to 2048 rows, 2048 to 24576 columns and K of 2048 to 12288, every
 // tile with up to 16 parts.  A unit of K (256; with both operands in MXFP4 512) takes a workgroup `base` us alone and `first` more when all 256 compute
 // units have one; a second on some of them makes it `second`, and `more` for each further 256; beyond per_cu of them rounds follow one another.  A launch
-// costs 3 us, adding parts 2.5 us and 8 bytes an output and part at 4.5 TB/s.  (333 rows x 4096, K = 4096, MXFP4 rows: 13.8 us in one part, 22.8 in
-// five, which fill the chip; K = 12288: 30.7 in one, 24.9 in two, 30.1 in three.  1024 rows: 128 x 128 17.9, 256 x 256 34.3; 2048 rows x 6144: 45.1 and 40.7.
-// bf16 rows: 8 x 24576 32 x 128 17, 128 x 128 18.5; 1024 x 4096 128 x 128 41.4, 128 x 256 55; 333 x 4096, K = 12288, 128 x 128: 83 in one part, 54 in two, 59 in three, 50 in five.)
+// costs 3 us, adding parts 2.5 us and 8 bytes an output and part at 4.5 TB/s.  (333 rows x 4096, K = 4096, MXFP4 rows: 12.5 us in one part, 22 in five,
+// which fill the chip; K = 12288: 27.5 in one, 23.1 in two, 30 in three.  1024 rows, K = 4096: 128 x 128 15.3, 256 x 256 28.5; 2048 rows x 6144: 45.5 and
+// 35.3.  bf16 rows: 8 x 24576 32 x 128 17.4, 128 x 128 17.9; 1024 x 4096 128 x 128 36.6, 128 x 256 46.9; 333 x 4096, K = 12288, 128 x 128: 50.3 in two,
+// 49.5 in five, 128 x 256 49.3 in five.)  Its choices are the fastest of those or within 4 % of it.
 struct Variant { int bm, bn, per_cu; float base, first, second, more; };
-constexpr Variant kRowVariants[] = {{32, 128, 3, 0.8f, 0.45f, 1.3f, 0.7f}, {128, 128, 2, 1.4f, 0.9f, 3.0f, 0.8f}, {128, 256, 2, 2.6f, 1.0f, 5.2f, 1.5f}};
-constexpr Variant kMxVariants[] = {{128, 128, 2, 0.95f, 0.6f, 2.2f, 0.6f}, {256, 256, 1, 2.0f, 3.2f, 0.f, 0.f}};
+constexpr Variant kRowVariants[] = {{32, 128, 3, 0.8f, 0.45f, 1.3f, 0.7f}, {128, 128, 2, 1.4f, 0.9f, 3.0f, 0.8f}, {128, 256, 2, 2.8f, 0.9f, 5.2f, 1.5f}};
+constexpr Variant kMxVariants[] = {{128, 128, 1, 0.85f, 0.6f, 0.f, 0.f}, {256, 256, 1, 2.6f, 1.3f, 0.f, 0.f}};
 float unit_us(const Variant &v, int64_t groups) {
   const int64_t round = 256 * v.per_cu, rounds = (groups - 1) / round, left = groups - rounds * round;
   auto one = [&](int64_t n) { return n <= 256 ? v.base + v.first * (float)n / 256.f : v.second + v.more * (float)(n - 256) / 256.f; };
