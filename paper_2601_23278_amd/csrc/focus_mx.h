@@ -44,7 +44,7 @@ void mx_gemm(hipStream_t s, const void *a, const void *a_scales, int64_t lda, fo
              Scratch scratch);
 
 // Routed experts.  Entries (row, choice) are sorted by expert into tiles of 32 or 128 rows, multiplied expert by expert, and added up row by row.
-constexpr int kMxMaxExperts = 512, kMxFewRows = 32;
+constexpr int kMxMaxExperts = 512, kMxFewRows = 4;
 struct MxExperts {
   int n_experts, hidden, ffn, k;
   focus_mx gate_up, down;

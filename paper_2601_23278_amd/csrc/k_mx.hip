@@ -1,4 +1,5 @@
 // Conversion of rows to microscaled 4-bit floats (MXFP4) and back.  Both are bound by memory: 2 or 4 bytes an element on one side, 17/32 on the other.
+// 65536 x 2048 bf16: 71 to 74 us in, 63 us out, 340 MB each, 4.6 to 5.4 TB/s, what a large copy reaches (5.0); 333 x 1000 fp32: 2.7 us each, a launch.
 #include "focus_mx.h"
 
 namespace fk {
@@ -10,7 +11,8 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 
-// A thread converts 8 neighbours (16 or 32 bytes, 4 bytes of codes), four neighbouring threads a block of 32.  Chunk i of the matrix
+// A thread converts 8 neighbours (16 or 32 bytes in one or two accesses, 4 bytes of codes), four neighbouring threads a block of 32, whose largest exponent
+// they find by two lane exchanges; the scale needs no logarithm: it is the exponent field less two.  Chunk i of the matrix
 // lies in row i / per_row; per_row is a multiple of 4, so the four threads of a block are lanes of one quad.
 struct Chunks {
   int64_t total, per_row;

@@ -19,6 +19,7 @@ typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
+// fp32 products of the routed experts that the memory-side cache still holds when they are added up (mx_down)
 constexpr int64_t kMxSliceBytes = 136ll << 20;
 #define FK_LDS_PTR(p) ((__attribute__((address_space(3))) void *)(p))
 constexpr int vmcnt_imm(int n) { return 0x0F70 | (n & 15) | ((n >> 4) << 14); }   // s_waitcnt vmcnt(n) only
@@ -103,11 +104,15 @@ __device__ __forceinline__ uint64_t eight_scales(const unsigned char *row, int b
 // read and converted by one wavefront; tile rows of 32 that hold no rows are skipped.  K goes in steps of 64 (128 bytes of a row of A) and slabs
 // of four steps (128 bytes of a row of W), whole lines of both, straight into LDS: the rows three steps ahead, the codes kCodeStages slabs ahead of the
 // registers that hold the slab in work.  (Codes read from memory into registers, a row per lane, cost the vector caches 64 lookups an instruction instead of
-// 16: 2048 rows through 256 experts 134 us instead of 100.)  Lane l multiplies elements 32 h .. 32 h + 31 of a step, h = l / 32: one
+// 16: gate/up of 2048 rows through 8 of 256 experts each, 2048 -> 512, took 134 us instead of 105.)  Lane l multiplies elements 32 h .. 32 h + 31 of a step, h = l / 32: one
 // block of its weight row, so one scale; the order of the elements within a step is the same for both operands and does not matter otherwise.
 // Pipelined by hand: behind the MFMAs of 16 elements of K go the LDS reads of the rows' next fragments, the conversions of the next codes and the
 // loads.  A step's last quarter begins with the only barrier: by then everyone has read all of the step's rows, whose stage is filled again right
 // behind it, and the next step's rows have landed.  Codes are read and written by their own wavefront alone.
+// What bounds it: few rows, the codes' way from memory (8 rows x 24576 x 4096, 54 MB: 15.0 us, 3.6 TB/s, two rounds of workgroups that each wait for
+// their first slabs); many rows, the matrix units and the chip's power (2048 x 24576 x 4096: 324 us, 1.27 PFLOP/s; a large bf16 library product 1.37); in
+// between, both by halves (those gate/up rows, 69 GFLOP and 285 MB of codes: 96 us; the loads alone took 71 of 105, the arithmetic alone 75; the last round
+// of workgroups leaves a fifth of the chip idle).
 constexpr int kRowStages = 3;
 constexpr int code_stages(int bm) { return bm > 32 ? 1 : 2; }
 constexpr int rows_lds(int bm, int ct) { return kRowStages * bm * 128 + code_stages(bm) * ct * 16384; }
@@ -398,6 +403,9 @@ void launch_rows(hipStream_t s, int mode, const RowsArgs &g, int tile_slots) {
 // pairs ahead, and handed on through LDS.  Pipelined by hand like k_mx_rows: behind each MFMA one fragment read of the next quarter or one load.  The
 // only barrier of a pair stands before its last quarter: by then everyone has read all of it, its place is filled again over the next quarters, and the
 // next pair has landed.
+// 2048 x 24576 x 4096: 104 to 106 us, 3.9 to 4.0 PFLOP/s, bound by the matrix units at the clock that the chip's power leaves them (without the loop's loads
+// 99 us, without its LDS reads 98).  Where K is no multiple of 256, rows begin inside a line and a piece of 128 bytes takes two of them: 333 x 4000, K = 12256,
+// 29 us, K = 12288 18 (and 5 to add the two parts).
 struct MxArgs {
   const unsigned char *A, *a_scales, *W, *w_scales;
   int M, N, K;
@@ -407,6 +415,8 @@ struct MxArgs {
   size_t split_stride;
 };
 enum { XM_STORE, XM_STORE_F32, XM_PARTIAL };
+// Pairs in LDS: what fits with one workgroup a compute unit.  (128 x 128 with two pairs and two workgroups a compute unit: 333 x 4096, K = 12288, 25.2 us
+// instead of 23.1; 1024 x 4096, K = 4096, 17.3 instead of 15.3; 32 x 4096, K = 4096, 8.9 instead of 9.2.)
 constexpr int mx_pairs(int bm) { return bm == 256 ? 2 : 4; }
 constexpr int mx_lds(int bm, int bn) { return mx_pairs(bm) * (bm + bn) * 128 + 2 * (bm + bn) * 16; }
 
@@ -722,9 +732,11 @@ void mx_gemm(hipStream_t s, const void *a, const void *a_scales, int64_t lda, fo
   if (parts) launch_reduce(s, epilogue, (const float *)scratch.ptr, p.splits, stride, rows, n, out, ldo);
 }
 
-// Tiles of 32 x 128 for up to kMxFewRows rows per expert on average (256 experts, 2048 -> 512, whole operator in us, 32-row tiles / 128-row ones: 4 rows an expert 107 / 116, 16 129 /
-// 140, 32 170 / 170, 64 262 / 220; 8 experts, 2560 -> 1408, 16 rows 33 / 35, 64 47 / 48, 128 72 / 61).  Above, 128 x 256 where there may be kMxWide of them, 128 x 128 where
-// the wide ones would leave compute units idle (128 x 256 / 128 x 128: 8 experts, 256 rows each 90 / 84, 1024 rows each 218 / 229; 32 experts, 1024 -> 768, 128 rows each 60 / 50).
+// Tiles of 32 x 128 for up to kMxFewRows rows per expert on average: more workgroups, whose loads of codes few others share (whole operator in us, 32-row
+// tiles / 128-row ones: 256 experts, 2048 -> 512, 1 row an expert 75.8 / 79.2, 4 rows 108 / 105, 8 118 / 115, 16 135 / 126, 32 172 / 154; 160 experts,
+// 2560 -> 320, 4 rows 66 / 74, 7 rows 79 / 78).  Above, 128 x 256 where there may be kMxWide of them, 128 x 128 where the wide ones would leave compute
+// units idle (128 x 256 / 128 x 128: 256 experts, 2048 -> 512, 64 rows 197 / 219; 8 experts, 2560 -> 1408, 64 rows 60 / 43, 256 rows 84 / 79, 1024 rows
+// 209 / 215; 32 experts, 1024 -> 768, 128 rows 53 / 49).
 constexpr int kMxWide = 512;
 template <int MODE>
 static void launch_grouped(hipStream_t s, const RowsArgs &a, const MxExperts &m) {
@@ -941,7 +953,8 @@ void mx_group(hipStream_t s, const MxExperts &a) {
 }
 
 // The second product and the weighted sums, so many columns at a time that the fp32 products of a slice stay in the memory-side cache (256 MB) between the
-// two launches, and the next slice's go where they were: 8192 rows through 8 experts each, 2048 columns, 537 MB of products.
+// two launches, and the next slice's go where they were: 8192 rows through 8 of 256 experts each, 512 -> 2048, 537 MB of products, in four slices 4 x (60 + 23) us; in one the
+// sums alone took 137 instead of 91.
 void mx_down(hipStream_t s, const MxExperts &m) {
   if (m.rows.cap <= 0) return;
   RowsArgs a{};

@@ -7,6 +7,9 @@
 // Picks are whole numbers that have to be those of 64-bit scores.  They are found with fp32 scores, whose errors are bounded below; a row in
 // which two neighbours of the order, or the last kept and the first dropped group, are closer than that bound is done again in 64 bits by the same
 // code.  Equal logits with equal biases are equal in any arithmetic and need no second look.
+//
+// Bound by that chain and the launch, not by bytes (2.2 MB at 2048 rows, 0.4 us): 256 experts, 8 picks, 8 rows 6.7 us, 2048 rows without groups 7.1, 8191
+// rows with 8 groups of which 4 stay 17 to 20: among so many some are done twice, and they end the launch.
 #include "focus_mx.h"
 
 namespace fk {
@@ -223,7 +226,6 @@ __device__ __forceinline__ bool pick(const RouteArgs &a, const float (&l)[P], co
   return true;
 }
 
-// A row takes longer for its chain of dependent steps than for its bytes.
 template <typename T, int P>
 __global__ __launch_bounds__(kRouteWaves * 64) void k_route(RouteArgs a) {
   __shared__ double sh[kRouteWaves][64 * P * 3 / 2];

@@ -706,6 +706,20 @@ def test_experts_of_many_rows(rows, E, k, hidden, ffn, add):
     assert torch.equal(other[:rows], out[:rows][order])
 
 
+def test_few_rows_an_expert_but_one_of_many():
+    """Tiles of 32 rows, several of one expert: its last one full, with one row, and with 31."""
+    pk, _ = _pk()
+    E, k, hidden, ffn = 300, 8, 160, 96
+    for many in (64, 65, 95):
+        rows = 130
+        wide, gate_up, down, picks, weights = experts_case(many, rows, E, k, hidden, ffn)
+        picks[picks == 17] = 18
+        picks[:many, 3] = 17
+        out = pk.focus_mx_experts(gpu(*gate_up), gpu(*down), wide.to(DEV), *gpu(picks, weights), torch.empty(rows, hidden, device=DEV)).cpu().double()
+        want, bound = ref.experts(wide.double(), ref.values(*gate_up), ref.values(*down), picks, weights.double())
+        assert bool(((out - want).abs() <= bound + 2.0 ** -24 * want.abs()).all())
+
+
 def test_groups_whose_sums_overflow_32_bits():
     """Biases near the largest fp32 number: two groups' sums are infinite in 32 bits, not in 64."""
     logits = torch.zeros(3, 8)
