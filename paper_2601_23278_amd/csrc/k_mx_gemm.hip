@@ -469,7 +469,7 @@ __global__ __launch_bounds__(256, mx_lds(BM, BN) > 80 * 1024 ? 1 : 2) void k_mx_
 #pragma unroll
     for (int u = 0; u < SI; ++u) {
       if (WHOLE) {
-        fetched[u] = *(const u32x4 *)(srow[u] + min(b0, blocks - 16));
+        __builtin_memcpy(&fetched[u], srow[u] + min(b0, blocks - 16), 16);
       } else {
         const uint64_t lo = eight_scales(srow[u], b0, blocks), hi = eight_scales(srow[u], b0 + 8, blocks);
         fetched[u] = u32x4{(unsigned)lo, (unsigned)(lo >> 32), (unsigned)hi, (unsigned)(hi >> 32)};
