@@ -445,14 +445,14 @@ __global__ __launch_bounds__(256, mx_lds(BM, BN) > 80 * 1024 ? 1 : 2) void k_mx_
   __amdgpu_buffer_rsrc_t rs_a = __builtin_amdgcn_make_buffer_rsrc((void *)(g.A + (size_t)m0 * (K / 2)), 0, (unsigned)valid_m * (unsigned)(K / 2), 0x00020000);
   __amdgpu_buffer_rsrc_t rs_w = __builtin_amdgcn_make_buffer_rsrc((void *)(g.W + (size_t)n0 * (K / 2)), 0, (unsigned)valid_n * (unsigned)(K / 2), 0x00020000);
   // An instruction fills 8 rows; lane l fetches chunk (block) (l % 8) ^ ((row / 2) % 8) of row l / 8, so that LDS reads spread over the banks.
-  // Rows beyond the matrix lie outside the descriptors.
+  // Rows beyond the matrix lie outside the descriptors.  Behind a row's end come the next row's codes; their scales are taken as 0, 2^-127 on either side,
+  // and 32 products of at most 36 times 2^-254 are nothing in fp32.
   const int chunk = (lane & 7) ^ ((4 * (wave & 1) + (lane >> 4)) & 7);
   const unsigned vo = (unsigned)(wave * 8 + (lane >> 3)) * (unsigned)(K / 2) + chunk * 16, row_step = 32u * (unsigned)(K / 2);
   auto load = [&](int pair, int stage, int q) __attribute__((always_inline)) {          // q: 0 .. IA - 1 the rows, then the weights
     const unsigned so = 2 * pair < slabs ? (unsigned)(slab0 + 2 * pair) * 64u : kOutside;
-    const bool gone = !WHOLE && (slab0 + 2 * pair) * 4 + chunk >= blocks;
     const int r = q < IA ? q : q - IA;
-    const unsigned v = gone ? kOutside : vo + r * row_step;
+    const unsigned v = vo + r * row_step;
     if (q < IA) __builtin_amdgcn_raw_ptr_buffer_load_lds(rs_a, FK_LDS_PTR(lds + stage * ASTAGE + (r * 4 + wave) * 1024), 16, v, so, 0, 0);
     else __builtin_amdgcn_raw_ptr_buffer_load_lds(rs_w, FK_LDS_PTR(lds + WBASE + stage * WSTAGE + (r * 4 + wave) * 1024), 16, v, so, 0, 0);
   };
@@ -464,16 +464,19 @@ __global__ __launch_bounds__(256, mx_lds(BM, BN) > 80 * 1024 ? 1 : 2) void k_mx_
     srow[u] = r < BM ? g.a_scales + (size_t)(m0 + min(r, valid_m - 1)) * blocks : g.w_scales + (size_t)(n0 + min(r - BM, valid_n - 1)) * blocks;
   }
   u32x4 fetched[SI];
+  // quads of which the row has all 16 blocks; behind the last of them it is not the quad's own scales that are fetched, and they count for nothing
+  const int full = min(per_split, blocks / 16 - split * per_split);
   auto fetch_scales = [&](int quad) __attribute__((always_inline)) {
+    const int b0 = min(slab0 * 4 + quad * 16, blocks - 16);
+#pragma unroll
+    for (int u = 0; u < SI; ++u) __builtin_memcpy(&fetched[u], srow[u] + b0, 16);
+  };
+  auto fetch_some_scales = [&](int quad) __attribute__((always_inline)) {      // any quad; slower, and many registers
     const int b0 = slab0 * 4 + quad * 16;
 #pragma unroll
     for (int u = 0; u < SI; ++u) {
-      if (WHOLE) {
-        __builtin_memcpy(&fetched[u], srow[u] + min(b0, blocks - 16), 16);
-      } else {
-        const uint64_t lo = eight_scales(srow[u], b0, blocks), hi = eight_scales(srow[u], b0 + 8, blocks);
-        fetched[u] = u32x4{(unsigned)lo, (unsigned)(lo >> 32), (unsigned)hi, (unsigned)(hi >> 32)};
-      }
+      const uint64_t lo = eight_scales(srow[u], b0, blocks), hi = eight_scales(srow[u], b0 + 8, blocks);
+      fetched[u] = u32x4{(unsigned)lo, (unsigned)(lo >> 32), (unsigned)hi, (unsigned)(hi >> 32)};
     }
   };
   auto hand_on_scales = [&](int quad) __attribute__((always_inline)) {
@@ -518,7 +521,8 @@ __global__ __launch_bounds__(256, mx_lds(BM, BN) > 80 * 1024 ? 1 : 2) void k_mx_
   };
   auto in_order = []() __attribute__((always_inline)) { loads_asked_for(); __builtin_amdgcn_sched_barrier(0); };
   if (slabs > 0) {
-    fetch_scales(0);
+    if (WHOLE) fetch_scales(0);
+    else fetch_some_scales(0);
     in_order();
 #pragma unroll
     for (int p = 0; p < R; ++p) {
@@ -532,8 +536,9 @@ __global__ __launch_bounds__(256, mx_lds(BM, BN) > 80 * 1024 ? 1 : 2) void k_mx_
     read_scales(0, 0, 0);
 #pragma unroll
     for (int s = 0; s < NF; ++s) read(s, 0, 0);
-    // OF: slab of its quad of slabs, whose pairs lie at `stage` and behind it
-    auto slab_of = [&](auto which, int quad) __attribute__((always_inline)) {
+    // OF: slab of its quad of slabs, whose pairs lie at `stage` and behind it; MORE: scales of another quad are to be fetched
+    auto slab_of = [&](auto which, int quad, auto more) __attribute__((always_inline)) {
+      constexpr bool MORE = decltype(more)::value;
       constexpr int OF = decltype(which)::value, SLOT = OF & 1, NEXT = (OF + 1) & 3;
       const int pair = 2 * quad + OF / 2, stage = R == 2 ? OF / 2 : (2 * quad & (R - 1)) + OF / 2, after = OF < 2 ? stage + 1 : R == 2 ? 0 : (stage + 1) & (R - 1);
       shift_scales(SLOT);
@@ -542,11 +547,11 @@ __global__ __launch_bounds__(256, mx_lds(BM, BN) > 80 * 1024 ? 1 : 2) void k_mx_
         constexpr int FIRST = 2 * (OF & 1);
         const int q = FIRST + ks;              // of the pair
         if (q == 3) {
-          if (OF == 3) hand_on_scales(quad + 1);
+          if (MORE && OF == 3) hand_on_scales(quad + 1);
           // the next pair has landed: younger are those of the pairs behind it (and scales, which are not counted)
           __builtin_amdgcn_s_waitcnt(vmcnt_imm((R - 2) * L));
           asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-          if (OF == 1) { fetch_scales(quad + 1); in_order(); }
+          if (MORE && OF == 1) { fetch_scales(quad + 1); in_order(); }
         }
         if (ks == 1) read_scales(OF == 3 ? quad + 1 : quad, NEXT, SLOT ^ 1);
 #pragma unroll
@@ -570,17 +575,26 @@ __global__ __launch_bounds__(256, mx_lds(BM, BN) > 80 * 1024 ? 1 : 2) void k_mx_
     constexpr std::integral_constant<int, 1> s1;
     constexpr std::integral_constant<int, 2> s2;
     constexpr std::integral_constant<int, 3> s3;
+    constexpr std::integral_constant<bool, true> yes;
+    constexpr std::integral_constant<bool, false> no;
     int quad = 0;
-    for (; 4 * quad + 4 <= slabs; ++quad) {
-      slab_of(s0, quad);
-      slab_of(s1, quad);
-      slab_of(s2, quad);
-      slab_of(s3, quad);
+    for (; quad < full; ++quad) {
+      slab_of(s0, quad, yes);
+      slab_of(s1, quad, yes);
+      slab_of(s2, quad, yes);
+      slab_of(s3, quad, yes);
     }
     if (!WHOLE && 4 * quad < slabs) {
-      slab_of(s0, quad);
-      if (4 * quad + 1 < slabs) slab_of(s1, quad);
-      if (4 * quad + 2 < slabs) slab_of(s2, quad);
+      if (quad > 0) {
+        fetch_some_scales(quad);
+        hand_on_scales(quad);
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        read_scales(quad, 0, 0);
+      }
+      slab_of(s0, quad, no);
+      if (4 * quad + 1 < slabs) slab_of(s1, quad, no);
+      if (4 * quad + 2 < slabs) slab_of(s2, quad, no);
+      if (4 * quad + 3 < slabs) slab_of(s3, quad, no);
     }
   }
   __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
