@@ -403,9 +403,9 @@ void launch_rows(hipStream_t s, int mode, const RowsArgs &g, int tile_slots) {
 // pairs ahead, and handed on through LDS.  Pipelined by hand like k_mx_rows: behind each MFMA one fragment read of the next quarter or one load.  The
 // only barrier of a pair stands before its last quarter: by then everyone has read all of it, its place is filled again over the next quarters, and the
 // next pair has landed.
-// 2048 x 24576 x 4096: 104 to 106 us, 3.9 to 4.0 PFLOP/s, bound by the matrix units at the clock that the chip's power leaves them (without the loop's loads
+// 2048 x 24576 x 4096: 104 to 110 us by card, 3.8 to 4.0 PFLOP/s, bound by the matrix units at the clock that the chip's power leaves them (without the loop's loads
 // 99 us, without its LDS reads 98).  Where K is no multiple of 256, rows begin inside a line and a piece of 128 bytes takes two of them: 333 x 4000, K = 12256,
-// 29 us, K = 12288 18 (and 5 to add the two parts).
+// 24.5 us, K = 12288 18 (and 5 to add the two parts).
 struct MxArgs {
   const unsigned char *A, *a_scales, *W, *w_scales;
   int M, N, K;
