@@ -398,11 +398,12 @@ void launch_rows(hipStream_t s, int mode, const RowsArgs &g, int tile_slots) {
 
 // ---------------------------------------------------------------------------------------------
 // MXFP4 rows x MXFP4 weights: 2 x 2 wavefronts.  K goes in pairs of slabs of 128: whole lines of 128 bytes of codes a row, straight into LDS, through
-// a ring of mx_pairs() pairs (from the caches, lines of 128 bytes come at 34 TB/s over all compute units, pieces of 64 at 17).  Lane l supplies row l % 32 and, of the four quarters of 64 elements of a pair, block 2 q + l / 32: 16 bytes of codes and one
-// scale.  Scales are fetched 16 bytes a row, for two pairs at once (a row per lane costs the vector caches a lookup per lane whatever its size), two
-// pairs ahead, and handed on through LDS.  Pipelined by hand like k_mx_rows: behind each MFMA one fragment read of the next quarter or one load.  The
-// only barrier of a pair stands before its last quarter: by then everyone has read all of it, its place is filled again over the next quarters, and the
-// next pair has landed.
+// a ring of mx_pairs() pairs (from the caches, lines of 128 bytes come at 34 TB/s over all compute units, pieces of 64 at 17).  Lane l supplies row
+// l % 32 and, of the four quarters of 64 elements of a pair, block 2 q + l / 32: 16 bytes of codes and one scale.  Scales are fetched 16 bytes a row, for
+// two pairs at once (a row per lane costs the vector caches a lookup per lane whatever its size), two pairs ahead, and handed on through LDS; those of a
+// row's last blocks, where they are not 16, behind the loop.  Pipelined by hand like k_mx_rows: behind each MFMA one fragment read of the next quarter or
+// one load.  The only barrier of a pair stands before its last quarter: by then everyone has read all of it, its place is filled again over the next
+// quarters, and the next pair has landed.
 // 2048 x 24576 x 4096: 104 to 110 us by card, 3.8 to 4.0 PFLOP/s, bound by the matrix units at the clock that the chip's power leaves them (without the loop's loads
 // 99 us, without its LDS reads 98).  Where K is no multiple of 256, rows begin inside a line and a piece of 128 bytes takes two of them: 333 x 4000, K = 12256,
 // 24.5 us, K = 12288 18 (and 5 to add the two parts).

@@ -582,6 +582,30 @@ def test_gemm_tiles(a_type, m, n, k):
         assert bool(((got - x @ y.t()).abs() <= product_bound(x, y, torch.float32)).all())
 
 
+@pytest.mark.parametrize("a_type", ["bf16", "mx4"])
+@pytest.mark.parametrize("base", [0, 512, 1536])
+def test_gemm_every_remainder_of_k(a_type, base):
+    """K ends after any number of blocks of a slab, a pair of them or a quad; what lies behind a row's end, with the largest scales and scale 255, counts for nothing."""
+    pk, _ = _pk()
+    for blocks in range(1, 17):
+        m, n, k = 70, 140, base + 32 * blocks
+        gen = torch.Generator().manual_seed(k)
+        w, am = ref.random_mx(gen, n, k), ref.random_mx(gen, m, k)
+        w[1][3, 0], am[1][7, 0], w[1][20, 0], am[1][33, 0] = 254 - 60, 254 - 60, 255, 255
+        if a_type == "bf16":
+            a = torch.randn(m, k, generator=gen).to(torch.bfloat16)
+            av, a = a.double(), a.to(DEV)
+        else:
+            av, a = ref.values(*am), gpu(*am)
+        c = pk.focus_mx_gemm(a, gpu(*w), torch.empty(m, n, device=DEV)).cpu().double()
+        wv = ref.values(*w)
+        bad = torch.isnan(av).any(1).view(-1, 1) | torch.isnan(wv).any(1).view(1, -1)
+        av, wv = torch.nan_to_num(av, nan=0.0), torch.nan_to_num(wv, nan=0.0)
+        want = av @ wv.t()
+        ok = ~bad & (want.abs() < 1e38)
+        assert bool(torch.isnan(c[bad]).all()) and bool(((c - want).abs()[ok] <= product_bound(av, wv, torch.float32)[ok]).all()), k
+
+
 @pytest.mark.parametrize("parts", [1, 2, 3, 5])
 @pytest.mark.parametrize("a_type", ["bf16", "mx4"])
 def test_gemm_with_less_workspace_than_it_asks_for(a_type, parts):
