@@ -125,7 +125,8 @@ __device__ __forceinline__ bool pick(const RouteArgs &a, const float (&l)[P], co
       t2 = low > high ? low : high;
       t1 = o1 > t1 ? o1 : t1;
     }
-    R value = r.group_top == 2 && S > 1 ? t1 + t2 : t1;
+    const R second = r.group_top == 2 && S > 1 ? t2 : (R)0;
+    R value = t1 + second;
     if (value != value) value = kLow<R>;
     int rank = 0;
     for (int o = 0; o < G; ++o) {
@@ -134,12 +135,16 @@ __device__ __forceinline__ bool pick(const RouteArgs &a, const float (&l)[P], co
     }
     const bool lead = sub == 0 && g < G;
     if (F32 && r.groups_kept < G) {
-      const R in = lane_of(value, __ffsll((unsigned long long)__ballot(lead && rank == r.groups_kept - 1)) - 1);
-      const R out = lane_of(value, __ffsll((unsigned long long)__ballot(lead && rank == r.groups_kept)) - 1);
+      // A choice is off by at most 1.4e-6 of the row's largest score (exp, sum, division) and half an ulp of itself, and a sum by half an ulp of itself:
+      // ulps of the choices, which may be large and cancel.  So every group has its own bound, and every kept one has to stay above every dropped one
+      // within them.  An infinite choice (no number, or an infinite bias) is infinite in any arithmetic; a sum of two finite ones that overflowed says nothing.
       top_score = largest(top_score);
-      // each choice is off by at most 2e-6 of the row's largest score (exp, sum, division) and half an ulp of itself
-      // (neither holds where a sum of two large biases overflowed)
-      if (!(in - out > (R)8e-6 * top_score + (R)1e-6 * (fabs(in) + fabs(out)))) return false;
+      const bool infinite = fabs(t1) == (R)INFINITY || fabs(second) == (R)INFINITY;
+      const R off = infinite ? (R)0 : (R)3e-6 * top_score + (R)2.5e-7 * (fabs(t1) + fabs(second));
+      const bool known = infinite || (off < (R)INFINITY && fabs(value) < (R)INFINITY);
+      const R least = -largest(lead && rank < r.groups_kept ? (known ? off - value : (R)INFINITY) : kLow<R>);
+      const R most = largest(lead && rank >= r.groups_kept ? (known ? value + off : (R)INFINITY) : kLow<R>);
+      if (!(least > most)) return false;
     }
     const uint64_t kept = __ballot(lead && rank < r.groups_kept);
     const unsigned by_s = ((1u << 20) + S - 1) / S;                 // e / S = e * by_s >> 20 for e < 512
