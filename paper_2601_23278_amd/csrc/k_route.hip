@@ -207,10 +207,10 @@ __device__ __forceinline__ bool pick(const RouteArgs &a, const float (&l)[P], co
   if (!F32) return true;
   // Neighbours of the order that fp32 does not tell apart: closer than their errors, and not equal in logit and bias (those are equal, whatever the
   // arithmetic, and ordered by their index).  Scores are off by at most 6e-7 of themselves (sigmoid), 1.2e-6 and 1.2e-7 per unit of distance from the
-  // largest logit (softmax).
+  // largest logit (softmax; the distance may be infinite, and its score 0 then), and by what those below the smallest normal number lose.
   auto too_close = [&](R above, R s_above, float l_above, R below, R s_below, float l_below) {
-    const float rel = r.score == FOCUS_SCORE_SIGMOID ? 6e-7f : 1.2e-6f + 1.2e-7f * (top_logit - fminf(l_above, l_below));
-    return above - below <= rel * (s_above + s_below) + 2e-7f * (fabsf((float)above) + fabsf((float)below));
+    const float rel = r.score == FOCUS_SCORE_SIGMOID ? 6e-7f : 1.2e-6f + 1.2e-7f * fminf(top_logit - fminf(l_above, l_below), 1e30f);
+    return above - below <= rel * (s_above + s_below) + 2e-7f * (fabsf((float)above) + fabsf((float)below)) + 1e-37f;
   };
   const float ml = lane < found ? sh_l[idx] : 0.f, mb = lane < found ? sh_b[idx] : 0.f;
   const R below = __shfl_down(choice, 1), s_below = __shfl_down(score, 1);

@@ -21,3 +21,30 @@ def test_groups_whose_biases_cancel(kind, a, spread):
     half[1::2] = 0.0
     for bias in (both, half.view(-1)):
         check_route(l, bias, kind, G, 8, 2, 8, 1, 1.0)
+
+
+def test_scores_that_32_bits_do_not_hold():
+    """An expert whose score is too small for 32 bits still comes before those with none at all; scores near the smallest numbers keep their order."""
+    inf = float("inf")
+    l = torch.full((8, 16), -inf)
+    l[0, [1, 3, 4]] = torch.tensor([0.0, -1.0, -150.0])
+    l[1, [15, 7, 14]] = torch.tensor([-400.0, 5.0, -300.0])
+    l[2, [2, 9]] = torch.tensor([3e38, 2e38])
+    l[3, 5:] = -110.0 - torch.arange(11) * 0.25
+    l[3, 8] = 0.0
+    l[4] = torch.tensor([0.0, -150.0]).repeat(8)
+    l[5, 12] = 88.0
+    l[5, [10, 11]] = torch.tensor([-61.9, -62.0])
+    l[6, [0, 2, 3]] = torch.tensor([-150.0, -140.0, 0.0])
+    l[7, [9, 11, 15]] = torch.tensor([-500.0, -499.0, 1.0])
+    for kind in ("softmax", "sigmoid"):
+        for renorm in (0, 1):
+            for k in (2, 3, 5, 16):
+                check_route(l, None, kind, 1, 1, 1, k, renorm, 1.0)
+                check_route(l, torch.zeros(16), kind, 4, 2, 2, min(k, 8), renorm, 1.0)
+    gen = torch.Generator().manual_seed(5)
+    l = -87.0 - 17.0 * torch.rand(60, 64, generator=gen)
+    l[:, 1::2] = l[:, ::2] + torch.randint(-2, 3, (60, 32), generator=gen) * 2.0 ** -17      # neighbours in fp32
+    l[:, 63] = 0.0
+    for kind in ("softmax", "sigmoid"):
+        check_route(l, None, kind, 1, 1, 1, 32, 0, 1.0)
