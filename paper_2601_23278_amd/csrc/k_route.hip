@@ -68,7 +68,7 @@ __device__ __forceinline__ bool pick(const RouteArgs &a, const float (&l)[P], co
   constexpr bool F32 = sizeof(R) == 4;
   const focus_router &r = a.router;
   const int lane = threadIdx.x & 63, E = r.n_experts, k = r.experts_per_token, G = r.n_groups, first = lane * P;
-  R s[P], c[P];
+  R s[P], c[P], top_score = 1;       // no score is larger
   float top_logit = -INFINITY;
   if (r.score == FOCUS_SCORE_SIGMOID) {
 #pragma unroll
@@ -87,6 +87,7 @@ __device__ __forceinline__ bool pick(const RouteArgs &a, const float (&l)[P], co
     sum = total(sum);
 #pragma unroll
     for (int i = 0; i < P; ++i) s[i] = sum > 0 ? s[i] / sum : (R)0;
+    top_score = sum > 0 ? (R)1 / sum : (R)0;
   }
   if (forced) {
 #pragma unroll
@@ -99,12 +100,11 @@ __device__ __forceinline__ bool pick(const RouteArgs &a, const float (&l)[P], co
     return true;
   }
   unsigned alive = 0;
-  R top_score = 0;
 #pragma unroll
   for (int i = 0; i < P; ++i) {
     c[i] = s[i] + (R)bias[i];
     if (l[i] != l[i] || c[i] != c[i]) c[i] = kLow<R>;
-    if (first + i < E) { alive |= 1u << i; top_score = s[i] > top_score ? s[i] : top_score; }
+    if (first + i < E) alive |= 1u << i;
   }
   if (G > 1) {
     // a group per 64 / ceil2(G) lanes: each lane looks at every such-and-such element, then the lanes' two best are merged
@@ -138,7 +138,6 @@ __device__ __forceinline__ bool pick(const RouteArgs &a, const float (&l)[P], co
       // A choice is off by at most 1.4e-6 of the row's largest score (exp, sum, division) and half an ulp of itself, and a sum by half an ulp of itself:
       // ulps of the choices, which may be large and cancel.  So every group has its own bound, and every kept one has to stay above every dropped one
       // within them.  An infinite choice (no number, or an infinite bias) is infinite in any arithmetic; a sum of two finite ones that overflowed says nothing.
-      top_score = largest(top_score);
       const bool infinite = fabs(t1) == (R)INFINITY || fabs(second) == (R)INFINITY;
       const R off = infinite ? (R)0 : (R)3e-6 * top_score + (R)2.5e-7 * (fabs(t1) + fabs(second));
       const bool known = infinite || (off < (R)INFINITY && fabs(value) < (R)INFINITY);
@@ -154,6 +153,13 @@ __device__ __forceinline__ bool pick(const RouteArgs &a, const float (&l)[P], co
       if (first + i < E && !((kept >> (group * step)) & 1)) alive &= ~(1u << i);
     }
   }
+  // What fp32 may be off by in a choice c of score s and logit l.  Sigmoid: 6e-7 of the score; softmax: 1.2e-6, and 1.2e-7 per unit of distance from
+  // the largest logit (which may be infinite, the score 0 then); what scores below the smallest normal number lose; the choice's own rounding.
+  auto off = [&](R c, R s, float l) {
+    const float rel = r.score == FOCUS_SCORE_SIGMOID ? 6e-7f : 1.2e-6f + 1.2e-7f * fminf(top_logit - l, 1e30f);
+    return rel * s + 2e-7f * fabsf((float)c) + 1e-37f;
+  };
+  const float score_off = r.score == FOCUS_SCORE_SIGMOID ? 6e-7f : 1.3e-6f * (float)top_score;      // of any score: d exp(-d) is at most 0.37
   // each lane's elements by falling choice, ties by the lower element; those that cannot be chosen come last
   constexpr int kNone = 0x7FFFFFFF;
   int order[P];
@@ -196,39 +202,35 @@ __device__ __forceinline__ bool pick(const RouteArgs &a, const float (&l)[P], co
     }
     return e;
   };
-  for (int j = 0; j < (F32 ? k + 1 : k); ++j) {
+  for (int j = 0; j < k; ++j) {
     R best;
     const int e = next_best(best);
-    if (e < 0) break;                                               // as many as there are (j = k)
+    if (e < 0) break;
     if (lane == j) { idx = e; choice = best; }
     found = j + 1;
   }
   if (lane < found) score = sh[idx];
   if (!F32) return true;
-  // Neighbours of the order that fp32 does not tell apart: closer than their errors, and not equal in logit and bias (those are equal, whatever the
-  // arithmetic, and ordered by their index).  Scores are off by at most 6e-7 of themselves (sigmoid), 1.2e-6 and 1.2e-7 per unit of distance from the
-  // largest logit (softmax; the distance may be infinite, and its score 0 then), and by what those below the smallest normal number lose.
-  auto too_close = [&](R above, R s_above, float l_above, R below, R s_below, float l_below) {
-    const float rel = r.score == FOCUS_SCORE_SIGMOID ? 6e-7f : 1.2e-6f + 1.2e-7f * fminf(top_logit - fminf(l_above, l_below), 1e30f);
-    return above - below <= rel * (s_above + s_below) + 2e-7f * (fabsf((float)above) + fabsf((float)below)) + 1e-37f;
-  };
+  // Each pick has to stay above the next, and the last above everything that was not picked, within their errors.  Experts of equal logit and bias
+  // are equal, whatever the arithmetic, and ordered by their index.
   const float ml = lane < found ? sh_l[idx] : 0.f, mb = lane < found ? sh_b[idx] : 0.f;
-  const R below = __shfl_down(choice, 1), s_below = __shfl_down(score, 1);
+  const R mine = off(choice, score, ml);
+  const R below = __shfl_down(choice, 1), off_below = __shfl_down(mine, 1);
   const float l_below = __shfl_down(ml, 1), b_below = __shfl_down(mb, 1);
-  const bool same = ml == l_below && mb == b_below;
-  if (__ballot(lane + 1 < found && !same && too_close(choice, score, ml, below, s_below, l_below))) return false;
-  // equals of the last pick may go on behind it, and what follows them has to be far enough too
-  bool equal = found > k && (__ballot(same) >> (k - 1) & 1);
-  const R end_c = lane_of(choice, k - 1), end_s = lane_of(score, k - 1);
+  if (__ballot(lane + 1 < found && !(ml == l_below && mb == b_below) && choice - below <= mine + off_below)) return false;
+  const R end = lane_of(choice, k - 1), least = end - lane_of(mine, k - 1), next = largest(c[0]);
+  // c + 2e-7 |c| grows with c, so that the largest of the rest stands for all of them where no score's error reaches across
+  if (next == kLow<R> || next + 2e-7f * fabsf((float)next) + score_off + 1e-37f < least) return true;
+  const int end_e = __builtin_amdgcn_readlane(idx, k - 1);
   const float end_l = lane_of(ml, k - 1), end_b = lane_of(mb, k - 1);
-  while (equal) {
-    R best;
-    const int e = next_best(best);
-    if (e < 0) break;
-    equal = sh_l[e] == end_l && sh_b[e] == end_b;
-    if (!equal && too_close(end_c, end_s, end_l, best, sh[e], sh_l[e])) return false;
+  bool beyond = false;
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    const R si = sh[first + i], ci = si + (R)bias[i];                // not a number: nothing below holds
+    const bool pick = ci > end || (ci == end && first + i <= end_e);
+    if (((alive >> i) & 1) && l[i] == l[i] && ci > kLow<R> && !pick && !(l[i] == end_l && bias[i] == end_b)) beyond |= !(ci + off(ci, si, l[i]) < least);
   }
-  return true;
+  return __ballot(beyond) == 0;
 }
 
 template <typename T, int P>

@@ -48,3 +48,24 @@ def test_scores_that_32_bits_do_not_hold():
     l[:, 63] = 0.0
     for kind in ("softmax", "sigmoid"):
         check_route(l, None, kind, 1, 1, 1, 32, 0, 1.0)
+
+
+@pytest.mark.parametrize("kind", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("E,k", [(64, 28), (200, 20), (512, 32)])
+def test_a_score_that_its_bias_cancels_against_small_scores(kind, E, k):
+    """One expert's score of 0.9 is known to some 1e-7 in 32 bits, and so is its choice, 1e-6 by its bias; the small scores around it lie 2e-8 apart and are
+    known far better.  Whether it is among the picks, and where, is not a matter of its neighbours' distances alone."""
+    gen = torch.Generator().manual_seed(E)
+    rows = 160
+    w = torch.empty(rows, E, dtype=torch.float64)
+    w[:, 1:9] = 0.0125 * (1 + 0.01 * torch.arange(8, dtype=torch.float64))
+    small = 1e-6 + 2e-8 * torch.arange(E - 9, dtype=torch.float64) * (1 + 0.1 * torch.rand(rows, E - 9, generator=gen, dtype=torch.float64))
+    w[:, 9:] = small[:, torch.randperm(E - 9, generator=gen)]
+    last = float(small.sort(dim=1, descending=True).values[:, k - 9].mean())       # about the last of the k
+    w[:, 0] = 0.9 + 3e-7 * torch.randn(rows, generator=gen, dtype=torch.float64)
+    bias = torch.zeros(E)
+    bias[0] = last - 0.9
+    logits = torch.log(w) if kind == "softmax" else torch.log(w / (1 - w))
+    if kind == "softmax":
+        bias[0] = last - float((w[:, 0] / w.sum(1)).mean())
+    check_route(logits.float(), bias, kind, 1, 1, 1, k, 1, 1.0)
