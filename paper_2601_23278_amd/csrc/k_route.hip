@@ -5,8 +5,18 @@
 // a lane make ties easy: the lowest expert among equals is the lowest lane's lowest element.
 //
 // Picks are whole numbers that have to be those of 64-bit scores.  They are found with fp32 scores, whose errors are bounded below; a row in
-// which two neighbours of the order, or the last kept and the first dropped group, are closer than that bound is done again in 64 bits by the same
-// code.  Equal logits with equal biases are equal in any arithmetic and need no second look.
+// which two neighbours of the picks, the last pick and anything behind it, or a kept and a dropped group are closer than that bound is done again in 64
+// bits by the same code.  Equal logits with equal biases are equal in any arithmetic and need no second look.
+//
+// The bounds, in u = 2^-24, half an ulp (expf is off by 2 u at most, additions and divisions are rounded to nearest):
+//   sigmoid   exp 2 u, 1 + exp u, quotient u: 4 u = 2.4e-7 of the score; taken as 6e-7.
+//   softmax   of a logit d below the largest: d itself is rounded, d u; exp 2 u; quotient u; the sum of up to 512 terms: 7 additions in a lane and 6 across the
+//             lanes, 13 u, its terms' exp 2 u and their distances, at most 4 u (the mean of d under the softmax of 512 numbers is below 4).
+//             (22 + d) u = 1.31e-6 + 6e-8 d of the score; taken as 1.5e-6 + 1.2e-7 d.  As d exp(-d) is at most 0.37, no more than 1.35e-6 of the largest score.
+//   choice    u of itself for score + bias, and as much for each comparison's own arithmetic; taken as 2e-7.
+//   all       scores below the smallest normal number, 1.2e-38, have absolute errors of a few 2^-149, and an exp that overflows loses a score of 3e-39;
+//             taken as 1e-37.
+// They are bounds of each choice, so two whose bounds do not meet are in the order of the exact ones, and a chain of such pairs is.
 //
 // Bound by that chain and the launch, not by bytes (2.2 MB at 2048 rows, 0.4 us): 256 experts, 8 picks, 8 rows 6.7 us, 2048 rows without groups 7.1, 8191
 // rows with 8 groups of which 4 stay 17 to 20: among so many some are done twice, and they end the launch.
@@ -153,13 +163,12 @@ __device__ __forceinline__ bool pick(const RouteArgs &a, const float (&l)[P], co
       if (first + i < E && !((kept >> (group * step)) & 1)) alive &= ~(1u << i);
     }
   }
-  // What fp32 may be off by in a choice c of score s and logit l.  Sigmoid: 6e-7 of the score; softmax: 1.2e-6, and 1.2e-7 per unit of distance from
-  // the largest logit (which may be infinite, the score 0 then); what scores below the smallest normal number lose; the choice's own rounding.
+  // What fp32 may be off by in a choice c of score s and logit l (see the top); the distance from the largest logit may be infinite, the score 0 then
   auto off = [&](R c, R s, float l) {
-    const float rel = r.score == FOCUS_SCORE_SIGMOID ? 6e-7f : 1.2e-6f + 1.2e-7f * fminf(top_logit - l, 1e30f);
+    const float rel = r.score == FOCUS_SCORE_SIGMOID ? 6e-7f : 1.5e-6f + 1.2e-7f * fminf(top_logit - l, 1e30f);
     return rel * s + 2e-7f * fabsf((float)c) + 1e-37f;
   };
-  const float score_off = r.score == FOCUS_SCORE_SIGMOID ? 6e-7f : 1.3e-6f * (float)top_score;      // of any score: d exp(-d) is at most 0.37
+  const float score_off = r.score == FOCUS_SCORE_SIGMOID ? 6e-7f : 1.6e-6f * (float)top_score;      // of any score: 1.5e-6 + 0.37 * 1.2e-7
   // each lane's elements by falling choice, ties by the lower element; those that cannot be chosen come last
   constexpr int kNone = 0x7FFFFFFF;
   int order[P];
