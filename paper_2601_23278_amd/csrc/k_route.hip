@@ -12,7 +12,7 @@
 //   sigmoid   exp 2 u, 1 + exp u, quotient u: 4 u = 2.4e-7 of the score; taken as 6e-7.
 //   softmax   of a logit d below the largest: d itself is rounded, d u; exp 2 u; quotient u; the sum of up to 512 terms: 7 additions in a lane and 6 across the
 //             lanes, 13 u, its terms' exp 2 u and their distances, at most 4 u (the mean of d under the softmax of 512 numbers is below 4).
-//             (22 + d) u = 1.31e-6 + 6e-8 d of the score; taken as 1.5e-6 + 1.2e-7 d.  As d exp(-d) is at most 0.37, no more than 1.35e-6 of the largest score.
+//             (22 + d) u = 1.31e-6 + 6e-8 d of the score; taken as 1.4e-6 + 7e-8 d.  As d exp(-d) is at most 0.37, no more than 1.35e-6 of the largest score.
 //   choice    u of itself for score + bias, and as much for each comparison's own arithmetic; taken as 2e-7.
 //   all       scores below the smallest normal number, 1.2e-38, have absolute errors of a few 2^-149, and an exp that overflows loses a score of 3e-39;
 //             taken as 1e-37.
@@ -165,10 +165,10 @@ __device__ __forceinline__ bool pick(const RouteArgs &a, const float (&l)[P], co
   }
   // What fp32 may be off by in a choice c of score s and logit l (see the top); the distance from the largest logit may be infinite, the score 0 then
   auto off = [&](R c, R s, float l) {
-    const float rel = r.score == FOCUS_SCORE_SIGMOID ? 6e-7f : 1.5e-6f + 1.2e-7f * fminf(top_logit - l, 1e30f);
+    const float rel = r.score == FOCUS_SCORE_SIGMOID ? 6e-7f : 1.4e-6f + 7e-8f * fminf(top_logit - l, 1e30f);
     return rel * s + 2e-7f * fabsf((float)c) + 1e-37f;
   };
-  const float score_off = r.score == FOCUS_SCORE_SIGMOID ? 6e-7f : 1.6e-6f * (float)top_score;      // of any score: 1.5e-6 + 0.37 * 1.2e-7
+  const float score_off = r.score == FOCUS_SCORE_SIGMOID ? 6e-7f : 1.45e-6f * (float)top_score;      // of any score: 1.4e-6 + 0.37 * 7e-8
   // each lane's elements by falling choice, ties by the lower element; those that cannot be chosen come last
   constexpr int kNone = 0x7FFFFFFF;
   int order[P];
