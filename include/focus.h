@@ -342,7 +342,7 @@ typedef struct focus_router {
 
 /* The experts and weights of n_rows rows.
  *   dtype    FOCUS_F32 or FOCUS_BF16, of the logits; scores and weights are fp32
- *   logits   device [n_rows, ld], E of each row used; ld >= E;  n_rows below 2^26
+ *   logits   device [n_rows, ld], E of each row used; ld >= E;  n_rows at most 2^26 - 4
  *   bias     device [E] fp32, or NULL
  *   experts  device [n_rows, k] int32; weights device [n_rows, k] fp32 */
 int focus_route(const focus_router *router, void *hip_stream, int32_t n_rows, int32_t dtype, const void *logits, int64_t ld,
@@ -361,7 +361,7 @@ typedef struct focus_mx {
 /* Rows to MXFP4.  The scale of a block is 2^(floor(log2(max |x|)) - 2), within 2^-127 and 2^127 (2^-127 for zeros); x / scale is rounded to
  * the nearest code, half way to the even mantissa, magnitudes over 6 to 6.  A block with an infinity or a NaN gets scale 255 and zero codes.  Elements
  * beyond cols in a row's last block are coded as zeros.
- *   dtype    FOCUS_F32 or FOCUS_BF16;  x device [rows, ldx], ldx >= cols;  rows * ceil(cols / 32) below 2^30 */
+ *   dtype    FOCUS_F32 or FOCUS_BF16;  x device [rows, ldx], ldx >= cols;  rows * ceil(cols / 32) at most 2^30 - 64 */
 int focus_mx_quantize(void *hip_stream, int32_t dtype, int64_t rows, int32_t cols, const void *x, int64_t ldx, void *codes, void *scales);
 
 /* The values of codes and scales, exact in both dtypes (magnitudes beyond the largest finite number become infinite).  Writes cols elements of each
@@ -370,8 +370,8 @@ int focus_mx_dequantize(void *hip_stream, int32_t dtype, int64_t rows, int32_t c
 
 /* C[m, n] = sum_k A[m, k] W[n, k], summed in fp32 and rounded once.
  *   k            a multiple of 32 (the quantiser fills a row's last block with zeros), at most 2^22; 0: C = 0.  n * k below 2^32, and C at most
- *                2^24 tiles of 128 x 128
- *   a_type       FOCUS_BF16: A device [m, lda] bf16, 16-byte aligned, lda a multiple of 8; a_scales NULL.
+ *                2^24 - 8 tiles of 128 x 128
+ *   a_type       FOCUS_BF16: A device [m, lda] bf16, 16-byte aligned, lda a multiple of 8 and at most 2^22; a_scales NULL.
  *                FOCUS_MX4: A the codes [m, k / 2] (lda ignored), a_scales [m, k / 32]
  *   w            MXFP4 [n, k]
  *   c_type       FOCUS_F32 or FOCUS_BF16; C device [m, ldc]
