@@ -200,12 +200,21 @@ def _rows_of(t: torch.Tensor, name: str):
     if t.dim() != 2:
         _bad("%s must be a matrix", name)
     (rows, cols), (ld, step) = t.shape, t.stride()
+    if rows >= 2 ** 31 or cols >= 2 ** 31:
+        _bad("%s is too large", name)
     if (cols > 1 and step != 1) or (rows > 1 and ld < cols):
         _bad("%s must be a matrix with contiguous rows that do not overlap", name)
     code = _DTYPES.get(t.dtype)
     if code is None:
         _bad("%s has an unsupported dtype", name)
     return rows, cols, ld if rows > 1 else cols, code
+
+
+def _int32(**sizes):
+    """The C entries take 32-bit sizes, and ctypes cuts longer ones off."""
+    for name, n in sizes.items():
+        if not -2 ** 31 <= n < 2 ** 31:
+            _bad("%s is too large", name)
 
 
 def _plain(t: torch.Tensor, name: str, shape, dtype, device=None):
@@ -217,6 +226,7 @@ def _mx_of(mx, name: str, *lead: int, device=None) -> tuple:
     """(focus_mx, K) of a pair of codes [*lead, K / 2] and scales [*lead, K / 32]."""
     codes, scales = mx
     blocks = scales.shape[-1] if scales.dim() else 0
+    _int32(**{name: 32 * blocks})
     _plain(codes, name + " (codes)", (*lead, 16 * blocks), torch.uint8, device)
     _plain(scales, name + " (scales)", (*lead, blocks), torch.uint8, device)
     return focus_mx(codes.data_ptr(), scales.data_ptr()), 32 * blocks
@@ -290,6 +300,7 @@ def focus_mx_dequantize(codes: torch.Tensor, scales: torch.Tensor, out: torch.Te
 
 
 def focus_mx_gemm_bytes(m: int, n: int, k: int, a_type: int) -> int:
+    _int32(m=m, n=n, k=k)
     nbytes = C.c_size_t()
     _check(_lib.focus_mx_gemm_bytes(m, n, k, a_type, C.byref(nbytes)))
     return nbytes.value
@@ -319,6 +330,7 @@ def focus_mx_gemm(a, w, out: torch.Tensor, workspace: Optional[torch.Tensor] = N
 
 
 def focus_mx_experts_bytes(n_experts: int, hidden: int, ffn: int, n_rows: int, k: int) -> int:
+    _int32(n_experts=n_experts, hidden=hidden, ffn=ffn, n_rows=n_rows, k=k)
     nbytes = C.c_size_t()
     _check(_lib.focus_mx_experts_bytes(n_experts, hidden, ffn, n_rows, k, C.byref(nbytes)))
     return nbytes.value
@@ -337,6 +349,7 @@ def focus_mx_experts(gate_up, down, x: torch.Tensor, experts: torch.Tensor, weig
     if gate_up[0].dim() != 3 or experts.dim() != 2:
         _bad("gate_up has three dimensions, experts two")
     (E, two_ffn, _), k = gate_up[0].shape, experts.shape[1]
+    _int32(gate_up=E, experts=k)
     mg, hidden_g = _mx_of(gate_up, "gate_up", E, two_ffn, device=dev)
     md, ffn = _mx_of(down, "down", E, hidden, device=dev)
     if hidden_g != hidden or two_ffn != 2 * ffn or out_rows != rows or out_cols != hidden:

@@ -2,7 +2,9 @@
 import ctypes as C
 
 import pytest
+import torch
 
+import paper_2601_23278_amd as pk
 from test_mx_refusals import P, lib, refused, router
 from paper_2601_23278_amd import binding
 
@@ -31,3 +33,19 @@ def test_gemm_refuses_tiles_that_make_a_launch_too_large(at, scales, tiles):
         refused(lib.focus_mx_gemm(None, m, cols, 32, at, P, scales, 32, C.byref(mx), 0, P, cols, None, 0), "large")
         refused(lib.focus_mx_gemm_bytes(m, cols, 32, at, C.byref(n)), "large")
     assert lib.focus_mx_gemm_bytes(128 * (2 ** 24 - 8), 100, 32, at, C.byref(n)) == 0
+
+
+def test_python_refuses_sizes_that_do_not_fit_32_bits():
+    """The C entries take 32-bit sizes: a longer one must not arrive as its lower half."""
+    for call in (lambda: pk.focus_mx_gemm_bytes(2 ** 32 + 5, 8, 64, 1), lambda: pk.focus_mx_gemm_bytes(5, 2 ** 32 + 8, 64, 1), lambda: pk.focus_mx_gemm_bytes(5, 8, 2 ** 32 + 64, 2),
+                 lambda: pk.focus_mx_gemm_bytes(-2 ** 32 + 5, 8, 64, 1), lambda: pk.focus_mx_experts_bytes(8, 64, 32, 2 ** 32 + 4, 2),
+                 lambda: pk.focus_mx_experts_bytes(2 ** 32 + 8, 64, 32, 4, 2), lambda: pk.focus_mx_experts_bytes(8, 64, 32, 4, 2 ** 32 + 2)):
+        with pytest.raises(pk.FocusError):
+            call()
+    for shape in ((2 ** 32 + 5, 1), (2 ** 31, 32), (3, 2 ** 32 + 32)):
+        with pytest.raises(pk.FocusError):
+            binding._rows_of(torch.empty(shape, dtype=torch.bfloat16, device="meta"), "x")
+    assert binding._rows_of(torch.empty(2 ** 31 - 1, 32, dtype=torch.bfloat16, device="meta"), "x")[0] == 2 ** 31 - 1
+    long = torch.empty((1, 2 ** 31), dtype=torch.uint8, device="meta"), torch.empty((1, 2 ** 27), dtype=torch.uint8, device="meta")
+    with pytest.raises(pk.FocusError):
+        binding._mx_of(long, "w", 1)
