@@ -309,7 +309,8 @@ int focus_get_kernel_time(focus_ctx *ctx, int32_t kernel_class, float *total_ms,
 
 /* Infrastructure.  Destroys the context; the borrowed buffers stay the caller's. */
 int focus_free(focus_ctx *ctx);
-/* Infrastructure.  Text of the last error of ctx, or of the last failed call without a context when ctx is NULL. */
+/* Infrastructure.  Text of the last error of ctx; with ctx NULL, of the calling thread's last failed call without a context, or, where that thread has had
+ * none, of any thread's. */
 const char *focus_last_error(const focus_ctx *ctx);
 
 /* ---------------------------------------------------------------------------------------------------------------------
@@ -317,7 +318,7 @@ const char *focus_last_error(const focus_ctx *ctx);
  *
  * The entries with a stream and no context need none: they enqueue on the stream of the current device, allocate nothing, keep nothing
  * between calls, never synchronise and may be captured; calls may overlap if their outputs and workspaces do not.  The same call on the
- * same inputs gives the same bits.  Errors are reported through focus_last_error(NULL), which is kept per host thread.  Operands must not
+ * same inputs gives the same bits.  Errors are reported through focus_last_error(NULL).  Operands must not
  * overlap outputs. */
 
 /* A router: how a row's E logits l become k experts and their mixing weights.

@@ -6,13 +6,18 @@
 #include <string.h>
 
 #include <algorithm>
+#include <mutex>
 #include <new>
 
 #include "focus_mx.h"
 
 namespace {
 
-thread_local std::string g_error;   // last error of a call that had no context
+// Last error of a call that had no context: of this thread, and of any.
+constexpr int kErrorText = 512;
+thread_local char g_error[kErrorText];
+char g_any_error[kErrorText];
+std::mutex g_any_error_lock;
 
 // Scratch of focus_select_compact_noalloc: per-sequence retained counts and the packed row total.  One copy per GPU, held
 // until the process ends.  In host code the array's name is only a handle for hipGetSymbolAddress: the device address of
@@ -264,19 +269,25 @@ struct focus_ctx {
 namespace {
 
 int fail(focus_ctx *ctx, int code, const char *fmt, ...) {
-  char buf[512];
+  char buf[kErrorText] = {};
   va_list ap;
   va_start(ap, fmt);
   vsnprintf(buf, sizeof buf, fmt, ap);
   va_end(ap);
-  (ctx ? ctx->error : g_error) = buf;
+  if (ctx) {
+    ctx->error = buf;
+    return code;
+  }
+  memcpy(g_error, buf, sizeof buf);
+  std::lock_guard<std::mutex> hold(g_any_error_lock);
+  memcpy(g_any_error, buf, sizeof buf);
   return code;
 }
 
 }  // namespace
 
 int fk::fail_call(int code, const char *fmt, ...) {
-  char buf[512];
+  char buf[kErrorText] = {};
   va_list ap;
   va_start(ap, fmt);
   vsnprintf(buf, sizeof buf, fmt, ap);
@@ -649,7 +660,15 @@ int focus_free(focus_ctx *ctx) {
   return FOCUS_OK;
 }
 
-const char *focus_last_error(const focus_ctx *ctx) { return ctx ? ctx->error.c_str() : g_error.c_str(); }
+const char *focus_last_error(const focus_ctx *ctx) {
+  if (ctx) return ctx->error.c_str();
+  if (g_error[0]) return g_error;
+  // a thread without an error of its own: a copy, which the next failed call of another thread leaves alone
+  static thread_local char text[kErrorText];
+  std::lock_guard<std::mutex> hold(g_any_error_lock);
+  memcpy(text, g_any_error, sizeof text);
+  return text;
+}
 
 int focus_set_timing(focus_ctx *ctx, int32_t enable) {
   if (!ctx) return fail(nullptr, FOCUS_EINVAL, "null context");

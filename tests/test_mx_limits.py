@@ -49,3 +49,24 @@ def test_python_refuses_sizes_that_do_not_fit_32_bits():
     long = torch.empty((1, 2 ** 31), dtype=torch.uint8, device="meta"), torch.empty((1, 2 ** 27), dtype=torch.uint8, device="meta")
     with pytest.raises(pk.FocusError):
         binding._mx_of(long, "w", 1)
+
+
+def test_errors_of_other_threads():
+    """A thread that had no failed call reads the last one of any thread, as a program does that opens contexts on one thread and reports from another; a thread
+    that had one reads its own."""
+    import threading
+
+    def on_a_thread(f):
+        got = []
+        t = threading.Thread(target=lambda: got.append(f()))
+        t.start()
+        t.join()
+        return got[0]
+
+    def fail_then_wait():
+        rc = lib.focus_workspace_bytes(None, None)
+        on_a_thread(lambda: lib.focus_route(None, None, 1, 0, P, 16, None, P, P))
+        return rc, lib.focus_last_error(None).decode()
+    rc, own = on_a_thread(fail_then_wait)
+    assert rc == binding.FOCUS_EINVAL and own == "null argument"
+    assert on_a_thread(lambda: lib.focus_last_error(None).decode()) == "null router"
