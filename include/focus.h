@@ -369,7 +369,8 @@ int focus_mx_quantize(void *hip_stream, int32_t dtype, int64_t rows, int32_t col
  * row of x [rows, ldx]. */
 int focus_mx_dequantize(void *hip_stream, int32_t dtype, int64_t rows, int32_t cols, const focus_mx *mx, void *x, int64_t ldx);
 
-/* C[m, n] = sum_k A[m, k] W[n, k], summed in fp32 and rounded once.
+/* C[m, n] = sum_k A[m, k] W[n, k], summed in fp32 and rounded once.  With bf16 rows a weight of 2^128 or more, beyond bf16, counts as infinite (scales 253 and
+ * 254, which focus_mx_quantize never writes); with MXFP4 rows it counts with its value.
  *   k            a multiple of 32 (the quantiser fills a row's last block with zeros), at most 2^22; 0: C = 0.  n * k below 2^32, and C at most
  *                2^24 - 8 tiles of 128 x 128
  *   a_type       FOCUS_BF16: A device [m, lda] bf16, 16-byte aligned, lda a multiple of 8 and at most 2^22; a_scales NULL.
@@ -384,7 +385,8 @@ int focus_mx_gemm(void *hip_stream, int32_t m, int32_t n, int32_t k, int32_t a_t
 
 /* Routed SwiGLU experts with MXFP4 weights, on bf16 rows:
  *   out[r] = sum_j weights[r, j] * Down_e( silu(Gate_e x_r) * (Up_e x_r) ),  e = experts[r, j], j < k ascending
- * in fp32, except that the inner activations silu(..) * (..) are rounded to bf16, the operand type of the second product.  An entry of experts outside 0..E-1
+ * in fp32, except that the inner activations silu(..) * (..) are rounded to bf16, the operand type of the second product; weights of
+ * 2^128 or more count as infinite.  An entry of experts outside 0..E-1
  * contributes nothing (experts that live elsewhere); a row may name an expert twice.
  *   hidden, ffn  multiples of 32
  *   gate_up      MXFP4 [E, 2 ffn, hidden]: per expert ffn gate rows, then ffn up rows;  down  MXFP4 [E, hidden, ffn]

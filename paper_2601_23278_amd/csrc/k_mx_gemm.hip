@@ -1,7 +1,7 @@
 // Products with microscaled 4-bit (MXFP4) weights on the matrix cores: dense, and grouped by expert.
 //
-// Two forms.  bf16 rows: codes become bf16 in registers (a 4-bit float times a power of two is exact in bf16) and go through
-// v_mfma_f32_32x32x16_bf16.  MXFP4 rows: codes and scales go as they are through v_mfma_scale_f32_32x32x64_f8f6f4, four times the rate.
+// Two forms.  bf16 rows: codes become bf16 in registers (a 4-bit float times a power of two from 2^-127 on is exact in bf16 below 2^128, infinite from
+// there on) and go through v_mfma_f32_32x32x16_bf16, which takes numbers below the smallest normal one.  MXFP4 rows: codes and scales go as they are through v_mfma_scale_f32_32x32x64_f8f6f4, four times the rate.
 #include <algorithm>
 #include <iterator>
 #include <type_traits>

@@ -1,8 +1,11 @@
 """Calls of the expert router and the MXFP4 operators at the edges of what their documentation allows, against plain 64-bit forms (mx_reference.py)."""
+import math
+
 import pytest
 import torch
 
-from test_gpu_mx import check_route
+import mx_reference as ref
+from test_gpu_mx import DEV, _pk, check_route, experts_case, gpu, product_bound
 
 pytestmark = pytest.mark.gpu
 
@@ -69,3 +72,52 @@ def test_a_score_that_its_bias_cancels_against_small_scores(kind, E, k):
     if kind == "softmax":
         bias[0] = last - float((w[:, 0] / w.sum(1)).mean())
     check_route(logits.float(), bias, kind, 1, 1, 1, k, 1, 1.0)
+
+
+# -- products ---------------------------------------------------------------------------------
+@pytest.mark.parametrize("a_type", ["bf16", "mx4"])
+@pytest.mark.parametrize("k", [96, 512])
+def test_gemm_with_the_smallest_scales_against_large_rows(a_type, k):
+    """Weights from 2^-128 on, most of them below the smallest normal number, times rows around 2^100: normal results, to which every weight counts."""
+    pk, _ = _pk()
+    m, n = 40, 140
+    gen = torch.Generator().manual_seed(k)
+    codes = torch.randint(0, 256, (n, k // 2), generator=gen, dtype=torch.uint8)
+    scales = torch.randint(0, 4, (n, k // 32), generator=gen, dtype=torch.uint8)
+    scales[:20], scales[20:40] = 0, 1
+    wv = ref.values(codes, scales)
+    if a_type == "bf16":
+        a = (torch.randn(m, k, generator=gen) * 2.0 ** 100).to(torch.bfloat16)
+        av, ga = a.double(), a.to(DEV)
+    else:
+        am = ref.random_mx(gen, m, k)
+        am[1].add_(100)
+        av, ga = ref.values(*am), gpu(*am)
+    c = pk.focus_mx_gemm(ga, gpu(codes, scales), torch.empty(m, n, device=DEV)).cpu().double()
+    want = av @ wv.t()
+    assert float(want.abs().median()) > 2.0 ** -40                  # the bound's own smallest numbers are nothing beside them
+    assert bool(((c - want).abs() <= product_bound(av, wv, torch.float32)).all())
+
+
+@pytest.mark.parametrize("scale", [251, 252, 253, 254])
+def test_gemm_with_the_largest_scales(scale):
+    """Rows in MXFP4: every weight counts with its value.  Rows in bf16: weights of 2^128 and more, beyond bf16, count as infinite; those that the quantiser writes
+    (scales up to 252) are smaller."""
+    pk, _ = _pk()
+    n, k = 16, 64
+    codes = torch.zeros(n, k // 2, dtype=torch.uint8)
+    codes[:, 5] = torch.arange(n, dtype=torch.uint8) << 4            # element 11 of row c is code c, all others are zero
+    w = codes, torch.full((n, k // 32), scale, dtype=torch.uint8)
+    value = ref.values(*w)[:, 11]
+    a = torch.zeros(3, k)
+    a[0, 11], a[1, 11], a[2, 11] = 2.0 ** -20, -1.5, 2.0 ** -125
+    want = a.double()[:, 11:12] * value
+    want = torch.where(want.abs() < 2.0 ** 128, want, torch.sign(want) * math.inf)
+    got = pk.focus_mx_gemm(pk.focus_mx_quantize(a.to(DEV)), gpu(*w), torch.empty(3, n, device=DEV)).cpu().double()
+    assert torch.equal(got, want)
+    want = torch.where(value.abs() < 2.0 ** 128, want, torch.sign(a[:, 11:12].double()) * torch.sign(value) * math.inf)
+    got = pk.focus_mx_gemm(a.to(torch.bfloat16).to(DEV), gpu(*w), torch.empty(3, n, device=DEV)).cpu().double()
+    assert torch.equal(got, want)
+    top = torch.full((1, 32), torch.finfo(torch.float32).max)
+    for dtype in (torch.float32, torch.bfloat16):
+        assert pk.focus_mx_quantize(top.to(dtype).clamp(max=torch.finfo(dtype).max).to(DEV))[1].tolist() == [[252]]
