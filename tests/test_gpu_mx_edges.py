@@ -5,7 +5,7 @@ import pytest
 import torch
 
 import mx_reference as ref
-from test_gpu_mx import DEV, _pk, check_route, experts_case, gpu, product_bound
+from test_gpu_mx import DEV, MATRICES, _pk, check_route, experts_case, gpu, product_bound, small
 
 pytestmark = pytest.mark.gpu
 
@@ -121,3 +121,48 @@ def test_gemm_with_the_largest_scales(scale):
     top = torch.full((1, 32), torch.finfo(torch.float32).max)
     for dtype in (torch.float32, torch.bfloat16):
         assert pk.focus_mx_quantize(top.to(dtype).clamp(max=torch.finfo(dtype).max).to(DEV))[1].tolist() == [[252]]
+
+
+# -- inside a context -------------------------------------------------------------------------
+@pytest.mark.parametrize("E,k,batch,ratio,kept,hint", [
+    (64, 4, 5, 0.25, 0x00010001, 10),      # ten rows and a hint of ten: tiles of 32 rows, their list behind the counts
+    (64, 4, 5, 0.25, 0xFFFFFFFF, 8),       # the same launches with 160 rows in them
+    (300, 8, 5, 0.25, 0xFFFFFFFF, 5),      # 1280 entries of 300 experts where 40 were expected
+    (64, 4, 2, 0.25, 0xFFFF0FF1, 0),       # 64 rows and no hint: still 32-row tiles
+    (48, 2, 1, 1 / 32, None, 0)])          # one row a step, whose counts leave no room for the tiles behind them
+def test_context_in_tiles_of_32_rows(E, k, batch, ratio, kept, hint):
+    """Few rows an expert, as the row hint has it, which need not be true: every row's residual stream against a context on the same values in bf16, and against
+    one whose experts give nothing, so that a row that lost an expert shows.  Only the experts differ, so that all select the same positions.  The same values are
+    summed in another order and rounded to bf16 between kernels: the tolerance of the bf16 model's parity tests, of what the experts give."""
+    pk, runner = _pk()
+    wl = small(n_experts=E, experts_per_token=k, batch=batch, keep_ratio=ratio)
+    n = wl.batch
+    forced = None if kept is None else torch.full((n,), kept, dtype=torch.int64, device=DEV)
+    routes = torch.tensor(wl.route_override(n), dtype=torch.int32, device=DEV)
+    got = {}
+    for which in ("bf16", "mx", "none"):
+        sess = runner.open_session(wl, DEV)
+        layers = []
+        for w in sess.weights[3]:
+            pairs = {}
+            for name in MATRICES[2:4]:
+                if name in w:
+                    t = w[name]
+                    c, s = pk.focus_mx_quantize(t.reshape(-1, t.shape[-1]))
+                    pk.focus_mx_dequantize(c, s, t.view(-1, t.shape[-1]))
+                    pairs[name] = (c.view(*t.shape[:-1], -1) * (which == "mx"), s.view(*t.shape[:-1], -1))
+            layers.append(pairs)
+        if which != "bf16":
+            sess.focus.focus_set_mx_weights(layers)
+        sess.focus.focus_set_route_override(routes)
+        if hint:
+            sess.focus.focus_set_row_hint(hint, wl.block_size)
+        hidden = torch.zeros(n * wl.block_size, wl.hidden, device=DEV)
+        cu = torch.zeros(n + 1, dtype=torch.int32, device=DEV)
+        sess.focus.focus_step(n, out=pk.make_step_out(hidden_packed=hidden, cu_seqlens=cu), keep_override=forced)
+        torch.cuda.synchronize()
+        got[which] = hidden[:int(cu[n])].double().cpu()
+        sess.focus.focus_free()
+    assert got["mx"].shape[0] == n * (1 if kept is None else bin(kept).count("1"))
+    given = (got["bf16"] - got["none"]).norm(dim=1)
+    assert bool((given > 0).all()) and bool(((got["mx"] - got["bf16"]).norm(dim=1) <= 2e-2 * given).all()), float(((got["mx"] - got["bf16"]).norm(dim=1) / given).max())
