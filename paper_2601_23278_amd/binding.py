@@ -450,7 +450,7 @@ class Focus:
 
     def focus_set_router(self, router: Optional[focus_router], bias: Optional[Sequence[Optional[torch.Tensor]]] = None):
         """bias: one fp32 tensor [E], or None, per layer."""
-        E = self.cfg.n_experts
+        E, bias = self.cfg.n_experts, None if bias is None else list(bias)
         for b in bias or ():
             if b is not None:
                 _plain(b, "bias", (E,), torch.float32, self.workspace.device)
@@ -458,7 +458,7 @@ class Focus:
             _bad("one bias per layer")
         arr = None if bias is None else (C.c_void_p * len(bias))(*[None if b is None else b.data_ptr() for b in bias])
         _check(_lib.focus_set_router(self._ctx, None if router is None else C.byref(router), arr), self._ctx)
-        self._router_bias = bias             # borrowed by the library
+        self._router_bias = None if router is None else bias             # borrowed by the library
 
     def focus_set_mx_weights(self, layers: Optional[Sequence[Dict[str, tuple]]]):
         """layers: per layer a dict of matrix name (w_gate_up, w_expert_down, ...) -> pair (codes, scales); {} leaves a layer as it is."""
@@ -472,6 +472,7 @@ class Focus:
         shapes = {"w_gate_up": (2 * g.ffn, g.hidden), "w_down": (g.hidden, g.ffn),
                   "w_expert_gate_up": (g.n_experts, 2 * g.expert_ffn, g.hidden), "w_expert_down": (g.n_experts, g.hidden, g.expert_ffn),
                   "w_shared_gate_up": (2 * g.shared_ffn, g.hidden), "w_shared_down": (g.hidden, g.shared_ffn)}
+        layers = [{name: tuple(pair) for name, pair in l.items()} for l in layers]
         w, arrays = focus_mx_weights(), []
         for name in _MX_FIELDS:
             if any(name in l for l in layers):

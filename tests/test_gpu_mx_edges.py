@@ -1,5 +1,7 @@
 """Calls of the expert router and the MXFP4 operators at the edges of what their documentation allows, against plain 64-bit forms (mx_reference.py)."""
+import gc
 import math
+import weakref
 
 import pytest
 import torch
@@ -166,3 +168,39 @@ def test_context_in_tiles_of_32_rows(E, k, batch, ratio, kept, hint):
     assert got["mx"].shape[0] == n * (1 if kept is None else bin(kept).count("1"))
     given = (got["bf16"] - got["none"]).norm(dim=1)
     assert bool((given > 0).all()) and bool(((got["mx"] - got["bf16"]).norm(dim=1) <= 2e-2 * given).all()), float(((got["mx"] - got["bf16"]).norm(dim=1) / given).max())
+
+
+def expert_pairs(pk, E, ffn, hidden):
+    up, down = pk.focus_mx_quantize(torch.ones(E * 2 * ffn, hidden, device=DEV)), pk.focus_mx_quantize(torch.ones(E * hidden, ffn, device=DEV))
+    return dict(w_expert_gate_up=tuple(t.view(E, 2 * ffn, -1) for t in up), w_expert_down=tuple(t.view(E, hidden, -1) for t in down))
+
+
+def test_a_context_keeps_what_it_borrows():
+    """The caller's lists and dicts may change or go once a setter has returned; a refused call keeps what was there."""
+    pk, runner = _pk()
+    sess = runner.open_session(small(), DEV)
+    f, E = sess.focus, 16
+    layers = [{}, expert_pairs(pk, E, 128, 512), expert_pairs(pk, E, 128, 512)]
+    biases = [torch.zeros(E, device=DEV) for _ in range(3)]
+    router = pk.focus_router(n_experts=E, experts_per_token=4, score=1, n_groups=4, groups_kept=2, group_top=2, renormalize=1, route_scale=1.0)
+    tensors = [weakref.ref(t) for l in layers for pair in l.values() for t in pair] + [weakref.ref(b) for b in biases]
+    f.focus_set_mx_weights(layers)
+    f.focus_set_router(router, biases)
+    layers[1].clear()
+    layers.clear()
+    biases.clear()
+    gc.collect()
+    assert len(tensors) == 11 and all(t() is not None for t in tensors)
+    with pytest.raises(pk.FocusError):
+        f.focus_set_mx_weights([{}])
+    with pytest.raises(pk.FocusError):
+        f.focus_set_router(router, [None])
+    gc.collect()
+    assert all(t() is not None for t in tensors)
+    f.focus_step(sess.wl.batch)
+    torch.cuda.synchronize()
+    f.focus_set_mx_weights(None)
+    f.focus_set_router(None)
+    gc.collect()
+    assert all(t() is None for t in tensors)
+    f.focus_free()
