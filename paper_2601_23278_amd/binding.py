@@ -461,7 +461,8 @@ class Focus:
         self._router_bias = None if router is None else bias             # borrowed by the library
 
     def focus_set_mx_weights(self, layers: Optional[Sequence[Dict[str, tuple]]]):
-        """layers: per layer a dict of matrix name (w_gate_up, w_expert_down, ...) -> pair (codes, scales); {} leaves a layer as it is."""
+        """layers: per layer a dict of matrix name (w_gate_up, w_expert_down, ...) -> pair (codes, scales); {} leaves a layer on the matrices
+        the context was made with."""
         if layers is None:
             _check(_lib.focus_set_mx_weights(self._ctx, None), self._ctx)
             self._mx_layers = None
@@ -473,6 +474,8 @@ class Focus:
                   "w_expert_gate_up": (g.n_experts, 2 * g.expert_ffn, g.hidden), "w_expert_down": (g.n_experts, g.hidden, g.expert_ffn),
                   "w_shared_gate_up": (2 * g.shared_ffn, g.hidden), "w_shared_down": (g.hidden, g.shared_ffn)}
         layers = [{name: tuple(pair) for name, pair in l.items()} for l in layers]
+        for name in {name for l in layers for name in l}.difference(shapes):
+            _bad("%s is no matrix of a feed-forward", name)
         w, arrays = focus_mx_weights(), []
         for name in _MX_FIELDS:
             if any(name in l for l in layers):

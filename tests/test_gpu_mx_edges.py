@@ -204,3 +204,13 @@ def test_a_context_keeps_what_it_borrows():
     gc.collect()
     assert all(t() is None for t in tensors)
     f.focus_free()
+
+
+def test_setters_refuse_names_that_no_matrix_has():
+    pk, runner = _pk()
+    sess = runner.open_session(small(), DEV)
+    good = expert_pairs(pk, 16, 128, 512)
+    for name in ("w_expert_gateup", "w_qkv", "gate_up"):
+        with pytest.raises(pk.FocusError):
+            sess.focus.focus_set_mx_weights([{}, dict(good, **{name: good["w_expert_down"]}), good])
+    sess.focus.focus_free()
