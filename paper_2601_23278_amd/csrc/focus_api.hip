@@ -504,7 +504,8 @@ void moe_ffn(focus_ctx *c, hipStream_t s, int l, const RowSet &rs, float *resid,
                   FOCUS_F32, resid, g.hidden, true, a.list, 128, (int2 *)a.tile_e, a.n_tiles, a.pos, a.arow, a.act, a.y};
   const int cap = a.rows.cap, few = fk::mx_tile_rows(a.rows.expected(), m.k, m.n_experts);
   const size_t counts = ((size_t)fk::mx_chunks(cap, m.k) * m.n_experts * 4 + 255) & ~(size_t)255;
-  if (counts + (size_t)fk::mx_tile_slots(cap, m.k, m.n_experts, few) * 8 <= (size_t)m.n_experts * cap * 4) {
+  if (counts + (size_t)fk::mx_tile_slots(cap, m.k, m.n_experts, few) * 8 <= (size_t)m.n_experts * cap * 4 &&
+      fk::mx_experts_launch(cap, m.k, m.n_experts, few, m.hidden, m.ffn)) {
     m.tile_rows = few;
     m.tiles = (int2 *)((char *)a.list + counts);
   }
@@ -1179,7 +1180,12 @@ int focus_set_mx_weights(focus_ctx *ctx, const focus_mx_weights *weights) {
       if (((uintptr_t)up[l].codes | (uintptr_t)down[l].codes) & 15) return fail(ctx, FOCUS_EINVAL, "layer %d: codes must be 16-byte aligned", l);
       if (p == 0 ? ctx->moe_layer(l) : !ctx->moe_layer(l) || inner[p] == 0) return fail(ctx, FOCUS_EINVAL, "layer %d has no such matrix", l);
       if (g.hidden % 32 || inner[p] % 32) return fail(ctx, FOCUS_EINVAL, "hidden and the inner width must be multiples of 32");
-      if ((int64_t)2 * inner[p] * (g.hidden / 2) >= (1ll << 31) || (int64_t)std::max(ctx->plan.max_rows, kPrefillRows) * g.hidden >= (1ll << 30))
+      // the sizes of the products, and 32-bit offsets of the rows that the experts gather
+      const int rows = std::max(ctx->plan.max_rows, kPrefillRows);
+      const char *e = fk::check_mx_product(rows, g.hidden, inner[p]);       // K first: an inner width of at most 2^22
+      if (!e) e = fk::check_mx_product(rows, 2 * inner[p], g.hidden);
+      if (e) return fail(ctx, FOCUS_EINVAL, "layer %d: %s", l, e);
+      if ((int64_t)rows * g.hidden >= (1ll << 30) || (p == 1 && !fk::mx_experts_launch(rows, g.experts_per_token, g.n_experts, 128, g.hidden, inner[p])))
         return fail(ctx, FOCUS_EINVAL, "the model is too large for MXFP4 weights");
     }
   }

@@ -27,6 +27,11 @@ const char *check_router(const focus_router &r);   // what is wrong with it, or 
 void route(hipStream_t s, const RouteArgs &a);
 
 // ---- MXFP4 --------------------------------------------------------------------------------------
+// A launch has at most 2^32 - 1 threads, in workgroups of 256: so many workgroups are too many.
+constexpr int64_t kMaxGroups = 1 << 24;
+const char *check_mx_product(int32_t m, int32_t n, int32_t k);     // what is wrong with the sizes of a product, or null
+bool mx_experts_launch(int rows, int k, int n_experts, int tile_rows, int hidden, int ffn);     // the experts' grids are not too large
+
 void mx_quantize(hipStream_t s, int dtype, int64_t rows, int cols, const void *x, int64_t ldx, void *codes, void *scales);
 void mx_dequantize(hipStream_t s, int dtype, int64_t rows, int cols, focus_mx mx, void *x, int64_t ldx);
 

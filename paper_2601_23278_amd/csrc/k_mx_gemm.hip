@@ -702,7 +702,7 @@ Shape shape_of(int rows, int n, int k, bool a_mx) {
   for (const Variant *v = a_mx ? kMxVariants : kRowVariants, *end = a_mx ? std::end(kMxVariants) : std::end(kRowVariants); v != end; ++v) {
     const int tiles_m = (rows + v->bm - 1) / v->bm;
     const int64_t tiles = (int64_t)tiles_m * ((n + v->bn - 1) / v->bn);
-    if (tiles > (1 << 24) - 8) continue;              // more threads than a launch may have
+    if (tiles > kMaxGroups - 8) continue;
     // tile rows of 32 that hold no rows are skipped
     const float live = a_mx || v->bm == 32 ? 1.f : 0.4f + 0.6f * (float)((rows + 31) / 32) / (float)(tiles_m * v->bm / 32);
     for (int parts = 1; parts <= std::min(units, 16); ++parts) {

@@ -15,15 +15,9 @@ int launched() {
   return e == hipSuccess ? FOCUS_OK : fail_call(FOCUS_EHIP, "launch: %s", hipGetErrorString(e));
 }
 
-// A launch has at most 2^32 - 1 threads, in workgroups of 256: so many workgroups are too many.
-constexpr int64_t kMaxGroups = 1 << 24;
-
 const char *check_product(int32_t m, int32_t n, int32_t k, int32_t a_type) {
-  if (m < 0 || n < 0 || k < 0 || k % 32) return "m, n and k must not be negative and k a multiple of 32";
   if (a_type != FOCUS_BF16 && a_type != FOCUS_MX4) return "a_type must be FOCUS_BF16 or FOCUS_MX4";
-  if (k > (1 << 22)) return "k must be at most 2^22";
-  if ((int64_t)n * (k / 2) >= (1ll << 31) || ((int64_t)m + 127) / 128 * (((int64_t)n + 127) / 128) > kMaxGroups - 8) return "m, n and k too large";   // rounded up to the eight XCDs
-  return nullptr;
+  return fk::check_mx_product(m, n, k);
 }
 
 const char *check_experts(int32_t n_experts, int32_t hidden, int32_t ffn, int32_t n_rows, int32_t k) {
@@ -31,13 +25,22 @@ const char *check_experts(int32_t n_experts, int32_t hidden, int32_t ffn, int32_
   if (hidden < 32 || hidden % 32 || ffn < 32 || ffn % 32) return "hidden and ffn must be positive multiples of 32";
   if (hidden > (1 << 20) || ffn > (1 << 20) || (int64_t)hidden * ffn >= (1ll << 31)) return "hidden and ffn too large";
   if (n_rows < 0 || k < 1 || k > 32 || (int64_t)n_rows * k >= (1 << 24)) return "n_rows must not be negative, k in 1..32 and n_rows * k below 2^24";
-  // the launches have a workgroup per 128 columns and tile of rows
-  const int64_t tiles = fk::mx_tile_slots(n_rows, k, n_experts, fk::mx_tile_rows(n_rows, k, n_experts));
-  if (tiles * ((std::max(hidden, 2 * ffn) + 127) / 128) >= kMaxGroups) return "hidden, ffn and n_rows too large";
+  if (!fk::mx_experts_launch(n_rows, k, n_experts, fk::mx_tile_rows(n_rows, k, n_experts), hidden, ffn)) return "hidden, ffn and n_rows too large";
   return nullptr;
 }
 
 }  // namespace
+
+const char *fk::check_mx_product(int32_t m, int32_t n, int32_t k) {
+  if (m < 0 || n < 0 || k < 0 || k % 32) return "m, n and k must not be negative and k a multiple of 32";
+  if (k > (1 << 22)) return "k must be at most 2^22";
+  if ((int64_t)n * (k / 2) >= (1ll << 31) || ((int64_t)m + 127) / 128 * (((int64_t)n + 127) / 128) > kMaxGroups - 8) return "m, n and k too large";   // rounded up to the eight XCDs
+  return nullptr;
+}
+
+bool fk::mx_experts_launch(int rows, int k, int n_experts, int tile_rows, int hidden, int ffn) {      // a workgroup per 128 columns and tile of rows
+  return (int64_t)mx_tile_slots(rows, k, n_experts, tile_rows) * ((std::max(hidden, 2 * ffn) + 127) / 128) < kMaxGroups;
+}
 
 extern "C" {
 
@@ -45,7 +48,7 @@ int focus_route(const focus_router *router, void *hip_stream, int32_t n_rows, in
                 int32_t *experts, float *weights) {
   if (!router) return fail_call(FOCUS_EINVAL, "null router");
   if (const char *e = fk::check_router(*router)) return fail_call(FOCUS_EINVAL, "%s", e);
-  if (n_rows < 0 || n_rows > 4 * (kMaxGroups - 1)) return fail_call(FOCUS_EINVAL, "n_rows must be in 0..2^26 - 4");         // four rows a workgroup
+  if (n_rows < 0 || n_rows > 4 * (fk::kMaxGroups - 1)) return fail_call(FOCUS_EINVAL, "n_rows must be in 0..2^26 - 4");         // four rows a workgroup
   if (dtype != FOCUS_F32 && dtype != FOCUS_BF16) return fail_call(FOCUS_EINVAL, "dtype must be FOCUS_F32 or FOCUS_BF16");
   if (ld < router->n_experts) return fail_call(FOCUS_EINVAL, "ld is less than n_experts");
   if (n_rows == 0) return FOCUS_OK;
@@ -62,7 +65,7 @@ static int check_conversion(int32_t dtype, int64_t rows, int32_t cols, const voi
   if (rows < 0 || cols < 0) return fail_call(FOCUS_EINVAL, "rows and cols must not be negative");
   if (ldx < cols) return fail_call(FOCUS_EINVAL, "ldx is less than cols");
   // 64 blocks of 32 a workgroup
-  if (rows >= (1ll << 30) || rows * (((int64_t)cols + 31) / 32) > 64 * (kMaxGroups - 1)) return fail_call(FOCUS_EINVAL, "rows and cols too large");
+  if (rows >= (1ll << 30) || rows * (((int64_t)cols + 31) / 32) > 64 * (fk::kMaxGroups - 1)) return fail_call(FOCUS_EINVAL, "rows and cols too large");
   if (rows == 0 || cols == 0) return FOCUS_OK;
   if (!x || !codes || !scales) return fail_call(FOCUS_EINVAL, "null x, codes or scales");
   if (!aligned(codes, 16)) return fail_call(FOCUS_EINVAL, "codes must be 16-byte aligned");

@@ -214,3 +214,22 @@ def test_setters_refuse_names_that_no_matrix_has():
         with pytest.raises(pk.FocusError):
             sess.focus.focus_set_mx_weights([{}, dict(good, **{name: good["w_expert_down"]}), good])
     sess.focus.focus_free()
+
+
+def test_context_refuses_mx_matrices_wider_than_its_kernels_take():
+    """K, and the distance of rows, of at most 2^22, as for the product without a context.  Nothing is read: the context is never run."""
+    pk, _ = _pk()
+    for ffn, ok in ((2 ** 22, True), (2 ** 22 + 32, False)):
+        cfg = pk.focus_config(n_layers=2, hidden=64, n_q_heads=1, n_kv_heads=1, head_dim=64, ffn=ffn, vocab=64, dtype=pk.FOCUS_BF16, rms_eps=1e-6, rope_base=1e4,
+                              block_size=1, mask_token_id=63, max_batch=1, max_prefix_len=8, page_size=16, n_pages=1, evict_layer=1, maxpool_k=3, budget_mode=1,
+                              keep_ratio=1.0, conf_threshold=0.9)
+        one = torch.zeros(64, dtype=torch.bfloat16, device=DEV)
+        pool = torch.zeros(pk.focus_kv_pool_bytes(cfg), dtype=torch.uint8, device=DEV)
+        f = pk.Focus(cfg, one, one, one, [{n: one for n in ("attn_norm", "w_qkv", "w_o", "mlp_norm", "w_gate_up", "w_down")}] * 2, pool)
+        up, down = (tuple(torch.empty(r, c // per, dtype=torch.uint8, device=DEV) for per in (2, 32)) for r, c in ((2 * ffn, 64), (64, ffn)))
+        if ok:
+            f.focus_set_mx_weights([dict(w_gate_up=up, w_down=down)] * 2)
+        else:
+            with pytest.raises(pk.FocusError, match="layer 0"):
+                f.focus_set_mx_weights([dict(w_gate_up=up, w_down=down)] * 2)
+        f.focus_free()
