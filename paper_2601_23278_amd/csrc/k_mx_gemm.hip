@@ -725,6 +725,8 @@ void mx_gemm(hipStream_t s, const void *a, const void *a_scales, int64_t lda, fo
   if (rows.cap <= 0 || n <= 0) return;
   const bool a_mx = a_scales != nullptr;
   Shape p = shape_of(rows.expected(), n, k, a_mx);
+  // the grid has room for rows.cap, however few are expected
+  if (!a_mx && (int64_t)((rows.cap + p.bm - 1) / p.bm) * ((n + p.bn - 1) / p.bn) * p.splits > kMaxGroups - 8) p = {128, 128, 1};
   const size_t stride = (size_t)rows.cap * n;
   const int units = a_mx ? (k / 32 + 15) / 16 : (k / 32 + 7) / 8;
   if (p.splits > 1) p.splits = whole_parts((int)std::max<size_t>(1, std::min<size_t>(p.splits, scratch.ptr ? scratch.bytes / (stride * 4) : 0)), units);
