@@ -401,14 +401,17 @@ int focus_mx_experts(void *hip_stream, int32_t n_experts, int32_t hidden, int32_
 
 /* From now on the mixture-of-experts layers of the context choose experts by this router instead of the one focus_config describes
  * (softmax, no bias, no groups, renormalised).  n_experts and experts_per_token must be the configuration's; the router's route_scale
- * counts.  Forced experts (focus_set_route_override) get this router's scores as weights.  router NULL: back to the configuration's.
- *   bias     host array of n_layers device pointers ([E] fp32 each, borrowed until replaced), entries or the array may be NULL */
+ * counts.  Forced experts (focus_set_route_override) get this router's scores as weights.  router NULL: back to the configuration's.  A captured step goes on
+ * reading the biases that it was captured with.
+ *   bias     host array of n_layers device pointers ([E] fp32 each, borrowed until replaced and the steps enqueued before have run), entries or the array may
+ *            be NULL */
 int focus_set_router(focus_ctx *ctx, const focus_router *router, const float *const *bias);
 
 /* From now on the feed-forward layers listed here run on MXFP4 weights (bf16 models).  Every member is a host array of n_layers, or NULL; an
  * entry with NULL codes leaves that layer on the matrices given to focus_init.  A layer's two matrices are given together.  The
- * device memory is borrowed until replaced; the context copies the arrays.  weights NULL: back to the matrices of focus_init.  Inner widths and
- * hidden must be multiples of 32. */
+ * device memory is borrowed until replaced and the steps enqueued before have run; the context copies the arrays.  weights NULL: back to the matrices of
+ * focus_init, which still has to be given them.  A captured step goes on reading the weights that it was captured with.  Inner widths and hidden must be multiples of
+ * 32, inner widths at most 2^22. */
 typedef struct focus_mx_weights {
   const focus_mx *w_gate_up, *w_down;                 /* dense layers: [2 F, hidden], [hidden, F] */
   const focus_mx *w_expert_gate_up, *w_expert_down;   /* [E, 2 F_e, hidden], [E, hidden, F_e] */

@@ -28,7 +28,7 @@ constexpr unsigned kOutside = 0x80000000u;   // an offset beyond every descripto
 // A wavefront's results of 32 rows and 8 G columns into C, through LDS of its own (32 tile_pitch() bytes): value(g) of lane l are C[l % 32][8 g + 4 (l / 32) + 0 .. 3]
 // (four registers of the product of transposed operands), so four neighbours go into LDS at once, and whole pieces of rows come out, 16 bytes a lane.
 // Stored straight from the registers, an element per lane and instruction, with an address and two comparisons for each, 2048 x 24576 x 4096 with both
-// operands in MXFP4 took 125 us instead of 104.
+// operands in MXFP4 took a fifth longer (125 us against 104, in turn on one card).
 // rows, cols: of the tile that exist; wide: the rows of C are 16-byte aligned.
 #if defined(__HIP_DEVICE_COMPILE__)
 __device__ __forceinline__ void wave_lds_order() {      // the lanes' traffic runs in order, only the compiler has to keep it so
@@ -110,7 +110,7 @@ __device__ __forceinline__ uint64_t eight_scales(const unsigned char *row, int b
 // loads.  A step's last quarter begins with the only barrier: by then everyone has read all of the step's rows, whose stage is filled again right
 // behind it, and the next step's rows have landed.  Codes are read and written by their own wavefront alone.
 // What bounds it: few rows, the codes' way from memory (8 rows x 24576 x 4096, 54 MB: 15.0 us, 3.6 TB/s, two rounds of workgroups that each wait for
-// their first slabs); many rows, the matrix units and the chip's power (2048 x 24576 x 4096: 324 us, 1.27 PFLOP/s; a large bf16 library product 1.37); in
+// their first slabs); many rows, the matrix units, busy in 67 % of the cycles (2048 x 24576 x 4096: 318 us, 1.30 PFLOP/s; a large bf16 library product 1.37); in
 // between, both by halves (those gate/up rows, 69 GFLOP and 285 MB of codes: 96 us; the loads alone took 71 of 105, the arithmetic alone 75; the last round
 // of workgroups leaves a fifth of the chip idle).
 constexpr int kRowStages = 3;
@@ -404,9 +404,10 @@ void launch_rows(hipStream_t s, int mode, const RowsArgs &g, int tile_slots) {
 // row's last blocks, where they are not 16, behind the loop.  Pipelined by hand like k_mx_rows: behind each MFMA one fragment read of the next quarter or
 // one load.  The only barrier of a pair stands before its last quarter: by then everyone has read all of it, its place is filled again over the next
 // quarters, and the next pair has landed.
-// 2048 x 24576 x 4096: 104 to 110 us by card, 3.8 to 4.0 PFLOP/s, bound by the matrix units at the clock that the chip's power leaves them (without the loop's loads
-// 99 us, without its LDS reads 98).  Where K is no multiple of 256, rows begin inside a line and a piece of 128 bytes takes two of them: 333 x 4000, K = 12256,
-// 24.5 us, K = 12288 18 (and 5 to add the two parts).
+// 2048 x 24576 x 4096: 106 to 110 us by card, 3.75 to 3.9 PFLOP/s.  The matrix units are busy in 43 % of the cycles, the loop without its loads takes 99 us and
+// without its LDS reads 98, so none of the three alone is the bound; one workgroup a compute unit, in three rounds, overlaps neither its first loads nor its
+// stores with anything.  Where K is no multiple of 256, rows begin inside a line and a piece of 128 bytes takes two of them: 333 x 4000, K = 12256, 25 us,
+// K = 12288 20 (and 4 to 6 to add the two parts).
 struct MxArgs {
   const unsigned char *A, *a_scales, *W, *w_scales;
   int M, N, K;
@@ -763,6 +764,9 @@ static void launch_grouped(hipStream_t s, const RowsArgs &a, const MxExperts &m)
   else launch_rows<128, 1, MODE, true>(s, a, slots);
 }
 
+// The activations are rounded to bf16, the operand type of the matrix instruction that multiplies them with the down matrices (in fp32 they would be two bf16
+// operands, and the second product twice as long).  1024 rows through 8 of 64 experts, 2048 -> 512, against 64 bits: relative error 1.7e-3 with fp32 results (1.5e-5
+// against 64 bits with the same rounding), 2.3e-3 with bf16 results, whose own rounding alone gives 1.7e-3.
 void mx_up(hipStream_t s, const MxExperts &m) {
   if (m.rows.cap <= 0) return;
   RowsArgs a{};
