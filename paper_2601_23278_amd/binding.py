@@ -210,11 +210,10 @@ def _rows_of(t: torch.Tensor, name: str):
     return rows, cols, ld if rows > 1 else cols, code
 
 
-def _int32(**sizes):
+def _int32(*sizes: int):
     """The C entries take 32-bit sizes, and ctypes cuts longer ones off."""
-    for name, n in sizes.items():
-        if not -2 ** 31 <= n < 2 ** 31:
-            _bad("%s is too large", name)
+    if max(sizes) >= 2 ** 31 or min(sizes) < -2 ** 31:
+        _bad("a size is too large: %s", sizes)
 
 
 def _plain(t: torch.Tensor, name: str, shape, dtype, device=None):
@@ -226,7 +225,8 @@ def _mx_of(mx, name: str, *lead: int, device=None) -> tuple:
     """(focus_mx, K) of a pair of codes [*lead, K / 2] and scales [*lead, K / 32]."""
     codes, scales = mx
     blocks = scales.shape[-1] if scales.dim() else 0
-    _int32(**{name: 32 * blocks})
+    if blocks >= 2 ** 26:
+        _bad("%s is too large", name)
     _plain(codes, name + " (codes)", (*lead, 16 * blocks), torch.uint8, device)
     _plain(scales, name + " (scales)", (*lead, blocks), torch.uint8, device)
     return focus_mx(codes.data_ptr(), scales.data_ptr()), 32 * blocks
@@ -300,7 +300,7 @@ def focus_mx_dequantize(codes: torch.Tensor, scales: torch.Tensor, out: torch.Te
 
 
 def focus_mx_gemm_bytes(m: int, n: int, k: int, a_type: int) -> int:
-    _int32(m=m, n=n, k=k)
+    _int32(m, n, k)
     nbytes = C.c_size_t()
     _check(_lib.focus_mx_gemm_bytes(m, n, k, a_type, C.byref(nbytes)))
     return nbytes.value
@@ -330,7 +330,7 @@ def focus_mx_gemm(a, w, out: torch.Tensor, workspace: Optional[torch.Tensor] = N
 
 
 def focus_mx_experts_bytes(n_experts: int, hidden: int, ffn: int, n_rows: int, k: int) -> int:
-    _int32(n_experts=n_experts, hidden=hidden, ffn=ffn, n_rows=n_rows, k=k)
+    _int32(n_experts, hidden, ffn, n_rows, k)
     nbytes = C.c_size_t()
     _check(_lib.focus_mx_experts_bytes(n_experts, hidden, ffn, n_rows, k, C.byref(nbytes)))
     return nbytes.value
@@ -349,7 +349,7 @@ def focus_mx_experts(gate_up, down, x: torch.Tensor, experts: torch.Tensor, weig
     if gate_up[0].dim() != 3 or experts.dim() != 2:
         _bad("gate_up has three dimensions, experts two")
     (E, two_ffn, _), k = gate_up[0].shape, experts.shape[1]
-    _int32(gate_up=E, experts=k)
+    _int32(E, k)
     mg, hidden_g = _mx_of(gate_up, "gate_up", E, two_ffn, device=dev)
     md, ffn = _mx_of(down, "down", E, hidden, device=dev)
     if hidden_g != hidden or two_ffn != 2 * ffn or out_rows != rows or out_cols != hidden:

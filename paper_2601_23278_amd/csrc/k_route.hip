@@ -19,7 +19,7 @@
 // They are bounds of each choice, so two whose bounds do not meet are in the order of the exact ones, and a chain of such pairs is.
 //
 // Bound by that chain and the launch, not by bytes (2.2 MB at 2048 rows, 0.4 us): 256 experts, 8 picks, 8 rows 6.6 us, 2048 rows without groups 7.2, 8191
-// rows with 8 groups of which 4 stay 17 to 21: among so many some (14) are done twice, and they end the launch.
+// rows with 8 groups of which 4 stay 17 to 21: among so many about a dozen are done twice, and they end the launch.
 #include "focus_mx.h"
 
 namespace fk {
