@@ -262,8 +262,8 @@ __global__ __launch_bounds__(kRouteWaves * 64) void k_route(RouteArgs a) {
   float f = 0.f, sum = 0.f, weight;
   bool decided = pick<float, P>(a, l, bias, (float *)sh[wave], forced, idx, f);
   for (int j = 0; j < k; ++j) sum += lane_of(f, j);
-  // scores that fp32 holds with few bits or not at all (sigmoids of logits far below zero) have quotients all the same
-  decided = decided && !(a.router.renormalize && sum < 1e-30f);
+  // scores that fp32 holds with few bits or not at all (of logits far below zero, or far below the largest) have quotients all the same
+  decided = decided && !(a.router.renormalize && (sum < 1e-30f || __ballot(lane < k && f < 1.2e-38f)));
   if (decided) {
     weight = a.router.renormalize ? a.router.route_scale * f / sum : a.router.route_scale * f;
   } else {

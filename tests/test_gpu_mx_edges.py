@@ -233,3 +233,12 @@ def test_context_refuses_mx_matrices_wider_than_its_kernels_take():
             with pytest.raises(pk.FocusError, match="layer 0"):
                 f.focus_set_mx_weights([dict(w_gate_up=up, w_down=down)] * 2)
         f.focus_free()
+
+
+def test_weights_of_scores_below_the_smallest_normal_number():
+    """Biases pick experts whose scores 32 bits hold with few bits or not at all, beside others that they do hold: the quotients count in full."""
+    for rows, E, k, seed, size in ((40, 32, 20, 1, 100.0), (40, 16, 7, 2, 60.0), (7, 256, 22, 3, 30.0)):
+        gen = torch.Generator().manual_seed(seed)
+        l = torch.randn(rows, E, generator=gen) * size
+        check_route(l, torch.randn(E, generator=gen) * 100, "softmax", 1, 1, 1, k, 1, 2.5)
+        check_route(l, torch.randn(E, generator=gen) * 100, "sigmoid", 4, 3, 2, min(k, 3 * E // 4), 1, 2.5)
