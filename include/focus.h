@@ -419,6 +419,93 @@ typedef struct focus_mx_weights {
 } focus_mx_weights;
 int focus_set_mx_weights(focus_ctx *ctx, const focus_mx_weights *weights);
 
+/* ---------------------------------------------------------------------------------------------------------------------
+ * Generation that branches over the paged cache: beams, several samples of a prompt, trees of drafted tokens.
+ *
+ * These entries work on a K/V pool of the layout above without a context (a context's own pool among them), in the manner of the entries above: they enqueue
+ * on the stream of the current device, allocate nothing, keep nothing between calls, never synchronise and may be captured; the same call on the same inputs
+ * gives the same bits; errors through focus_last_error(NULL).  Sequences are rows of a page table: token t of row b lives in page
+ * page_table[b * table_stride + t / page_size] at place t % page_size.  A row holds its entries up to the first negative one.  Lists on the device are not
+ * checked by the host: a page outside the pool, a token behind the table's last page or an index that no list has is neither read nor written. */
+
+/* A paged K/V pool.  page_size: a multiple of 8, at most 1024; head_dim: 64 or 128; n_kv_heads 1..256; n_layers 1..1024; n_pages at most 2^30. */
+typedef struct focus_kv {
+  void   *pool;             /* device, 16-byte aligned: [n_layers][n_pages] pages */
+  int32_t dtype;            /* FOCUS_F32 or FOCUS_BF16 */
+  int32_t n_layers, n_pages, page_size, n_kv_heads, head_dim;
+} focus_kv;
+
+/* Rows of keys and values into the cache: row r of sequence b (cu_rows[b] <= r < cu_rows[b + 1]) becomes token lens[b] + r - cu_rows[b] of one layer.
+ *   n_seq, n_rows  rows at most 2^22; rows behind cu_rows[n_seq] are not read
+ *   cu_rows        device [n_seq + 1], ascending;  lens  device [n_seq]: tokens that the sequences have already
+ *   page_table     device [n_seq, table_stride]
+ *   k, v           device [n_rows, ldk], [n_rows, ldv] of the pool's type, H_kv * D of each row used (keys after the rotary embedding) */
+int focus_kv_append(const focus_kv *kv, void *hip_stream, int32_t layer, int32_t n_seq, int32_t n_rows, const int32_t *cu_rows, const int32_t *lens,
+                    const int32_t *page_table, int32_t table_stride, const void *k, int64_t ldk, const void *v, int64_t ldv);
+
+/* Attention of drafted tokens: query row r of sequence b, with i = r - cu_rows[b], attends to the cached tokens t < lens[b] and to those drafted tokens j (token
+ * lens[b] + j of the cache, j < the sequence's number of rows) whose bit is set in the row's set:  out = sum_t p_t v_t,  p = softmax(scale * q . k_t), fp32.
+ * Tokens that a row does not see add nothing, whatever their K and V hold; a row that sees nothing is zero.  A single row per sequence is the step of
+ * ordinary decoding, many rows with seen == NULL a part of a prompt.
+ *   seen           device [n_rows, seen_words] uint64, bit j % 64 of word j / 64: drafted token j; seen_words 1..16; drafted tokens beyond its bits are unseen.
+ *                  NULL: row i sees the drafted tokens j <= i
+ *   n_q_heads      a multiple of n_kv_heads, at most 1024; query head h reads key head h / (n_q_heads / n_kv_heads)
+ *   q, out         device [n_rows, ldq], [n_rows, ldo] of the pool's type; rows behind cu_rows[n_seq] are neither read nor written
+ *   max_rows, max_len   what the host knows of the sequences' rows and of their longest lens[b] + rows (0: nothing).  Launches are shaped for it, results do
+ *                  not depend on it but for the rounding order of sums
+ *   workspace      device, 256-byte aligned, focus_tree_attention_bytes() with the same sizes (0 for many); with less the work is spread less */
+int focus_tree_attention_bytes(const focus_kv *kv, int32_t n_seq, int32_t n_rows, int32_t max_rows, int32_t max_len, int32_t table_stride, int32_t n_q_heads, size_t *bytes);
+int focus_tree_attention(const focus_kv *kv, void *hip_stream, int32_t layer, int32_t n_seq, int32_t n_rows, int32_t max_rows, int32_t max_len, const int32_t *cu_rows,
+                         const int32_t *lens, const int32_t *page_table, int32_t table_stride, const uint64_t *seen, int32_t seen_words, int32_t n_q_heads,
+                         float scale, const void *q, int64_t ldq, void *out, int64_t ldo, void *workspace, size_t workspace_bytes);
+
+/* Moves the tokens that stay together, in every layer: token start[b] + keep[cu_keep[b] + i] of row b's pages in page_table becomes token start[b] + i of its
+ * pages in to_table, 0 <= i < cu_keep[b + 1] - cu_keep[b].  The path of a tree that was accepted, or what an eviction leaves of a cache.  Nothing else is written.
+ *   keep           device [n_keep], ascending and not negative within a sequence (else that sequence's tokens are unspecified)
+ *   to_table       device [n_seq, to_stride]; may be page_table or name the same pages for the same sequence: then the tokens move down in place.  A page that
+ *                  is written must belong to no other sequence of the call
+ *   n_seq * n_kv_heads * n_layers below 2^24 */
+int focus_kv_compact(const focus_kv *kv, void *hip_stream, int32_t n_seq, int32_t n_keep, const int32_t *start, const int32_t *cu_keep, const int32_t *keep, const int32_t *page_table,
+                     int32_t table_stride, const int32_t *to_table, int32_t to_stride);
+
+/* Pages and who holds them.  refs, device [n_pages]: how many table entries hold a page; 0: free.  New pages are the lowest free ones, in the order of the
+ * rows and of the tokens in them; where the pool has none left, the last ones wait and `lacking` counts them.
+ *
+ * focus_kv_fork: new rows that continue old ones.  Row i of new_table continues row parents[i] of page_table: it shares the pages that are full.  The pages
+ * behind them (the one that lens[parent] ends in, and reserved ones) go to the parent's first child as they are; every other child gets a page of its own with
+ * a copy of the tokens in it, in all layers.  Old rows give up what they held: a parent without children frees its pages, n_new = 0 those of all rows.
+ * page_table and lens are only read and no longer hold anything afterwards.
+ *   parents        device [n_new] rows of page_table; one outside 0..n_old-1 makes an empty row
+ *   lens           device [n_old] (cut to the pages that a row holds);  new_lens  device [n_new] out
+ *   new_table      device [n_new, table_stride] out, -1 behind the pages;  lacking  device [n_new] out: 1 where there was no page for the copy; that row's
+ *                  length is cut to its full pages
+ *   a page that is not full, or lies behind the tokens, must be held by one row only
+ *   n_old + n_new below 2^20, times table_stride below 2^31, n_new * n_kv_heads * n_layers below 2^24;  workspace  device, 16-byte aligned, focus_kv_fork_bytes() */
+int focus_kv_fork_bytes(int32_t n_new, size_t *bytes);
+int focus_kv_fork(const focus_kv *kv, void *hip_stream, int32_t n_old, int32_t n_new, const int32_t *parents, const int32_t *lens, const int32_t *page_table,
+                  int32_t table_stride, int32_t *new_lens, int32_t *new_table, int32_t *refs, int32_t *lacking, void *workspace, size_t workspace_bytes);
+
+/* Gives rows the pages that lens[b] + room tokens need, in place.
+ *   room           0 or more, the same for all rows;  lacking  device [n_seq] out: pages that a row still wants (the pool or the row's entries ran out)
+ *   n_pages        of refs, at most 2^30;  n_seq below 2^20, n_seq * table_stride below 2^31;  workspace  device, 16-byte aligned, focus_kv_reserve_bytes() */
+int focus_kv_reserve_bytes(int32_t n_seq, size_t *bytes);
+int focus_kv_reserve(void *hip_stream, int32_t n_seq, int32_t page_size, int32_t n_pages, const int32_t *lens, int32_t room, int32_t *page_table, int32_t table_stride,
+                     int32_t *refs, int32_t *lacking, void *workspace, size_t workspace_bytes);
+
+/* A step of beam search: of every request's n_beams * vocab candidates the k with the largest scores,
+ *   score(beam, token) = scores[beam] + (logit - log(sum over the vocabulary of exp(logits)))
+ * in descending order, compared in 64 bits (ties: lower beam; within a beam the larger logit, then the lower token).  A finished beam has one candidate, end_token
+ * with the beam's score unchanged; its logits are not read.  Candidates without a finite score are not picked (logits or beams at -inf, rows with a NaN or +inf).
+ *   n_seq, n_beams, k   n_beams 1..64, k 1..64, n_seq * n_beams at most 2^20;  vocab 1..2^24
+ *   logits         device [n_seq * n_beams, ld], FOCUS_F32 or FOCUS_BF16;  scores  device [n_seq, n_beams] fp32
+ *   done           device [n_seq, n_beams] bytes, not 0: finished; or NULL
+ *   rows           device [n_seq, k] out: row of logits that a pick continues (what focus_kv_fork takes as parents), -1: none was left
+ *   tokens         device [n_seq, k] out, -1: none;  new_scores  device [n_seq, k] fp32 out, -inf: none
+ *   workspace      device, 256-byte aligned, focus_beam_select_bytes() */
+int focus_beam_select_bytes(int32_t n_seq, int32_t n_beams, int32_t vocab, int32_t k, size_t *bytes);
+int focus_beam_select(void *hip_stream, int32_t n_seq, int32_t n_beams, int32_t vocab, int32_t k, int32_t dtype, const void *logits, int64_t ld, const float *scores,
+                      const uint8_t *done, int32_t end_token, int32_t *rows, int32_t *tokens, float *new_scores, void *workspace, size_t workspace_bytes);
+
 #ifdef __cplusplus
 }
 #endif

@@ -68,6 +68,10 @@ class focus_mx(C.Structure):
     _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p)]
 
 
+class focus_kv(C.Structure):
+    _fields_ = [("pool", C.c_void_p)] + [(n, C.c_int32) for n in ("dtype", "n_layers", "n_pages", "page_size", "n_kv_heads", "head_dim")]
+
+
 _MX_FIELDS = ("w_gate_up", "w_down", "w_expert_gate_up", "w_expert_down", "w_shared_gate_up", "w_shared_down")
 
 
@@ -114,6 +118,16 @@ def load_library() -> C.CDLL:
         "focus_mx_experts": [P, I, I, I, C.POINTER(focus_mx), C.POINTER(focus_mx), I, I, P, C.c_int64, P, P, I, P, C.c_int64, I, P, C.c_size_t],
         "focus_set_router": [P, C.POINTER(focus_router), C.POINTER(P)],
         "focus_set_mx_weights": [P, C.POINTER(focus_mx_weights)],
+        "focus_kv_append": [C.POINTER(focus_kv), P, I, I, I, P, P, P, I, P, C.c_int64, P, C.c_int64],
+        "focus_tree_attention_bytes": [C.POINTER(focus_kv), I, I, I, I, I, I, SZ],
+        "focus_tree_attention": [C.POINTER(focus_kv), P, I, I, I, I, I, P, P, P, I, P, I, I, C.c_float, P, C.c_int64, P, C.c_int64, P, C.c_size_t],
+        "focus_kv_compact": [C.POINTER(focus_kv), P, I, I, P, P, P, P, I, P, I],
+        "focus_kv_fork_bytes": [I, SZ],
+        "focus_kv_fork": [C.POINTER(focus_kv), P, I, I, P, P, P, I, P, P, P, P, P, C.c_size_t],
+        "focus_kv_reserve_bytes": [I, SZ],
+        "focus_kv_reserve": [P, I, I, I, P, I, P, I, P, P, P, C.c_size_t],
+        "focus_beam_select_bytes": [I, I, I, I, SZ],
+        "focus_beam_select": [P, I, I, I, I, I, P, C.c_int64, P, P, I, P, P, P, P, C.c_size_t],
     }
     for name, args in sig.items():
         f = getattr(lib, name)
@@ -126,7 +140,9 @@ _lib = load_library()
 EXPORTS = ["focus_workspace_bytes", "focus_kv_pool_bytes", "focus_init", "focus_prefill_kv", "focus_step",
            "focus_select_compact", "focus_select_compact_noalloc", "focus_commit", "focus_run_layers", "focus_finalize_blocks", "focus_set_route_override", "focus_set_row_hint", "focus_run_steps", "focus_get_state", "focus_set_state", "focus_set_timing",
            "focus_get_kernel_time", "focus_free", "focus_last_error", "focus_route", "focus_mx_quantize", "focus_mx_dequantize",
-           "focus_mx_gemm_bytes", "focus_mx_gemm", "focus_mx_experts_bytes", "focus_mx_experts", "focus_set_router", "focus_set_mx_weights"]
+           "focus_mx_gemm_bytes", "focus_mx_gemm", "focus_mx_experts_bytes", "focus_mx_experts", "focus_set_router", "focus_set_mx_weights",
+           "focus_kv_append", "focus_tree_attention_bytes", "focus_tree_attention", "focus_kv_compact", "focus_kv_fork_bytes", "focus_kv_fork", "focus_kv_reserve_bytes",
+           "focus_kv_reserve", "focus_beam_select_bytes", "focus_beam_select"]
 
 
 def _check(rc: int, ctx=None):
@@ -362,6 +378,212 @@ def focus_mx_experts(gate_up, down, x: torch.Tensor, experts: torch.Tensor, weig
     if rc:
         _check(rc)
     return out
+
+
+# -- generation that branches over the paged cache (no context) ---------------------------------------
+# A pool is a contiguous tensor [n_layers, n_pages, 2, H_kv, page_size, D], fp32 or bf16 (the values, its second half, are kept transposed: [H_kv, D, page_size]).
+# Page tables [rows, stride], lengths, reference counts and lists are contiguous int32 tensors.
+
+def _kv_of(pool: torch.Tensor) -> focus_kv:
+    shape = pool.shape
+    code = _DTYPES.get(pool.dtype)
+    if len(shape) != 6 or shape[2] != 2 or code is None or not pool.is_contiguous():
+        _bad("a pool is a contiguous fp32 or bf16 tensor [n_layers, n_pages, 2, H_kv, page_size, D]")
+    _int32(*shape)
+    return focus_kv(pool.data_ptr(), code, shape[0], shape[1], shape[4], shape[3], shape[5])
+
+
+def _table_of(table: torch.Tensor, name: str, device):
+    """(rows, stride) of a page table."""
+    if table.dim() != 2 or table.dtype != torch.int32 or not table.is_contiguous() or table.device != device:
+        _bad("%s must be a contiguous int32 matrix on %s", name, device)
+    _int32(*table.shape)
+    return table.shape
+
+
+def _cu_of(cu: torch.Tensor, name: str, n: int, device):
+    _plain(cu, name, (n + 1,), torch.int32, device)
+    return cu.data_ptr()
+
+
+def focus_kv_append(pool: torch.Tensor, layer: int, k: torch.Tensor, v: torch.Tensor, cu_rows: torch.Tensor, lens: torch.Tensor, page_table: torch.Tensor, stream=None):
+    """Rows of k and v [rows, H_kv * D] become the next tokens of their sequences: row r of sequence b (cu_rows[b] <= r < cu_rows[b + 1]) token
+    lens[b] + r - cu_rows[b] of a layer of the pool."""
+    kv, dev = _kv_of(pool), pool.device
+    to = _begin(dev, stream)
+    n, stride = _table_of(page_table, "page_table", dev)
+    rows, cols, ldk, k_type = _rows_of(k, "k")
+    v_rows, v_cols, ldv, v_type = _rows_of(v, "v")
+    if k.device != dev or v.device != dev or k_type != kv.dtype or v_type != kv.dtype or v_rows != rows or cols != kv.n_kv_heads * kv.head_dim or v_cols != cols:
+        _bad("k and v must be matrices [rows, %d] of the pool's type on %s", kv.n_kv_heads * kv.head_dim, dev)
+    _plain(lens, "lens", (n,), torch.int32, dev)
+    _int32(layer)
+    rc = _lib.focus_kv_append(kv, to, layer, n, rows, _cu_of(cu_rows, "cu_rows", n, dev), lens.data_ptr(), page_table.data_ptr(), stride, k.data_ptr(), ldk, v.data_ptr(), ldv)
+    if rc:
+        _check(rc)
+
+
+def focus_tree_attention(pool: torch.Tensor, layer: int, q: torch.Tensor, cu_rows: torch.Tensor, lens: torch.Tensor, page_table: torch.Tensor,
+                         seen: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, scale: Optional[float] = None, max_rows: int = 0, max_len: int = 0,
+                         workspace: Optional[torch.Tensor] = None, stream=None):
+    """Attention of the query rows q [rows, H_q * D] over the cached tokens of their sequences and over the drafted ones behind them that the bits of seen
+    ([rows] or [rows, words] int64, contiguous; None: a chain) show.  max_rows, max_len: the most rows of a sequence, and the longest lens[b] + rows, as far as
+    the caller knows.  scale: 1 / sqrt(D)."""
+    kv, dev = _kv_of(pool), pool.device
+    to = _begin(dev, stream)
+    n, stride = _table_of(page_table, "page_table", dev)
+    rows, cols, ldq, q_type = _rows_of(q, "q")
+    if q.device != dev or q_type != kv.dtype or cols % kv.head_dim or cols == 0:
+        _bad("q must be a matrix of heads of %d, of the pool's type, on %s", kv.head_dim, dev)
+    if out is None:
+        out = _new((rows, cols), q.dtype, dev, stream)
+        ldo = cols
+    else:
+        out_rows, out_cols, ldo, out_type = _rows_of(out, "out")
+        if out_rows != rows or out_cols != cols or out_type != q_type or out.device != dev:
+            _bad("out must be like q")
+    words = 0
+    if seen is not None:
+        words = seen.shape[1] if seen.dim() == 2 else 1
+        _int32(words)
+        _plain(seen, "seen", (rows, words) if seen.dim() == 2 else (rows,), torch.int64, dev)
+    _plain(lens, "lens", (n,), torch.int32, dev)
+    _int32(layer, max_rows, max_len)
+    heads = cols // kv.head_dim
+    if workspace is None:
+        nbytes = C.c_size_t()
+        rc = _lib.focus_tree_attention_bytes(kv, n, rows, max_rows, max_len, stride, heads, nbytes)
+        if rc:
+            _check(rc)
+        ws, ws_bytes, keep = _scratch(None, nbytes.value, dev, stream)
+    else:
+        ws, ws_bytes, keep = _scratch(workspace, 0, dev, stream)
+    rc = _lib.focus_tree_attention(kv, to, layer, n, rows, max_rows, max_len, _cu_of(cu_rows, "cu_rows", n, dev), lens.data_ptr(), page_table.data_ptr(), stride,
+                                   None if seen is None else seen.data_ptr(), words, heads, kv.head_dim ** -0.5 if scale is None else scale, q.data_ptr(), ldq,
+                                   out.data_ptr(), ldo, ws, ws_bytes)
+    if rc:
+        _check(rc)
+    return out
+
+
+def focus_kv_compact(pool: torch.Tensor, start: torch.Tensor, cu_keep: torch.Tensor, keep: torch.Tensor, page_table: torch.Tensor, to_table: Optional[torch.Tensor] = None,
+                     stream=None):
+    """Token start[b] + keep[cu_keep[b] + i] of row b's pages in page_table becomes token start[b] + i of its pages in to_table (None: page_table, in place), in
+    every layer.  keep ascends within a sequence."""
+    kv, dev = _kv_of(pool), pool.device
+    to = _begin(dev, stream)
+    n, stride = _table_of(page_table, "page_table", dev)
+    if to_table is None:
+        to_table = page_table
+    to_rows, to_stride = _table_of(to_table, "to_table", dev)
+    if to_rows != n:
+        _bad("to_table must have a row for each of page_table")
+    _plain(start, "start", (n,), torch.int32, dev)
+    if keep.dim() != 1:
+        _bad("keep must be a list")
+    _int32(keep.shape[0])
+    _plain(keep, "keep", keep.shape, torch.int32, dev)
+    rc = _lib.focus_kv_compact(kv, to, n, keep.shape[0], start.data_ptr(), _cu_of(cu_keep, "cu_keep", n, dev), keep.data_ptr(), page_table.data_ptr(), stride, to_table.data_ptr(),
+                               to_stride)
+    if rc:
+        _check(rc)
+
+
+def _int32_out(t: Optional[torch.Tensor], name: str, shape, device, stream):
+    if t is None:
+        return _new(shape, torch.int32, device, stream)
+    _plain(t, name, shape, torch.int32, device)
+    return t
+
+
+def focus_kv_fork(pool: torch.Tensor, parents: torch.Tensor, lens: torch.Tensor, page_table: torch.Tensor, refs: torch.Tensor, new_lens: Optional[torch.Tensor] = None,
+                  new_table: Optional[torch.Tensor] = None, lacking: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None):
+    """(new_lens, new_table, lacking) of rows that continue the rows parents of page_table; refs [n_pages], how many entries hold a page, follows.  No parents: all
+    rows give their pages back."""
+    kv, dev = _kv_of(pool), pool.device
+    to = _begin(dev, stream)
+    n_old, stride = _table_of(page_table, "page_table", dev)
+    if parents.dim() != 1:
+        _bad("parents must be a list")
+    n_new = parents.shape[0]
+    _int32(n_new)
+    _plain(parents, "parents", (n_new,), torch.int32, dev)
+    _plain(lens, "lens", (n_old,), torch.int32, dev)
+    _plain(refs, "refs", (kv.n_pages,), torch.int32, dev)
+    new_lens = _int32_out(new_lens, "new_lens", (n_new,), dev, stream)
+    new_table = _int32_out(new_table, "new_table", (n_new, stride), dev, stream)
+    lacking = _int32_out(lacking, "lacking", (n_new,), dev, stream)
+    if workspace is None:
+        nbytes = C.c_size_t()
+        rc = _lib.focus_kv_fork_bytes(n_new, nbytes)
+        if rc:
+            _check(rc)
+        ws, ws_bytes, keep = _scratch(None, nbytes.value, dev, stream)
+    else:
+        ws, ws_bytes, keep = _scratch(workspace, 0, dev, stream)
+    rc = _lib.focus_kv_fork(kv, to, n_old, n_new, parents.data_ptr(), lens.data_ptr(), page_table.data_ptr(), stride, new_lens.data_ptr(), new_table.data_ptr(),
+                            refs.data_ptr(), lacking.data_ptr(), ws, ws_bytes)
+    if rc:
+        _check(rc)
+    return new_lens, new_table, lacking
+
+
+def focus_kv_reserve(lens: torch.Tensor, room: int, page_table: torch.Tensor, refs: torch.Tensor, page_size: int, lacking: Optional[torch.Tensor] = None,
+                     workspace: Optional[torch.Tensor] = None, stream=None):
+    """Gives the rows of page_table the pages that lens + room tokens need; returns how many pages each still lacks."""
+    dev = page_table.device
+    to = _begin(dev, stream)
+    n, stride = _table_of(page_table, "page_table", dev)
+    if refs.dim() != 1:
+        _bad("refs must be a list")
+    _int32(refs.shape[0], room, page_size)
+    _plain(refs, "refs", refs.shape, torch.int32, dev)
+    _plain(lens, "lens", (n,), torch.int32, dev)
+    lacking = _int32_out(lacking, "lacking", (n,), dev, stream)
+    if workspace is None:
+        nbytes = C.c_size_t()
+        rc = _lib.focus_kv_reserve_bytes(n, nbytes)
+        if rc:
+            _check(rc)
+        ws, ws_bytes, keep = _scratch(None, nbytes.value, dev, stream)
+    else:
+        ws, ws_bytes, keep = _scratch(workspace, 0, dev, stream)
+    rc = _lib.focus_kv_reserve(to, n, page_size, refs.shape[0], lens.data_ptr(), room, page_table.data_ptr(), stride, refs.data_ptr(), lacking.data_ptr(), ws, ws_bytes)
+    if rc:
+        _check(rc)
+    return lacking
+
+
+def focus_beam_select(logits: torch.Tensor, scores: torch.Tensor, k: int, done: Optional[torch.Tensor] = None, end_token: int = 0, rows: Optional[torch.Tensor] = None,
+                      tokens: Optional[torch.Tensor] = None, new_scores: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None):
+    """(rows, tokens, new_scores), each [n, k]: the k best of every request's candidates; logits [n * n_beams, vocab] fp32 or bf16, scores [n, n_beams] fp32, done
+    [n, n_beams] bool or uint8.  rows are rows of logits, -1 where no candidate was left."""
+    n_rows, vocab, ld, dtype = _rows_of(logits, "logits")
+    dev = logits.device
+    to = _begin(dev, stream)
+    if scores.dim() != 2 or scores.shape[0] * scores.shape[1] != n_rows:
+        _bad("scores must be a matrix with a value for each of the %d rows of logits", n_rows)
+    n, beams = scores.shape
+    _int32(n, beams, k, end_token)
+    _plain(scores, "scores", (n, beams), torch.float32, dev)
+    if done is not None:
+        _plain(done, "done", (n, beams), torch.bool if done.dtype == torch.bool else torch.uint8, dev)
+    nbytes = C.c_size_t()
+    rc = _lib.focus_beam_select_bytes(n, beams, vocab, k, nbytes)
+    if rc:
+        _check(rc)
+    rows = _int32_out(rows, "rows", (n, k), dev, stream)
+    tokens = _int32_out(tokens, "tokens", (n, k), dev, stream)
+    if new_scores is None:
+        new_scores = _new((n, k), torch.float32, dev, stream)
+    else:
+        _plain(new_scores, "new_scores", (n, k), torch.float32, dev)
+    ws, ws_bytes, keep = _scratch(workspace, nbytes.value, dev, stream)
+    rc = _lib.focus_beam_select(to, n, beams, vocab, k, dtype, logits.data_ptr(), ld, scores.data_ptr(), None if done is None else done.data_ptr(), end_token,
+                                rows.data_ptr(), tokens.data_ptr(), new_scores.data_ptr(), ws, ws_bytes)
+    if rc:
+        _check(rc)
+    return rows, tokens, new_scores
 
 
 def make_step_out(**tensors) -> focus_step_out:

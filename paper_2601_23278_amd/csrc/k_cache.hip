@@ -1,0 +1,341 @@
+// The paged cache of sequences that branch: rows of K/V into pages, tokens that stay moved together, pages shared, copied, given out and given back.
+//
+// A page holds K [H_kv][P][D], then V transposed [H_kv][D][P]: a token is a row of 2 D bytes (bf16) in K and a column in V.  All of these are bound by
+// the bytes they move (nothing is computed) or, for a request's few tokens, by a chain of dependent loads: row -> sequence -> page -> data.
+#include "focus_branch.h"
+
+namespace fk {
+
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+template <int ES> struct Word;
+template <> struct Word<2> { typedef uint16_t type; };
+template <> struct Word<4> { typedef uint32_t type; };
+
+// ---------------------------------------------------------------------------------------------
+// Append.  A workgroup takes 64 rows of one kv head (in row order, whatever their sequences).  K rows are copied in 16-byte pieces; V goes through LDS, so that
+// the lanes of a wavefront are 64 rows and a store of one d writes neighbouring tokens of a page.
+template <int ES, int D>
+__global__ __launch_bounds__(256) void k_append(AppendArgs a) {
+  typedef typename Word<ES>::type T;
+  constexpr int PIECES = D * ES / 16, PER = 16 / ES;
+  __shared__ int page_s[64], place_s[64];
+  __shared__ T vs[64][D + 16 / ES / 2];
+  const int r0 = blockIdx.x * 64, h = blockIdx.y, tid = threadIdx.x, P = a.g.page_size;
+  if (tid < 64) {
+    const int r = r0 + tid;
+    int page = -1, place = 0;
+    if (r < a.n_rows && r >= a.cu[0] && r < a.cu[a.n_seq]) {
+      const int b = sequence_of(a.cu, a.n_seq, r);
+      const int64_t t = (int64_t)max(a.lens[b], 0) + r - a.cu[b];
+      page = page_of_token(a.g, a.g.table, a.g.stride, b, t);
+      place = (int)(t % P);
+    }
+    page_s[tid] = page;
+    place_s[tid] = place;
+  }
+  __syncthreads();
+  const T *k = (const T *)a.k + (size_t)h * D, *v = (const T *)a.v + (size_t)h * D;
+  const size_t page_size = page_bytes(a.g, D, ES);
+  const bool wide = ((uintptr_t)k % 16 == 0) && ((uintptr_t)v % 16 == 0) && (a.ldk * ES) % 16 == 0 && (a.ldv * ES) % 16 == 0;
+  for (int i = tid; i < 64 * PIECES; i += 256) {
+    const int row = i / PIECES, c = i % PIECES, page = page_s[row];
+    if (page < 0) continue;
+    T *to = (T *)(a.g.pool + (size_t)page * page_size) + ((size_t)h * P + place_s[row]) * D + c * PER;
+    const T *kr = k + (size_t)(r0 + row) * a.ldk + c * PER, *vr = v + (size_t)(r0 + row) * a.ldv + c * PER;
+    if (wide) {
+      const u32x4 kk = *(const u32x4 *)kr, vv = *(const u32x4 *)vr;
+      *(u32x4 *)to = kk;
+#pragma unroll
+      for (int e = 0; e < PER; ++e) vs[row][c * PER + e] = ((const T *)&vv)[e];
+    } else {
+      for (int e = 0; e < PER; ++e) {
+        to[e] = kr[e];
+        vs[row][c * PER + e] = vr[e];
+      }
+    }
+  }
+  __syncthreads();
+  const int row = tid & 63, page = page_s[row];
+  if (page < 0) return;
+  T *to = (T *)(a.g.pool + (size_t)page * page_size) + (size_t)(a.g.n_kv_heads + h) * P * D + place_s[row];
+  for (int d = tid >> 6; d < D; d += 4) to[(size_t)d * P] = vs[row][d];
+}
+
+void kv_append(hipStream_t s, const AppendArgs &a) {
+  const dim3 grid((a.n_rows + 63) / 64, a.g.n_kv_heads);
+  if (a.dtype == FOCUS_F32)
+    a.head_dim == 64 ? k_append<4, 64><<<grid, 256, 0, s>>>(a) : k_append<4, 128><<<grid, 256, 0, s>>>(a);
+  else
+    a.head_dim == 64 ? k_append<2, 64><<<grid, 256, 0, s>>>(a) : k_append<2, 128><<<grid, 256, 0, s>>>(a);
+}
+
+// ---------------------------------------------------------------------------------------------
+// Compaction.  A workgroup takes one (sequence, head, layer) and moves its tokens 64 at a time, in ascending order.  In place that is safe: place i is read from
+// place keep[i] >= i, a batch is read whole before any of it is written, and later batches read places behind everything that was written.
+template <int ES, int D>
+__global__ __launch_bounds__(256) void k_compact(CompactArgs a) {
+  typedef typename Word<ES>::type T;
+  constexpr int PIECES = D * ES / 16, NK = 64 * PIECES / 256, NV = D / 4;
+  __shared__ int from_s[64], from_at[64], to_s[64], to_at[64];
+  const int H = a.g.n_kv_heads, b = blockIdx.x / H, h = blockIdx.x % H, tid = threadIdx.x, P = a.g.page_size;
+  const int c0 = min(max(a.cu[b], 0), a.n_keep), n = min(a.cu[b + 1], a.n_keep) - c0;
+  const int64_t start = max(a.start[b], 0);
+  const size_t page_size = page_bytes(a.g, D, ES);
+  char *const pool = a.g.pool + (size_t)blockIdx.y * a.g.n_pages * page_size;
+  for (int i0 = 0; i0 < n; i0 += 64) {
+    if (tid < 64) {
+      int from = -1, to = -1;
+      int64_t tf = 0, tt = 0;
+      if (i0 + tid < n) {
+        tf = start + a.keep[c0 + i0 + tid];
+        tt = start + i0 + tid;
+        from = page_of_token(a.g, a.g.table, a.g.stride, b, tf);
+        to = page_of_token(a.g, a.to_table, a.to_stride, b, tt);
+        if (from < 0) to = -1;
+      }
+      from_s[tid] = from; from_at[tid] = (int)(tf % P);
+      to_s[tid] = to; to_at[tid] = (int)(tt % P);
+    }
+    __syncthreads();
+    u32x4 kk[NK];
+    T vv[NV];
+#pragma unroll
+    for (int j = 0; j < NK; ++j) {
+      const int i = tid + 256 * j, t = i / PIECES, c = i % PIECES;
+      if (to_s[t] >= 0) kk[j] = *(const u32x4 *)(pool + (size_t)from_s[t] * page_size + (((size_t)h * P + from_at[t]) * D) * ES + c * 16);
+    }
+    const int t = tid & 63, d0 = tid >> 6;
+    const T *vf = (const T *)(pool + (size_t)max(from_s[t], 0) * page_size) + (size_t)(H + h) * P * D + from_at[t];
+    T *vt = (T *)(pool + (size_t)max(to_s[t], 0) * page_size) + (size_t)(H + h) * P * D + to_at[t];
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+      if (to_s[t] >= 0) vv[j] = vf[(size_t)(d0 + 4 * j) * P];
+    __syncthreads();                                   // the whole batch has been read
+#pragma unroll
+    for (int j = 0; j < NK; ++j) {
+      const int i = tid + 256 * j, t = i / PIECES, c = i % PIECES;
+      if (to_s[t] >= 0) *(u32x4 *)(pool + (size_t)to_s[t] * page_size + (((size_t)h * P + to_at[t]) * D) * ES + c * 16) = kk[j];
+    }
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+      if (to_s[t] >= 0) vt[(size_t)(d0 + 4 * j) * P] = vv[j];
+    __syncthreads();                                   // before the places of the next batch
+  }
+}
+
+void kv_compact(hipStream_t s, const CompactArgs &a) {
+  const dim3 grid(a.n_seq * a.g.n_kv_heads, a.g.n_layers);
+  if (a.dtype == FOCUS_F32)
+    a.head_dim == 64 ? k_compact<4, 64><<<grid, 256, 0, s>>>(a) : k_compact<4, 128><<<grid, 256, 0, s>>>(a);
+  else
+    a.head_dim == 64 ? k_compact<2, 64><<<grid, 256, 0, s>>>(a) : k_compact<2, 128><<<grid, 256, 0, s>>>(a);
+}
+
+// ---------------------------------------------------------------------------------------------
+// Page bookkeeping.
+
+// Entries of a row up to the first negative one; the whole workgroup.
+__device__ int held_pages(const int32_t *row, int stride) {
+  __shared__ int first;
+  for (int j0 = 0; j0 < stride; j0 += blockDim.x) {
+    if (threadIdx.x == 0) first = stride;
+    __syncthreads();
+    const int j = j0 + threadIdx.x;
+    if (j < stride && row[j] < 0) atomicMin(&first, j);
+    __syncthreads();
+    const int f = first;
+    __syncthreads();
+    if (f < stride) return f;
+  }
+  return stride;
+}
+
+// Work buffers of a fork: per new row whether it wants a page, the page it copies from, the page it got (-1: none), and the tokens to copy.
+struct ForkWork {
+  int32_t *start, *from, *to, *tokens;
+};
+__host__ __device__ inline ForkWork fork_work(const ForkArgs &a) {
+  return ForkWork{a.work, a.work + a.n_new + 1, a.work + 2 * (size_t)a.n_new + 1, a.work + 3 * (size_t)a.n_new + 1};
+}
+
+// Workgroups 0 .. n_old - 1: what an old row held changes by its children.  The others: the entries of a new row.  The counts are whole numbers, so the order of
+// the atomics does not show.
+__global__ __launch_bounds__(256) void k_fork_rows(ForkArgs a) {
+  __shared__ int count;
+  const int tid = threadIdx.x, P = a.g.page_size, stride = a.g.stride;
+  const bool old = (int)blockIdx.x < a.n_old;
+  const int i = old ? blockIdx.x : blockIdx.x - a.n_old;
+  const int p = old ? i : a.parents[i];
+  const bool valid = p >= 0 && p < a.n_old;
+  if (tid == 0) count = 0;
+  __syncthreads();
+  int mine = 0;                                        // children of an old row; of a new one, those of its parent before it
+  for (int j = tid; j < (old ? a.n_new : i); j += 256) mine += a.parents[j] == p;
+  if (mine) atomicAdd(&count, mine);
+  __syncthreads();
+  const int32_t *row = a.g.table + (size_t)(valid ? p : 0) * stride;
+  const int held = valid ? held_pages(row, stride) : 0;
+  const int64_t room = (int64_t)held * P;
+  const int len = valid ? (int)min((int64_t)max(a.lens[p], 0), room) : 0;
+  const int whole = len / P, left = len % P;
+  if (old) {
+    for (int j = tid; j < held; j += 256) {
+      const int change = j < whole ? count - 1 : count > 0 ? 0 : -1, page = row[j];
+      if (change && page < a.g.n_pages) atomicAdd(&a.refs[page], change);
+    }
+    return;
+  }
+  const int keeps = count == 0 ? held : whole;         // the first child takes everything
+  int32_t *to = a.new_table + (size_t)i * stride;
+  for (int j = tid; j < stride; j += 256) to[j] = j < keeps ? row[j] : -1;
+  if (tid == 0) {
+    const ForkWork w = fork_work(a);
+    const bool wants = valid && count > 0 && left > 0;
+    a.new_lens[i] = len;
+    w.start[i] = wants;
+    w.from[i] = wants ? row[whole] : -1;
+    w.tokens[i] = left;
+    w.to[i] = -1;
+  }
+}
+
+// Sum of v over the threads before this one; *all = the sum of all.  `part` holds one value per wavefront.
+__device__ __forceinline__ int sum_before(int v, int *part, int *all) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = blockDim.x >> 6;
+  int x = v;
+  for (int o = 1; o < 64; o <<= 1) {
+    const int y = __shfl_up(x, o);
+    if (lane >= o) x += y;
+  }
+  if (lane == 63) part[wave] = x;
+  __syncthreads();
+  int before = 0, total = 0;
+  for (int w = 0; w < n; ++w) {
+    if (w < wave) before += part[w];
+    total += part[w];
+  }
+  __syncthreads();
+  *all = total;
+  return before + x - v;
+}
+
+// One workgroup.  start[i]: pages that row i wants; becomes the number of pages wanted by the rows before it.  Returns the sum.
+__device__ int order_wants(int32_t *start, int n, int *part) {
+  int total = 0;
+  for (int i0 = 0; i0 < n; i0 += blockDim.x) {
+    const int i = i0 + threadIdx.x, v = i < n ? start[i] : 0;
+    int all;
+    const int before = sum_before(v, part, &all);
+    if (i < n) start[i] = total + before;
+    total += all;
+  }
+  if (threadIdx.x == 0) start[n] = total;
+  __syncthreads();
+  return total;
+}
+
+// One workgroup: hands the lowest free pages out, give(rank, page) for page number `rank` of those wanted.  Returns how many there were.
+template <typename F>
+__device__ int hand_out(int32_t *refs, int n_pages, int wanted, int *part, F give) {
+  int found = 0;
+  for (int p0 = 0; p0 < n_pages && found < wanted; p0 += 4 * blockDim.x) {
+    const int p = p0 + 4 * threadIdx.x;
+    int free[4], mine = 0, all;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) mine += free[e] = p + e < n_pages && refs[p + e] == 0;
+    int rank = found + sum_before(mine, part, &all);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (free[e]) {
+        if (rank < wanted) {
+          refs[p + e] = 1;
+          give(rank, p + e);
+        }
+        ++rank;
+      }
+    found += all;
+  }
+  __syncthreads();
+  return min(found, wanted);
+}
+
+__global__ __launch_bounds__(1024) void k_fork_pages(ForkArgs a) {
+  __shared__ int part[16];
+  const ForkWork w = fork_work(a);
+  const int wanted = order_wants(w.start, a.n_new, part);
+  const int got = hand_out(a.refs, a.g.n_pages, wanted, part, [&](int rank, int page) {
+    const int i = sequence_of(w.start, a.n_new, rank);            // the row that wants page number `rank`
+    w.to[i] = page;
+    a.new_table[(size_t)i * a.g.stride + a.new_lens[i] / a.g.page_size] = page;
+  });
+  for (int i = threadIdx.x; i < a.n_new; i += blockDim.x) {
+    const bool lacks = w.start[i + 1] > w.start[i] && w.start[i] >= got;
+    a.lacking[i] = lacks;
+    if (lacks) a.new_lens[i] -= w.tokens[i];
+  }
+}
+
+// The tokens of a page that has begun, into a page of the row's own: one head of one layer a workgroup.
+template <int ES>
+__global__ __launch_bounds__(256) void k_fork_copy(ForkArgs a) {
+  typedef typename Word<ES>::type T;
+  constexpr int PER = 16 / ES;
+  const ForkWork w = fork_work(a);
+  const int H = a.g.n_kv_heads, i = blockIdx.x / H, h = blockIdx.x % H, P = a.g.page_size, D = a.head_dim;
+  const int from = w.from[i], to = w.to[i], n = w.tokens[i];
+  if (to < 0 || from < 0 || from >= a.g.n_pages) return;
+  const size_t page_size = page_bytes(a.g, D, ES);
+  char *const pool = a.g.pool + (size_t)blockIdx.y * a.g.n_pages * page_size;
+  const char *src = pool + (size_t)from * page_size;
+  char *dst = pool + (size_t)to * page_size;
+  const size_t k0 = (size_t)h * P * D * ES, v0 = (size_t)(H + h) * P * D * ES;
+  for (int j = threadIdx.x; j < n * D / PER; j += 256) *(u32x4 *)(dst + k0 + j * 16) = *(const u32x4 *)(src + k0 + j * 16);
+  const int pieces = (n + PER - 1) / PER;
+  for (int j = threadIdx.x; j < D * pieces; j += 256) {
+    const int d = j / pieces, c = j % pieces;
+    const size_t at = v0 + ((size_t)d * P + c * PER) * ES;
+    if ((c + 1) * PER <= n) {
+      *(u32x4 *)(dst + at) = *(const u32x4 *)(src + at);
+    } else {
+      for (int e = 0; c * PER + e < n; ++e) ((T *)(dst + at))[e] = ((const T *)(src + at))[e];
+    }
+  }
+}
+
+void kv_fork(hipStream_t s, const ForkArgs &a) {
+  k_fork_rows<<<a.n_old + a.n_new, 256, 0, s>>>(a);
+  if (a.n_new == 0) return;
+  k_fork_pages<<<1, 1024, 0, s>>>(a);
+  const dim3 grid(a.n_new * a.g.n_kv_heads, a.g.n_layers);
+  a.dtype == FOCUS_F32 ? k_fork_copy<4><<<grid, 256, 0, s>>>(a) : k_fork_copy<2><<<grid, 256, 0, s>>>(a);
+}
+
+// Work buffers of a reservation: pages wanted by the rows before, pages held, pages wanted at all.
+__global__ __launch_bounds__(64) void k_reserve_rows(ReserveArgs a) {
+  const int b = blockIdx.x;
+  const int held = held_pages(a.table + (size_t)b * a.stride, a.stride);
+  if (threadIdx.x == 0) {
+    const int64_t need = ((int64_t)max(a.lens[b], 0) + a.room + a.page_size - 1) / a.page_size, wants = max(need - held, (int64_t)0);
+    a.work[b] = (int)min(wants, (int64_t)(a.stride - held));
+    a.work[a.n_seq + 1 + b] = held;
+    a.work[2 * (size_t)a.n_seq + 1 + b] = (int)wants;
+  }
+}
+
+__global__ __launch_bounds__(1024) void k_reserve_pages(ReserveArgs a) {
+  __shared__ int part[16];
+  int32_t *const start = a.work, *const held = a.work + a.n_seq + 1, *const wants = a.work + 2 * (size_t)a.n_seq + 1;
+  const int wanted = order_wants(start, a.n_seq, part);
+  const int got = hand_out(a.refs, a.n_pages, wanted, part, [&](int rank, int page) {
+    const int b = sequence_of(start, a.n_seq, rank);
+    a.table[(size_t)b * a.stride + held[b] + rank - start[b]] = page;
+  });
+  for (int b = threadIdx.x; b < a.n_seq; b += blockDim.x) a.lacking[b] = wants[b] - max(0, min(got, start[b + 1]) - start[b]);
+}
+
+void kv_reserve(hipStream_t s, const ReserveArgs &a) {
+  k_reserve_rows<<<a.n_seq, 64, 0, s>>>(a);
+  k_reserve_pages<<<1, 1024, 0, s>>>(a);
+}
+
+}  // namespace fk
