@@ -1,65 +1,623 @@
-// Attention of drafted tokens over the paged cache.
+// Attention of drafted tokens over the paged cache, on the matrix cores.
+//
+// A sequence's query rows that share a key head (rows x heads of the group: its "pairs") are multiplied against one tile of cached tokens after the other, with the
+// running maximum and sum of a softmax, so K and V are read once per (sequence, key head, 32 to 128 pairs) and the kernel is bound by that stream as long as pairs
+// are few.  A wavefront holds 32 pairs, a workgroup 1, 2 or 4 wavefronts on the same tile.
+//
+// Work is a line of tiles: sequence after sequence, key head after key head, block of pairs after block of pairs ("unit"), every unit as many tiles as its
+// sequence is long.  The line is cut into equal pieces, one for each workgroup that the chip holds at once, so lengths need not be alike; the sums of a unit that
+// a cut goes through are put together by a second, small launch in the order of the pieces.  Where the pieces lie follows from the lengths alone.
+//
+// A tile is 128 bytes of V^T rows: 64 bf16 tokens or 32 of fp32; as bytes both types are laid out alike.  Per tile and wavefront
+//   S^T = K Q^T   A = K rows from LDS, B = Q in registers: a lane owns one pair, and its scores are in its own registers
+//   O^T = V^T P^T  the probabilities go as they are into the B operand, V^T rows from LDS are A
+// bf16: v_mfma_f32_32x32x16_bf16; lane l of the first product takes K row sigma(l % 32) (bits 2 and 3 swapped), which makes the eight scores of a lane eight
+// neighbouring tokens.  fp32: v_mfma_f32_32x32x2_f32, four for each 16-byte piece; its own lane layout has four neighbouring tokens already.
+// Probabilities in bf16 are rounded once (2^-8 relative), as operand of the second product; their sum is taken before.
+#include <algorithm>
+
 #include "focus_branch.h"
 
 namespace fk {
 
-template <typename T> __device__ __forceinline__ float to_f(T v) { return (float)v; }
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-// One workgroup of four wavefronts per (row, query head): a wavefront takes every fourth token, all lanes on one token.
-template <typename T, int D>
-__global__ __launch_bounds__(256) void k_tree_row(TreeArgs a) {
-  constexpr int NE = D / 64;
-  __shared__ float osh[4][D], msh[4], lsh[4];
-  const int r = blockIdx.x, hq = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  if (r < a.cu[0] || r >= a.cu[a.n_seq]) return;
-  const int H = a.g.n_kv_heads, P = a.g.page_size, h = hq / (a.n_q_heads / H);
-  const int b = sequence_of(a.cu, a.n_seq, r), r0 = a.cu[b], n = min(a.cu[b + 1], a.n_rows) - r0;
-  const int64_t L = max(a.lens[b], 0), total = min(L + n, (int64_t)a.g.stride * P);
-  const size_t page_size = page_bytes(a.g, D, sizeof(T));
-  float q[NE], o[NE], m = -INFINITY, l = 0.f;
-  for (int e = 0; e < NE; ++e) {
-    q[e] = to_f(((const T *)a.q)[(size_t)r * a.ldq + (size_t)hq * D + lane + 64 * e]);
-    o[e] = 0.f;
-  }
-  for (int64_t t = wave; t < total; t += 4) {
-    if (t >= L) {
-      const int j = (int)(t - L);
-      if (a.seen ? j >= 64 * a.seen_words || !((a.seen[(size_t)r * a.seen_words + j / 64] >> (j % 64)) & 1) : j > r - r0) continue;
-    }
-    const int page = page_of_token(a.g, a.g.table, a.g.stride, b, t);
-    if (page < 0) continue;
-    const T *kp = (const T *)(a.g.pool + (size_t)page * page_size) + ((size_t)h * P + t % P) * D;
-    const T *vp = (const T *)(a.g.pool + (size_t)page * page_size) + (size_t)(H + h) * P * D + t % P;
-    float s = 0.f;
-    for (int e = 0; e < NE; ++e) s += q[e] * to_f(kp[lane + 64 * e]);
-    for (int x = 32; x > 0; x >>= 1) s += __shfl_xor(s, x);
-    s *= a.scale;
-    const float mn = fmaxf(m, s), mu = mn == -INFINITY ? 0.f : mn, corr = __expf(m - mu), p = __expf(s - mu);
-    l = l * corr + p;
-    for (int e = 0; e < NE; ++e) o[e] = o[e] * corr + p * to_f(vp[(size_t)(lane + 64 * e) * P]);
-    m = mn;
-  }
-  for (int e = 0; e < NE; ++e) osh[wave][lane + 64 * e] = o[e];
-  if (lane == 0) { msh[wave] = m; lsh[wave] = l; }
-  __syncthreads();
-  if (threadIdx.x >= D) return;
-  float mm = fmaxf(fmaxf(msh[0], msh[1]), fmaxf(msh[2], msh[3])), num = 0.f, den = 0.f;
-  for (int w = 0; w < 4; ++w) {
-    const float c = msh[w] == -INFINITY ? 0.f : __expf(msh[w] - mm);
-    den += lsh[w] * c;
-    num += osh[w][threadIdx.x] * c;
-  }
-  ((T *)a.out)[(size_t)r * a.ldo + (size_t)hq * D + threadIdx.x] = (T)(den == 0.f ? 0.f : num / den);
+// s_waitcnt immediate that waits for at most n outstanding vector-memory operations and for nothing else
+constexpr int vmcnt_imm(int n) { return (n & 15) | ((n >> 4) << 14) | (7 << 4) | (15 << 8); }
+#define FK_LDS_PTR(p) ((__attribute__((address_space(3))) void *)(p))
+#define FK_GLB_PTR(p) ((const __attribute__((address_space(1))) void *)(p))
+constexpr int kNonTemporal = 2;      // cache policy of a load (NT bit)
+
+// How a call's line of tiles is cut.
+struct TreePlan {
+  int nw;                  // wavefronts of a workgroup, 32 pairs each
+  int pieces;              // workgroups
+  bool cut;                // pieces end anywhere; else at the end of a unit (no room for partial sums)
+  bool starts_given;       // `starts` was written by an earlier launch
+  int64_t *starts;         // [n_seq + 1] first tile (cut) or unit of every sequence
+  float *part_o, *part_ml; // [2 * pieces, nw * 32, D] and [.., 2]: sums of a piece's first unit, if it began before, and of its last one, if it goes on
+};
+constexpr int kFewSequences = 256;   // so many starts are summed up by every workgroup for itself
+
+__device__ __forceinline__ int rows_of(const TreeArgs &a, int b) { return max(0, min(a.cu[b + 1], a.n_rows) - max(a.cu[b], 0)); }
+// Tokens of a sequence that its row of the table has room for (below 2^31 - 64, so that tiles of tokens can be counted in 32 bits)
+__device__ __forceinline__ int tokens_of(const TreeArgs &a, int b, int rows) {
+  const int64_t room = min((int64_t)a.g.stride * a.g.page_size, (int64_t)(1u << 31) - 128);
+  return (int)min((int64_t)max(a.lens[b], 0) + rows, room);
+}
+struct Units {
+  int blocks, tiles;     // blocks of pairs, tiles of tokens
+};
+template <int TT>
+__device__ __forceinline__ Units units_of(const TreeArgs &a, int b, int nw) {
+  const int rows = rows_of(a, b), pairs = rows * (a.n_q_heads / a.g.n_kv_heads);
+  return Units{(pairs + nw * 32 - 1) / (nw * 32), rows > 0 ? (tokens_of(a, b, rows) + TT - 1) / TT : 0};
+}
+template <int TT>
+__device__ __forceinline__ int64_t length_of(const TreeArgs &a, int b, const TreePlan &p) {
+  const Units u = units_of<TT>(a, b, p.nw);
+  return (int64_t)u.blocks * a.g.n_kv_heads * (p.cut ? u.tiles : 1);
 }
 
-size_t tree_scratch(const TreeArgs &a) { return 0; }
+// starts[0 .. n] by a whole wavefront; n at most kFewSequences.
+template <int TT>
+__device__ void sum_starts(const TreeArgs &a, const TreePlan &p, int64_t *starts) {
+  constexpr int PER = kFewSequences / 64;
+  const int lane = threadIdx.x & 63;
+  int64_t v[PER], sum = 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int b = lane * PER + i;
+    v[i] = b < a.n_seq ? length_of<TT>(a, b, p) : 0;
+  }
+#pragma unroll
+  for (int i = 0; i < PER; ++i) sum += v[i];
+  int64_t before = sum;
+  for (int o = 1; o < 64; o <<= 1) {
+    const int64_t y = __shfl_up((long long)before, o);
+    if (lane >= o) before += y;
+  }
+  before -= sum;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int b = lane * PER + i;
+    if (b < a.n_seq) starts[b] = before;
+    before += v[i];
+    if (b == a.n_seq - 1) starts[a.n_seq] = before;
+  }
+}
+// The same by one workgroup for any number of sequences.
+template <int TT>
+__global__ __launch_bounds__(1024) void k_tree_starts(TreeArgs a, TreePlan p) {
+  __shared__ int64_t part[16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int64_t total = 0;
+  for (int b0 = 0; b0 < a.n_seq; b0 += 1024) {
+    const int b = b0 + threadIdx.x;
+    const int64_t v = b < a.n_seq ? length_of<TT>(a, b, p) : 0;
+    int64_t x = v;
+    for (int o = 1; o < 64; o <<= 1) {
+      const int64_t y = __shfl_up((long long)x, o);
+      if (lane >= o) x += y;
+    }
+    if (lane == 63) part[wave] = x;
+    __syncthreads();
+    int64_t before = 0, all = 0;
+    for (int w = 0; w < 16; ++w) {
+      if (w < wave) before += part[w];
+      all += part[w];
+    }
+    if (b < a.n_seq) p.starts[b] = total + before + x - v;
+    total += all;
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) p.starts[a.n_seq] = total;
+}
+__device__ __forceinline__ int find_start(const int64_t *starts, int n, int64_t at) {     // the last b with starts[b] <= at
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (starts[mid] <= at) lo = mid; else hi = mid;
+  }
+  return lo;
+}
+constexpr int kLeastTiles = 2;       // of a piece
+__device__ __forceinline__ int64_t piece_length(const TreePlan &p, int64_t total) {
+  const int64_t n = (total + p.pieces - 1) / p.pieces;
+  return p.cut && n < kLeastTiles ? kLeastTiles : n < 1 ? 1 : n;
+}
+
+// Whether one of the elements of 16 bytes is an infinity or not a number, and the bytes with zeros in their place.
+template <typename T> __device__ __forceinline__ bool not_finite(u32x4 v) {
+  bool odd = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) odd |= (v[i] & 0x7f800000u) == 0x7f800000u || (sizeof(T) == 2 && (v[i] & 0x7f80u) == 0x7f80u);
+  return odd;
+}
+template <typename T> __device__ __forceinline__ u32x4 finite_part(u32x4 v) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const bool hi = (v[i] & 0x7f800000u) == 0x7f800000u, lo = (v[i] & 0x7f80u) == 0x7f80u;
+    v[i] &= sizeof(T) == 4 ? (hi ? 0u : ~0u) : (lo ? 0xffff0000u : ~0u) & (hi ? 0xffffu : ~0u);
+  }
+  return v;
+}
+// 1 where an element of 16 bytes is +inf (kind 0), -inf (1), not a number (2), else 0.
+template <typename T> __device__ __forceinline__ u32x4 which(u32x4 v, int kind);
+template <> __device__ __forceinline__ u32x4 which<bf16_t>(u32x4 v, int kind) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    unsigned out = 0;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const unsigned x = v[i] >> (16 * h) & 0xffffu;
+      const bool is = kind == 0 ? x == 0x7f80u : kind == 1 ? x == 0xff80u : (x & 0x7fffu) > 0x7f80u;
+      out |= is ? 0x3f80u << (16 * h) : 0u;
+    }
+    v[i] = out;
+  }
+  return v;
+}
+template <> __device__ __forceinline__ u32x4 which<float>(u32x4 v, int kind) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const bool is = kind == 0 ? v[i] == 0x7f800000u : kind == 1 ? v[i] == 0xff800000u : (v[i] & 0x7fffffffu) > 0x7f800000u;
+    v[i] = is ? 0x3f800000u : 0u;
+  }
+  return v;
+}
+
+// acc += A B^T of 16-byte pieces along the contracted index.
+template <typename T> __device__ __forceinline__ f32x16 multiply(u32x4 a, u32x4 b, f32x16 acc);
+template <> __device__ __forceinline__ f32x16 multiply<bf16_t>(u32x4 a, u32x4 b, f32x16 acc) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), acc, 0, 0, 0);
+}
+template <> __device__ __forceinline__ f32x16 multiply<float>(u32x4 a, u32x4 b, f32x16 acc) {
+  const f32x4 x = __builtin_bit_cast(f32x4, a), y = __builtin_bit_cast(f32x4, b);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(x[e], y[e], acc, 0, 0, 0);
+  return acc;
+}
+
+// Token of a tile, counted within 32, that register r of a product of K rows holds for lanes of half `half`.
+template <typename T> __device__ __forceinline__ constexpr int token_of(int r, int half) {
+  return sizeof(T) == 2 ? 16 * (r >> 3) + 8 * half + (r & 7) : 8 * (r >> 2) + 4 * half + (r & 3);
+}
+
+// ONE: a tile lies in one page (the page size is a multiple of the tile's tokens); else groups of 8 tokens are looked up one by one.
+template <typename T, int D, int NW, bool ONE>
+__global__ __launch_bounds__(NW * 64, NW == 1 && D == 128 ? 1 : 2) void k_tree(TreeArgs a, TreePlan plan) {
+  constexpr int ES = sizeof(T), TT = 128 / ES, RB = D * ES, TILE = 128 * D, IPW = TILE / 1024 / NW, LPR = RB / 16;
+  constexpr int KS = RB / 32, U = TT / 32, DS = D / 32, GROUPS = TT / 8;
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[2 * TILE];
+  __shared__ int64_t starts_s[kFewSequences + 1];
+  __shared__ int found_s[NW];
+  unsigned char *const Ks = lds, *const Vs = lds + TILE;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5, col = lane & 31;
+  const int H = a.g.n_kv_heads, g = a.n_q_heads / H, P = a.g.page_size;
+  const int64_t *starts = plan.starts;
+  if (!plan.starts_given) {
+    if (wave == 0) sum_starts<TT>(a, plan, starts_s);
+    __syncthreads();
+    starts = starts_s;
+    if (plan.cut && blockIdx.x == 0)                   // for the launch that puts cut units together
+      for (int i = tid; i <= a.n_seq; i += NW * 64) plan.starts[i] = starts_s[i];
+  }
+  const int64_t total_work = starts[a.n_seq], per = piece_length(plan, total_work);
+  int64_t at = per * blockIdx.x;
+  const int64_t end = min(at + per, total_work);
+  if (at >= end) return;
+
+  // K rows of 1 KB a load instruction: lane l fills the 16-byte slot l of a 1 KB block of LDS, so the swizzle against bank conflicts is applied to what it fetches.
+  auto swizzle = [](int row) { return RB == 128 ? (row >> 1) & 7 : row & 15; };
+  int k_row[IPW], k_off[IPW], v_row[IPW], v_chunk[IPW];
+#pragma unroll
+  for (int q = 0; q < IPW; ++q) {
+    const int blk = wave * IPW + q;
+    k_row[q] = blk * (1024 / RB) + lane / LPR;
+    k_off[q] = ((lane % LPR) ^ swizzle(k_row[q])) * 16;
+    v_row[q] = blk * 8 + (lane >> 3);
+    v_chunk[q] = (lane & 7) ^ ((v_row[q] >> 1) & 7);
+  }
+  const size_t page_size = page_bytes(a.g, D, ES);
+  const bool wide_q = ((uintptr_t)a.q | (uintptr_t)(a.ldq * ES)) % 16 == 0, wide_o = ((uintptr_t)a.out | (uintptr_t)(a.ldo * ES)) % 16 == 0;
+  // The scale's sign goes into Q; a scale of zero makes Q zero.
+  const float sc = a.scale == 0.f ? 1.f : fabsf(a.scale) * 1.4426950408889634f;      // scores in the log2 domain
+  const unsigned flip = a.scale < 0.f ? (ES == 2 ? 0x80008000u : 0x80000000u) : 0u;
+
+  int b = find_start(starts, a.n_seq, at);
+  while (at < end) {
+    while (starts[b + 1] <= at) ++b;
+    const Units un = units_of<TT>(a, b, NW);
+    const int64_t in = at - starts[b];
+    const int unit = (int)(plan.cut ? in / un.tiles : in), tile0 = plan.cut ? (int)(in - (int64_t)unit * un.tiles) : 0;
+    const int tile1 = plan.cut ? (int)min((int64_t)un.tiles, tile0 + (end - at)) : un.tiles;
+    at += plan.cut ? tile1 - tile0 : 1;
+    const int h = unit / un.blocks, q0 = (unit % un.blocks) * NW * 32;
+    const int r0 = max(a.cu[b], 0), rows = rows_of(a, b), L = max(a.lens[b], 0), total = tokens_of(a, b, rows);
+    const int pair = q0 + wave * 32 + col;
+    const bool valid = pair < rows * g;
+    const int i_row = valid ? pair / g : 0, r = r0 + i_row, head = h * g + (valid ? pair % g : 0);
+    const int32_t *table = a.g.table + (size_t)b * a.g.stride;
+    const unsigned char *const k_base = (const unsigned char *)a.g.pool + (size_t)h * P * RB, *const v_base = (const unsigned char *)a.g.pool + (size_t)(H + h) * P * RB;
+
+    // Pages.  ONE: lane i holds the page of tile first + i.  Else lane i < GROUPS holds the page of the i-th 8 tokens of the next tile that will be fetched.
+    // A page that is none is read as page 0, and its tokens are masked.
+    int pages, first = tile0;
+    auto page_at = [&](int64_t t) {
+      const int64_t i = t / P;
+      const int p = i < a.g.stride ? table[i] : -1;
+      return p < a.g.n_pages ? p : -1;
+    };
+    auto look_up = [&](int tile) {
+      if (ONE) {
+        pages = page_at((int64_t)min(tile + lane, un.tiles - 1) * TT);
+        first = tile;
+      } else {
+        pages = page_at((int64_t)tile * TT + 8 * (lane & (GROUPS - 1)));
+      }
+    };
+    auto issue_k = [&](int tile) {
+      if (ONE) {
+        const int page = __builtin_amdgcn_readlane(pages, tile - first);
+        const unsigned char *base = k_base + (size_t)max(page, 0) * page_size + (size_t)(tile * (unsigned)TT % P) * RB;
+#pragma unroll
+        for (int q = 0; q < IPW; ++q)
+          __builtin_amdgcn_global_load_lds(FK_GLB_PTR(base + k_row[q] * RB + k_off[q]), FK_LDS_PTR(Ks + (wave * IPW + q) * 1024), 16, 0, kNonTemporal);
+      } else {
+#pragma unroll
+        for (int q = 0; q < IPW; ++q) {
+          const int page = __shfl(pages, k_row[q] >> 3);
+          const unsigned place = ((unsigned)tile * TT + k_row[q]) % P;
+          __builtin_amdgcn_global_load_lds(FK_GLB_PTR(k_base + (size_t)max(page, 0) * page_size + (size_t)place * RB + k_off[q]), FK_LDS_PTR(Ks + (wave * IPW + q) * 1024), 16, 0, kNonTemporal);
+        }
+      }
+    };
+    auto issue_v = [&](int tile, int pg) {
+      if (ONE) {
+        const int page = __builtin_amdgcn_readlane(pg, tile - first);
+        const unsigned char *base = v_base + (size_t)max(page, 0) * page_size + (size_t)(tile * (unsigned)TT % P) * ES;
+#pragma unroll
+        for (int q = 0; q < IPW; ++q)
+          __builtin_amdgcn_global_load_lds(FK_GLB_PTR(base + (size_t)v_row[q] * P * ES + v_chunk[q] * 16), FK_LDS_PTR(Vs + (wave * IPW + q) * 1024), 16, 0, kNonTemporal);
+      } else {
+#pragma unroll
+        for (int q = 0; q < IPW; ++q) {
+          const int t = v_chunk[q] * (16 / ES), page = __shfl(pg, t >> 3);
+          const unsigned place = ((unsigned)tile * TT + t) % P;
+          __builtin_amdgcn_global_load_lds(FK_GLB_PTR(v_base + (size_t)max(page, 0) * page_size + ((size_t)v_row[q] * P + place) * ES), FK_LDS_PTR(Vs + (wave * IPW + q) * 1024), 16, 0, kNonTemporal);
+        }
+      }
+    };
+    // Bit i: the page of the tile's i-th 8 tokens is one.
+    auto pages_there = [&](int tile, int pg) -> unsigned {
+      return ONE ? (__builtin_amdgcn_readlane(pg, tile - first) >= 0 ? (1u << GROUPS) - 1 : 0u) : (unsigned)__builtin_amdgcn_ballot_w64(pg >= 0) & ((1u << GROUPS) - 1);
+    };
+    // Word w of the row's set of drafted tokens.
+    auto seen_word = [&](int w) -> uint64_t {
+      if (a.seen) return w >= 0 && w < a.seen_words ? a.seen[(size_t)r * a.seen_words + w] : 0ull;
+      const int last = i_row - 64 * w;
+      return w < 0 || last < 0 ? 0ull : last >= 63 ? ~0ull : (2ull << last) - 1;
+    };
+
+    u32x4 qf[KS];
+    {
+      const T *qp = (const T *)a.q + (size_t)r * a.ldq + (size_t)head * D;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        u32x4 v = {0, 0, 0, 0};
+        const T *from = qp + (2 * ks + half) * (16 / ES);
+        if (valid && a.scale != 0.f) {
+          if (wide_q) {
+            v = *(const u32x4 *)from;
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              v[e] = ES == 2 ? (unsigned)((const uint16_t *)from)[2 * e] | (unsigned)((const uint16_t *)from)[2 * e + 1] << 16 : ((const uint32_t *)from)[e];
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] ^= flip;
+        }
+        qf[ks] = v;
+      }
+    }
+    const uint64_t seen0 = seen_word(0);
+    f32x16 o[DS];
+#pragma unroll
+    for (int i = 0; i < DS; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
+    float m = -INFINITY, l = 0.f;
+
+    // One K buffer and one V buffer, each filled again as soon as the product that reads it is done.  Loads complete in order, so "at most IPW outstanding" means
+    // that the older tile is there.
+    look_up(tile0);
+    __builtin_amdgcn_s_barrier();                      // the unit before has read its last V
+    issue_k(tile0);
+    issue_v(tile0, pages);
+    int pages_v = pages;                               // of the tile whose V is fetched or in use
+    for (int tile = tile0; tile < tile1; ++tile) {
+      const bool more = tile + 1 < tile1;
+      const unsigned there = pages_there(tile, pages_v);
+      if (more && !ONE) look_up(tile + 1);
+      __builtin_amdgcn_s_waitcnt(vmcnt_imm(IPW));      // K of this tile is in LDS
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      f32x16 s[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[u][e] = 0.f;
+        const int tl = 32 * u + (ES == 2 ? (col & ~12) | (col & 4) << 1 | (col & 8) >> 1 : col);
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          const u32x4 kf = *(const u32x4 *)(Ks + tl * RB + (((2 * ks + half) ^ swizzle(tl)) << 4));
+          s[u] = multiply<T>(kf, qf[ks], s[u]);
+        }
+      }
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_s_barrier();                    // every wavefront has read K
+      if (ONE && more && tile + 1 - first == 64) {
+        look_up(tile + 1);
+        __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+      }
+      if (more) issue_k(tile + 1);
+      // Which of the tile's tokens the pair sees: bit t, token tile * TT + t.
+      const int ahead = L - tile * TT;                 // tokens of the tile that are cached ones
+      const bool masked = ahead < TT || there != (1u << GROUPS) - 1;
+      uint64_t mask = ~0ull;
+      if (masked) {
+        if (ahead < TT) {
+          if (ahead > 0) {
+            mask = ((1ull << ahead) - 1) | seen0 << ahead;
+          } else {
+            const int j = -ahead, w = j >> 6, by = j & 63;
+            mask = w == 0 ? seen0 : seen_word(w);
+            if (by) mask = mask >> by | seen_word(w + 1) << (64 - by);
+          }
+          const int left = total - tile * TT;
+          if (left < 64) mask &= (1ull << left) - 1;
+        }
+#pragma unroll
+        for (int i = 0; i < GROUPS; ++i)
+          if (!(there >> i & 1)) mask &= ~(0xffull << (8 * i));
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int word = (int)((unsigned)(mask >> (32 * u)) >> ((ES == 2 ? 8 : 4) * half));      // a lane's tokens at places that the compiler knows
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int keep = __builtin_amdgcn_sbfe(word, token_of<T>(e, 0), 1);
+            s[u][e] = __int_as_float((keep & __float_as_int(s[u][e])) | (~keep & (int)0xff800000));
+          }
+        }
+      }
+      float mx = -INFINITY;
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[u][e]);
+      mx = fmaxf(mx, __shfl_xor(mx, 32)) * sc;
+      const float m_new = fmaxf(m, mx), m_use = m_new == -INFINITY ? 0.f : m_new, corr = __builtin_amdgcn_exp2f(m - m_use);
+      m = m_new;
+      u32x4 pf[4];
+      float sum = 0.f;
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk) {
+#pragma unroll
+        for (int e = 0; e < 16 / ES; ++e) {
+          const int x = kk * (16 / ES) + e;            // register of the scores, counted through
+          const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x >> 4][x & 15], sc, -m_use));
+          sum += p;
+          ((T *)&pf[kk])[e] = (T)p;
+        }
+      }
+      l = l * corr + sum;
+      if (__builtin_amdgcn_ballot_w64(corr != 1.0f) != 0) {       // a pair's maximum moved
+#pragma unroll
+        for (int i = 0; i < DS; ++i)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o[i][e] *= corr;
+      }
+      if (more) __builtin_amdgcn_s_waitcnt(vmcnt_imm(IPW)); else __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));   // V is in LDS
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      auto v_piece = [&](int ds, int kk) {
+        const int vr = 32 * ds + col;
+        return *(const u32x4 *)(Vs + vr * 128 + (((2 * kk + half) ^ ((vr >> 1) & 7)) << 4));
+      };
+      if (masked) {
+        // A weight of zero times what is no number would be none either.  So the product takes the finite values of a tile that not every pair sees whole; where a
+        // token that exists holds others, counts of +inf, -inf and NaN among the tokens that a pair sees are added up in products of their own first.
+        int found = 0;                                 // 1: values that are no numbers; 3: in tokens that exist
+#pragma unroll 2
+        for (int i = 0; i < IPW; ++i) {
+          const int vr = (wave * IPW + i) * 8 + (lane >> 3), t0 = ((lane & 7) ^ ((vr >> 1) & 7)) * (16 / ES);
+          if (not_finite<T>(*(const u32x4 *)(Vs + (wave * IPW + i) * 1024 + lane * 16))) {
+            const bool exists = tile * TT + t0 < total && (there >> (t0 >> 3) & 1);
+            found |= exists ? 3 : 1;
+          }
+        }
+        found = (__builtin_amdgcn_ballot_w64(found & 1) != 0 ? 1 : 0) | (__builtin_amdgcn_ballot_w64(found & 2) != 0 ? 2 : 0);
+        if (NW > 1) {
+          if (lane == 0) found_s[wave] = found;
+          __syncthreads();
+#pragma unroll
+          for (int w = 0; w < NW; ++w) found |= found_s[w];
+        }
+        found = __builtin_amdgcn_readfirstlane(found);
+        if (found & 2) {
+          u32x4 sf[4];
+#pragma unroll
+          for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+            for (int e = 0; e < 16 / ES; ++e) ((T *)&sf[kk])[e] = (T)(float)(mask >> ((2 * kk + half) * (16 / ES) + e) & 1);
+#pragma unroll 1
+          for (int kind = 0; kind < 3; ++kind) {
+            const float is = kind == 0 ? INFINITY : kind == 1 ? -INFINITY : NAN;
+#pragma unroll
+            for (int ds = 0; ds < DS; ++ds) {
+              f32x16 count;
+#pragma unroll
+              for (int e = 0; e < 16; ++e) count[e] = 0.f;
+#pragma unroll
+              for (int kk = 0; kk < 4; ++kk) {
+                count = multiply<T>(which<T>(v_piece(ds, kk), kind), sf[kk], count);
+                asm volatile("" ::: "memory");
+              }
+#pragma unroll
+              for (int e = 0; e < 16; ++e) o[ds][e] += count[e] > 0.f ? is : 0.f;
+            }
+          }
+          __syncthreads();                             // nobody reads the values as they were any more
+        }
+        if (found) {
+#pragma unroll 1
+          for (int i = 0; i < IPW; ++i) {
+            u32x4 *const at_v = (u32x4 *)(Vs + (wave * IPW + i) * 1024 + lane * 16);
+            *at_v = finite_part<T>(*at_v);
+          }
+          __syncthreads();
+        }
+      }
+#pragma unroll
+      for (int ds = 0; ds < DS; ++ds)
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) o[ds] = multiply<T>(v_piece(ds, kk), pf[kk], o[ds]);
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_s_barrier();                    // every wavefront has read V
+      if (more) {
+        pages_v = pages;
+        issue_v(tile + 1, pages_v);
+      }
+    }
+
+    const float l_tot = l + __shfl_xor(l, 32);
+    if (!valid) continue;
+    if (tile0 == 0 && tile1 == un.tiles) {
+      const float inv = l_tot == 0.f ? 0.f : 1.0f / l_tot;
+      T *to = (T *)a.out + (size_t)r * a.ldo + (size_t)head * D;
+#pragma unroll
+      for (int ds = 0; ds < DS; ++ds)
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) {
+          T v[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = (T)(o[ds][4 * q4 + e] * inv);
+          T *t = to + 32 * ds + 8 * q4 + 4 * half;
+          if (wide_o) {
+            if (ES == 2) *(uint64_t *)t = __builtin_bit_cast(uint64_t, *(const bf16x4 *)v); else *(f32x4 *)t = *(const f32x4 *)v;
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) t[e] = v[e];
+          }
+        }
+    } else {
+      const size_t slot = ((size_t)2 * blockIdx.x + (tile0 == 0)) * (NW * 32) + wave * 32 + col;
+      float *po = plan.part_o + slot * D;
+#pragma unroll
+      for (int ds = 0; ds < DS; ++ds)
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4)
+          *(f32x4 *)(po + 32 * ds + 8 * q4 + 4 * half) = f32x4{o[ds][4 * q4], o[ds][4 * q4 + 1], o[ds][4 * q4 + 2], o[ds][4 * q4 + 3]};
+      if (half == 0) {
+        plan.part_ml[slot * 2] = m;
+        plan.part_ml[slot * 2 + 1] = l_tot;
+      }
+    }
+  }
+}
+
+// Units that a cut went through: out = sum_i o_i 2^(m_i - M) / sum_i l_i 2^(m_i - M) over the pieces in their order.  D / 4 lanes per (row, query head).
+template <typename T, int D>
+__global__ __launch_bounds__(256) void k_tree_join(TreeArgs a, TreePlan plan) {
+  constexpr int TT = 128 / sizeof(T), LANES = D / 4, PER = 256 / LANES;
+  const int64_t id = (int64_t)blockIdx.x * PER + threadIdx.x / LANES;
+  const int c = threadIdx.x % LANES;
+  const int r = (int)(id / a.n_q_heads), head = (int)(id % a.n_q_heads);
+  if (r >= a.n_rows || r < a.cu[0] || r >= a.cu[a.n_seq]) return;
+  const int b = sequence_of(a.cu, a.n_seq, r), g = a.n_q_heads / a.g.n_kv_heads, h = head / g;
+  const Units un = units_of<TT>(a, b, plan.nw);
+  const int pair = (r - max(a.cu[b], 0)) * g + head % g, per_block = plan.nw * 32;
+  const int64_t from = plan.starts[b] + ((int64_t)h * un.blocks + pair / per_block) * un.tiles, per = piece_length(plan, plan.starts[a.n_seq]);
+  const int64_t w0 = from / per, w1 = (from + un.tiles - 1) / per;
+  if (w0 == w1) return;
+  auto slot_of = [&](int64_t w) { return (size_t)(2 * w + (w == w0)) * per_block + pair % per_block; };
+  float mm = -INFINITY;
+  for (int64_t w = w0; w <= w1; ++w) mm = fmaxf(mm, plan.part_ml[slot_of(w) * 2]);
+  f32x4 num = {0.f, 0.f, 0.f, 0.f};
+  float den = 0.f;
+  for (int64_t w = w0; w <= w1; ++w) {
+    const size_t s = slot_of(w);
+    const float m = plan.part_ml[s * 2], k = m == -INFINITY ? 0.f : exp2f(m - mm);
+    const f32x4 v = *(const f32x4 *)(plan.part_o + s * D + c * 4);
+    den += plan.part_ml[s * 2 + 1] * k;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) num[e] += m == -INFINITY ? 0.f : v[e] * k;
+  }
+  const float inv = den == 0.f ? 0.f : 1.0f / den;
+  T *to = (T *)a.out + (size_t)r * a.ldo + (size_t)head * D + c * 4;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) to[e] = (T)(num[e] * inv);
+}
+
+// ---------------------------------------------------------------------------------------------
+namespace {
+
+struct Shape {
+  int nw, pieces;
+  size_t starts_bytes, bytes;
+};
+Shape shape_of(const TreeArgs &a) {
+  const int g = a.n_q_heads / a.g.n_kv_heads, es = a.dtype == FOCUS_F32 ? 4 : 2, tt = 128 / es;
+  const int64_t rows = a.max_rows > 0 ? std::min(a.max_rows, a.n_rows) : std::min((int64_t)a.n_rows, 2 * (((int64_t)a.n_rows + a.n_seq - 1) / a.n_seq)), pairs = rows * g;
+  Shape s;
+  s.nw = pairs <= 32 ? 1 : pairs <= 64 ? 2 : 4;
+  const int64_t tokens = std::min((int64_t)a.g.stride * a.g.page_size, a.max_len > 0 ? (int64_t)a.max_len : INT64_MAX);
+  const int64_t blocks = ((int64_t)a.n_rows * g + s.nw * 32 - 1) / (s.nw * 32) + a.n_seq;
+  const int64_t tiles = std::min((int64_t)1 << 40, blocks * a.g.n_kv_heads) * ((tokens + tt - 1) / tt);
+  s.pieces = (int)std::max((int64_t)1, std::min((int64_t)256 * (s.nw == 4 ? 2 : a.head_dim == 64 ? 8 : 4), (tiles + kLeastTiles - 1) / kLeastTiles));
+  s.starts_bytes = ((size_t)a.n_seq + 1) * 8;
+  s.starts_bytes = (s.starts_bytes + 255) / 256 * 256;
+  s.bytes = s.starts_bytes + (size_t)2 * s.pieces * s.nw * 32 * (a.head_dim + 2) * 4;
+  return s;
+}
+
+template <typename T, int D, int NW>
+void launch(hipStream_t s, const TreeArgs &a, const TreePlan &p) {
+  if (a.g.page_size % (128 / sizeof(T)) == 0)
+    k_tree<T, D, NW, true><<<p.pieces, NW * 64, 0, s>>>(a, p);
+  else
+    k_tree<T, D, NW, false><<<p.pieces, NW * 64, 0, s>>>(a, p);
+}
+template <typename T, int D>
+void run(hipStream_t s, const TreeArgs &a, const TreePlan &p) {
+  if (p.starts_given) k_tree_starts<128 / sizeof(T)><<<1, 1024, 0, s>>>(a, p);
+  p.nw == 1 ? launch<T, D, 1>(s, a, p) : p.nw == 2 ? launch<T, D, 2>(s, a, p) : launch<T, D, 4>(s, a, p);
+  if (p.cut) k_tree_join<T, D><<<(unsigned)(((int64_t)a.n_rows * a.n_q_heads + 1024 / D - 1) / (1024 / D)), 256, 0, s>>>(a, p);
+}
+
+}  // namespace
+
+size_t tree_scratch(const TreeArgs &a) { return shape_of(a).bytes; }
 
 void tree_attention(hipStream_t s, const TreeArgs &a) {
-  const dim3 grid(a.n_rows, a.n_q_heads);
+  const Shape sh = shape_of(a);
+  TreePlan p{};
+  p.nw = sh.nw;
+  p.pieces = sh.pieces;
+  p.starts = (int64_t *)a.scratch.ptr;
+  p.cut = a.scratch.bytes >= sh.bytes;
+  p.starts_given = a.n_seq > kFewSequences && a.scratch.bytes >= sh.starts_bytes;
+  p.part_o = (float *)((char *)a.scratch.ptr + sh.starts_bytes);
+  p.part_ml = p.part_o + (size_t)2 * sh.pieces * sh.nw * 32 * a.head_dim;
   if (a.dtype == FOCUS_F32)
-    a.head_dim == 64 ? k_tree_row<float, 64><<<grid, 256, 0, s>>>(a) : k_tree_row<float, 128><<<grid, 256, 0, s>>>(a);
+    a.head_dim == 64 ? run<float, 64>(s, a, p) : run<float, 128>(s, a, p);
   else
-    a.head_dim == 64 ? k_tree_row<bf16_t, 64><<<grid, 256, 0, s>>>(a) : k_tree_row<bf16_t, 128><<<grid, 256, 0, s>>>(a);
+    a.head_dim == 64 ? run<bf16_t, 64>(s, a, p) : run<bf16_t, 128>(s, a, p);
 }
 
 }  // namespace fk
