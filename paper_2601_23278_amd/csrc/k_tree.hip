@@ -39,6 +39,7 @@ struct TreePlan {
   bool cut;                // pieces end anywhere; else at the end of a unit (no room for partial sums)
   bool starts_given;       // `starts` was written by an earlier launch
   int64_t *starts;         // [n_seq + 1] first tile (cut) or unit of every sequence
+  int *cuts;               // [pieces, 8] of the unit that begins in a piece and goes on behind it: first row, pairs before it, its pairs, key head, pieces of it; 0 pairs: none
   float *part_o, *part_ml; // [2 * pieces, nw * 32, D] and [.., 2]: sums of a piece's first unit, if it began before, and of its last one, if it goes on
 };
 constexpr int kFewSequences = 256;   // so many starts are summed up by every workgroup for itself
@@ -70,10 +71,10 @@ __device__ void sum_starts(const TreeArgs &a, const TreePlan &p, int64_t *starts
   const int lane = threadIdx.x & 63;
   int64_t v[PER], sum = 0;
 #pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const int b = lane * PER + i;
-    v[i] = b < a.n_seq ? length_of<TT>(a, b, p) : 0;
-  }
+  for (int i = 0; i < PER; ++i) v[i] = length_of<TT>(a, min(lane * PER + i, a.n_seq - 1), p);
+#pragma unroll
+  for (int i = 0; i < PER; ++i)
+    if (lane * PER + i >= a.n_seq) v[i] = 0;
 #pragma unroll
   for (int i = 0; i < PER; ++i) sum += v[i];
   int64_t before = sum;
@@ -146,27 +147,23 @@ template <typename T> __device__ __forceinline__ u32x4 finite_part(u32x4 v) {
   }
   return v;
 }
-// 1 where an element of 16 bytes is +inf (kind 0), -inf (1), not a number (2), else 0.
-template <typename T> __device__ __forceinline__ u32x4 which(u32x4 v, int kind);
-template <> __device__ __forceinline__ u32x4 which<bf16_t>(u32x4 v, int kind) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    unsigned out = 0;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const unsigned x = v[i] >> (16 * h) & 0xffffu;
-      const bool is = kind == 0 ? x == 0x7f80u : kind == 1 ? x == 0xff80u : (x & 0x7fffu) > 0x7f80u;
-      out |= is ? 0x3f80u << (16 * h) : 0u;
-    }
-    v[i] = out;
-  }
-  return v;
+// 1 where an element of 16 bytes, without the bits that `of` lacks, is one of lo .. lo + span, else 0.  Bits of +inf, -inf and NaN are such ranges.
+struct BitRange {
+  unsigned of, lo, span;
+};
+template <typename T> __device__ __forceinline__ BitRange bits_of(int kind) {     // +inf, -inf, NaN
+  constexpr unsigned inf = sizeof(T) == 2 ? 0x7f80u : 0x7f800000u, all = sizeof(T) == 2 ? 0xffffu : ~0u;
+  return kind == 0 ? BitRange{all, inf, 0u} : kind == 1 ? BitRange{all, inf | (all ^ (all >> 1)), 0u} : BitRange{all >> 1, inf + 1, (all >> 1) - inf - 1};
 }
-template <> __device__ __forceinline__ u32x4 which<float>(u32x4 v, int kind) {
+template <typename T> __device__ __forceinline__ u32x4 which(u32x4 v, BitRange is) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const bool is = kind == 0 ? v[i] == 0x7f800000u : kind == 1 ? v[i] == 0xff800000u : (v[i] & 0x7fffffffu) > 0x7f800000u;
-    v[i] = is ? 0x3f800000u : 0u;
+    if (sizeof(T) == 2) {
+      const unsigned lo = ((v[i] & 0xffffu & is.of) - is.lo) <= is.span ? 0x3f80u : 0u, hi = ((v[i] >> 16 & is.of) - is.lo) <= is.span ? 0x3f800000u : 0u;
+      v[i] = lo | hi;
+    } else {
+      v[i] = ((v[i] & is.of) - is.lo) <= is.span ? 0x3f800000u : 0u;
+    }
   }
   return v;
 }
@@ -204,37 +201,32 @@ __global__ __launch_bounds__(NW * 64, NW == 1 && D == 128 ? 1 : 2) void k_tree(T
     if (wave == 0) sum_starts<TT>(a, plan, starts_s);
     __syncthreads();
     starts = starts_s;
-    if (plan.cut && blockIdx.x == 0)                   // for the launch that puts cut units together
-      for (int i = tid; i <= a.n_seq; i += NW * 64) plan.starts[i] = starts_s[i];
   }
   const int64_t total_work = starts[a.n_seq], per = piece_length(plan, total_work);
   int64_t at = per * blockIdx.x;
   const int64_t end = min(at + per, total_work);
+  if (plan.cut && tid == 0) plan.cuts[(size_t)blockIdx.x * 8 + 2] = 0;
   if (at >= end) return;
 
   // K rows of 1 KB a load instruction: lane l fills the 16-byte slot l of a 1 KB block of LDS, so the swizzle against bank conflicts is applied to what it fetches.
   auto swizzle = [](int row) { return RB == 128 ? (row >> 1) & 7 : row & 15; };
-  int k_row[IPW], k_off[IPW], v_row[IPW], v_chunk[IPW];
-#pragma unroll
-  for (int q = 0; q < IPW; ++q) {
-    const int blk = wave * IPW + q;
-    k_row[q] = blk * (1024 / RB) + lane / LPR;
-    k_off[q] = ((lane % LPR) ^ swizzle(k_row[q])) * 16;
-    v_row[q] = blk * 8 + (lane >> 3);
-    v_chunk[q] = (lane & 7) ^ ((v_row[q] >> 1) & 7);
-  }
+  // Instruction q of a wavefront fetches K rows (V^T rows) from row0 + q * RPI (8 q) on; the bits of the two do not overlap, so a lane needs one offset for each.
+  constexpr int RPI = 1024 / RB;
+  const int k_row0 = wave * IPW * RPI + lane / LPR, v_row0 = wave * IPW * 8 + (lane >> 3);
+  const unsigned k_lane = k_row0 * RB + (((lane % LPR) ^ swizzle(k_row0)) << 4);
+  const unsigned v_chunk0 = (lane & 7) ^ ((v_row0 >> 1) & 7);
   const size_t page_size = page_bytes(a.g, D, ES);
   const bool wide_q = ((uintptr_t)a.q | (uintptr_t)(a.ldq * ES)) % 16 == 0, wide_o = ((uintptr_t)a.out | (uintptr_t)(a.ldo * ES)) % 16 == 0;
   // The scale's sign goes into Q; a scale of zero makes Q zero.
   const float sc = a.scale == 0.f ? 1.f : fabsf(a.scale) * 1.4426950408889634f;      // scores in the log2 domain
   const unsigned flip = a.scale < 0.f ? (ES == 2 ? 0x80008000u : 0x80000000u) : 0u;
 
-  int b = find_start(starts, a.n_seq, at);
+  int b = __builtin_amdgcn_readfirstlane(find_start(starts, a.n_seq, at));
   while (at < end) {
     while (starts[b + 1] <= at) ++b;
     const Units un = units_of<TT>(a, b, NW);
     const int64_t in = at - starts[b];
-    const int unit = (int)(plan.cut ? in / un.tiles : in), tile0 = plan.cut ? (int)(in - (int64_t)unit * un.tiles) : 0;
+    const int unit = (int)(!plan.cut ? in : in < (1ll << 32) ? (unsigned)in / (unsigned)un.tiles : in / un.tiles), tile0 = plan.cut ? (int)(in - (int64_t)unit * un.tiles) : 0;
     const int tile1 = plan.cut ? (int)min((int64_t)un.tiles, tile0 + (end - at)) : un.tiles;
     at += plan.cut ? tile1 - tile0 : 1;
     const int h = unit / un.blocks, q0 = (unit % un.blocks) * NW * 32;
@@ -248,49 +240,46 @@ __global__ __launch_bounds__(NW * 64, NW == 1 && D == 128 ? 1 : 2) void k_tree(T
     // Pages.  ONE: lane i holds the page of tile first + i.  Else lane i < GROUPS holds the page of the i-th 8 tokens of the next tile that will be fetched.
     // A page that is none is read as page 0, and its tokens are masked.
     int pages, first = tile0;
-    auto page_at = [&](int64_t t) {
-      const int64_t i = t / P;
-      const int p = i < a.g.stride ? table[i] : -1;
+    auto page_at = [&](unsigned t) {
+      const unsigned i = t / (unsigned)P;
+      const int p = i < (unsigned)a.g.stride ? table[i] : -1;
       return p < a.g.n_pages ? p : -1;
     };
     auto look_up = [&](int tile) {
       if (ONE) {
-        pages = page_at((int64_t)min(tile + lane, un.tiles - 1) * TT);
+        pages = page_at((unsigned)min(tile + lane, un.tiles - 1) * TT);
         first = tile;
       } else {
-        pages = page_at((int64_t)tile * TT + 8 * (lane & (GROUPS - 1)));
+        pages = page_at((unsigned)tile * TT + 8 * (lane & (GROUPS - 1)));
       }
     };
     auto issue_k = [&](int tile) {
-      if (ONE) {
-        const int page = __builtin_amdgcn_readlane(pages, tile - first);
-        const unsigned char *base = k_base + (size_t)max(page, 0) * page_size + (size_t)(tile * (unsigned)TT % P) * RB;
+      const unsigned char *base = k_base;
+      if (ONE) base += (size_t)max(__builtin_amdgcn_readlane(pages, tile - first), 0) * page_size + (size_t)((unsigned)tile * TT % (unsigned)P) * RB;
 #pragma unroll
-        for (int q = 0; q < IPW; ++q)
-          __builtin_amdgcn_global_load_lds(FK_GLB_PTR(base + k_row[q] * RB + k_off[q]), FK_LDS_PTR(Ks + (wave * IPW + q) * 1024), 16, 0, kNonTemporal);
-      } else {
-#pragma unroll
-        for (int q = 0; q < IPW; ++q) {
-          const int page = __shfl(pages, k_row[q] >> 3);
-          const unsigned place = ((unsigned)tile * TT + k_row[q]) % P;
-          __builtin_amdgcn_global_load_lds(FK_GLB_PTR(k_base + (size_t)max(page, 0) * page_size + (size_t)place * RB + k_off[q]), FK_LDS_PTR(Ks + (wave * IPW + q) * 1024), 16, 0, kNonTemporal);
+      for (int q = 0; q < IPW; ++q) {
+        unsigned off = (k_lane ^ (swizzle(q * RPI) << 4)) + q * 1024;
+        if (!ONE) {
+          const int row = k_row0 + q * RPI, place = ((unsigned)tile * TT + row) % (unsigned)P;
+          base = k_base + (size_t)max(__shfl(pages, row >> 3), 0) * page_size;
+          off += (place - row) * RB;
         }
+        __builtin_amdgcn_global_load_lds(FK_GLB_PTR(base + off), FK_LDS_PTR(Ks + (wave * IPW + q) * 1024), 16, 0, kNonTemporal);
       }
     };
     auto issue_v = [&](int tile, int pg) {
-      if (ONE) {
-        const int page = __builtin_amdgcn_readlane(pg, tile - first);
-        const unsigned char *base = v_base + (size_t)max(page, 0) * page_size + (size_t)(tile * (unsigned)TT % P) * ES;
+      const unsigned char *base = v_base;
+      if (ONE) base += (size_t)max(__builtin_amdgcn_readlane(pg, tile - first), 0) * page_size + (size_t)((unsigned)tile * TT % (unsigned)P) * ES;
 #pragma unroll
-        for (int q = 0; q < IPW; ++q)
-          __builtin_amdgcn_global_load_lds(FK_GLB_PTR(base + (size_t)v_row[q] * P * ES + v_chunk[q] * 16), FK_LDS_PTR(Vs + (wave * IPW + q) * 1024), 16, 0, kNonTemporal);
-      } else {
-#pragma unroll
-        for (int q = 0; q < IPW; ++q) {
-          const int t = v_chunk[q] * (16 / ES), page = __shfl(pg, t >> 3);
-          const unsigned place = ((unsigned)tile * TT + t) % P;
-          __builtin_amdgcn_global_load_lds(FK_GLB_PTR(v_base + (size_t)max(page, 0) * page_size + ((size_t)v_row[q] * P + place) * ES), FK_LDS_PTR(Vs + (wave * IPW + q) * 1024), 16, 0, kNonTemporal);
+      for (int q = 0; q < IPW; ++q) {
+        const unsigned chunk = v_chunk0 ^ (q * 4 & 7);
+        unsigned off = (unsigned)v_row0 * (P * ES) + chunk * 16;
+        if (!ONE) {
+          const int t = chunk * (16 / ES);
+          base = v_base + (size_t)max(__shfl(pg, t >> 3), 0) * page_size;
+          off += (((unsigned)tile * TT + t) % (unsigned)P - t) * ES;
         }
+        __builtin_amdgcn_global_load_lds(FK_GLB_PTR(base + (size_t)q * 8 * P * ES + off), FK_LDS_PTR(Vs + (wave * IPW + q) * 1024), 16, 0, kNonTemporal);
       }
     };
     // Bit i: the page of the tile's i-th 8 tokens is one.
@@ -450,14 +439,10 @@ __global__ __launch_bounds__(NW * 64, NW == 1 && D == 128 ? 1 : 2) void k_tree(T
         }
         found = __builtin_amdgcn_readfirstlane(found);
         if (found & 2) {
-          u32x4 sf[4];
-#pragma unroll
-          for (int kk = 0; kk < 4; ++kk)
-#pragma unroll
-            for (int e = 0; e < 16 / ES; ++e) ((T *)&sf[kk])[e] = (T)(float)(mask >> ((2 * kk + half) * (16 / ES) + e) & 1);
 #pragma unroll 1
           for (int kind = 0; kind < 3; ++kind) {
             const float is = kind == 0 ? INFINITY : kind == 1 ? -INFINITY : NAN;
+            const BitRange range = bits_of<T>(kind);
 #pragma unroll
             for (int ds = 0; ds < DS; ++ds) {
               f32x16 count;
@@ -465,7 +450,11 @@ __global__ __launch_bounds__(NW * 64, NW == 1 && D == 128 ? 1 : 2) void k_tree(T
               for (int e = 0; e < 16; ++e) count[e] = 0.f;
 #pragma unroll
               for (int kk = 0; kk < 4; ++kk) {
-                count = multiply<T>(which<T>(v_piece(ds, kk), kind), sf[kk], count);
+                u32x4 sees;
+                const unsigned seen_bits = (unsigned)(mask >> ((2 * kk + half) * (16 / ES)));
+#pragma unroll
+                for (int e = 0; e < 16 / ES; ++e) ((T *)&sees)[e] = (T)(float)(int)(seen_bits >> e & 1);
+                count = multiply<T>(which<T>(v_piece(ds, kk), range), sees, count);
                 asm volatile("" ::: "memory");
               }
 #pragma unroll
@@ -496,6 +485,10 @@ __global__ __launch_bounds__(NW * 64, NW == 1 && D == 128 ? 1 : 2) void k_tree(T
     }
 
     const float l_tot = l + __shfl_xor(l, 32);
+    if (tile0 == 0 && tile1 < un.tiles && tid == 0) {
+      int *const c = plan.cuts + (size_t)blockIdx.x * 8;
+      c[0] = r0; c[1] = q0; c[2] = min(rows * g - q0, NW * 32); c[3] = h; c[4] = (int)((un.tiles - tile1 + per - 1) / per) + 1;
+    }
     if (!valid) continue;
     if (tile0 == 0 && tile1 == un.tiles) {
       const float inv = l_tot == 0.f ? 0.f : 1.0f / l_tot;
@@ -531,35 +524,48 @@ __global__ __launch_bounds__(NW * 64, NW == 1 && D == 128 ? 1 : 2) void k_tree(T
   }
 }
 
-// Units that a cut went through: out = sum_i o_i 2^(m_i - M) / sum_i l_i 2^(m_i - M) over the pieces in their order.  D / 4 lanes per (row, query head).
+// Units that a cut went through: out = sum_i o_i 2^(m_i - M) / sum_i l_i 2^(m_i - M), i over the pieces in their order.  A workgroup looks after the unit that
+// begins in piece blockIdx.x, a wavefront takes one pair: 64 / (D / 4) groups of lanes take every so manieth piece, four at a time, and their sums are added in group order.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void k_tree_join(TreeArgs a, TreePlan plan) {
-  constexpr int TT = 128 / sizeof(T), LANES = D / 4, PER = 256 / LANES;
-  const int64_t id = (int64_t)blockIdx.x * PER + threadIdx.x / LANES;
-  const int c = threadIdx.x % LANES;
-  const int r = (int)(id / a.n_q_heads), head = (int)(id % a.n_q_heads);
-  if (r >= a.n_rows || r < a.cu[0] || r >= a.cu[a.n_seq]) return;
-  const int b = sequence_of(a.cu, a.n_seq, r), g = a.n_q_heads / a.g.n_kv_heads, h = head / g;
-  const Units un = units_of<TT>(a, b, plan.nw);
-  const int pair = (r - max(a.cu[b], 0)) * g + head % g, per_block = plan.nw * 32;
-  const int64_t from = plan.starts[b] + ((int64_t)h * un.blocks + pair / per_block) * un.tiles, per = piece_length(plan, plan.starts[a.n_seq]);
-  const int64_t w0 = from / per, w1 = (from + un.tiles - 1) / per;
-  if (w0 == w1) return;
-  auto slot_of = [&](int64_t w) { return (size_t)(2 * w + (w == w0)) * per_block + pair % per_block; };
+  constexpr int LANES = D / 4, GROUPS = 64 / LANES;
+  const int *const rec = plan.cuts + (size_t)blockIdx.x * 8;
+  const int lane = threadIdx.x & 63, pair = blockIdx.y * 4 + (threadIdx.x >> 6), c = lane % LANES, grp = lane / LANES;
+  const int r0 = rec[0], q0 = rec[1], pairs = rec[2], h = rec[3], n = rec[4];
+  if (pair >= pairs) return;
+  const int g = a.n_q_heads / a.g.n_kv_heads, per_block = plan.nw * 32;
+  auto slot_of = [&](int i) { return ((size_t)2 * (blockIdx.x + i) + (i == 0)) * per_block + pair; };
   float mm = -INFINITY;
-  for (int64_t w = w0; w <= w1; ++w) mm = fmaxf(mm, plan.part_ml[slot_of(w) * 2]);
+  for (int i = lane; i < n; i += 64) mm = fmaxf(mm, plan.part_ml[slot_of(i) * 2]);
+  for (int x = 32; x > 0; x >>= 1) mm = fmaxf(mm, __shfl_xor(mm, x));
   f32x4 num = {0.f, 0.f, 0.f, 0.f};
   float den = 0.f;
-  for (int64_t w = w0; w <= w1; ++w) {
-    const size_t s = slot_of(w);
-    const float m = plan.part_ml[s * 2], k = m == -INFINITY ? 0.f : exp2f(m - mm);
-    const f32x4 v = *(const f32x4 *)(plan.part_o + s * D + c * 4);
-    den += plan.part_ml[s * 2 + 1] * k;
+  for (int i0 = grp; i0 < n; i0 += 4 * GROUPS) {
+    f32x4 v[4];
+    float2 ml[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) num[e] += m == -INFINITY ? 0.f : v[e] * k;
+    for (int j = 0; j < 4; ++j) {
+      const size_t s = slot_of(min(i0 + j * GROUPS, n - 1));
+      v[j] = *(const f32x4 *)(plan.part_o + s * D + c * 4);
+      ml[j] = *(const float2 *)(plan.part_ml + s * 2);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const bool there = i0 + j * GROUPS < n && ml[j].x != -INFINITY;
+      const float k = there ? exp2f(ml[j].x - mm) : 0.f;
+      den += there ? ml[j].y * k : 0.f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) num[e] += there ? v[j][e] * k : 0.f;
+    }
   }
+  for (int x = LANES; x < 64; x <<= 1) {
+    den += __shfl_xor(den, x);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) num[e] += __shfl_xor(num[e], x);
+  }
+  if (grp != 0) return;
   const float inv = den == 0.f ? 0.f : 1.0f / den;
-  T *to = (T *)a.out + (size_t)r * a.ldo + (size_t)head * D + c * 4;
+  T *to = (T *)a.out + (size_t)(r0 + (q0 + pair) / g) * a.ldo + (size_t)(h * g + (q0 + pair) % g) * D + c * 4;
 #pragma unroll
   for (int e = 0; e < 4; ++e) to[e] = (T)(num[e] * inv);
 }
@@ -569,7 +575,7 @@ namespace {
 
 struct Shape {
   int nw, pieces;
-  size_t starts_bytes, bytes;
+  size_t starts_bytes, cuts_bytes, bytes;
 };
 Shape shape_of(const TreeArgs &a) {
   const int g = a.n_q_heads / a.g.n_kv_heads, es = a.dtype == FOCUS_F32 ? 4 : 2, tt = 128 / es;
@@ -582,7 +588,8 @@ Shape shape_of(const TreeArgs &a) {
   s.pieces = (int)std::max((int64_t)1, std::min((int64_t)256 * (s.nw == 4 ? 2 : a.head_dim == 64 ? 8 : 4), (tiles + kLeastTiles - 1) / kLeastTiles));
   s.starts_bytes = ((size_t)a.n_seq + 1) * 8;
   s.starts_bytes = (s.starts_bytes + 255) / 256 * 256;
-  s.bytes = s.starts_bytes + (size_t)2 * s.pieces * s.nw * 32 * (a.head_dim + 2) * 4;
+  s.cuts_bytes = ((size_t)s.pieces * 32 + 255) / 256 * 256;
+  s.bytes = s.starts_bytes + s.cuts_bytes + (size_t)2 * s.pieces * s.nw * 32 * (a.head_dim + 2) * 4;
   return s;
 }
 
@@ -597,7 +604,7 @@ template <typename T, int D>
 void run(hipStream_t s, const TreeArgs &a, const TreePlan &p) {
   if (p.starts_given) k_tree_starts<128 / sizeof(T)><<<1, 1024, 0, s>>>(a, p);
   p.nw == 1 ? launch<T, D, 1>(s, a, p) : p.nw == 2 ? launch<T, D, 2>(s, a, p) : launch<T, D, 4>(s, a, p);
-  if (p.cut) k_tree_join<T, D><<<(unsigned)(((int64_t)a.n_rows * a.n_q_heads + 1024 / D - 1) / (1024 / D)), 256, 0, s>>>(a, p);
+  if (p.cut) k_tree_join<T, D><<<dim3(p.pieces, p.nw * 8), 256, 0, s>>>(a, p);
 }
 
 }  // namespace
@@ -612,7 +619,8 @@ void tree_attention(hipStream_t s, const TreeArgs &a) {
   p.starts = (int64_t *)a.scratch.ptr;
   p.cut = a.scratch.bytes >= sh.bytes;
   p.starts_given = a.n_seq > kFewSequences && a.scratch.bytes >= sh.starts_bytes;
-  p.part_o = (float *)((char *)a.scratch.ptr + sh.starts_bytes);
+  p.cuts = (int *)((char *)a.scratch.ptr + sh.starts_bytes);
+  p.part_o = (float *)((char *)p.cuts + sh.cuts_bytes);
   p.part_ml = p.part_o + (size_t)2 * sh.pieces * sh.nw * 32 * a.head_dim;
   if (a.dtype == FOCUS_F32)
     a.head_dim == 64 ? run<float, 64>(s, a, p) : run<float, 128>(s, a, p);
