@@ -189,6 +189,7 @@ static const char *check_beams(int32_t n_seq, int32_t n_beams, int32_t vocab, in
   if (n_beams < 1 || n_beams > fk::kMaxBeams || k < 1 || k > fk::kMaxPicks) return "n_beams and k must be in 1..64";
   if (n_seq < 0 || (int64_t)n_seq * n_beams > kMaxRows) return "n_seq must not be negative and n_seq * n_beams at most 2^20";
   if (vocab < 1 || vocab > (1 << 24)) return "vocab must be in 1..2^24";
+  if (fk::beam_groups(n_seq, n_beams, vocab, k) >= fk::kMaxGroups) return "n_seq, n_beams and vocab too large";
   return nullptr;
 }
 

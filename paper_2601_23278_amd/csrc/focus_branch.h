@@ -99,6 +99,7 @@ struct BeamArgs {
   float *new_scores;
   void *work;                       // beam_scratch() bytes
 };
+int64_t beam_groups(int n_seq, int n_beams, int vocab, int k);     // workgroups of the larger launch
 size_t beam_scratch(int n_seq, int n_beams, int vocab, int k);
 void beam_select(hipStream_t s, const BeamArgs &a);
 
