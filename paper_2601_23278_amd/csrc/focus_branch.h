@@ -15,11 +15,14 @@ struct Paged {
 
 // Bytes of a page; es = bytes of an element.
 __host__ __device__ __forceinline__ size_t page_bytes(const Paged &g, int head_dim, int es) { return (size_t)2 * g.n_kv_heads * g.page_size * head_dim * es; }
-// Page of token t of row b, -1: it has none.
-__device__ __forceinline__ int page_of_token(const Paged &g, const int32_t *table, int stride, int b, int64_t t) {
-  if (t < 0 || t / g.page_size >= stride) return -1;
-  const int p = table[(size_t)b * stride + t / g.page_size];
-  return p < g.n_pages ? p : -1;
+// Where token t of row b lies; page -1: nowhere.  Tokens are below 2^32 (a length and a position, 31 bits each).
+struct Place {
+  int page, at;
+};
+__device__ __forceinline__ Place place_of(const Paged &g, const int32_t *table, int stride, int b, int64_t t) {
+  const unsigned i = (unsigned)t / (unsigned)g.page_size;
+  const int p = t >= 0 && i < (unsigned)stride ? table[(size_t)b * stride + i] : -1;
+  return Place{p < g.n_pages ? p : -1, (int)((unsigned)t - i * (unsigned)g.page_size)};
 }
 // The last b with cu[b] <= r among 0..n - 1 (n >= 1).  The caller checks that r < cu[b + 1].
 __device__ __forceinline__ int sequence_of(const int32_t *cu, int n, int r) {

@@ -23,15 +23,14 @@ __global__ __launch_bounds__(256) void k_append(AppendArgs a) {
   const int r0 = blockIdx.x * 64, h = blockIdx.y, tid = threadIdx.x, P = a.g.page_size;
   if (tid < 64) {
     const int r = r0 + tid;
-    int page = -1, place = 0;
+    Place at{-1, 0};
     if (r < a.n_rows && r >= a.cu[0] && r < a.cu[a.n_seq]) {
       const int b = sequence_of(a.cu, a.n_seq, r);
       const int64_t t = (int64_t)max(a.lens[b], 0) + r - a.cu[b];
-      page = page_of_token(a.g, a.g.table, a.g.stride, b, t);
-      place = (int)(t % P);
+      at = place_of(a.g, a.g.table, a.g.stride, b, t);
     }
-    page_s[tid] = page;
-    place_s[tid] = place;
+    page_s[tid] = at.page;
+    place_s[tid] = at.at;
   }
   __syncthreads();
   const T *k = (const T *)a.k + (size_t)h * D, *v = (const T *)a.v + (size_t)h * D;
@@ -70,65 +69,89 @@ void kv_append(hipStream_t s, const AppendArgs &a) {
 }
 
 // ---------------------------------------------------------------------------------------------
-// Compaction.  A workgroup takes one (sequence, head, layer) and moves its tokens 64 at a time, in ascending order.  In place that is safe: place i is read from
-// place keep[i] >= i, a batch is read whole before any of it is written, and later batches read places behind everything that was written.
-template <int ES, int D>
+// Compaction.  A workgroup takes one (sequence, head, layer), or a slice of its columns where those are few, and moves tokens in ascending order, 64 at a time.
+// In place that is safe: place i is read from place keep[i] >= i, so nothing that was written is read later; and every column of K (16 bytes) and every row of
+// V^T belongs to one wavefront, which loads all of a batch before it stores any of it.  So wavefronts do not wait for each other's data, only for the list of
+// where the next 256 tokens move, which is looked up while the last ones do.  Batches begin at every 64th token of what is written: a store to V^T fills a line.
+template <int ES, int D, int SLICES>
 __global__ __launch_bounds__(256) void k_compact(CompactArgs a) {
   typedef typename Word<ES>::type T;
-  constexpr int PIECES = D * ES / 16, NK = 64 * PIECES / 256, NV = D / 4;
-  __shared__ int from_s[64], from_at[64], to_s[64], to_at[64];
-  const int H = a.g.n_kv_heads, b = blockIdx.x / H, h = blockIdx.x % H, tid = threadIdx.x, P = a.g.page_size;
+  constexpr int COLS = D * ES / 16 / SLICES / 4, ROWS = D / SLICES;        // columns of K that a wavefront has, rows of V^T of the workgroup
+  constexpr int TOKENS = 64 / COLS, NK = COLS, NV = ROWS / 4 < 8 ? ROWS / 4 : 8;
+  __shared__ int4 move_s[2][256];                      // pages and places, from and to
+  const int H = a.g.n_kv_heads, b = blockIdx.x / H, h = blockIdx.x % H, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, P = a.g.page_size;
   const int c0 = min(max(a.cu[b], 0), a.n_keep), n = min(a.cu[b + 1], a.n_keep) - c0;
-  const int64_t start = max(a.start[b], 0);
+  if (n <= 0) return;
+  const int64_t start = max(a.start[b], 0), base = start & ~(int64_t)63;
+  const int skip = (int)(start - base), end = skip + n;      // places base + j, skip <= j < end, are written
   const size_t page_size = page_bytes(a.g, D, ES);
   char *const pool = a.g.pool + (size_t)blockIdx.y * a.g.n_pages * page_size;
-  for (int i0 = 0; i0 < n; i0 += 64) {
-    if (tid < 64) {
-      int from = -1, to = -1;
-      int64_t tf = 0, tt = 0;
-      if (i0 + tid < n) {
-        tf = start + a.keep[c0 + i0 + tid];
-        tt = start + i0 + tid;
-        from = page_of_token(a.g, a.g.table, a.g.stride, b, tf);
-        to = page_of_token(a.g, a.to_table, a.to_stride, b, tt);
-        if (from < 0) to = -1;
+  const size_t k_head = (size_t)h * P * D * ES + (blockIdx.z * 4 + wave) * COLS * 16, v_head = (size_t)(H + h) * P * D * ES + (size_t)blockIdx.z * ROWS * P * ES;
+  auto kept = [&](int j) { return j >= skip && j < end ? a.keep[c0 + j - skip] : -1; };
+  auto where = [&](int j, int keep) {
+    if (j < skip || j >= end) return int4{-1, 0, -1, 0};
+    const Place from = place_of(a.g, a.g.table, a.g.stride, b, keep < 0 ? -1 : start + keep), to = place_of(a.g, a.to_table, a.to_stride, b, base + j);
+    return int4{from.page, from.at, from.page < 0 ? -1 : to.page, to.at};
+  };
+  // A few tokens in all are told apart by few lanes of V's loads; else a lane is a token.
+  const bool few = end - skip <= 32;
+  const int bits = !few ? 6 : n > 16 ? 5 : n > 8 ? 4 : n > 4 ? 3 : n > 2 ? 2 : n - 1, by = 256 >> bits;
+  move_s[0][tid] = where(tid, kept(tid));
+  __syncthreads();
+  for (int j0 = 0, buf = 0; j0 < end; j0 += 256, buf ^= 1) {
+    const int next = kept(j0 + 256 + tid);
+    const int last = min(end - j0, 256), begin = max(skip - j0, 0);
+    // with few tokens one batch from the first token on, across the 64
+    for (int s0 = few ? begin : 0; s0 < last; s0 += 64) {
+      const int lo = max(begin, s0), hi = min(last, s0 + 64);
+      int4 km[NK];
+      u32x4 kk[NK];
+#pragma unroll
+      for (int x = 0; x < NK; ++x) {
+        const int t = lo + x * TOKENS + lane / COLS;
+        km[x] = t < hi ? move_s[buf][t] : int4{-1, 0, -1, 0};
+        if (km[x].z >= 0) kk[x] = *(const u32x4 *)(pool + (size_t)km[x].x * page_size + k_head + (size_t)km[x].y * D * ES + lane % COLS * 16);
       }
-      from_s[tid] = from; from_at[tid] = (int)(tf % P);
-      to_s[tid] = to; to_at[tid] = (int)(tt % P);
+      const int vt = s0 + (tid & ((1 << bits) - 1)), vd = tid >> bits;
+      const int4 vm = vt >= lo && vt < hi ? move_s[buf][vt] : int4{-1, 0, -1, 0};
+      const T *const vf = (const T *)(pool + (size_t)max(vm.x, 0) * page_size + v_head) + vm.y;
+      T *const vto = (T *)(pool + (size_t)max(vm.z, 0) * page_size + v_head) + vm.w;
+      for (int d0 = vd; d0 < ROWS; d0 += by * NV) {
+        T vv[NV];
+#pragma unroll
+        for (int x = 0; x < NV; ++x)
+          if (vm.z >= 0 && d0 + by * x < ROWS) vv[x] = vf[(size_t)(d0 + by * x) * P];
+#pragma unroll
+        for (int x = 0; x < NV; ++x)
+          if (vm.z >= 0 && d0 + by * x < ROWS) vto[(size_t)(d0 + by * x) * P] = vv[x];
+      }
+#pragma unroll
+      for (int x = 0; x < NK; ++x)
+        if (km[x].z >= 0) *(u32x4 *)(pool + (size_t)km[x].z * page_size + k_head + (size_t)km[x].w * D * ES + lane % COLS * 16) = kk[x];
     }
-    __syncthreads();
-    u32x4 kk[NK];
-    T vv[NV];
-#pragma unroll
-    for (int j = 0; j < NK; ++j) {
-      const int i = tid + 256 * j, t = i / PIECES, c = i % PIECES;
-      if (to_s[t] >= 0) kk[j] = *(const u32x4 *)(pool + (size_t)from_s[t] * page_size + (((size_t)h * P + from_at[t]) * D) * ES + c * 16);
+    if (j0 + 256 < end) {
+      move_s[buf ^ 1][tid] = where(j0 + 256 + tid, next);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // the list is there; stores need not be
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
     }
-    const int t = tid & 63, d0 = tid >> 6;
-    const T *vf = (const T *)(pool + (size_t)max(from_s[t], 0) * page_size) + (size_t)(H + h) * P * D + from_at[t];
-    T *vt = (T *)(pool + (size_t)max(to_s[t], 0) * page_size) + (size_t)(H + h) * P * D + to_at[t];
-#pragma unroll
-    for (int j = 0; j < NV; ++j)
-      if (to_s[t] >= 0) vv[j] = vf[(size_t)(d0 + 4 * j) * P];
-    __syncthreads();                                   // the whole batch has been read
-#pragma unroll
-    for (int j = 0; j < NK; ++j) {
-      const int i = tid + 256 * j, t = i / PIECES, c = i % PIECES;
-      if (to_s[t] >= 0) *(u32x4 *)(pool + (size_t)to_s[t] * page_size + (((size_t)h * P + to_at[t]) * D) * ES + c * 16) = kk[j];
-    }
-#pragma unroll
-    for (int j = 0; j < NV; ++j)
-      if (to_s[t] >= 0) vt[(size_t)(d0 + 4 * j) * P] = vv[j];
-    __syncthreads();                                   // before the places of the next batch
   }
 }
 
-void kv_compact(hipStream_t s, const CompactArgs &a) {
-  const dim3 grid(a.n_seq * a.g.n_kv_heads, a.g.n_layers);
-  if (a.dtype == FOCUS_F32)
-    a.head_dim == 64 ? k_compact<4, 64><<<grid, 256, 0, s>>>(a) : k_compact<4, 128><<<grid, 256, 0, s>>>(a);
+template <int ES, int D>
+void compact_of(hipStream_t s, const CompactArgs &a) {
+  constexpr int SLICES = D * ES / 16 / 4 < 4 ? D * ES / 16 / 4 : 4;
+  const int groups = a.n_seq * a.g.n_kv_heads;
+  if ((int64_t)groups * a.g.n_layers <= 1024)
+    k_compact<ES, D, SLICES><<<dim3(groups, a.g.n_layers, SLICES), 256, 0, s>>>(a);
   else
-    a.head_dim == 64 ? k_compact<2, 64><<<grid, 256, 0, s>>>(a) : k_compact<2, 128><<<grid, 256, 0, s>>>(a);
+    k_compact<ES, D, 1><<<dim3(groups, a.g.n_layers), 256, 0, s>>>(a);
+}
+void kv_compact(hipStream_t s, const CompactArgs &a) {
+  if (a.dtype == FOCUS_F32)
+    a.head_dim == 64 ? compact_of<4, 64>(s, a) : compact_of<4, 128>(s, a);
+  else
+    a.head_dim == 64 ? compact_of<2, 64>(s, a) : compact_of<2, 128>(s, a);
 }
 
 // ---------------------------------------------------------------------------------------------
