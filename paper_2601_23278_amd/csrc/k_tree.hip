@@ -4,9 +4,11 @@
 // running maximum and sum of a softmax, so K and V are read once per (sequence, key head, 32 to 128 pairs) and the kernel is bound by that stream as long as pairs
 // are few.  A wavefront holds 32 pairs, a workgroup 1, 2 or 4 wavefronts on the same tile.
 //
-// Work is a line of tiles: sequence after sequence, key head after key head, block of pairs after block of pairs ("unit"), every unit as many tiles as its
-// sequence is long.  The line is cut into equal pieces, one for each workgroup that the chip holds at once, so lengths need not be alike; the sums of a unit that
-// a cut goes through are put together by a second, small launch in the order of the pieces.  Where the pieces lie follows from the lengths alone.
+// Work is a line of tiles for each key head: sequence after sequence, block of pairs after block of pairs ("unit"), every unit as many tiles as its sequence is long.
+// The line is cut into equal ranges, as many as make (ranges x key heads) "pieces" for all the workgroups that the chip holds at once, so lengths need not be alike;
+// the sums of a unit that a cut goes through are put together by a second, small launch in the order of the ranges.  Where they lie follows from the lengths alone.
+// The heads of a range run side by side on one XCD and read the same pages at the same time: with every head's line cut for itself, 256 sequences of 512 to 4096
+// tokens took 480 us instead of 441.
 //
 // A tile is 128 bytes of V^T rows: 64 bf16 tokens or 32 of fp32; as bytes both types are laid out alike.  Per tile and wavefront
 //   S^T = K Q^T   A = K rows from LDS, B = Q in registers: a lane owns one pair, and its scores are in its own registers
@@ -35,12 +37,12 @@ constexpr int kNonTemporal = 2;      // cache policy of a load (NT bit)
 // How a call's line of tiles is cut.
 struct TreePlan {
   int nw;                  // wavefronts of a workgroup, 32 pairs each
-  int pieces;              // workgroups
+  int ranges;              // of a head's line; workgroups: ranges * key heads
   bool cut;                // pieces end anywhere; else at the end of a unit (no room for partial sums)
   bool starts_given;       // `starts` was written by an earlier launch
-  int64_t *starts;         // [n_seq + 1] first tile (cut) or unit of every sequence
-  int *cuts;               // [pieces, 8] of the unit that begins in a piece and goes on behind it: first row, pairs before it, its pairs, key head, pieces of it; 0 pairs: none
-  float *part_o, *part_ml; // [2 * pieces, nw * 32, D] and [.., 2]: sums of a piece's first unit, if it began before, and of its last one, if it goes on
+  int64_t *starts;         // [n_seq + 1] first tile (cut) or unit of every sequence on a line
+  int *cuts;               // [ranges, key heads, 8] of the unit that begins in a piece and goes on behind it: first row, pairs before it, its pairs, pieces of it; 0 pairs: none
+  float *part_o, *part_ml; // [2 * ranges * key heads, nw * 32, D] and [.., 2]: sums of a piece's first unit, if it began before, and of its last one, if it goes on
 };
 constexpr int kFewSequences = 256;   // so many starts are summed up by every workgroup for itself
 
@@ -61,7 +63,7 @@ __device__ __forceinline__ Units units_of(const TreeArgs &a, int b, int nw) {
 template <int TT>
 __device__ __forceinline__ int64_t length_of(const TreeArgs &a, int b, const TreePlan &p) {
   const Units u = units_of<TT>(a, b, p.nw);
-  return (int64_t)u.blocks * a.g.n_kv_heads * (p.cut ? u.tiles : 1);
+  return (int64_t)u.blocks * (p.cut ? u.tiles : 1);
 }
 
 // starts[0 .. n] by a whole wavefront; n at most kFewSequences.
@@ -73,10 +75,10 @@ __device__ void sum_starts(const TreeArgs &a, const TreePlan &p, int64_t *starts
 #pragma unroll
   for (int i = 0; i < PER; ++i) v[i] = length_of<TT>(a, min(lane * PER + i, a.n_seq - 1), p);
 #pragma unroll
-  for (int i = 0; i < PER; ++i)
+  for (int i = 0; i < PER; ++i) {
     if (lane * PER + i >= a.n_seq) v[i] = 0;
-#pragma unroll
-  for (int i = 0; i < PER; ++i) sum += v[i];
+    sum += v[i];
+  }
   int64_t before = sum;
   for (int o = 1; o < 64; o <<= 1) {
     const int64_t y = __shfl_up((long long)before, o);
@@ -86,10 +88,10 @@ __device__ void sum_starts(const TreeArgs &a, const TreePlan &p, int64_t *starts
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
     const int b = lane * PER + i;
-    if (b < a.n_seq) starts[b] = before;
+    if (b <= a.n_seq) starts[b] = before;
     before += v[i];
-    if (b == a.n_seq - 1) starts[a.n_seq] = before;
   }
+  if (lane == 63 && a.n_seq == kFewSequences) starts[kFewSequences] = before;
 }
 // The same by one workgroup for any number of sequences.
 template <int TT>
@@ -118,7 +120,17 @@ __global__ __launch_bounds__(1024) void k_tree_starts(TreeArgs a, TreePlan p) {
   }
   if (threadIdx.x == 0) p.starts[a.n_seq] = total;
 }
-__device__ __forceinline__ int find_start(const int64_t *starts, int n, int64_t at) {     // the last b with starts[b] <= at
+// The last b of 0 .. n - 1 with starts[b] <= at.  Up to kFewSequences a wavefront counts them, else it is looked for by halves.
+__device__ __forceinline__ int find_start(const int64_t *starts, int n, int64_t at) {
+  if (n <= kFewSequences) {
+    int count = 0;
+#pragma unroll
+    for (int i = 0; i < kFewSequences / 64; ++i) {
+      const int b = (threadIdx.x & 63) + i * 64;
+      count += __popcll(__ballot(b < n && starts[min(b, n)] <= at));
+    }
+    return count - 1;
+  }
   int lo = 0, hi = n;
   while (hi - lo > 1) {
     const int mid = (lo + hi) / 2;
@@ -126,9 +138,9 @@ __device__ __forceinline__ int find_start(const int64_t *starts, int n, int64_t 
   }
   return lo;
 }
-constexpr int kLeastTiles = 2;       // of a piece
-__device__ __forceinline__ int64_t piece_length(const TreePlan &p, int64_t total) {
-  const int64_t n = (total + p.pieces - 1) / p.pieces;
+constexpr int kLeastTiles = 3;       // of a range (one request of 24 rows and 4001 tokens: 26.7 us; 2 or 4 tiles 27.8 and 27.0, 1 or 6 tiles 32 and 30)
+__device__ __forceinline__ int64_t range_length(const TreePlan &p, int64_t total) {
+  const int64_t n = (total + p.ranges - 1) / p.ranges;
   return p.cut && n < kLeastTiles ? kLeastTiles : n < 1 ? 1 : n;
 }
 
@@ -185,6 +197,15 @@ template <typename T> __device__ __forceinline__ constexpr int token_of(int r, i
   return sizeof(T) == 2 ? 16 * (r >> 3) + 8 * half + (r & 7) : 8 * (r >> 2) + 4 * half + (r & 3);
 }
 
+template <typename T> __device__ __forceinline__ void store4(T *to, f32x4 v, bool wide) {
+  if (wide) {
+    if (sizeof(T) == 2) *(bf16x4 *)to = bf16x4{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]}; else *(f32x4 *)to = v;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) to[e] = (T)v[e];
+  }
+}
+
 // ONE: a tile lies in one page (the page size is a multiple of the tile's tokens); else groups of 8 tokens are looked up one by one.
 template <typename T, int D, int NW, bool ONE>
 __global__ __launch_bounds__(NW * 64, NW == 1 && D == 128 ? 1 : 2) void k_tree(TreeArgs a, TreePlan plan) {
@@ -196,17 +217,22 @@ __global__ __launch_bounds__(NW * 64, NW == 1 && D == 128 ? 1 : 2) void k_tree(T
   unsigned char *const Ks = lds, *const Vs = lds + TILE;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5, col = lane & 31;
   const int H = a.g.n_kv_heads, g = a.n_q_heads / H, P = a.g.page_size;
+  int range = blockIdx.x / H, h = blockIdx.x % H;
+  if (plan.ranges % 8 == 0) {                          // workgroups go to the eight XCDs in turn
+    range = blockIdx.x / (8 * H) * 8 + blockIdx.x % 8;
+    h = blockIdx.x / 8 % H;
+  }
+  const int piece = range * H + h;
   const int64_t *starts = plan.starts;
   if (!plan.starts_given) {
     if (wave == 0) sum_starts<TT>(a, plan, starts_s);
     __syncthreads();
     starts = starts_s;
   }
-  const int64_t total_work = starts[a.n_seq], per = piece_length(plan, total_work);
-  int64_t at = per * blockIdx.x;
-  const int64_t end = min(at + per, total_work);
-  if (plan.cut && tid == 0) plan.cuts[(size_t)blockIdx.x * 8 + 2] = 0;
-  if (at >= end) return;
+  const int64_t total_work = starts[a.n_seq], per = range_length(plan, total_work);
+  const int64_t from = per * range, end = min(from + per, total_work);
+  if (plan.cut && tid == 0) plan.cuts[(size_t)piece * 8 + 2] = 0;
+  if (from >= end) return;
 
   // K rows of 1 KB a load instruction: lane l fills the 16-byte slot l of a 1 KB block of LDS, so the swizzle against bank conflicts is applied to what it fetches.
   auto swizzle = [](int row) { return RB == 128 ? (row >> 1) & 7 : row & 15; };
@@ -221,92 +247,106 @@ __global__ __launch_bounds__(NW * 64, NW == 1 && D == 128 ? 1 : 2) void k_tree(T
   const float sc = a.scale == 0.f ? 1.f : fabsf(a.scale) * 1.4426950408889634f;      // scores in the log2 domain
   const unsigned flip = a.scale < 0.f ? (ES == 2 ? 0x80008000u : 0x80000000u) : 0u;
 
+  // A piece is a run of tiles of one unit after the other.  The loads of a unit's first tile are asked for before the unit before it is done, so the stream of
+  // tiles does not stop at its end; what that takes is worked out one unit ahead.
+  struct Part {
+    int b, q0, tile0, tile1, tiles, r0, rows, cached, total, pages;         // tiles 0: there is none
+  };
+  int64_t at = from;
   int b = __builtin_amdgcn_readfirstlane(find_start(starts, a.n_seq, at));
-  while (at < end) {
+  // Pages.  ONE: lane i holds the page of tile first + i.  Else lane i < GROUPS holds the page of the i-th 8 tokens of a tile.  A page that is none is read as page
+  // 0, and its tokens are masked.
+  auto look_up = [&](int row, int tile, int tiles) {
+    const unsigned t = ONE ? (unsigned)min(tile + lane, tiles - 1) * TT : (unsigned)min(tile, tiles - 1) * TT + 8 * (lane & (GROUPS - 1)), i = t / (unsigned)P;
+    const int p = i < (unsigned)a.g.stride ? a.g.table[(size_t)row * a.g.stride + i] : -1;
+    return p < a.g.n_pages ? p : -1;
+  };
+  auto next_part = [&]() {
+    Part p{};
+    if (at >= end) return p;
     while (starts[b + 1] <= at) ++b;
     const Units un = units_of<TT>(a, b, NW);
     const int64_t in = at - starts[b];
-    const int unit = (int)(!plan.cut ? in : in < (1ll << 32) ? (unsigned)in / (unsigned)un.tiles : in / un.tiles), tile0 = plan.cut ? (int)(in - (int64_t)unit * un.tiles) : 0;
-    const int tile1 = plan.cut ? (int)min((int64_t)un.tiles, tile0 + (end - at)) : un.tiles;
-    at += plan.cut ? tile1 - tile0 : 1;
-    const int h = unit / un.blocks, q0 = (unit % un.blocks) * NW * 32;
-    const int r0 = max(a.cu[b], 0), rows = rows_of(a, b), L = max(a.lens[b], 0), total = tokens_of(a, b, rows);
-    const int pair = q0 + wave * 32 + col;
-    const bool valid = pair < rows * g;
-    const int i_row = valid ? pair / g : 0, r = r0 + i_row, head = h * g + (valid ? pair % g : 0);
-    const int32_t *table = a.g.table + (size_t)b * a.g.stride;
-    const unsigned char *const k_base = (const unsigned char *)a.g.pool + (size_t)h * P * RB, *const v_base = (const unsigned char *)a.g.pool + (size_t)(H + h) * P * RB;
+    const int unit = __builtin_amdgcn_readfirstlane((int)(!plan.cut ? in : in < (1ll << 32) ? (unsigned)in / (unsigned)un.tiles : in / un.tiles));
+    p.b = b;
+    p.tiles = __builtin_amdgcn_readfirstlane(un.tiles);
+    p.tile0 = plan.cut ? __builtin_amdgcn_readfirstlane((int)(in - (int64_t)unit * un.tiles)) : 0;
+    p.tile1 = plan.cut ? (int)min((int64_t)p.tiles, p.tile0 + (end - at)) : p.tiles;
+    at += plan.cut ? p.tile1 - p.tile0 : 1;
+    p.q0 = unit * NW * 32;
+    p.r0 = max(a.cu[b], 0);
+    p.rows = rows_of(a, b);
+    p.cached = max(a.lens[b], 0);
+    p.total = tokens_of(a, b, p.rows);
+    p.pages = look_up(b, p.tile0, p.tiles);
+    return p;
+  };
+  const unsigned char *const k_base = (const unsigned char *)a.g.pool + (size_t)h * P * RB, *const v_base = (const unsigned char *)a.g.pool + (size_t)(H + h) * P * RB;
+  auto issue_k = [&](int tile, int pages, int first) {
+    const unsigned char *base = k_base;
+    if (ONE) base += (size_t)max(__builtin_amdgcn_readlane(pages, tile - first), 0) * page_size + (size_t)((unsigned)tile * TT % (unsigned)P) * RB;
+#pragma unroll
+    for (int q = 0; q < IPW; ++q) {
+      unsigned off = (k_lane ^ (swizzle(q * RPI) << 4)) + q * 1024;
+      if (!ONE) {
+        const int row = k_row0 + q * RPI, place = ((unsigned)tile * TT + row) % (unsigned)P;
+        base = k_base + (size_t)max(__shfl(pages, row >> 3), 0) * page_size;
+        off += (place - row) * RB;
+      }
+      __builtin_amdgcn_global_load_lds(FK_GLB_PTR(base + off), FK_LDS_PTR(Ks + (wave * IPW + q) * 1024), 16, 0, kNonTemporal);
+    }
+  };
+  auto issue_v = [&](int tile, int pages, int first) {
+    const unsigned char *base = v_base;
+    if (ONE) base += (size_t)max(__builtin_amdgcn_readlane(pages, tile - first), 0) * page_size + (size_t)((unsigned)tile * TT % (unsigned)P) * ES;
+#pragma unroll
+    for (int q = 0; q < IPW; ++q) {
+      const unsigned chunk = v_chunk0 ^ (q * 4 & 7);
+      unsigned off = (unsigned)v_row0 * (P * ES) + chunk * 16;
+      if (!ONE) {
+        const int t = chunk * (16 / ES);
+        base = v_base + (size_t)max(__shfl(pages, t >> 3), 0) * page_size;
+        off += (((unsigned)tile * TT + t) % (unsigned)P - t) * ES;
+      }
+      __builtin_amdgcn_global_load_lds(FK_GLB_PTR(base + (size_t)q * 8 * P * ES + off), FK_LDS_PTR(Vs + (wave * IPW + q) * 1024), 16, 0, kNonTemporal);
+    }
+  };
+  // Bit i: the page of the tile's i-th 8 tokens is one.
+  auto pages_there = [&](int tile, int pages, int first) -> unsigned {
+    return ONE ? (__builtin_amdgcn_readlane(pages, tile - first) >= 0 ? (1u << GROUPS) - 1 : 0u) : (unsigned)__builtin_amdgcn_ballot_w64(pages >= 0) & ((1u << GROUPS) - 1);
+  };
 
-    // Pages.  ONE: lane i holds the page of tile first + i.  Else lane i < GROUPS holds the page of the i-th 8 tokens of the next tile that will be fetched.
-    // A page that is none is read as page 0, and its tokens are masked.
-    int pages, first = tile0;
-    auto page_at = [&](unsigned t) {
-      const unsigned i = t / (unsigned)P;
-      const int p = i < (unsigned)a.g.stride ? table[i] : -1;
-      return p < a.g.n_pages ? p : -1;
-    };
-    auto look_up = [&](int tile) {
-      if (ONE) {
-        pages = page_at((unsigned)min(tile + lane, un.tiles - 1) * TT);
-        first = tile;
-      } else {
-        pages = page_at((unsigned)tile * TT + 8 * (lane & (GROUPS - 1)));
-      }
-    };
-    auto issue_k = [&](int tile) {
-      const unsigned char *base = k_base;
-      if (ONE) base += (size_t)max(__builtin_amdgcn_readlane(pages, tile - first), 0) * page_size + (size_t)((unsigned)tile * TT % (unsigned)P) * RB;
-#pragma unroll
-      for (int q = 0; q < IPW; ++q) {
-        unsigned off = (k_lane ^ (swizzle(q * RPI) << 4)) + q * 1024;
-        if (!ONE) {
-          const int row = k_row0 + q * RPI, place = ((unsigned)tile * TT + row) % (unsigned)P;
-          base = k_base + (size_t)max(__shfl(pages, row >> 3), 0) * page_size;
-          off += (place - row) * RB;
-        }
-        __builtin_amdgcn_global_load_lds(FK_GLB_PTR(base + off), FK_LDS_PTR(Ks + (wave * IPW + q) * 1024), 16, 0, kNonTemporal);
-      }
-    };
-    auto issue_v = [&](int tile, int pg) {
-      const unsigned char *base = v_base;
-      if (ONE) base += (size_t)max(__builtin_amdgcn_readlane(pg, tile - first), 0) * page_size + (size_t)((unsigned)tile * TT % (unsigned)P) * ES;
-#pragma unroll
-      for (int q = 0; q < IPW; ++q) {
-        const unsigned chunk = v_chunk0 ^ (q * 4 & 7);
-        unsigned off = (unsigned)v_row0 * (P * ES) + chunk * 16;
-        if (!ONE) {
-          const int t = chunk * (16 / ES);
-          base = v_base + (size_t)max(__shfl(pg, t >> 3), 0) * page_size;
-          off += (((unsigned)tile * TT + t) % (unsigned)P - t) * ES;
-        }
-        __builtin_amdgcn_global_load_lds(FK_GLB_PTR(base + (size_t)q * 8 * P * ES + off), FK_LDS_PTR(Vs + (wave * IPW + q) * 1024), 16, 0, kNonTemporal);
-      }
-    };
-    // Bit i: the page of the tile's i-th 8 tokens is one.
-    auto pages_there = [&](int tile, int pg) -> unsigned {
-      return ONE ? (__builtin_amdgcn_readlane(pg, tile - first) >= 0 ? (1u << GROUPS) - 1 : 0u) : (unsigned)__builtin_amdgcn_ballot_w64(pg >= 0) & ((1u << GROUPS) - 1);
-    };
+  Part now = next_part();
+  // `pages` and `first` are those of the tile whose loads are asked for next, or that is in use; ONE false: `ahead` those of the tile after it.
+  int pages = now.pages, first = now.tile0, pages_ahead = 0;
+  issue_k(now.tile0, pages, first);
+  issue_v(now.tile0, pages, first);
+  unsigned there = pages_there(now.tile0, pages, first);
+  while (now.tiles > 0) {
+    const int L = now.cached, total = now.total;
+    const int pair = now.q0 + wave * 32 + col;
+    const bool valid = pair < now.rows * g;
+    const int i_row = valid ? pair / g : 0, r = now.r0 + i_row, head = h * g + (valid ? pair % g : 0);
     // Word w of the row's set of drafted tokens.
     auto seen_word = [&](int w) -> uint64_t {
       if (a.seen) return w >= 0 && w < a.seen_words ? a.seen[(size_t)r * a.seen_words + w] : 0ull;
       const int last = i_row - 64 * w;
       return w < 0 || last < 0 ? 0ull : last >= 63 ? ~0ull : (2ull << last) - 1;
     };
-
     u32x4 qf[KS];
     {
       const T *qp = (const T *)a.q + (size_t)r * a.ldq + (size_t)head * D;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
         u32x4 v = {0, 0, 0, 0};
-        const T *from = qp + (2 * ks + half) * (16 / ES);
+        const T *from_q = qp + (2 * ks + half) * (16 / ES);
         if (valid && a.scale != 0.f) {
           if (wide_q) {
-            v = *(const u32x4 *)from;
+            v = *(const u32x4 *)from_q;
           } else {
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              v[e] = ES == 2 ? (unsigned)((const uint16_t *)from)[2 * e] | (unsigned)((const uint16_t *)from)[2 * e + 1] << 16 : ((const uint32_t *)from)[e];
+              v[e] = ES == 2 ? (unsigned)((const uint16_t *)from_q)[2 * e] | (unsigned)((const uint16_t *)from_q)[2 * e + 1] << 16 : ((const uint32_t *)from_q)[e];
           }
 #pragma unroll
           for (int e = 0; e < 4; ++e) v[e] ^= flip;
@@ -315,6 +355,8 @@ __global__ __launch_bounds__(NW * 64, NW == 1 && D == 128 ? 1 : 2) void k_tree(T
       }
     }
     const uint64_t seen0 = seen_word(0);
+    const Part next = next_part();
+    if (!ONE) pages_ahead = now.tile0 + 1 < now.tile1 ? look_up(now.b, now.tile0 + 1, now.tiles) : next.pages;
     f32x16 o[DS];
 #pragma unroll
     for (int i = 0; i < DS; ++i)
@@ -324,15 +366,9 @@ __global__ __launch_bounds__(NW * 64, NW == 1 && D == 128 ? 1 : 2) void k_tree(T
 
     // One K buffer and one V buffer, each filled again as soon as the product that reads it is done.  Loads complete in order, so "at most IPW outstanding" means
     // that the older tile is there.
-    look_up(tile0);
-    __builtin_amdgcn_s_barrier();                      // the unit before has read its last V
-    issue_k(tile0);
-    issue_v(tile0, pages);
-    int pages_v = pages;                               // of the tile whose V is fetched or in use
-    for (int tile = tile0; tile < tile1; ++tile) {
-      const bool more = tile + 1 < tile1;
-      const unsigned there = pages_there(tile, pages_v);
-      if (more && !ONE) look_up(tile + 1);
+    for (int tile = now.tile0; tile < now.tile1; ++tile) {
+      const bool more = tile + 1 < now.tile1, any = more || next.tiles > 0;
+      const int tile_n = more ? tile + 1 : next.tile0;
       __builtin_amdgcn_s_waitcnt(vmcnt_imm(IPW));      // K of this tile is in LDS
       __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
@@ -350,14 +386,27 @@ __global__ __launch_bounds__(NW * 64, NW == 1 && D == 128 ? 1 : 2) void k_tree(T
       }
       asm volatile("" ::: "memory");
       __builtin_amdgcn_s_barrier();                    // every wavefront has read K
-      if (ONE && more && tile + 1 - first == 64) {
-        look_up(tile + 1);
-        __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+      const unsigned there_now = there;
+      if (any) {
+        if (ONE) {
+          if (!more) {
+            pages = next.pages;
+            first = next.tile0;
+          } else if (tile + 1 - first == 64) {
+            pages = look_up(now.b, tile + 1, now.tiles);
+            first = tile + 1;
+            __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+          }
+        } else {
+          pages = pages_ahead;
+        }
+        issue_k(tile_n, pages, first);
+        there = pages_there(tile_n, pages, first);
+        if (!ONE && more) pages_ahead = tile + 2 < now.tile1 ? look_up(now.b, tile + 2, now.tiles) : next.pages;
       }
-      if (more) issue_k(tile + 1);
-      // Which of the tile's tokens the pair sees: bit t, token tile * TT + t.
+    // Which of the tile's tokens the pair sees: bit t, token tile * TT + t.
       const int ahead = L - tile * TT;                 // tokens of the tile that are cached ones
-      const bool masked = ahead < TT || there != (1u << GROUPS) - 1;
+      const bool masked = ahead < TT || there_now != (1u << GROUPS) - 1;
       uint64_t mask = ~0ull;
       if (masked) {
         if (ahead < TT) {
@@ -373,7 +422,7 @@ __global__ __launch_bounds__(NW * 64, NW == 1 && D == 128 ? 1 : 2) void k_tree(T
         }
 #pragma unroll
         for (int i = 0; i < GROUPS; ++i)
-          if (!(there >> i & 1)) mask &= ~(0xffull << (8 * i));
+          if (!(there_now >> i & 1)) mask &= ~(0xffull << (8 * i));
 #pragma unroll
         for (int u = 0; u < U; ++u) {
           const int word = (int)((unsigned)(mask >> (32 * u)) >> ((ES == 2 ? 8 : 4) * half));      // a lane's tokens at places that the compiler knows
@@ -411,7 +460,7 @@ __global__ __launch_bounds__(NW * 64, NW == 1 && D == 128 ? 1 : 2) void k_tree(T
 #pragma unroll
           for (int e = 0; e < 16; ++e) o[i][e] *= corr;
       }
-      if (more) __builtin_amdgcn_s_waitcnt(vmcnt_imm(IPW)); else __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));   // V is in LDS
+      if (any) __builtin_amdgcn_s_waitcnt(vmcnt_imm(IPW)); else __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));   // V is in LDS
       __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
       auto v_piece = [&](int ds, int kk) {
@@ -426,7 +475,7 @@ __global__ __launch_bounds__(NW * 64, NW == 1 && D == 128 ? 1 : 2) void k_tree(T
         for (int i = 0; i < IPW; ++i) {
           const int vr = (wave * IPW + i) * 8 + (lane >> 3), t0 = ((lane & 7) ^ ((vr >> 1) & 7)) * (16 / ES);
           if (not_finite<T>(*(const u32x4 *)(Vs + (wave * IPW + i) * 1024 + lane * 16))) {
-            const bool exists = tile * TT + t0 < total && (there >> (t0 >> 3) & 1);
+            const bool exists = tile * TT + t0 < total && (there_now >> (t0 >> 3) & 1);
             found |= exists ? 3 : 1;
           }
         }
@@ -478,103 +527,111 @@ __global__ __launch_bounds__(NW * 64, NW == 1 && D == 128 ? 1 : 2) void k_tree(T
         for (int kk = 0; kk < 4; ++kk) o[ds] = multiply<T>(v_piece(ds, kk), pf[kk], o[ds]);
       asm volatile("" ::: "memory");
       __builtin_amdgcn_s_barrier();                    // every wavefront has read V
-      if (more) {
-        pages_v = pages;
-        issue_v(tile + 1, pages_v);
-      }
+      if (any) issue_v(tile_n, pages, first);
     }
 
     const float l_tot = l + __shfl_xor(l, 32);
-    if (tile0 == 0 && tile1 < un.tiles && tid == 0) {
-      int *const c = plan.cuts + (size_t)blockIdx.x * 8;
-      c[0] = r0; c[1] = q0; c[2] = min(rows * g - q0, NW * 32); c[3] = h; c[4] = (int)((un.tiles - tile1 + per - 1) / per) + 1;
+    if (now.tile0 == 0 && now.tile1 < now.tiles && tid == 0) {
+      int *const c = plan.cuts + (size_t)piece * 8;
+      c[0] = now.r0; c[1] = now.q0; c[2] = min(now.rows * g - now.q0, NW * 32); c[3] = (int)((now.tiles - now.tile1 + per - 1) / per) + 1;
     }
-    if (!valid) continue;
-    if (tile0 == 0 && tile1 == un.tiles) {
+    if (now.tile0 == 0 && now.tile1 == now.tiles) {
       const float inv = l_tot == 0.f ? 0.f : 1.0f / l_tot;
       T *to = (T *)a.out + (size_t)r * a.ldo + (size_t)head * D;
 #pragma unroll
       for (int ds = 0; ds < DS; ++ds)
 #pragma unroll
-        for (int q4 = 0; q4 < 4; ++q4) {
-          T v[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] = (T)(o[ds][4 * q4 + e] * inv);
-          T *t = to + 32 * ds + 8 * q4 + 4 * half;
-          if (wide_o) {
-            if (ES == 2) *(uint64_t *)t = __builtin_bit_cast(uint64_t, *(const bf16x4 *)v); else *(f32x4 *)t = *(const f32x4 *)v;
-          } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) t[e] = v[e];
-          }
-        }
+        for (int q4 = 0; q4 < 4; ++q4)
+          if (valid) store4<T>(to + 32 * ds + 8 * q4 + 4 * half, f32x4{o[ds][4 * q4], o[ds][4 * q4 + 1], o[ds][4 * q4 + 2], o[ds][4 * q4 + 3]} * inv, wide_o);
     } else {
-      const size_t slot = ((size_t)2 * blockIdx.x + (tile0 == 0)) * (NW * 32) + wave * 32 + col;
-      float *po = plan.part_o + slot * D;
+      // Sums go out register by register, 1 KB of all lanes at a time (16 bytes of every pair at a time, 32 pairs apart, took 26 us more for 33 MB).
+      const size_t slot = ((size_t)2 * piece + (now.tile0 == 0)) * NW + wave;
+      float *const po = plan.part_o + slot * 32 * D + lane * 4;
 #pragma unroll
       for (int ds = 0; ds < DS; ++ds)
 #pragma unroll
         for (int q4 = 0; q4 < 4; ++q4)
-          *(f32x4 *)(po + 32 * ds + 8 * q4 + 4 * half) = f32x4{o[ds][4 * q4], o[ds][4 * q4 + 1], o[ds][4 * q4 + 2], o[ds][4 * q4 + 3]};
-      if (half == 0) {
-        plan.part_ml[slot * 2] = m;
-        plan.part_ml[slot * 2 + 1] = l_tot;
-      }
+          if (valid) *(f32x4 *)(po + (ds * 4 + q4) * 256) = f32x4{o[ds][4 * q4], o[ds][4 * q4 + 1], o[ds][4 * q4 + 2], o[ds][4 * q4 + 3]};
+      if (valid && half == 0) *(float2 *)(plan.part_ml + (slot * 32 + col) * 2) = make_float2(m, l_tot);
     }
+    now = next;
   }
 }
 
-// Units that a cut went through: out = sum_i o_i 2^(m_i - M) / sum_i l_i 2^(m_i - M), i over the pieces in their order.  A workgroup looks after the unit that
-// begins in piece blockIdx.x, a wavefront takes one pair: 64 / (D / 4) groups of lanes take every so manieth piece, four at a time, and their sums are added in group order.
-template <typename T, int D>
+// Units that a cut went through: out = sum_i o_i 2^(m_i - M) / sum_i l_i 2^(m_i - M), i over the pieces in their order.  blockIdx.x is the piece that the unit begins
+// in; a wavefront takes four columns for each half of its lanes of 32 pairs, as they were written, from eight pieces at a time with a running maximum.  FAR: the four
+// wavefronts of a workgroup share the pieces of such columns, for few sequences in many pieces.  The launch takes what its chain of loads takes: a record, then
+// everything.
+template <typename T, int D, bool FAR>
 __global__ __launch_bounds__(256) void k_tree_join(TreeArgs a, TreePlan plan) {
-  constexpr int LANES = D / 4, GROUPS = 64 / LANES;
+  constexpr int LINES = D / 8, AT_ONCE = 8;
+  __shared__ f32x4 num_s[FAR ? 4 : 1][64];
+  __shared__ float2 den_s[FAR ? 4 : 1][64];
   const int *const rec = plan.cuts + (size_t)blockIdx.x * 8;
-  const int lane = threadIdx.x & 63, pair = blockIdx.y * 4 + (threadIdx.x >> 6), c = lane % LANES, grp = lane / LANES;
-  const int r0 = rec[0], q0 = rec[1], pairs = rec[2], h = rec[3], n = rec[4];
-  if (pair >= pairs) return;
-  const int g = a.n_q_heads / a.g.n_kv_heads, per_block = plan.nw * 32;
-  auto slot_of = [&](int i) { return ((size_t)2 * (blockIdx.x + i) + (i == 0)) * per_block + pair; };
-  float mm = -INFINITY;
-  for (int i = lane; i < n; i += 64) mm = fmaxf(mm, plan.part_ml[slot_of(i) * 2]);
-  for (int x = 32; x > 0; x >>= 1) mm = fmaxf(mm, __shfl_xor(mm, x));
+  const int lane = threadIdx.x & 63, half = lane >> 5, w = threadIdx.x >> 6, id = FAR ? blockIdx.y : blockIdx.y * 4 + w, wave = id / LINES, line = id % LINES;
+  const int pair = wave * 32 + (lane & 31);
+  const int r0 = rec[0], q0 = rec[1], pairs = rec[2], all = rec[3], H = a.g.n_kv_heads;
+  if (wave * 32 >= pairs) return;
+  const int share = FAR ? (all + 3) / 4 : all, n = FAR ? min(all, (w + 1) * share) : all;
   f32x4 num = {0.f, 0.f, 0.f, 0.f};
-  float den = 0.f;
-  for (int i0 = grp; i0 < n; i0 += 4 * GROUPS) {
-    f32x4 v[4];
-    float2 ml[4];
+  float den = 0.f, mm = -INFINITY;
+  for (int i0 = FAR ? w * share : 0; i0 < n; i0 += AT_ONCE) {
+    f32x4 v[AT_ONCE];
+    float2 ml[AT_ONCE];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const size_t s = slot_of(min(i0 + j * GROUPS, n - 1));
-      v[j] = *(const f32x4 *)(plan.part_o + s * D + c * 4);
-      ml[j] = *(const float2 *)(plan.part_ml + s * 2);
+    for (int j = 0; j < AT_ONCE; ++j) {
+      const int i = min(i0 + j, n - 1);
+      const size_t slot = ((size_t)2 * (blockIdx.x + (size_t)i * H) + (i == 0)) * plan.nw + wave;
+      v[j] = *(const f32x4 *)(plan.part_o + slot * 32 * D + line * 256 + lane * 4);
+      ml[j] = *(const float2 *)(plan.part_ml + (slot * 32 + (lane & 31)) * 2);
     }
+    float top = mm;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const bool there = i0 + j * GROUPS < n && ml[j].x != -INFINITY;
-      const float k = there ? exp2f(ml[j].x - mm) : 0.f;
-      den += there ? ml[j].y * k : 0.f;
+    for (int j = 0; j < AT_ONCE; ++j) top = fmaxf(top, ml[j].x);         // the last piece twice is no other maximum
+    const float old = mm == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mm - top);
+    den *= old;
+    num *= old;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) num[e] += there ? v[j][e] * k : 0.f;
+    for (int j = 0; j < AT_ONCE; ++j) {
+      const bool sees = i0 + j < n && (ml[j].x != -INFINITY || ml[j].y != 0.f);       // else nothing was seen there; weights that are no numbers come through
+      const float k = sees ? __builtin_amdgcn_exp2f(ml[j].x - top) : 0.f;
+      den += sees ? ml[j].y * k : 0.f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) num[e] += sees ? v[j][e] * k : 0.f;
+    }
+    mm = top;
+  }
+  if (FAR) {
+    num_s[w][lane] = num;
+    den_s[w][lane] = make_float2(mm, den);
+    __syncthreads();
+    if (w != 0) return;
+    float2 x[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = den_s[i][lane];
+    const float top = fmaxf(fmaxf(x[0].x, x[1].x), fmaxf(x[2].x, x[3].x));
+    num = f32x4{0.f, 0.f, 0.f, 0.f};
+    den = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const bool sees = x[i].x != -INFINITY || x[i].y != 0.f;
+      const float k = sees ? __builtin_amdgcn_exp2f(x[i].x - top) : 0.f;
+      den += sees ? x[i].y * k : 0.f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) num[e] += sees ? num_s[i][lane][e] * k : 0.f;
     }
   }
-  for (int x = LANES; x < 64; x <<= 1) {
-    den += __shfl_xor(den, x);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) num[e] += __shfl_xor(num[e], x);
-  }
-  if (grp != 0) return;
-  const float inv = den == 0.f ? 0.f : 1.0f / den;
-  T *to = (T *)a.out + (size_t)(r0 + (q0 + pair) / g) * a.ldo + (size_t)(h * g + (q0 + pair) % g) * D + c * 4;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) to[e] = (T)(num[e] * inv);
+  if (pair >= pairs) return;
+  const int g = a.n_q_heads / H, row = r0 + (q0 + pair) / g, head = blockIdx.x % H * g + (q0 + pair) % g;
+  store4<T>((T *)a.out + (size_t)row * a.ldo + (size_t)head * D + 32 * (line / 4) + 8 * (line % 4) + 4 * half, num * (den == 0.f ? 0.f : 1.0f / den),
+            ((uintptr_t)a.out | (uintptr_t)(a.ldo * sizeof(T))) % 16 == 0);
 }
 
 // ---------------------------------------------------------------------------------------------
 namespace {
 
 struct Shape {
-  int nw, pieces;
+  int nw, ranges;
   size_t starts_bytes, cuts_bytes, bytes;
 };
 Shape shape_of(const TreeArgs &a) {
@@ -584,27 +641,33 @@ Shape shape_of(const TreeArgs &a) {
   s.nw = pairs <= 32 ? 1 : pairs <= 64 ? 2 : 4;
   const int64_t tokens = std::min((int64_t)a.g.stride * a.g.page_size, a.max_len > 0 ? (int64_t)a.max_len : INT64_MAX);
   const int64_t blocks = ((int64_t)a.n_rows * g + s.nw * 32 - 1) / (s.nw * 32) + a.n_seq;
-  const int64_t tiles = std::min((int64_t)1 << 40, blocks * a.g.n_kv_heads) * ((tokens + tt - 1) / tt);
-  s.pieces = (int)std::max((int64_t)1, std::min((int64_t)256 * (s.nw == 4 ? 2 : a.head_dim == 64 ? 8 : 4), (tiles + kLeastTiles - 1) / kLeastTiles));
+  const int64_t tiles = std::min((int64_t)1 << 40, blocks) * ((tokens + tt - 1) / tt);
+  const int at_once = 256 * (s.nw == 4 ? 2 : a.head_dim == 64 ? 8 : 4), most = std::max(1, at_once / a.g.n_kv_heads);
+  s.ranges = (int)std::max((int64_t)1, std::min((int64_t)most, (tiles + kLeastTiles - 1) / kLeastTiles));
+  if (s.ranges >= 8) s.ranges = std::min((s.ranges + 7) / 8 * 8, most / 8 * 8 ? most / 8 * 8 : most);
+  const size_t pieces = (size_t)s.ranges * a.g.n_kv_heads;
   s.starts_bytes = ((size_t)a.n_seq + 1) * 8;
   s.starts_bytes = (s.starts_bytes + 255) / 256 * 256;
-  s.cuts_bytes = ((size_t)s.pieces * 32 + 255) / 256 * 256;
-  s.bytes = s.starts_bytes + s.cuts_bytes + (size_t)2 * s.pieces * s.nw * 32 * (a.head_dim + 2) * 4;
+  s.cuts_bytes = (pieces * 32 + 255) / 256 * 256;
+  s.bytes = s.starts_bytes + s.cuts_bytes + 2 * pieces * s.nw * 32 * (a.head_dim + 2) * 4;
   return s;
 }
 
 template <typename T, int D, int NW>
 void launch(hipStream_t s, const TreeArgs &a, const TreePlan &p) {
   if (a.g.page_size % (128 / sizeof(T)) == 0)
-    k_tree<T, D, NW, true><<<p.pieces, NW * 64, 0, s>>>(a, p);
+    k_tree<T, D, NW, true><<<p.ranges * a.g.n_kv_heads, NW * 64, 0, s>>>(a, p);
   else
-    k_tree<T, D, NW, false><<<p.pieces, NW * 64, 0, s>>>(a, p);
+    k_tree<T, D, NW, false><<<p.ranges * a.g.n_kv_heads, NW * 64, 0, s>>>(a, p);
 }
 template <typename T, int D>
 void run(hipStream_t s, const TreeArgs &a, const TreePlan &p) {
   if (p.starts_given) k_tree_starts<128 / sizeof(T)><<<1, 1024, 0, s>>>(a, p);
   p.nw == 1 ? launch<T, D, 1>(s, a, p) : p.nw == 2 ? launch<T, D, 2>(s, a, p) : launch<T, D, 4>(s, a, p);
-  if (p.cut) k_tree_join<T, D><<<dim3(p.pieces, p.nw * 8), 256, 0, s>>>(a, p);
+  if (p.cut && a.n_seq < p.ranges)
+    k_tree_join<T, D, true><<<dim3(p.ranges * a.g.n_kv_heads, p.nw * (D / 8)), 256, 0, s>>>(a, p);
+  else if (p.cut)
+    k_tree_join<T, D, false><<<dim3(p.ranges * a.g.n_kv_heads, p.nw * (D / 8) / 4), 256, 0, s>>>(a, p);
 }
 
 }  // namespace
@@ -615,13 +678,13 @@ void tree_attention(hipStream_t s, const TreeArgs &a) {
   const Shape sh = shape_of(a);
   TreePlan p{};
   p.nw = sh.nw;
-  p.pieces = sh.pieces;
+  p.ranges = sh.ranges;
   p.starts = (int64_t *)a.scratch.ptr;
   p.cut = a.scratch.bytes >= sh.bytes;
   p.starts_given = a.n_seq > kFewSequences && a.scratch.bytes >= sh.starts_bytes;
   p.cuts = (int *)((char *)a.scratch.ptr + sh.starts_bytes);
   p.part_o = (float *)((char *)p.cuts + sh.cuts_bytes);
-  p.part_ml = p.part_o + (size_t)2 * sh.pieces * sh.nw * 32 * a.head_dim;
+  p.part_ml = p.part_o + (size_t)2 * sh.ranges * a.g.n_kv_heads * sh.nw * 32 * a.head_dim;
   if (a.dtype == FOCUS_F32)
     a.head_dim == 64 ? run<float, 64>(s, a, p) : run<float, 128>(s, a, p);
   else
