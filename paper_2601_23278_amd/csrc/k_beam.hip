@@ -1,6 +1,6 @@
 // A step of beam search: the best continuations of every request's beams.
 //
-// score(b, v) = scores[b] + (l_bv - lse_b) in 64 bits, lse = m + log(sum_v exp(l_v - m)).  Within a beam the order of the scores is that of the logits, so a beam
+// score(b, v) = scores[b] + (l_bv - lse_b) in 64 bits, lse = m + log(sum_v exp(l_v - m)) to 2^-34.  Within a beam the order of the scores is that of the logits, so a beam
 // gives its k largest logits (ties: lower token) and its lse, and the picks come from n_beams lists of k.
 //
 // Two launches.  k_beam_scan reads every logit once: a row is cut into parts, one workgroup each, which leaves the part's maximum, its sum of exponentials and its
@@ -27,32 +27,30 @@ __device__ __forceinline__ float key_logit(uint64_t key) {
 }
 __device__ __forceinline__ int key_token(uint64_t key) { return (int)~(uint32_t)key; }
 
-// exp(d) for -800 <= d <= 0, to 3e-13: d = n log 2 + r, |r| <= 0.347, and the Taylor series of exp(r) up to r^10 (r^11 / 11! = 2e-13).  n comes from the last bits
-// of a sum with 1.5 * 2^52, whose neighbours lie 1 apart, and 2^n goes into the exponent's bits.
+// exp(d) for -700 <= d <= 700, to 1.1e-12: d = n log 2 + r, |r| <= 0.347, and the polynomial of degree 8 that meets exp at nine Chebyshev nodes of that interval.
+// n comes from the last bits of a sum with 1.5 * 2^52, whose neighbours lie 1 apart, and 2^n goes into the exponent's bits.
 __device__ __forceinline__ double exp64(double d) {
   typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
   constexpr double unit = 6755399441055744.0;
   const double t = __builtin_fma(d, 1.4426950408889634074, unit);
   const double r = __builtin_fma(t - unit, -0.69314718055994530942, d);
-  double p = 1.0 / 3628800.0;
-  p = __builtin_fma(p, r, 1.0 / 362880.0);
-  p = __builtin_fma(p, r, 1.0 / 40320.0);
-  p = __builtin_fma(p, r, 1.0 / 5040.0);
-  p = __builtin_fma(p, r, 1.0 / 720.0);
-  p = __builtin_fma(p, r, 1.0 / 120.0);
-  p = __builtin_fma(p, r, 1.0 / 24.0);
-  p = __builtin_fma(p, r, 1.0 / 6.0);
-  p = __builtin_fma(p, r, 0.5);
-  p = __builtin_fma(p, r, 1.0);
+  double p = 2.487623871994097e-05;
+  p = __builtin_fma(p, r, 0.00019915941664891244);
+  p = __builtin_fma(p, r, 0.0013888821542986098);
+  p = __builtin_fma(p, r, 0.008333265963232838);
+  p = __builtin_fma(p, r, 0.041666666891631156);
+  p = __builtin_fma(p, r, 0.16666666891720291);
+  p = __builtin_fma(p, r, 0.49999999999797123);
+  p = __builtin_fma(p, r, 0.9999999999797041);
   p = __builtin_fma(p, r, 1.0);
   u32x2 w = __builtin_bit_cast(u32x2, p);
   w[1] += __builtin_bit_cast(u32x2, t)[0] << 20;
   return __builtin_bit_cast(double, w);
 }
-// Factor that takes a sum with maximum m to the maximum m_new >= m.
+// Factor that takes a sum of exp(l - m) to one of exp(l - m_new).
 __device__ __forceinline__ double rescale(float m, float m_new) {
   const double d = (double)m - (double)m_new;
-  return m == m_new ? 1.0 : d < -700.0 ? 0.0 : exp64(d);          // never of a NaN: maxima are none
+  return m == m_new ? 1.0 : d < -700.0 ? 0.0 : exp64(d);
 }
 
 constexpr int kMostLists = 1024;       // of a request
@@ -167,28 +165,35 @@ __global__ __launch_bounds__(256) void k_beam_scan(BeamArgs a, BeamPlan plan) {
   };
   auto fetch = [&](int i) { return i < nvec ? (u32x4)vec[i] : nothing; };
   u32x4 now = fetch(tid), next = fetch(tid + 256);
-  float m = extra == extra ? extra : none;
-  double sum = m == none ? 0.0 : 1.0;
+  // The sum is kept at a reference that moves only when a logit is far above it, not at the running maximum; second and at: the largest of a thread's other loads,
+  // and the load that its largest logit came with.
+  float m = extra == extra ? extra : none, ref = none, second = none;
+  double sum = 0.0;
   bool odd = extra != extra;
+  int at = -1;
 #pragma unroll 1
   for (int i0 = 0; i0 < nvec; i0 += 256) {
     const u32x4 after = fetch(i0 + tid + 512);
-    float top = m;
+    float top = none;
 #pragma unroll
     for (int x = 0; x < EPV; ++x) {
       const float y = element<T>(now, x);
       top = fmaxf(top, y);
       odd |= y != y;
     }
-    if (top > m) {
-      sum *= rescale(m, top);
-      m = top;
+    if (i0 == 0) ref = wavefront_max(top);
+    second = fmaxf(second, fminf(m, top));
+    at = top > m ? i0 + tid : at;
+    m = fmaxf(m, top);
+    if (m > ref + 500.f) {                             // exp(700) is near the end of 64 bits
+      sum = ref == none ? 0.0 : sum * rescale(ref, m);
+      ref = m;
     }
     // Weights below exp(-700) count as that, and so does what is no number; the end makes up for it.
-    const double ref = m == none ? 0.0 : (double)m;
+    const double at_ref = ref == none ? 0.0 : (double)ref;
     double more[2] = {0.0, 0.0};
 #pragma unroll
-    for (int x = 0; x < EPV; ++x) more[x & 1] += exp64(__builtin_fmax((double)element<T>(now, x) - ref, -700.0));
+    for (int x = 0; x < EPV; ++x) more[x & 1] += exp64(__builtin_fmax((double)element<T>(now, x) - at_ref, -700.0));
     sum += more[0] + more[1];
     now = next;
     next = after;
@@ -196,7 +201,9 @@ __global__ __launch_bounds__(256) void k_beam_scan(BeamArgs a, BeamPlan plan) {
   // The part's maximum and sum.  Every wavefront has a quarter of k logits that are not below such a one of its threads' maxima, so k of the part are not below the
   // lowest of the four.
   const float wave_top = wavefront_max(m);
-  sum = odd ? (double)NAN : sum * rescale(m, wave_top);
+  sum = ref == none ? 0.0 : sum * rescale(ref, wave_top);
+  if (extra == extra && extra != none) sum += rescale(extra, wave_top);
+  if (odd) sum = NAN;
   sum = wavefront_sum(sum);
   float left = m, nth = wave_top;
 #pragma unroll 1
@@ -211,11 +218,11 @@ __global__ __launch_bounds__(256) void k_beam_scan(BeamArgs a, BeamPlan plan) {
   }
   __syncthreads();
   const float lim = fmaxf(-FLT_MAX, fminf(fminf(nth_s[0], nth_s[1]), fminf(nth_s[2], nth_s[3])));          // -inf is no candidate
-  // The few threads that have one of the largest look through their logits once more.
+  // The few threads that have one of the largest look at them once more: at one load, or where they have several at all of theirs.
   if (extra >= lim) push(extra, loose);
   if (m >= lim) {
 #pragma unroll 1
-    for (int i = tid; i < nvec; i += 256) {
+    for (int i = second >= lim || at < 0 ? tid : at; i < nvec; i += second >= lim || at < 0 ? 256 : nvec) {
       const u32x4 v = vec[i];
       unsigned which = 0;
 #pragma unroll
@@ -317,7 +324,8 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(BeamArgs a, BeamPlan
       m = top;
     }
     sum = wavefront_sum(sum);
-    const double value = (double)m + log(sum);
+    // To whole 2^-34, far above the error of the sum (1e-12): rows of equal logits in another order tie.
+    const double value = __builtin_rint(((double)m + log(sum)) * 0x1p34) * 0x1p-34;
     if (lane == 0) {
       lse[b] = value;
       base_s[b] = a.scores[row0 + b];

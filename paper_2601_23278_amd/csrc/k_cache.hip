@@ -232,24 +232,29 @@ __device__ __forceinline__ int sum_before(int v, int *part, int *all) {
   }
   if (lane == 63) part[wave] = x;
   __syncthreads();
-  int before = 0, total = 0;
+  int y = lane < n ? part[lane] : 0, before = 0;       // every wavefront sums up the others
+#pragma unroll 1
   for (int w = 0; w < n; ++w) {
-    if (w < wave) before += part[w];
-    total += part[w];
+    const int s = __builtin_amdgcn_readlane(y, w);
+    before += w < wave ? s : 0;
+    *all = w == 0 ? s : *all + s;
   }
   __syncthreads();
-  *all = total;
   return before + x - v;
 }
 
-// One workgroup.  start[i]: pages that row i wants; becomes the number of pages wanted by the rows before it.  Returns the sum.
-__device__ int order_wants(int32_t *start, int n, int *part) {
+// One workgroup.  start[i]: pages that row i wants; becomes the number of pages wanted by the rows before it, and tell(i, wants, before) is called.  Returns the sum.
+template <typename F>
+__device__ int order_wants(int32_t *start, int n, int *part, F tell) {
   int total = 0;
   for (int i0 = 0; i0 < n; i0 += blockDim.x) {
     const int i = i0 + threadIdx.x, v = i < n ? start[i] : 0;
     int all;
-    const int before = sum_before(v, part, &all);
-    if (i < n) start[i] = total + before;
+    const int before = total + sum_before(v, part, &all);
+    if (i < n) {
+      start[i] = before;
+      tell(i, v, before);
+    }
     total += all;
   }
   if (threadIdx.x == 0) start[n] = total;
@@ -265,7 +270,9 @@ __device__ int hand_out(int32_t *refs, int n_pages, int wanted, int *part, F giv
     const int p = p0 + 4 * threadIdx.x;
     int free[4], mine = 0, all;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) mine += free[e] = p + e < n_pages && refs[p + e] == 0;
+    for (int e = 0; e < 4; ++e) free[e] = refs[min(p + e, n_pages - 1)];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) mine += free[e] = p + e < n_pages && free[e] == 0;
     int rank = found + sum_before(mine, part, &all);
 #pragma unroll
     for (int e = 0; e < 4; ++e)
@@ -282,19 +289,25 @@ __device__ int hand_out(int32_t *refs, int n_pages, int wanted, int *part, F giv
   return min(found, wanted);
 }
 
+// Rows that want a page, in their order; up to kWantsInLds of them are told to the page that they get without a search in memory.
+constexpr int kWantsInLds = 4096;
 __global__ __launch_bounds__(1024) void k_fork_pages(ForkArgs a) {
   __shared__ int part[16];
+  __shared__ int who[kWantsInLds];
   const ForkWork w = fork_work(a);
-  const int wanted = order_wants(w.start, a.n_new, part);
+  const int wanted = order_wants(w.start, a.n_new, part, [&](int i, int v, int before) {
+    if (v && before < kWantsInLds) who[before] = i;
+    a.lacking[i] = 0;
+  });
   const int got = hand_out(a.refs, a.g.n_pages, wanted, part, [&](int rank, int page) {
-    const int i = sequence_of(w.start, a.n_new, rank);            // the row that wants page number `rank`
+    const int i = rank < kWantsInLds ? who[rank] : sequence_of(w.start, a.n_new, rank);
     w.to[i] = page;
     a.new_table[(size_t)i * a.g.stride + a.new_lens[i] / a.g.page_size] = page;
   });
-  for (int i = threadIdx.x; i < a.n_new; i += blockDim.x) {
-    const bool lacks = w.start[i + 1] > w.start[i] && w.start[i] >= got;
-    a.lacking[i] = lacks;
-    if (lacks) a.new_lens[i] -= w.tokens[i];
+  for (int rank = got + threadIdx.x; rank < wanted; rank += blockDim.x) {      // no page was left
+    const int i = rank < kWantsInLds ? who[rank] : sequence_of(w.start, a.n_new, rank);
+    a.lacking[i] = 1;
+    a.new_lens[i] -= w.tokens[i];
   }
 }
 
@@ -312,15 +325,30 @@ __global__ __launch_bounds__(256) void k_fork_copy(ForkArgs a) {
   const char *src = pool + (size_t)from * page_size;
   char *dst = pool + (size_t)to * page_size;
   const size_t k0 = (size_t)h * P * D * ES, v0 = (size_t)(H + h) * P * D * ES;
-  for (int j = threadIdx.x; j < n * D / PER; j += 256) *(u32x4 *)(dst + k0 + j * 16) = *(const u32x4 *)(src + k0 + j * 16);
-  const int pieces = (n + PER - 1) / PER;
-  for (int j = threadIdx.x; j < D * pieces; j += 256) {
-    const int d = j / pieces, c = j % pieces;
-    const size_t at = v0 + ((size_t)d * P + c * PER) * ES;
-    if ((c + 1) * PER <= n) {
-      *(u32x4 *)(dst + at) = *(const u32x4 *)(src + at);
-    } else {
-      for (int e = 0; c * PER + e < n; ++e) ((T *)(dst + at))[e] = ((const T *)(src + at))[e];
+  const int row = D * ES / 16, pieces = (n + PER - 1) / PER, k_pieces = n * row, all = k_pieces + D * pieces;      // 16 bytes each
+  auto offset = [&](int j) {                           // of piece j: K's rows, then the begun pieces of V^T's
+    if (j < k_pieces) return k0 + (size_t)j * 16;
+    const int i = j - k_pieces, d = i / pieces;
+    return v0 + ((size_t)d * P + (i - d * pieces) * PER) * ES;
+  };
+  for (int j0 = threadIdx.x; j0 < all; j0 += 4 * 256) {
+    u32x4 v[4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+      if (j0 + x * 256 < all) v[x] = *(const u32x4 *)(src + offset(j0 + x * 256));
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const int j = j0 + x * 256;
+      if (j >= all) continue;
+      char *const to_v = dst + offset(j);
+      const int left = j < k_pieces ? PER : n - (j - k_pieces) % pieces * PER;         // tokens of the piece that are there
+      if (left >= PER) {
+        *(u32x4 *)to_v = v[x];
+      } else {
+#pragma unroll
+        for (int e = 0; e < PER; ++e)
+          if (e < left) ((T *)to_v)[e] = ((const T *)&v[x])[e];
+      }
     }
   }
 }
@@ -347,11 +375,15 @@ __global__ __launch_bounds__(64) void k_reserve_rows(ReserveArgs a) {
 
 __global__ __launch_bounds__(1024) void k_reserve_pages(ReserveArgs a) {
   __shared__ int part[16];
+  __shared__ int start_s[kWantsInLds];                 // where a row's wants begin, looked up here for up to so many rows
   int32_t *const start = a.work, *const held = a.work + a.n_seq + 1, *const wants = a.work + 2 * (size_t)a.n_seq + 1;
-  const int wanted = order_wants(start, a.n_seq, part);
+  const bool in_lds = a.n_seq <= kWantsInLds;
+  const int wanted = order_wants(start, a.n_seq, part, [&](int b, int, int before) {
+    if (in_lds) start_s[b] = before;
+  });
   const int got = hand_out(a.refs, a.n_pages, wanted, part, [&](int rank, int page) {
-    const int b = sequence_of(start, a.n_seq, rank);
-    a.table[(size_t)b * a.stride + held[b] + rank - start[b]] = page;
+    const int b = in_lds ? sequence_of(start_s, a.n_seq, rank) : sequence_of(start, a.n_seq, rank);
+    a.table[(size_t)b * a.stride + held[b] + rank - (in_lds ? start_s[b] : start[b])] = page;
   });
   for (int b = threadIdx.x; b < a.n_seq; b += blockDim.x) a.lacking[b] = wants[b] - max(0, min(got, start[b + 1]) - start[b]);
 }
