@@ -449,7 +449,7 @@ int focus_kv_append(const focus_kv *kv, void *hip_stream, int32_t layer, int32_t
  * ordinary decoding, many rows with seen == NULL a part of a prompt.
  *   seen           device [n_rows, seen_words] uint64, bit j % 64 of word j / 64: drafted token j; seen_words 1..16; drafted tokens beyond its bits are unseen.
  *                  NULL: row i sees the drafted tokens j <= i
- *   n_q_heads      a multiple of n_kv_heads, at most 1024; query head h reads key head h / (n_q_heads / n_kv_heads)
+ *   n_q_heads      a multiple of n_kv_heads, at most 1024, n_rows * n_q_heads below 2^31; query head h reads key head h / (n_q_heads / n_kv_heads)
  *   q, out         device [n_rows, ldq], [n_rows, ldo] of the pool's type; rows behind cu_rows[n_seq] are neither read nor written
  *   max_rows, max_len   what the host knows of the sequences' rows and of their longest lens[b] + rows (0: nothing).  Launches are shaped for it, results do
  *                  not depend on it but for the rounding order of sums

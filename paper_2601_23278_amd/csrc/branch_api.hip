@@ -52,6 +52,7 @@ const char *check_rows(const focus_kv *kv, int32_t layer, int32_t n_seq, int32_t
 const char *check_tree(const focus_kv *kv, int32_t n_seq, int32_t n_rows, int32_t max_rows, int32_t max_len, int32_t table_stride, int32_t n_q_heads) {
   if (const char *e = check_rows(kv, 0, n_seq, n_rows, table_stride)) return e;
   if (n_q_heads < 1 || n_q_heads > 1024 || n_q_heads % kv->n_kv_heads) return "n_q_heads must be a multiple of n_kv_heads, at most 1024";
+  if ((int64_t)n_rows * n_q_heads >= (1ll << 31)) return "n_rows * n_q_heads must be below 2^31";
   if (max_rows < 0 || max_len < 0) return "max_rows and max_len must not be negative";
   return nullptr;
 }

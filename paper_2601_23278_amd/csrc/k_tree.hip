@@ -676,12 +676,24 @@ size_t tree_scratch(const TreeArgs &a) { return shape_of(a).bytes; }
 
 void tree_attention(hipStream_t s, const TreeArgs &a) {
   const Shape sh = shape_of(a);
+  if (a.n_seq > kFewSequences && a.scratch.bytes < sh.starts_bytes) {      // nowhere to write the starts: a launch for each few sequences
+    for (int b = 0; b < a.n_seq; b += kFewSequences) {
+      TreeArgs few = a;
+      few.n_seq = std::min(kFewSequences, a.n_seq - b);
+      few.cu += b;
+      few.lens += b;
+      few.g.table += (size_t)b * a.g.stride;
+      few.scratch = Scratch{};
+      tree_attention(s, few);
+    }
+    return;
+  }
   TreePlan p{};
   p.nw = sh.nw;
   p.ranges = sh.ranges;
   p.starts = (int64_t *)a.scratch.ptr;
   p.cut = a.scratch.bytes >= sh.bytes;
-  p.starts_given = a.n_seq > kFewSequences && a.scratch.bytes >= sh.starts_bytes;
+  p.starts_given = a.n_seq > kFewSequences;
   p.cuts = (int *)((char *)a.scratch.ptr + sh.starts_bytes);
   p.part_o = (float *)((char *)p.cuts + sh.cuts_bytes);
   p.part_ml = p.part_o + (size_t)2 * sh.ranges * a.g.n_kv_heads * sh.nw * 32 * a.head_dim;

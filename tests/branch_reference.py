@@ -156,7 +156,7 @@ def beam(logits, scores, k, done, end_token):
                 found.append((base, a, 0, end_token))
                 continue
             lse = float(torch.logsumexp(l, 0)) if bool(torch.isfinite(l).any()) else math.nan
-            order = sorted(range(len(l)), key=lambda t: (-float(l[t]) if float(l[t]) == float(l[t]) else math.inf, t))[:k]
+            order = torch.sort(torch.where(torch.isnan(l), -math.inf, l), descending=True, stable=True).indices[:k].tolist()
             found += [(base + (float(l[t]) - lse), a, i, t) for i, t in enumerate(order)]
         found = sorted((f for f in found if math.isfinite(f[0])), key=lambda f: (-f[0], f[1], f[2]))[:k]
         rows.append([q * beams + f[1] for f in found] + [-1] * (k - len(found)))

@@ -103,7 +103,7 @@ def test_append_of_nothing():
 
 @pytest.mark.parametrize("over,text", [(dict(layer=-1), "layer"), (dict(layer=2), "layer"), (dict(n=-1), "n_seq"), (dict(n=1 << 20), "n_seq"), (dict(rows=-1), "n_rows"),
                                        (dict(rows=(1 << 22) + 1), "n_rows"), (dict(mr=-1), "max_rows"), (dict(ml=-1), "max_len"), (dict(stride=0), "stride"), (dict(words=0), "seen_words"),
-                                       (dict(words=17), "seen_words"), (dict(heads=0), "n_q_heads"), (dict(heads=3), "n_q_heads"), (dict(heads=1026), "n_q_heads"),
+                                       (dict(words=17), "seen_words"), (dict(heads=0), "n_q_heads"), (dict(heads=3), "n_q_heads"), (dict(heads=1026), "n_q_heads"), (dict(rows=1 << 22, heads=512, ldq=1 << 15, ldo=1 << 15), "2^31"),
                                        (dict(scale=math.nan), "scale"), (dict(scale=math.inf), "scale"), (dict(ldq=255), "ldq"), (dict(ldo=255), "ldo"), (dict(cu=None), "null"),
                                        (dict(lens=None), "null"), (dict(table=None), "null"), (dict(q=None), "null"), (dict(out=None), "null"), (dict(cu=P + 2), "aligned"),
                                        (dict(seen=P + 4), "aligned"), (dict(q=P + 1), "aligned"), (dict(out=P + 1), "aligned"), (dict(ws=P + 128, wb=64), "256")])
