@@ -632,6 +632,7 @@ namespace {
 
 struct Shape {
   int nw, ranges;
+  bool whole;              // units are not cut
   size_t starts_bytes, cuts_bytes, bytes;
 };
 Shape shape_of(const TreeArgs &a) {
@@ -643,13 +644,18 @@ Shape shape_of(const TreeArgs &a) {
   const int64_t blocks = ((int64_t)a.n_rows * g + s.nw * 32 - 1) / (s.nw * 32) + a.n_seq;
   const int64_t tiles = std::min((int64_t)1 << 40, blocks) * ((tokens + tt - 1) / tt);
   const int at_once = 256 * (s.nw == 4 ? 2 : a.head_dim == 64 ? 8 : 4), most = std::max(1, at_once / a.g.n_kv_heads);
-  s.ranges = (int)std::max((int64_t)1, std::min((int64_t)most, (tiles + kLeastTiles - 1) / kLeastTiles));
+  // A short unit is not cut: one launch, and a workgroup that begins a second unit or writes sums for the join runs code that has to arrive first (7 to 9 us).  us whole
+  // and cut, heads of 128: 1 sequence of 108 tokens 20.0 and 20.6, of 308 23.4 and 19.5; 8 of 308 23.2 and 26.4, of 708 38 and 35; 64 (as many units as half the
+  // workgroups) of 108 20 and 34, of 1008 60 and 70.  fp32: 8 of 104 25 and 27, of 204 34 and 27.
+  const int64_t units = (int64_t)a.n_seq * a.g.n_kv_heads * ((pairs + s.nw * 32 - 1) / (s.nw * 32));
+  s.whole = (tokens + tt - 1) / tt <= (es == 4 ? 4 : 2 * units >= at_once ? 16 : units >= 32 ? 6 : 3);
+  s.ranges = (int)std::max((int64_t)1, std::min((int64_t)most, s.whole ? blocks : (tiles + kLeastTiles - 1) / kLeastTiles));
   if (s.ranges >= 8) s.ranges = std::min((s.ranges + 7) / 8 * 8, most / 8 * 8 ? most / 8 * 8 : most);
   const size_t pieces = (size_t)s.ranges * a.g.n_kv_heads;
   s.starts_bytes = ((size_t)a.n_seq + 1) * 8;
   s.starts_bytes = (s.starts_bytes + 255) / 256 * 256;
   s.cuts_bytes = (pieces * 32 + 255) / 256 * 256;
-  s.bytes = s.starts_bytes + s.cuts_bytes + 2 * pieces * s.nw * 32 * (a.head_dim + 2) * 4;
+  s.bytes = s.whole ? (a.n_seq > kFewSequences ? s.starts_bytes : 0) : s.starts_bytes + s.cuts_bytes + 2 * pieces * s.nw * 32 * (a.head_dim + 2) * 4;
   return s;
 }
 
@@ -664,7 +670,7 @@ template <typename T, int D>
 void run(hipStream_t s, const TreeArgs &a, const TreePlan &p) {
   if (p.starts_given) k_tree_starts<128 / sizeof(T)><<<1, 1024, 0, s>>>(a, p);
   p.nw == 1 ? launch<T, D, 1>(s, a, p) : p.nw == 2 ? launch<T, D, 2>(s, a, p) : launch<T, D, 4>(s, a, p);
-  if (p.cut && a.n_seq < p.ranges)
+  if (p.cut && p.ranges >= 8 * (int64_t)a.n_seq)
     k_tree_join<T, D, true><<<dim3(p.ranges * a.g.n_kv_heads, p.nw * (D / 8)), 256, 0, s>>>(a, p);
   else if (p.cut)
     k_tree_join<T, D, false><<<dim3(p.ranges * a.g.n_kv_heads, p.nw * (D / 8) / 4), 256, 0, s>>>(a, p);
@@ -692,7 +698,7 @@ void tree_attention(hipStream_t s, const TreeArgs &a) {
   p.nw = sh.nw;
   p.ranges = sh.ranges;
   p.starts = (int64_t *)a.scratch.ptr;
-  p.cut = a.scratch.bytes >= sh.bytes;
+  p.cut = !sh.whole && a.scratch.bytes >= sh.bytes;
   p.starts_given = a.n_seq > kFewSequences;
   p.cuts = (int *)((char *)a.scratch.ptr + sh.starts_bytes);
   p.part_o = (float *)((char *)p.cuts + sh.cuts_bytes);
