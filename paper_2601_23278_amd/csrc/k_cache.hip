@@ -73,12 +73,18 @@ void kv_append(hipStream_t s, const AppendArgs &a) {
 // In place that is safe: place i is read from place keep[i] >= i, so nothing that was written is read later; and every column of K (16 bytes) and every row of
 // V^T belongs to one wavefront, which loads all of a batch before it stores any of it.  So wavefronts do not wait for each other's data, only for the list of
 // where the next 256 tokens move, which is looked up while the last ones do.  Batches begin at every 64th token of what is written: a store to V^T fills a line.
+// Rows of V^T that a batch's tokens come from are read in whole 16-byte pieces into LDS and picked from there, 16 bytes of neighbouring tokens a store, as long as
+// they span at most 256 tokens: single values, 64 lanes from three or four lines, took 342 us for a third of 8 x 8000 tokens (4 layers), this takes 263.
 template <int ES, int D, int SLICES>
 __global__ __launch_bounds__(256) void k_compact(CompactArgs a) {
   typedef typename Word<ES>::type T;
-  constexpr int COLS = D * ES / 16 / SLICES / 4, ROWS = D / SLICES;        // columns of K that a wavefront has, rows of V^T of the workgroup
+  // Columns of K of the workgroup, and of a wavefront that has any: at least four, so that its 16 bytes a lane lie side by side.  Rows of V^T of the workgroup.
+  constexpr int ALL_COLS = D * ES / 16 / SLICES, COLS = ALL_COLS / 4 < 4 ? 4 : ALL_COLS / 4, ROWS = D / SLICES;
   constexpr int TOKENS = 64 / COLS, NK = COLS, NV = ROWS / 4 < 8 ? ROWS / 4 : 8;
+  constexpr int RW = ROWS / 4, RG = RW < 8 ? RW : 8, SPAN = 256;           // rows of V^T of a wavefront, and of them at a time; tokens held of each
   __shared__ int4 move_s[2][256];                      // pages and places, from and to
+  __shared__ int token_s[2][256];                      // tokens that move, counted from the last 8th one up to `start`; -1: none
+  __shared__ __attribute__((aligned(16))) T stage_s[4][RG][SPAN + 16 / ES];      // rows four banks apart
   const int H = a.g.n_kv_heads, b = blockIdx.x / H, h = blockIdx.x % H, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, P = a.g.page_size;
   const int c0 = min(max(a.cu[b], 0), a.n_keep), n = min(a.cu[b + 1], a.n_keep) - c0;
   if (n <= 0) return;
@@ -86,8 +92,10 @@ __global__ __launch_bounds__(256) void k_compact(CompactArgs a) {
   const int skip = (int)(start - base), end = skip + n;      // places base + j, skip <= j < end, are written
   const size_t page_size = page_bytes(a.g, D, ES);
   char *const pool = a.g.pool + (size_t)blockIdx.y * a.g.n_pages * page_size;
-  const size_t k_head = (size_t)h * P * D * ES + (blockIdx.z * 4 + wave) * COLS * 16, v_head = (size_t)(H + h) * P * D * ES + (size_t)blockIdx.z * ROWS * P * ES;
+  const size_t k_head = (size_t)h * P * D * ES + (blockIdx.z * ALL_COLS + wave * COLS) * 16, v_head = (size_t)(H + h) * P * D * ES + (size_t)blockIdx.z * ROWS * P * ES;
   auto kept = [&](int j) { return j >= skip && j < end ? a.keep[c0 + j - skip] : -1; };
+  const int past = (int)(start & 7);
+  const int64_t start8 = start - past;
   auto where = [&](int j, int keep) {
     if (j < skip || j >= end) return int4{-1, 0, -1, 0};
     const Place from = place_of(a.g, a.g.table, a.g.stride, b, keep < 0 ? -1 : start + keep), to = place_of(a.g, a.to_table, a.to_stride, b, base + j);
@@ -96,7 +104,9 @@ __global__ __launch_bounds__(256) void k_compact(CompactArgs a) {
   // A few tokens in all are told apart by few lanes of V's loads; else a lane is a token.
   const bool few = end - skip <= 32;
   const int bits = !few ? 6 : n > 16 ? 5 : n > 8 ? 4 : n > 4 ? 3 : n > 2 ? 2 : n - 1, by = 256 >> bits;
-  move_s[0][tid] = where(tid, kept(tid));
+  const int keep_0 = kept(tid);
+  move_s[0][tid] = where(tid, keep_0);
+  token_s[0][tid] = move_s[0][tid].z >= 0 ? keep_0 + past : -1;
   __syncthreads();
   for (int j0 = 0, buf = 0; j0 < end; j0 += 256, buf ^= 1) {
     const int next = kept(j0 + 256 + tid);
@@ -109,28 +119,90 @@ __global__ __launch_bounds__(256) void k_compact(CompactArgs a) {
 #pragma unroll
       for (int x = 0; x < NK; ++x) {
         const int t = lo + x * TOKENS + lane / COLS;
-        km[x] = t < hi ? move_s[buf][t] : int4{-1, 0, -1, 0};
+        km[x] = t < hi && wave * COLS < ALL_COLS ? move_s[buf][t] : int4{-1, 0, -1, 0};
         if (km[x].z >= 0) kk[x] = *(const u32x4 *)(pool + (size_t)km[x].x * page_size + k_head + (size_t)km[x].y * D * ES + lane % COLS * 16);
       }
-      const int vt = s0 + (tid & ((1 << bits) - 1)), vd = tid >> bits;
-      const int4 vm = vt >= lo && vt < hi ? move_s[buf][vt] : int4{-1, 0, -1, 0};
-      const T *const vf = (const T *)(pool + (size_t)max(vm.x, 0) * page_size + v_head) + vm.y;
-      T *const vto = (T *)(pool + (size_t)max(vm.z, 0) * page_size + v_head) + vm.w;
-      for (int d0 = vd; d0 < ROWS; d0 += by * NV) {
-        T vv[NV];
+      bool staged = false;
+      if (!few) {
+        // chunk: the 8 tokens that the first of the batch is among; all others have to lie in the SPAN tokens from there
+        const int mine = s0 + lane >= lo && s0 + lane < hi ? token_s[buf][s0 + lane] : -1;
+        const uint64_t some = __ballot(mine >= 0);
+        const int chunk = some ? __builtin_amdgcn_readlane(mine, __builtin_ctzll(some)) >> 3 : 0;
+        staged = __ballot(mine >= 0 && (mine < chunk * 8 || mine >= chunk * 8 + SPAN)) == 0;
+        if (staged && some) {
+          const int last = __builtin_amdgcn_readlane(mine, 63 - __builtin_clzll(some)) >> 3;      // ascending: the last chunk too
+          const Place from = place_of(a.g, a.g.table, a.g.stride, b, start8 + (int64_t)(chunk + (lane & 31)) * 8);
+          const bool reads = from.page >= 0 && chunk + (lane & 31) <= last;
+          const T *const src = (const T *)(pool + (size_t)max(from.page, 0) * page_size + v_head) + from.at;
+          const int grp = lane & 7, r_out = lane >> 3;                 // a lane stores 8 neighbouring tokens of one row
+          int pick[8];
+          bool full = true;
+          int4 to_8 = {-1, 0, -1, 0};
 #pragma unroll
-        for (int x = 0; x < NV; ++x)
-          if (vm.z >= 0 && d0 + by * x < ROWS) vv[x] = vf[(size_t)(d0 + by * x) * P];
+          for (int e = 0; e < 8; ++e) {
+            const int t = s0 + grp * 8 + e;
+            const int tok = t >= lo && t < hi ? token_s[buf][t] : -1;
+            pick[e] = tok < 0 ? -1 : tok - chunk * 8;
+            full &= tok >= 0;
+            if (tok >= 0) to_8 = move_s[buf][t];
+          }
+          // the group's 8 tokens begin at a multiple of 8 and lie in one page
+          T *const out = (T *)(pool + (size_t)max(to_8.z, 0) * page_size + v_head) + (to_8.w & ~7);
+          for (int r0 = 0; r0 < RW; r0 += RG) {
 #pragma unroll
-        for (int x = 0; x < NV; ++x)
-          if (vm.z >= 0 && d0 + by * x < ROWS) vto[(size_t)(d0 + by * x) * P] = vv[x];
+            for (int x = 0; x < RG / 2; ++x) {
+              const int r = x * 2 + (lane >> 5);
+              if (reads) {
+                const u32x4 *const from_row = (const u32x4 *)(src + (size_t)(wave * RW + r0 + r) * P);
+#pragma unroll
+                for (int y = 0; y < ES / 2; ++y) *(u32x4 *)&stage_s[wave][r][(lane & 31) * 8 + y * (16 / ES)] = from_row[y];
+              }
+            }
+            __builtin_amdgcn_wave_barrier();
+            asm volatile("" ::: "memory");
+            if (r_out < RG && to_8.z >= 0) {
+              T v[8];
+#pragma unroll
+              for (int e = 0; e < 8; ++e) v[e] = stage_s[wave][r_out][max(pick[e], 0)];
+              T *const row = out + (size_t)(wave * RW + r0 + r_out) * P;
+              if (full) {
+#pragma unroll
+                for (int y = 0; y < ES / 2; ++y) ((u32x4 *)row)[y] = *(const u32x4 *)&v[y * (16 / ES)];
+              } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                  if (pick[e] >= 0) row[e] = v[e];
+              }
+            }
+            __builtin_amdgcn_wave_barrier();
+            asm volatile("" ::: "memory");
+          }
+        }
+      }
+      if (!staged) {
+        // Few tokens in all are told apart by few lanes; else a lane is a token, and the rows are those of the other form.
+        const int vt = s0 + (tid & ((1 << bits) - 1)), vd = few ? tid >> bits : wave * RW, step = few ? by : 1, v_end = few ? ROWS : wave * RW + RW;
+        const int4 vm = vt >= lo && vt < hi ? move_s[buf][vt] : int4{-1, 0, -1, 0};
+        const T *const vf = (const T *)(pool + (size_t)max(vm.x, 0) * page_size + v_head) + vm.y;
+        T *const vto = (T *)(pool + (size_t)max(vm.z, 0) * page_size + v_head) + vm.w;
+        for (int d0 = vd; d0 < v_end; d0 += step * NV) {
+          T vv[NV];
+#pragma unroll
+          for (int x = 0; x < NV; ++x)
+            if (vm.z >= 0 && d0 + step * x < v_end) vv[x] = vf[(size_t)(d0 + step * x) * P];
+#pragma unroll
+          for (int x = 0; x < NV; ++x)
+            if (vm.z >= 0 && d0 + step * x < v_end) vto[(size_t)(d0 + step * x) * P] = vv[x];
+        }
       }
 #pragma unroll
       for (int x = 0; x < NK; ++x)
         if (km[x].z >= 0) *(u32x4 *)(pool + (size_t)km[x].z * page_size + k_head + (size_t)km[x].w * D * ES + lane % COLS * 16) = kk[x];
     }
     if (j0 + 256 < end) {
-      move_s[buf ^ 1][tid] = where(j0 + 256 + tid, next);
+      const int4 then = where(j0 + 256 + tid, next);
+      move_s[buf ^ 1][tid] = then;
+      token_s[buf ^ 1][tid] = then.z >= 0 ? next + past : -1;
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // the list is there; stores need not be
       __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
