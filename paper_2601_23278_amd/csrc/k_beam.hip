@@ -68,8 +68,12 @@ __host__ __device__ inline BeamPlan beam_plan(int n_seq, int n_beams, int vocab,
   const int64_t most = kMostLists / n_beams, least = (vocab + most - 1) / most;
   if (part < least) part = (least + 2047) / 2048 * 2048;
   BeamPlan p;
-  p.part = (int)part;
   p.parts = (int)((vocab + part - 1) / part);
+  p.part = (int)part;
+  if (p.parts > 1 && vocab - (p.parts - 1) * part < part / 2) {       // a short last part rules little out and would be the last to end: parts alike
+    p.part = ((vocab + p.parts - 1) / p.parts + 63) / 64 * 64;        // (4 beams of 151936: 29.6 -> 16.6 us)
+    p.parts = (vocab + p.part - 1) / p.part;
+  }
   p.sum = (double *)work;
   p.keys = (uint64_t *)(p.sum + rows * p.parts);
   p.max = (float *)(p.keys + rows * p.parts * k);
@@ -198,16 +202,17 @@ __global__ __launch_bounds__(256) void k_beam_scan(BeamArgs a, BeamPlan plan) {
     now = next;
     next = after;
   }
-  // The part's maximum and sum.  Every wavefront has a quarter of k logits that are not below such a one of its threads' maxima, so k of the part are not below the
-  // lowest of the four.
+  // The part's maximum and sum.  Each of the wavefronts whose lanes all have logits has its share of k that are not below such a one of its threads' maxima, so k of
+  // the part are not below the lowest of these.
   const float wave_top = wavefront_max(m);
   sum = ref == none ? 0.0 : sum * rescale(ref, wave_top);
   if (extra == extra && extra != none) sum += rescale(extra, wave_top);
   if (odd) sum = NAN;
   sum = wavefront_sum(sum);
+  const int full = max(1, min(4, nvec / 64));          // (one with fewer lanes than k: nothing is ruled out)
   float left = m, nth = wave_top;
 #pragma unroll 1
-  for (int i = 4; i < k && nth != none; i += 4) {
+  for (int i = full; i < k && nth != none; i += full) {
     if (lane == __builtin_ctzll(__ballot(left == nth))) left = none;
     nth = wavefront_max(left);
   }
@@ -217,7 +222,10 @@ __global__ __launch_bounds__(256) void k_beam_scan(BeamArgs a, BeamPlan plan) {
     sum_s[wave] = sum;
   }
   __syncthreads();
-  const float lim = fmaxf(-FLT_MAX, fminf(fminf(nth_s[0], nth_s[1]), fminf(nth_s[2], nth_s[3])));          // -inf is no candidate
+  float lim = nth_s[0];
+#pragma unroll
+  for (int w = 1; w < 4; ++w) lim = w < full ? fminf(lim, nth_s[w]) : lim;
+  lim = fmaxf(-FLT_MAX, lim);                          // -inf is no candidate
   // The few threads that have one of the largest look at them once more: at one load, or where they have several at all of theirs.
   if (extra >= lim) push(extra, loose);
   if (m >= lim) {
