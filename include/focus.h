@@ -425,8 +425,8 @@ int focus_set_mx_weights(focus_ctx *ctx, const focus_mx_weights *weights);
  * These entries work on a K/V pool of the layout above without a context (a context's own pool among them), in the manner of the entries above: they enqueue
  * on the stream of the current device, allocate nothing, keep nothing between calls, never synchronise and may be captured; the same call on the same inputs
  * gives the same bits; errors through focus_last_error(NULL).  Sequences are rows of a page table: token t of row b lives in page
- * page_table[b * table_stride + t / page_size] at place t % page_size.  A row holds its entries up to the first negative one.  Lists on the device are not
- * checked by the host: a page outside the pool, a token behind the table's last page or an index that no list has is neither read nor written. */
+ * page_table[b * table_stride + t / page_size] at place t % page_size.  A row holds its entries up to the first negative one (append,
+ * attention and compaction look at a token's own entry alone: behind a negative one all have to be).  Lists on the device are not checked by the host: a page outside the pool, a token behind the table's last page or an index that no list has is neither read nor written. */
 
 /* A paged K/V pool.  page_size: a multiple of 8, at most 1024; head_dim: 64 or 128; n_kv_heads 1..256; n_layers 1..1024; n_pages at most 2^30. */
 typedef struct focus_kv {
@@ -461,7 +461,7 @@ int focus_tree_attention(const focus_kv *kv, void *hip_stream, int32_t layer, in
 
 /* Moves the tokens that stay together, in every layer: token start[b] + keep[cu_keep[b] + i] of row b's pages in page_table becomes token start[b] + i of its
  * pages in to_table, 0 <= i < cu_keep[b + 1] - cu_keep[b].  The path of a tree that was accepted, or what an eviction leaves of a cache.  Nothing else is written.
- *   keep           device [n_keep], ascending and not negative within a sequence (else that sequence's tokens are unspecified)
+ *   keep           device [n_keep], n_keep at most 2^30, ascending and not negative within a sequence (else that sequence's tokens are unspecified)
  *   to_table       device [n_seq, to_stride]; may be page_table or name the same pages for the same sequence: then the tokens move down in place.  A page that
  *                  is written must belong to no other sequence of the call
  *   n_seq * n_kv_heads * n_layers below 2^24 */
@@ -474,7 +474,7 @@ int focus_kv_compact(const focus_kv *kv, void *hip_stream, int32_t n_seq, int32_
  * focus_kv_fork: new rows that continue old ones.  Row i of new_table continues row parents[i] of page_table: it shares the pages that are full.  The pages
  * behind them (the one that lens[parent] ends in, and reserved ones) go to the parent's first child as they are; every other child gets a page of its own with
  * a copy of the tokens in it, in all layers.  Old rows give up what they held: a parent without children frees its pages, n_new = 0 those of all rows.
- * page_table and lens are only read and no longer hold anything afterwards.
+ * page_table and lens are only read and no longer hold anything afterwards; an output must not overlap an input.
  *   parents        device [n_new] rows of page_table; one outside 0..n_old-1 makes an empty row
  *   lens           device [n_old] (cut to the pages that a row holds);  new_lens  device [n_new] out
  *   new_table      device [n_new, table_stride] out, -1 behind the pages;  lacking  device [n_new] out: 1 where there was no page for the copy; that row's
@@ -500,7 +500,8 @@ int focus_kv_reserve(void *hip_stream, int32_t n_seq, int32_t page_size, int32_t
  *   logits         device [n_seq * n_beams, ld], FOCUS_F32 or FOCUS_BF16;  scores  device [n_seq, n_beams] fp32
  *   done           device [n_seq, n_beams] bytes, not 0: finished; or NULL
  *   rows           device [n_seq, k] out: row of logits that a pick continues (what focus_kv_fork takes as parents), -1: none was left
- *   tokens         device [n_seq, k] out, -1: none;  new_scores  device [n_seq, k] fp32 out, -inf: none
+ *   tokens         device [n_seq, k] out, -1: none;  new_scores  device [n_seq, k] fp32 out, -inf: none; may be
+ *                  scores itself where k is n_beams
  *   workspace      device, 256-byte aligned, focus_beam_select_bytes() */
 int focus_beam_select_bytes(int32_t n_seq, int32_t n_beams, int32_t vocab, int32_t k, size_t *bytes);
 int focus_beam_select(void *hip_stream, int32_t n_seq, int32_t n_beams, int32_t vocab, int32_t k, int32_t dtype, const void *logits, int64_t ld, const float *scores,

@@ -8,6 +8,10 @@ using fk::fail_call;
 namespace {
 
 bool aligned(const void *p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
+// Of words of 4 bytes.
+bool overlap(const void *p, int64_t np, const void *q, int64_t nq) {
+  return p && q && (uintptr_t)p < (uintptr_t)q + 4 * (uintptr_t)nq && (uintptr_t)q < (uintptr_t)p + 4 * (uintptr_t)np;
+}
 
 int launched() {
   const hipError_t e = hipGetLastError();
@@ -118,7 +122,7 @@ int focus_tree_attention(const focus_kv *kv, void *hip_stream, int32_t layer, in
 int focus_kv_compact(const focus_kv *kv, void *hip_stream, int32_t n_seq, int32_t n_keep, const int32_t *start, const int32_t *cu_keep, const int32_t *keep, const int32_t *page_table,
                      int32_t table_stride, const int32_t *to_table, int32_t to_stride) {
   if (const char *e = check_rows(kv, 0, n_seq, 0, table_stride)) return fail_call(FOCUS_EINVAL, "%s", e);
-  if (n_keep < 0) return fail_call(FOCUS_EINVAL, "n_keep must not be negative");
+  if (n_keep < 0 || n_keep > (1 << 30)) return fail_call(FOCUS_EINVAL, "n_keep must be in 0..2^30");
   if (to_stride < 1) return fail_call(FOCUS_EINVAL, "to_stride must be positive");
   if ((int64_t)n_seq * kv->n_kv_heads * kv->n_layers >= fk::kMaxGroups) return fail_call(FOCUS_EINVAL, "n_seq * n_kv_heads * n_layers must be below 2^24");
   if (n_seq == 0 || n_keep == 0) return FOCUS_OK;
@@ -152,6 +156,12 @@ int focus_kv_fork(const focus_kv *kv, void *hip_stream, int32_t n_old, int32_t n
     return fail_call(FOCUS_EINVAL, "the workspace must be 16-byte aligned, the others to their elements");
   if (new_table && (const int32_t *)new_table == page_table) return fail_call(FOCUS_EINVAL, "new_table must not be page_table");
   if (n_new > 0 && workspace_bytes < 4 * fk::fork_ints(n_new)) return fail_call(FOCUS_ENOMEM, "the workspace is too small");
+  // Workgroups read all of the inputs while others write the outputs.
+  const int64_t table = (int64_t)n_old * table_stride, entries = (int64_t)n_new * table_stride;
+  for (const void *out : {(const void *)new_lens, (const void *)new_table, (const void *)lacking}) {
+    const int64_t n = out == new_table ? entries : n_new;
+    if (overlap(out, n, parents, n_new) || overlap(out, n, lens, n_old) || overlap(out, n, page_table, table)) return fail_call(FOCUS_EINVAL, "an output must not overlap an input");
+  }
   fk::ForkArgs a{};
   a.dtype = kv->dtype; a.head_dim = kv->head_dim; a.g = paged(*kv, 0, page_table, table_stride);
   a.n_old = n_old; a.n_new = n_new; a.parents = parents; a.lens = lens; a.new_lens = new_lens; a.new_table = new_table; a.refs = refs; a.lacking = lacking;
@@ -211,6 +221,8 @@ int focus_beam_select(void *hip_stream, int32_t n_seq, int32_t n_beams, int32_t 
   if (!aligned(logits, esize(dtype)) || !aligned(scores, 4) || !aligned(rows, 4) || !aligned(tokens, 4) || !aligned(new_scores, 4) || !aligned(workspace, 256))
     return fail_call(FOCUS_EINVAL, "the workspace must be 256-byte aligned, the others to their elements");
   if (workspace_bytes < fk::beam_scratch(n_seq, n_beams, vocab, k)) return fail_call(FOCUS_ENOMEM, "the workspace is too small");
+  if (!(new_scores == scores && k == n_beams) && overlap(scores, (int64_t)n_seq * n_beams, new_scores, (int64_t)n_seq * k))       // a request's workgroup reads its own first
+    return fail_call(FOCUS_EINVAL, "new_scores may be scores where k is n_beams and must not overlap them otherwise");
   fk::BeamArgs a{};
   a.n_seq = n_seq; a.n_beams = n_beams; a.vocab = vocab; a.k = k; a.dtype = dtype; a.logits = logits; a.ld = ld; a.scores = scores; a.done = done; a.end_token = end_token;
   a.rows = rows; a.tokens = tokens; a.new_scores = new_scores; a.work = workspace;

@@ -159,6 +159,21 @@ def test_reserve_refuses(over, text):
     refused(reserve(**over), text)
 
 
+def test_outputs_over_inputs():
+    """Fork: parents, lens and page_table are read by all workgroups while others write.  Beams: a request's scores are read by its own workgroup, before it writes."""
+    d = dict(parents=P, lens=2 * P, table=3 * P, new_lens=4 * P, new_table=5 * P, refs=6 * P, lacking=7 * P, ws=8 * P)
+    for out in ("new_lens", "new_table", "lacking"):
+        for at in (P, P + 4 * 3, 2 * P, 2 * P + 4 * 2, 3 * P + 4 * 14):             # the last words of 4, 3 and 15
+            refused(fork(**dict(d, **{out: at})), "overlap")
+    refused(fork(**dict(d, new_table=3 * P - 4 * 19)), "overlap")
+    refused(fork(**dict(d, new_lens=2 * P - 4 * 3)), "overlap")
+    refused(beam(scores=P, new=P), "overlap")                                       # 3 beams, 4 picks
+    refused(beam(scores=P, new=P + 4 * 5), "overlap")
+    refused(beam(scores=P + 4 * 7, new=P), "overlap")
+    refused(beam(scores=P, new=P + 4, beams=4), "overlap")
+    refused(compact(keep_n=(1 << 30) + 1), "n_keep")
+
+
 def test_reserve_sizes():
     n = C.c_size_t()
     refused(lib.focus_kv_reserve_bytes(-1, C.byref(n)), "n_seq")

@@ -119,6 +119,23 @@ def test_beam_select_of_many_lists(n, beams, vocab, k):
         check_beam((torch.randn(n * beams, vocab, generator=gen) * 2).to(dtype), -torch.rand(n, beams, generator=gen), k)
 
 
+def test_beam_select_writes_scores_in_place():
+    pk, gen = _pk(), torch.Generator().manual_seed(8)
+    logits, scores = torch.randn(40 * 6, 5003, generator=gen).to(DEV), (-torch.rand(40, 6, generator=gen)).to(DEV)
+    want = pk.focus_beam_select(logits, scores, 6)
+    got = pk.focus_beam_select(logits, scores, 6, new_scores=scores)
+    assert all(torch.equal(a, b) for a, b in zip(want, got)) and got[2] is scores
+
+
+# parts alike instead of a short last one, a part of less than a wavefront's loads, and more picks than wavefronts that are full can rule out
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("vocab", [4096 * 2 + 1, 4096 * 2 + 2047, 4096 * 2 + 2048, 4096 * 5 + 65, 255, 256, 257, 511, 513, 767, 1025])
+def test_beam_select_of_parts_that_do_not_come_out_even(dtype, vocab):
+    gen = torch.Generator().manual_seed(vocab)
+    check_beam((torch.randn(6, vocab, generator=gen) * 2).to(dtype), -torch.rand(2, 3, generator=gen), 64)
+    check_beam(torch.randn(6, vocab, generator=gen).round().to(dtype), -torch.rand(2, 3, generator=gen), 5)
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_beam_select_of_logits_far_from_zero(dtype):
     """Maxima and masks far apart: weights that vanish, references that have to move."""
