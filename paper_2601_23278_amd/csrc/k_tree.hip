@@ -644,8 +644,8 @@ Shape shape_of(const TreeArgs &a) {
   const int64_t blocks = ((int64_t)a.n_rows * g + s.nw * 32 - 1) / (s.nw * 32) + a.n_seq;
   const int64_t tiles = std::min((int64_t)1 << 40, blocks) * ((tokens + tt - 1) / tt);
   const int at_once = 256 * (s.nw == 4 ? 2 : a.head_dim == 64 ? 8 : 4), most = std::max(1, at_once / a.g.n_kv_heads);
-  // A short unit is not cut: one launch, and a workgroup that begins a second unit or writes sums for the join runs code that has to arrive first (7 to 9 us).  us whole
-  // and cut, heads of 128: 1 sequence of 108 tokens 20.0 and 20.6, of 308 23.4 and 19.5; 8 of 308 23.2 and 26.4, of 708 38 and 35; 64 (as many units as half the
+  // A short unit is not cut: one launch, and a workgroup that writes sums for the join, and the join, take 7 to 9 us more.  us whole and
+  // cut, heads of 128: 1 sequence of 108 tokens 20.0 and 20.6, of 308 23.4 and 19.5; 8 of 308 23.2 and 26.4, of 708 38 and 35; 64 (as many units as half the
   // workgroups) of 108 20 and 34, of 1008 60 and 70.  fp32: 8 of 104 25 and 27, of 204 34 and 27.
   const int64_t units = (int64_t)a.n_seq * a.g.n_kv_heads * ((pairs + s.nw * 32 - 1) / (s.nw * 32));
   s.whole = (tokens + tt - 1) / tt <= (es == 4 ? 4 : 2 * units >= at_once ? 16 : units >= 32 ? 6 : 3);
