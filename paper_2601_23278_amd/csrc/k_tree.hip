@@ -17,6 +17,7 @@
 // neighbouring tokens.  fp32: v_mfma_f32_32x32x2_f32, four for each 16-byte piece; its own lane layout has four neighbouring tokens already.
 // Probabilities in bf16 are rounded once (2^-8 relative), as operand of the second product; their sum is taken before.
 #include <algorithm>
+#include <type_traits>
 
 #include "focus_branch.h"
 
@@ -46,23 +47,32 @@ struct TreePlan {
 };
 constexpr int kFewSequences = 256;   // so many starts are summed up by every workgroup for itself
 
-__device__ __forceinline__ int rows_of(const TreeArgs &a, int b) { return max(0, min(a.cu[b + 1], a.n_rows) - max(a.cu[b], 0)); }
-// Tokens of a sequence that its row of the table has room for (below 2^31 - 64, so that tiles of tokens can be counted in 32 bits)
-__device__ __forceinline__ int tokens_of(const TreeArgs &a, int b, int rows) {
+// A sequence's rows and tokens; its three numbers are asked for at once.
+struct Sequence {
+  int r0, rows, cached;
+  int total;             // tokens that its row of the table has room for (below 2^31 - 64, so that tiles of tokens can be counted in 32 bits)
+};
+__device__ __forceinline__ Sequence sequence(const TreeArgs &a, int b) {
+  const int c0 = a.cu[b], c1 = a.cu[b + 1], len = a.lens[b];
   const int64_t room = min((int64_t)a.g.stride * a.g.page_size, (int64_t)(1u << 31) - 128);
-  return (int)min((int64_t)max(a.lens[b], 0) + rows, room);
+  Sequence s;
+  s.r0 = max(c0, 0);
+  s.rows = max(0, min(c1, a.n_rows) - s.r0);
+  s.cached = max(len, 0);
+  s.total = (int)min((int64_t)s.cached + s.rows, room);
+  return s;
 }
 struct Units {
   int blocks, tiles;     // blocks of pairs, tiles of tokens
 };
 template <int TT>
-__device__ __forceinline__ Units units_of(const TreeArgs &a, int b, int nw) {
-  const int rows = rows_of(a, b), pairs = rows * (a.n_q_heads / a.g.n_kv_heads);
-  return Units{(pairs + nw * 32 - 1) / (nw * 32), rows > 0 ? (tokens_of(a, b, rows) + TT - 1) / TT : 0};
+__device__ __forceinline__ Units units_of(const TreeArgs &a, const Sequence &s, int nw) {
+  const int pairs = s.rows * (a.n_q_heads / a.g.n_kv_heads);
+  return Units{(pairs + nw * 32 - 1) / (nw * 32), s.rows > 0 ? (s.total + TT - 1) / TT : 0};
 }
 template <int TT>
 __device__ __forceinline__ int64_t length_of(const TreeArgs &a, int b, const TreePlan &p) {
-  const Units u = units_of<TT>(a, b, p.nw);
+  const Units u = units_of<TT>(a, sequence(a, b), p.nw);
   return (int64_t)u.blocks * (p.cut ? u.tiles : 1);
 }
 
@@ -192,6 +202,16 @@ template <> __device__ __forceinline__ f32x16 multiply<float>(u32x4 a, u32x4 b, 
   return acc;
 }
 
+// Four 16-byte pieces from LDS, with their wait.  In assembly because the compiler has a read of LDS wait for every load into LDS that is under way, the next tile's too:
+// that, and queries that were loaded one after the other, took 26.8 us for one request of 24 rows and 4001 tokens (24.2 so), 53 for nine ragged sequences (38).
+template <int OFFSET_0, int OFFSET_1, int OFFSET_2, int OFFSET_3>
+__device__ __forceinline__ void read_4(u32x4 (&to)[4], unsigned a0, unsigned a1, unsigned a2, unsigned a3) {
+  asm volatile("ds_read_b128 %0, %4 offset:%8\n\tds_read_b128 %1, %5 offset:%9\n\tds_read_b128 %2, %6 offset:%10\n\tds_read_b128 %3, %7 offset:%11\n\ts_waitcnt lgkmcnt(0)"
+               : "=&v"(to[0]), "=&v"(to[1]), "=&v"(to[2]), "=&v"(to[3])
+               : "v"(a0), "v"(a1), "v"(a2), "v"(a3), "n"(OFFSET_0), "n"(OFFSET_1), "n"(OFFSET_2), "n"(OFFSET_3)
+               : "memory");
+}
+
 // Token of a tile, counted within 32, that register r of a product of K rows holds for lanes of half `half`.
 template <typename T> __device__ __forceinline__ constexpr int token_of(int r, int half) {
   return sizeof(T) == 2 ? 16 * (r >> 3) + 8 * half + (r & 7) : 8 * (r >> 2) + 4 * half + (r & 3);
@@ -241,6 +261,9 @@ __global__ __launch_bounds__(NW * 64, NW == 1 && D == 128 ? 1 : 2) void k_tree(T
   const int k_row0 = wave * IPW * RPI + lane / LPR, v_row0 = wave * IPW * 8 + (lane >> 3);
   const unsigned k_lane = k_row0 * RB + (((lane % LPR) ^ swizzle(k_row0)) << 4);
   const unsigned v_chunk0 = (lane & 7) ^ ((v_row0 >> 1) & 7);
+  // Where a lane reads its pieces of K (row k_tl of 32) and of V^T (row col of 32); rows 32 further on lie at the same swizzle.
+  const int k_tl = ES == 2 ? (col & ~12) | (col & 4) << 1 | (col & 8) >> 1 : col;
+  const unsigned k_frag = (unsigned)(uintptr_t)FK_LDS_PTR(Ks) + k_tl * RB, v_frag = (unsigned)(uintptr_t)FK_LDS_PTR(Vs) + col * 128 + ((half ^ ((col >> 1) & 7)) << 4);
   const size_t page_size = page_bytes(a.g, D, ES);
   const bool wide_q = ((uintptr_t)a.q | (uintptr_t)(a.ldq * ES)) % 16 == 0, wide_o = ((uintptr_t)a.out | (uintptr_t)(a.ldo * ES)) % 16 == 0;
   // The scale's sign goes into Q; a scale of zero makes Q zero.
@@ -265,7 +288,8 @@ __global__ __launch_bounds__(NW * 64, NW == 1 && D == 128 ? 1 : 2) void k_tree(T
     Part p{};
     if (at >= end) return p;
     while (starts[b + 1] <= at) ++b;
-    const Units un = units_of<TT>(a, b, NW);
+    const Sequence sq = sequence(a, b);
+    const Units un = units_of<TT>(a, sq, NW);
     const int64_t in = at - starts[b];
     const int unit = __builtin_amdgcn_readfirstlane((int)(!plan.cut ? in : in < (1ll << 32) ? (unsigned)in / (unsigned)un.tiles : in / un.tiles));
     p.b = b;
@@ -274,10 +298,10 @@ __global__ __launch_bounds__(NW * 64, NW == 1 && D == 128 ? 1 : 2) void k_tree(T
     p.tile1 = plan.cut ? (int)min((int64_t)p.tiles, p.tile0 + (end - at)) : p.tiles;
     at += plan.cut ? p.tile1 - p.tile0 : 1;
     p.q0 = unit * NW * 32;
-    p.r0 = max(a.cu[b], 0);
-    p.rows = rows_of(a, b);
-    p.cached = max(a.lens[b], 0);
-    p.total = tokens_of(a, b, p.rows);
+    p.r0 = sq.r0;
+    p.rows = sq.rows;
+    p.cached = sq.cached;
+    p.total = sq.total;
     p.pages = look_up(b, p.tile0, p.tiles);
     return p;
   };
@@ -336,23 +360,24 @@ __global__ __launch_bounds__(NW * 64, NW == 1 && D == 128 ? 1 : 2) void k_tree(T
     u32x4 qf[KS];
     {
       const T *qp = (const T *)a.q + (size_t)r * a.ldq + (size_t)head * D;
+      // All are asked for before any is waited for; a pair that is none reads its sequence's first row.
+      if (wide_q) {
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        u32x4 v = {0, 0, 0, 0};
-        const T *from_q = qp + (2 * ks + half) * (16 / ES);
-        if (valid && a.scale != 0.f) {
-          if (wide_q) {
-            v = *(const u32x4 *)from_q;
-          } else {
+        for (int ks = 0; ks < KS; ++ks) qf[ks] = *(const u32x4 *)(qp + (2 * ks + half) * (16 / ES));
+      } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              v[e] = ES == 2 ? (unsigned)((const uint16_t *)from_q)[2 * e] | (unsigned)((const uint16_t *)from_q)[2 * e + 1] << 16 : ((const uint32_t *)from_q)[e];
-          }
+        for (int ks = 0; ks < KS; ++ks) {
+          const T *const from_q = qp + (2 * ks + half) * (16 / ES);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] ^= flip;
+          for (int e = 0; e < 4; ++e)
+            qf[ks][e] = ES == 2 ? (unsigned)((const uint16_t *)from_q)[2 * e] | (unsigned)((const uint16_t *)from_q)[2 * e + 1] << 16 : ((const uint32_t *)from_q)[e];
         }
-        qf[ks] = v;
       }
+      const unsigned keep = valid && a.scale != 0.f ? ~0u : 0u;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) qf[ks][e] = (qf[ks][e] ^ flip) & keep;
     }
     const uint64_t seen0 = seen_word(0);
     const Part next = next_part();
@@ -374,15 +399,22 @@ __global__ __launch_bounds__(NW * 64, NW == 1 && D == 128 ? 1 : 2) void k_tree(T
       asm volatile("" ::: "memory");
       f32x16 s[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
+      for (int u = 0; u < U; ++u)
 #pragma unroll
         for (int e = 0; e < 16; ++e) s[u][e] = 0.f;
-        const int tl = 32 * u + (ES == 2 ? (col & ~12) | (col & 4) << 1 | (col & 8) >> 1 : col);
+      constexpr int AT_ONCE = 4 / U;                   // pieces of 32 bytes of D
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          const u32x4 kf = *(const u32x4 *)(Ks + tl * RB + (((2 * ks + half) ^ swizzle(tl)) << 4));
-          s[u] = multiply<T>(kf, qf[ks], s[u]);
-        }
+      for (int ks = 0; ks < KS; ks += AT_ONCE) {
+        unsigned at_k[AT_ONCE];
+#pragma unroll
+        for (int x = 0; x < AT_ONCE; ++x) at_k[x] = k_frag + (((2 * (ks + x) + half) ^ swizzle(k_tl)) << 4);
+        u32x4 kf[4];
+        if constexpr (U == 2)
+          read_4<0, 32 * RB, 0, 32 * RB>(kf, at_k[0], at_k[0], at_k[AT_ONCE - 1], at_k[AT_ONCE - 1]);
+        else
+          read_4<0, 0, 0, 0>(kf, at_k[0], at_k[1 % AT_ONCE], at_k[2 % AT_ONCE], at_k[3 % AT_ONCE]);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) s[x % U] = multiply<T>(kf[x], qf[ks + x / U], s[x % U]);
       }
       asm volatile("" ::: "memory");
       __builtin_amdgcn_s_barrier();                    // every wavefront has read K
@@ -521,10 +553,19 @@ __global__ __launch_bounds__(NW * 64, NW == 1 && D == 128 ? 1 : 2) void k_tree(T
           __syncthreads();
         }
       }
+      auto add_rows = [&](auto rows) {                 // 32 rows of V^T
+        constexpr int ds = decltype(rows)::value;
+        u32x4 vf[4];
+        read_4<ds * 4096, ds * 4096, ds * 4096, ds * 4096>(vf, v_frag ^ (0 << 5), v_frag ^ (1 << 5), v_frag ^ (2 << 5), v_frag ^ (3 << 5));
 #pragma unroll
-      for (int ds = 0; ds < DS; ++ds)
-#pragma unroll
-        for (int kk = 0; kk < 4; ++kk) o[ds] = multiply<T>(v_piece(ds, kk), pf[kk], o[ds]);
+        for (int kk = 0; kk < 4; ++kk) o[ds] = multiply<T>(vf[kk], pf[kk], o[ds]);
+      };
+      add_rows(std::integral_constant<int, 0>());
+      add_rows(std::integral_constant<int, 1>());
+      if constexpr (DS == 4) {
+        add_rows(std::integral_constant<int, 2>());
+        add_rows(std::integral_constant<int, 3>());
+      }
       asm volatile("" ::: "memory");
       __builtin_amdgcn_s_barrier();                    // every wavefront has read V
       if (any) issue_v(tile_n, pages, first);
