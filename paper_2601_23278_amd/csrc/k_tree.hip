@@ -148,7 +148,7 @@ __device__ __forceinline__ int find_start(const int64_t *starts, int n, int64_t 
   }
   return lo;
 }
-constexpr int kLeastTiles = 3;       // of a range (one request of 24 rows and 4001 tokens: 26.7 us; 2 or 4 tiles 27.8 and 27.0, 1 or 6 tiles 32 and 30)
+constexpr int kLeastTiles = 3;       // of a range (one request of 24 rows and 4001 tokens: 24.2 us; 1, 2, 4, 6 tiles 31, 26, 23.9, 26; 33 single fp32 tokens 35.5; 35.5, 35.5, 40, 45)
 __device__ __forceinline__ int64_t range_length(const TreePlan &p, int64_t total) {
   const int64_t n = (total + p.ranges - 1) / p.ranges;
   return p.cut && n < kLeastTiles ? kLeastTiles : n < 1 ? 1 : n;
@@ -203,7 +203,7 @@ template <> __device__ __forceinline__ f32x16 multiply<float>(u32x4 a, u32x4 b, 
 }
 
 // Four 16-byte pieces from LDS, with their wait.  In assembly because the compiler has a read of LDS wait for every load into LDS that is under way, the next tile's too:
-// that, and queries that were loaded one after the other, took 26.8 us for one request of 24 rows and 4001 tokens (24.2 so), 53 for nine ragged sequences (38).
+// that, and queries that were loaded one after the other, took 26.8 us for one request of 24 rows and 4001 tokens (24.2 so).
 template <int OFFSET_0, int OFFSET_1, int OFFSET_2, int OFFSET_3>
 __device__ __forceinline__ void read_4(u32x4 (&to)[4], unsigned a0, unsigned a1, unsigned a2, unsigned a3) {
   asm volatile("ds_read_b128 %0, %4 offset:%8\n\tds_read_b128 %1, %5 offset:%9\n\tds_read_b128 %2, %6 offset:%10\n\tds_read_b128 %3, %7 offset:%11\n\ts_waitcnt lgkmcnt(0)"
@@ -685,11 +685,11 @@ Shape shape_of(const TreeArgs &a) {
   const int64_t blocks = ((int64_t)a.n_rows * g + s.nw * 32 - 1) / (s.nw * 32) + a.n_seq;
   const int64_t tiles = std::min((int64_t)1 << 40, blocks) * ((tokens + tt - 1) / tt);
   const int at_once = 256 * (s.nw == 4 ? 2 : a.head_dim == 64 ? 8 : 4), most = std::max(1, at_once / a.g.n_kv_heads);
-  // A short unit is not cut: one launch, and a workgroup that writes sums for the join, and the join, take 7 to 9 us more.  us whole and
-  // cut, heads of 128: 1 sequence of 108 tokens 20.0 and 20.6, of 308 23.4 and 19.5; 8 of 308 23.2 and 26.4, of 708 38 and 35; 64 (as many units as half the
-  // workgroups) of 108 20 and 34, of 1008 60 and 70.  fp32: 8 of 104 25 and 27, of 204 34 and 27.
+  // A short unit is not cut: one launch, and sums for the join, and the join, take 7 to 9 us more.  us whole and cut, 8 heads of 128, 8 rows: 1 sequence of 108 tokens
+  // 21 and 23, of 308 23 and 21; 8 of 308 24 and 25, of 708 40 and 34; 32 (as many units as compute units) of 108 20 and 30, of 1008 44 and 48; 64 of 108 19 and 34,
+  // of 1008 56 and 70.  4 heads of 64: 64 of 308 20 and 25, of 1008 42 and 44, 32 of 408 23 and 22.  fp32: 8 of 104 24 and 26, of 204 33 and 24.
   const int64_t units = (int64_t)a.n_seq * a.g.n_kv_heads * ((pairs + s.nw * 32 - 1) / (s.nw * 32));
-  s.whole = (tokens + tt - 1) / tt <= (es == 4 ? 4 : 2 * units >= at_once ? 16 : units >= 32 ? 6 : 3);
+  s.whole = (tokens + tt - 1) / tt <= (es == 4 ? 4 : units >= 256 ? 16 : units >= 32 ? 6 : 3);
   s.ranges = (int)std::max((int64_t)1, std::min((int64_t)most, s.whole ? blocks : (tiles + kLeastTiles - 1) / kLeastTiles));
   if (s.ranges >= 8) s.ranges = std::min((s.ranges + 7) / 8 * 8, most / 8 * 8 ? most / 8 * 8 : most);
   const size_t pieces = (size_t)s.ranges * a.g.n_kv_heads;
