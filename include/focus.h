@@ -474,7 +474,7 @@ int focus_kv_compact(const focus_kv *kv, void *hip_stream, int32_t n_seq, int32_
  * focus_kv_fork: new rows that continue old ones.  Row i of new_table continues row parents[i] of page_table: it shares the pages that are full.  The pages
  * behind them (the one that lens[parent] ends in, and reserved ones) go to the parent's first child as they are; every other child gets a page of its own with
  * a copy of the tokens in it, in all layers.  Old rows give up what they held: a parent without children frees its pages, n_new = 0 those of all rows.
- * page_table and lens are only read and no longer hold anything afterwards; an output must not overlap an input.
+ * page_table and lens are only read and no longer hold anything afterwards; outputs, refs and the workspace must overlap neither an input nor each other.
  *   parents        device [n_new] rows of page_table; one outside 0..n_old-1 makes an empty row
  *   lens           device [n_old] (cut to the pages that a row holds);  new_lens  device [n_new] out
  *   new_table      device [n_new, table_stride] out, -1 behind the pages;  lacking  device [n_new] out: 1 where there was no page for the copy; that row's

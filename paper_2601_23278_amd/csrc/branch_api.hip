@@ -1,6 +1,8 @@
 // C entries of the operators for generation that branches over the paged cache: argument checks and launches.
 #include <math.h>
 
+#include <initializer_list>
+
 #include "focus_branch.h"
 
 using fk::fail_call;
@@ -10,7 +12,21 @@ namespace {
 bool aligned(const void *p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
 // Of words of 4 bytes.
 bool overlap(const void *p, int64_t np, const void *q, int64_t nq) {
-  return p && q && (uintptr_t)p < (uintptr_t)q + 4 * (uintptr_t)nq && (uintptr_t)q < (uintptr_t)p + 4 * (uintptr_t)np;
+  return p && q && np > 0 && nq > 0 && (uintptr_t)p < (uintptr_t)q + 4 * (uintptr_t)nq && (uintptr_t)q < (uintptr_t)p + 4 * (uintptr_t)np;
+}
+
+// A list of a call, of words of 4 bytes.
+struct List {
+  const void *p;
+  int64_t words;
+  bool written;
+};
+// Whether one that is written overlaps another.
+bool collide(std::initializer_list<List> lists) {
+  for (const List *x = lists.begin(); x != lists.end(); ++x)
+    for (const List *y = x + 1; y != lists.end(); ++y)
+      if ((x->written || y->written) && overlap(x->p, x->words, y->p, y->words)) return true;
+  return false;
 }
 
 int launched() {
@@ -156,12 +172,11 @@ int focus_kv_fork(const focus_kv *kv, void *hip_stream, int32_t n_old, int32_t n
     return fail_call(FOCUS_EINVAL, "the workspace must be 16-byte aligned, the others to their elements");
   if (new_table && (const int32_t *)new_table == page_table) return fail_call(FOCUS_EINVAL, "new_table must not be page_table");
   if (n_new > 0 && workspace_bytes < 4 * fk::fork_ints(n_new)) return fail_call(FOCUS_ENOMEM, "the workspace is too small");
-  // Workgroups read all of the inputs while others write the outputs.
-  const int64_t table = (int64_t)n_old * table_stride, entries = (int64_t)n_new * table_stride;
-  for (const void *out : {(const void *)new_lens, (const void *)new_table, (const void *)lacking}) {
-    const int64_t n = out == new_table ? entries : n_new;
-    if (overlap(out, n, parents, n_new) || overlap(out, n, lens, n_old) || overlap(out, n, page_table, table)) return fail_call(FOCUS_EINVAL, "an output must not overlap an input");
-  }
+  // Workgroups read all of the inputs, and the counts, while others write the outputs.
+  const int64_t old_rows = n_old, new_rows = n_new;
+  if (collide({{new_lens, new_rows, true}, {new_table, new_rows * table_stride, true}, {lacking, new_rows, true}, {refs, kv->n_pages, true},
+               {workspace, n_new > 0 ? (int64_t)fk::fork_ints(n_new) : 0, true}, {parents, new_rows, false}, {lens, old_rows, false}, {page_table, old_rows * table_stride, false}}))
+    return fail_call(FOCUS_EINVAL, "outputs, refs and the workspace must overlap neither an input nor each other");
   fk::ForkArgs a{};
   a.dtype = kv->dtype; a.head_dim = kv->head_dim; a.g = paged(*kv, 0, page_table, table_stride);
   a.n_old = n_old; a.n_new = n_new; a.parents = parents; a.lens = lens; a.new_lens = new_lens; a.new_table = new_table; a.refs = refs; a.lacking = lacking;

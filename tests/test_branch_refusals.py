@@ -210,3 +210,26 @@ def test_the_binding_refuses_tensors_that_are_not_on_the_current_device():
                  lambda: pk.focus_beam_select(torch.zeros(2, 5), torch.zeros(1, 2), 1)):
         with pytest.raises(pk.FocusError):
             call()
+
+
+def test_fork_refuses_lists_that_are_written_over_each_other():
+    """The counts change while rows are read and written, and the workspace holds what the launches tell each other."""
+    d = dict(parents=P, lens=2 * P, table=3 * P, new_lens=4 * P, new_table=5 * P, refs=6 * P, lacking=7 * P, ws=8 * P)
+    words = dict(parents=4, lens=3, table=15, new_lens=4, new_table=20, refs=9, lacking=4, ws=20)
+    n = C.c_size_t()
+    assert lib.focus_kv_fork_bytes(4, C.byref(n)) == 0 and n.value == 4 * words["ws"]
+    written = ("new_lens", "new_table", "refs", "lacking", "ws")
+    for x in written:
+        for y in words:
+            if x == y:
+                continue
+            refused(fork(**dict(d, **{x: d[y]})), "must")                            # the same address; new_table over page_table has words of its own
+            if x != "ws":
+                refused(fork(**dict(d, **{x: d[y] + 4 * (words[y] - 1)})), "overlap")    # the last word of the other
+                refused(fork(**dict(d, **{x: d[y] - 4 * (words[x] - 1)})), "overlap")    # its last word on the first of the other
+    # the workspace is 16-byte aligned
+    refused(fork(**dict(d, ws=6 * P + 32)), "overlap")
+    refused(fork(**dict(d, ws=7 * P - 64)), "overlap")
+    # nothing but the counts is written where no row is new
+    for at in (2 * P, 3 * P + 4 * 14):
+        refused(fork(new=0, parents=None, lens=2 * P, table=3 * P, new_lens=None, new_table=None, refs=at, lacking=None, ws=None), "overlap")
