@@ -487,6 +487,7 @@ int focus_kv_fork(const focus_kv *kv, void *hip_stream, int32_t n_old, int32_t n
 
 /* Gives rows the pages that lens[b] + room tokens need, in place.
  *   room           0 or more, the same for all rows;  lacking  device [n_seq] out: pages that a row still wants (the pool or the row's entries ran out)
+ *   page_table, refs, lacking and the workspace must not overlap each other, nor lens any but lacking
  *   n_pages        of refs, at most 2^30;  n_seq below 2^20, n_seq * table_stride below 2^31;  workspace  device, 16-byte aligned, focus_kv_reserve_bytes() */
 int focus_kv_reserve_bytes(int32_t n_seq, size_t *bytes);
 int focus_kv_reserve(void *hip_stream, int32_t n_seq, int32_t page_size, int32_t n_pages, const int32_t *lens, int32_t room, int32_t *page_table, int32_t table_stride,

@@ -204,6 +204,11 @@ int focus_kv_reserve(void *hip_stream, int32_t n_seq, int32_t page_size, int32_t
   if (!aligned(lens, 4) || !aligned(page_table, 4) || !aligned(refs, 4) || !aligned(lacking, 4) || !aligned(workspace, 16))
     return fail_call(FOCUS_EINVAL, "the workspace must be 16-byte aligned, the others to their elements");
   if (workspace_bytes < 4 * fk::reserve_ints(n_seq)) return fail_call(FOCUS_ENOMEM, "the workspace is too small");
+  // Lengths are read by the first launch and `lacking` is written by the second.
+  const int64_t rows = n_seq;
+  if (collide({{page_table, rows * table_stride, true}, {refs, n_pages, true}, {workspace, (int64_t)fk::reserve_ints(n_seq), true}, {lens, rows, false}}) ||
+      collide({{lacking, rows, true}, {page_table, rows * table_stride, false}, {refs, n_pages, false}, {workspace, (int64_t)fk::reserve_ints(n_seq), false}}))
+    return fail_call(FOCUS_EINVAL, "page_table, refs, lacking and the workspace must not overlap each other, nor lens any but lacking");
   fk::ReserveArgs a{};
   a.n_seq = n_seq; a.page_size = page_size; a.n_pages = n_pages; a.room = room; a.stride = table_stride; a.lens = lens; a.table = page_table; a.refs = refs;
   a.lacking = lacking; a.work = (int32_t *)workspace;

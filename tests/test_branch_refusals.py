@@ -233,3 +233,20 @@ def test_fork_refuses_lists_that_are_written_over_each_other():
     # nothing but the counts is written where no row is new
     for at in (2 * P, 3 * P + 4 * 14):
         refused(fork(new=0, parents=None, lens=2 * P, table=3 * P, new_lens=None, new_table=None, refs=at, lacking=None, ws=None), "overlap")
+
+
+def test_reserve_refuses_lists_that_are_written_over_each_other():
+    d = dict(lens=P, table=2 * P, refs=3 * P, lacking=4 * P, ws=5 * P)
+    words = dict(lens=3, table=15, refs=9, lacking=3, ws=13)
+    n = C.c_size_t()
+    assert lib.focus_kv_reserve_bytes(3, C.byref(n)) == 0 and n.value == 4 * words["ws"]
+    for x in ("table", "refs", "lacking", "ws"):
+        for y in words:
+            if x == y or {x, y} == {"lens", "lacking"}:
+                continue
+            refused(reserve(**dict(d, **{x: d[y]})), "overlap")
+            if x != "ws":
+                refused(reserve(**dict(d, **{x: d[y] + 4 * (words[y] - 1)})), "overlap")
+                refused(reserve(**dict(d, **{x: d[y] - 4 * (words[x] - 1)})), "overlap")
+    refused(reserve(**dict(d, ws=3 * P + 32)), "overlap")
+    refused(reserve(**dict(d, ws=P - 48)), "overlap")
