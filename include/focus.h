@@ -502,7 +502,7 @@ int focus_kv_reserve(void *hip_stream, int32_t n_seq, int32_t page_size, int32_t
  *   done           device [n_seq, n_beams] bytes, not 0: finished; or NULL
  *   rows           device [n_seq, k] out: row of logits that a pick continues (what focus_kv_fork takes as parents), -1: none was left
  *   tokens         device [n_seq, k] out, -1: none;  new_scores  device [n_seq, k] fp32 out, -inf: none; may be
- *                  scores itself where k is n_beams
+ *                  scores itself where k is n_beams;  outputs and the workspace must overlap neither scores nor done otherwise, nor each other
  *   workspace      device, 256-byte aligned, focus_beam_select_bytes() */
 int focus_beam_select_bytes(int32_t n_seq, int32_t n_beams, int32_t vocab, int32_t k, size_t *bytes);
 int focus_beam_select(void *hip_stream, int32_t n_seq, int32_t n_beams, int32_t vocab, int32_t k, int32_t dtype, const void *logits, int64_t ld, const float *scores,

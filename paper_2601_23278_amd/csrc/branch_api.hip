@@ -10,22 +10,20 @@ using fk::fail_call;
 namespace {
 
 bool aligned(const void *p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
-// Of words of 4 bytes.
+// Of bytes.
 bool overlap(const void *p, int64_t np, const void *q, int64_t nq) {
-  return p && q && np > 0 && nq > 0 && (uintptr_t)p < (uintptr_t)q + 4 * (uintptr_t)nq && (uintptr_t)q < (uintptr_t)p + 4 * (uintptr_t)np;
+  return p && q && np > 0 && nq > 0 && (uintptr_t)p < (uintptr_t)q + (uintptr_t)nq && (uintptr_t)q < (uintptr_t)p + (uintptr_t)np;
 }
-
-// A list of a call, of words of 4 bytes.
-struct List {
+struct List {            // of a call
   const void *p;
-  int64_t words;
+  int64_t bytes;
   bool written;
 };
 // Whether one that is written overlaps another.
 bool collide(std::initializer_list<List> lists) {
   for (const List *x = lists.begin(); x != lists.end(); ++x)
     for (const List *y = x + 1; y != lists.end(); ++y)
-      if ((x->written || y->written) && overlap(x->p, x->words, y->p, y->words)) return true;
+      if ((x->written || y->written) && overlap(x->p, x->bytes, y->p, y->bytes)) return true;
   return false;
 }
 
@@ -173,9 +171,9 @@ int focus_kv_fork(const focus_kv *kv, void *hip_stream, int32_t n_old, int32_t n
   if (new_table && (const int32_t *)new_table == page_table) return fail_call(FOCUS_EINVAL, "new_table must not be page_table");
   if (n_new > 0 && workspace_bytes < 4 * fk::fork_ints(n_new)) return fail_call(FOCUS_ENOMEM, "the workspace is too small");
   // Workgroups read all of the inputs, and the counts, while others write the outputs.
-  const int64_t old_rows = n_old, new_rows = n_new;
-  if (collide({{new_lens, new_rows, true}, {new_table, new_rows * table_stride, true}, {lacking, new_rows, true}, {refs, kv->n_pages, true},
-               {workspace, n_new > 0 ? (int64_t)fk::fork_ints(n_new) : 0, true}, {parents, new_rows, false}, {lens, old_rows, false}, {page_table, old_rows * table_stride, false}}))
+  const int64_t old_bytes = 4 * (int64_t)n_old, new_bytes = 4 * (int64_t)n_new;
+  if (collide({{new_lens, new_bytes, true}, {new_table, new_bytes * table_stride, true}, {lacking, new_bytes, true}, {refs, 4 * (int64_t)kv->n_pages, true},
+               {workspace, n_new > 0 ? 4 * (int64_t)fk::fork_ints(n_new) : 0, true}, {parents, new_bytes, false}, {lens, old_bytes, false}, {page_table, old_bytes * table_stride, false}}))
     return fail_call(FOCUS_EINVAL, "outputs, refs and the workspace must overlap neither an input nor each other");
   fk::ForkArgs a{};
   a.dtype = kv->dtype; a.head_dim = kv->head_dim; a.g = paged(*kv, 0, page_table, table_stride);
@@ -205,9 +203,8 @@ int focus_kv_reserve(void *hip_stream, int32_t n_seq, int32_t page_size, int32_t
     return fail_call(FOCUS_EINVAL, "the workspace must be 16-byte aligned, the others to their elements");
   if (workspace_bytes < 4 * fk::reserve_ints(n_seq)) return fail_call(FOCUS_ENOMEM, "the workspace is too small");
   // Lengths are read by the first launch and `lacking` is written by the second.
-  const int64_t rows = n_seq;
-  if (collide({{page_table, rows * table_stride, true}, {refs, n_pages, true}, {workspace, (int64_t)fk::reserve_ints(n_seq), true}, {lens, rows, false}}) ||
-      collide({{lacking, rows, true}, {page_table, rows * table_stride, false}, {refs, n_pages, false}, {workspace, (int64_t)fk::reserve_ints(n_seq), false}}))
+  const List table = {page_table, 4 * (int64_t)n_seq * table_stride, true}, counts = {refs, 4 * (int64_t)n_pages, true}, work = {workspace, 4 * (int64_t)fk::reserve_ints(n_seq), true};
+  if (collide({table, counts, work, {lens, 4 * (int64_t)n_seq, false}}) || collide({table, counts, work, {lacking, 4 * (int64_t)n_seq, true}}))
     return fail_call(FOCUS_EINVAL, "page_table, refs, lacking and the workspace must not overlap each other, nor lens any but lacking");
   fk::ReserveArgs a{};
   a.n_seq = n_seq; a.page_size = page_size; a.n_pages = n_pages; a.room = room; a.stride = table_stride; a.lens = lens; a.table = page_table; a.refs = refs;
@@ -241,8 +238,13 @@ int focus_beam_select(void *hip_stream, int32_t n_seq, int32_t n_beams, int32_t 
   if (!aligned(logits, esize(dtype)) || !aligned(scores, 4) || !aligned(rows, 4) || !aligned(tokens, 4) || !aligned(new_scores, 4) || !aligned(workspace, 256))
     return fail_call(FOCUS_EINVAL, "the workspace must be 256-byte aligned, the others to their elements");
   if (workspace_bytes < fk::beam_scratch(n_seq, n_beams, vocab, k)) return fail_call(FOCUS_ENOMEM, "the workspace is too small");
-  if (!(new_scores == scores && k == n_beams) && overlap(scores, (int64_t)n_seq * n_beams, new_scores, (int64_t)n_seq * k))       // a request's workgroup reads its own first
-    return fail_call(FOCUS_EINVAL, "new_scores may be scores where k is n_beams and must not overlap them otherwise");
+  // A request's workgroup reads its own scores and done before it writes its picks, but not before others write theirs.
+  const int64_t picks = 4 * (int64_t)n_seq * k, beams = (int64_t)n_seq * n_beams, work = (int64_t)fk::beam_scratch(n_seq, n_beams, vocab, k);
+  for (const void *out : {(const void *)rows, (const void *)tokens, (const void *)new_scores})
+    if (!(out == scores && k == n_beams) && overlap(out, picks, scores, 4 * beams))
+      return fail_call(FOCUS_EINVAL, "new_scores may be scores where k is n_beams and must not overlap them otherwise, nor may another output");
+  if (collide({{rows, picks, true}, {tokens, picks, true}, {new_scores, picks, true}, {workspace, work, true}, {done, beams, false}}) || overlap(workspace, work, scores, 4 * beams))
+    return fail_call(FOCUS_EINVAL, "outputs and the workspace must overlap neither an input nor each other");
   fk::BeamArgs a{};
   a.n_seq = n_seq; a.n_beams = n_beams; a.vocab = vocab; a.k = k; a.dtype = dtype; a.logits = logits; a.ld = ld; a.scores = scores; a.done = done; a.end_token = end_token;
   a.rows = rows; a.tokens = tokens; a.new_scores = new_scores; a.work = workspace;

@@ -250,3 +250,24 @@ def test_reserve_refuses_lists_that_are_written_over_each_other():
                 refused(reserve(**dict(d, **{x: d[y] - 4 * (words[x] - 1)})), "overlap")
     refused(reserve(**dict(d, ws=3 * P + 32)), "overlap")
     refused(reserve(**dict(d, ws=P - 48)), "overlap")
+
+
+def test_beam_select_refuses_lists_that_are_written_over_each_other():
+    """2 requests of 3 beams, 4 picks; then of 4 beams, whose scores may be written in place."""
+    n = C.c_size_t()
+    assert lib.focus_beam_select_bytes(2, 3, 100, 4, C.byref(n)) == 0 and 256 < n.value < P
+    d = dict(scores=P, done=2 * P, rows=3 * P, tokens=4 * P, new=5 * P, ws=6 * P)
+    size = dict(scores=24, done=6, rows=32, tokens=32, new=32, ws=n.value)
+    for x in ("rows", "tokens", "new", "ws"):
+        for y in size:
+            if x == y:
+                continue
+            refused(beam(**dict(d, **{x: d[y]})), "overlap")
+            if x != "ws":
+                refused(beam(**dict(d, **{x: d[y] + (size[y] - 1) // 4 * 4})), "overlap")
+                refused(beam(**dict(d, **{x: d[y] - size[x] + 4})), "overlap")
+            elif y != "ws":
+                refused(beam(**dict(d, ws=d[y] - 256)), "overlap")
+    refused(beam(**dict(d, beams=4, new=P + 32 - 4)), "overlap")
+    refused(beam(**dict(d, beams=4, new=P, tokens=P)), "overlap")
+    refused(beam(**dict(d, beams=4, rows=P, new=P)), "overlap")
