@@ -387,7 +387,7 @@ def focus_mx_experts(gate_up, down, x: torch.Tensor, experts: torch.Tensor, weig
 def _kv_of(pool: torch.Tensor) -> focus_kv:
     shape = pool.shape
     code = _DTYPES.get(pool.dtype)
-    if len(shape) != 6 or shape[2] != 2 or code is None or not pool.is_contiguous():
+    if len(shape) != 6 or shape[2] != 2 or shape[5] == 0 or code is None or not pool.is_contiguous():
         _bad("a pool is a contiguous fp32 or bf16 tensor [n_layers, n_pages, 2, H_kv, page_size, D]")
     _int32(*shape)
     return focus_kv(pool.data_ptr(), code, shape[0], shape[1], shape[4], shape[3], shape[5])

@@ -271,3 +271,11 @@ def test_beam_select_refuses_lists_that_are_written_over_each_other():
     refused(beam(**dict(d, beams=4, new=P + 32 - 4)), "overlap")
     refused(beam(**dict(d, beams=4, new=P, tokens=P)), "overlap")
     refused(beam(**dict(d, beams=4, rows=P, new=P)), "overlap")
+
+
+def test_a_pool_of_heads_of_no_width_is_refused_like_any_other():
+    """Before its width divides the columns of a query."""
+    for shape in [(1, 2, 2, 1, 16, 0), (1, 2, 1, 1, 16, 64), (1, 2, 2, 16, 64)]:
+        with pytest.raises(pk.FocusError):
+            binding._kv_of(torch.zeros(shape))
+    assert binding._kv_of(torch.zeros(1, 2, 2, 1, 16, 64)).head_dim == 64
