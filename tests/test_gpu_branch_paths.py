@@ -84,3 +84,31 @@ def test_tree_attention_of_many_sequences_whose_units_are_cut(dtype, n, hint):
         got = [pk.focus_tree_attention(*args, seen=seen.to(DEV), max_rows=max_rows, max_len=max_len, workspace=ws).cpu() for _ in range(2)]
         assert torch.equal(got[0], got[1])
         held_against(got[0], *want, D)
+
+
+# -- values that are no numbers, each kind where the 64-bit form has it --------------------------------
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("P,D,far", [(64, 128, 40), (16, 64, 40), (64, 64, 900), (16, 128, 900)])
+@pytest.mark.parametrize("room", [None, 0])
+def test_tree_attention_tells_infinities_and_nan_apart(dtype, P, D, far, room):
+    """V alone holds them: +inf, -inf and NaN in columns of their own, +inf and -inf together in one, in drafted tokens that some rows see and in a cached one; with long caches
+    and a workspace the units are cut."""
+    pk, gen = _pk(), torch.Generator().manual_seed(P + D)
+    counts, lens, Hq, H = [20, 3, 9], [far, 0, far + 33], 4, 2
+    pool, q, cu, lens, table = ragged_tree(gen, dtype, Hq, H, P, D, lens, counts)
+    inf, nan = math.inf, math.nan
+    bad = [(0, far + 2, {3: inf}), (0, far + 7, {35: -inf}), (0, far + 11, {6: nan, 63: -inf}), (0, far + 4, {20: inf}), (0, far + 13, {20: -inf}), (1, 0, {0: -inf}), (1, 2, {0: inf, 33: nan}),
+           (2, 5, {50: -inf, 51: inf, 52: nan}), (2, far + 33 + 8, {50: inf, 7: -inf})]
+    for b, t, columns in bad:
+        page, place = ref.place_of(pool, table[b], t)
+        for d, x in columns.items():
+            pool[0, page, 1].view(H, D, P)[:, d, place] = x
+    kw = {} if room is None else dict(workspace=torch.empty(0, dtype=torch.uint8, device=DEV))
+    args = [pool.to(DEV), 0, q.to(DEV), cu.to(DEV), lens.to(DEV), table.to(DEV)]
+    for kind in ("tree", "all", "none", None):
+        seen = None if kind is None else tree_masks(gen, counts, 1, kind)
+        want = ref.attention(pool, 0, q, cu, lens, table, seen, D ** -0.5)
+        got = pk.focus_tree_attention(*args, seen=None if seen is None else seen.to(DEV), max_rows=20, max_len=far + 42, **kw).cpu()
+        held_against(got, *want, D)
+        if kind in ("all", None):
+            assert all(bool(f(want[0]).any()) for f in (torch.isnan, torch.isposinf, torch.isneginf))
