@@ -112,3 +112,100 @@ def test_tree_attention_tells_infinities_and_nan_apart(dtype, P, D, far, room):
         held_against(got, *want, D)
         if kind in ("all", None):
             assert all(bool(f(want[0]).any()) for f in (torch.isnan, torch.isposinf, torch.isneginf))
+
+
+# -- compaction ----------------------------------------------------------------------------------------
+def forms(keep, start):
+    """What the batches of a sequence's moves are: 'few' (one batch), or for each 64 places 'whole' or 'single' (its tokens lie further apart than what is held of a row)."""
+    skip = start & 63
+    if skip + len(keep) <= 32:
+        return {"few"}
+    found = set()
+    for j0 in range(0, skip + len(keep), 64):
+        mine = [keep[j - skip] + (start & 7) for j in range(max(j0, skip), min(j0 + 64, skip + len(keep)))]
+        if mine:
+            found.add("single" if mine[-1] >= mine[0] // 8 * 8 + 256 else "whole")
+    return found
+
+
+def moved(pool, start, cu, keep, table, to_table):
+    """The plain form with all tokens of a layer at once."""
+    H, P, D = pool.shape[3:]
+    src, dst = [], []
+    for b in range(len(start)):
+        for i in range(int(cu[b + 1]) - int(cu[b])):
+            x, y = ref.place_of(pool, table[b], int(start[b]) + int(keep[int(cu[b]) + i])), ref.place_of(pool, to_table[b], int(start[b]) + i)
+            if x is not None and y is not None:
+                src.append(x), dst.append(y)
+    (p, a), (r, c) = (tuple(torch.tensor(v).view(-1, 2).unbind(1)) for v in (src, dst))
+    want, v = pool.clone(), pool.clone()[:, :, 1].reshape(*pool.shape[:2], H, D, P)
+    want[:, r, 0, :, c] = pool[:, p, 0, :, a]
+    v[:, r, :, :, c] = pool[:, :, 1].reshape(*pool.shape[:2], H, D, P)[:, p, :, :, a]
+    want[:, :, 1] = v.reshape(*pool.shape[:2], H, P, D)
+    return want
+
+
+def check_compact(gen, dtype, layers, H, P, D, spans, keeps, start, in_place, holes=0):
+    pk = _pk()
+    pages = [-(-(a + b) // P) for a, b in zip(spans, start)]
+    both, n_pages = ragged_table(gen, pages + pages)
+    table, to = both[:len(spans)].clone(), both[len(spans):].clone()
+    for t in (table, to):
+        for _ in range(holes):                             # an entry that is no page, one that is none of the pool's
+            t.view(-1)[torch.randint(0, t.numel(), (2,), generator=gen)] = i32([-1, n_pages])
+    pool = make_pool(gen, layers, n_pages, H, P, D, dtype)
+    cu, flat, start = starts([len(k) for k in keeps]), i32([x for k in keeps for x in k]), i32(start)
+    want = moved(pool, start, cu, flat, table, table if in_place else to)
+    got = pool.to(DEV)
+    pk.focus_kv_compact(got, start.to(DEV), cu.to(DEV), flat.to(DEV), table.to(DEV), None if in_place else to.to(DEV))
+    as_bits = torch.int16 if dtype == torch.bfloat16 else torch.int32
+    assert torch.equal(got.cpu().view(as_bits), want.view(as_bits))
+
+
+def shares(gen, span, share):
+    """Tokens that stay, of a span whose parts stay with one share after the other."""
+    n = len(share)
+    return [x for x in range(span) if float(torch.rand(1, generator=gen)) < share[x * n // span]]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("in_place", [True, False])
+def test_compact_of_many_heads(dtype, D, in_place):
+    """More than 1024 (sequence, head, layer) triples: a workgroup takes all columns of its head.  One of few tokens, dense and sparse ones, and none."""
+    gen = torch.Generator().manual_seed(D)
+    layers, H, P = 4, 8, 16
+    spans = [0, 1, 2, 3, 5, 9, 17, 33, 40, 64, 65, 130, 300, 700] + [8] * 24
+    start = [int(torch.randint(0, 70, (1,), generator=gen)) for _ in spans]
+    keeps = [shares(gen, s, [0.9, 0.3, 0.1] if s > 200 else [0.6]) for s in spans]
+    keeps[1] = [0]
+    assert len(spans) * H * layers > 1024
+    found = set().union(*(forms(k, s) for k, s in zip(keeps, start)))
+    assert found == {"few", "whole", "single"}
+    check_compact(gen, dtype, layers, H, P, D, spans, keeps, start, in_place)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("P,D,start", [(8, 64, [3, 0, 61]), (24, 128, [7, 100, 64]), (64, 64, [0, 13, 63]), (64, 128, [1, 8, 250])])
+@pytest.mark.parametrize("in_place", [True, False])
+@pytest.mark.parametrize("many", [False, True])
+def test_compact_of_dense_and_sparse_stretches(dtype, P, D, start, in_place, many):
+    """Batches whose rows of V^T are held whole and batches of single columns in turn; `many`: beside enough others that a workgroup takes all columns."""
+    gen = torch.Generator().manual_seed(P + D)
+    share = [[0.95, 0.05, 0.9, 0.12, 0.2, 0.05, 1.0, 0.05], [0.2, 0.15], [0.05, 0.99, 0.04]]
+    spans = [3000, 2501, 1999]
+    keeps = [shares(gen, a, b) for a, b in zip(spans, share)]
+    assert all("single" in forms(k, s) for k, s in zip(keeps, start)) and all("whole" in forms(keeps[b], start[b]) for b in (0, 2))
+    if many:
+        spans, keeps, start = spans + [4] * 1100, keeps + [[0, 2]] * 1100, start + [5] * 1100
+    assert (len(spans) > 1024) == many
+    check_compact(gen, dtype, 1, 1, P, D, spans, keeps, start, in_place)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_compact_of_long_stretches_leaves_out_tokens_without_a_page(dtype):
+    gen = torch.Generator().manual_seed(5)
+    spans, start = [2000, 900], [9, 64]
+    keeps = [shares(gen, 2000, [0.9, 0.1]), shares(gen, 900, [0.5])]
+    for in_place in (True, False):
+        check_compact(gen, dtype, 2, 2, 16, 64, spans, keeps, start, in_place, holes=12)
