@@ -209,3 +209,13 @@ def test_compact_of_long_stretches_leaves_out_tokens_without_a_page(dtype):
     keeps = [shares(gen, 2000, [0.9, 0.1]), shares(gen, 900, [0.5])]
     for in_place in (True, False):
         check_compact(gen, dtype, 2, 2, 16, 64, spans, keeps, start, in_place, holes=12)
+
+
+# -- reservation -----------------------------------------------------------------------------------------
+def test_reserve_writes_what_lacks_over_the_lengths():
+    pk = _pk()
+    lens, refs = i32([20, 0, 50]).to(DEV), i32([0, 1, 0, 0, 0]).to(DEV)
+    table = i32([[1, -1, -1], [-1, -1, -1], [-1, -1, -1]]).to(DEV)
+    got = pk.focus_kv_reserve(lens, 1, table, refs, 16, lacking=lens)
+    assert got is lens and lens.tolist() == [0, 0, 2] and refs.tolist() == [1] * 5       # 50 + 1 tokens want four pages: two were left, and the row has three entries
+    assert table.tolist() == [[1, 0, -1], [2, -1, -1], [3, 4, -1]]
