@@ -495,7 +495,8 @@ int focus_kv_reserve(void *hip_stream, int32_t n_seq, int32_t page_size, int32_t
 
 /* A step of beam search: of every request's n_beams * vocab candidates the k with the largest scores,
  *   score(beam, token) = scores[beam] + (logit - log(sum over the vocabulary of exp(logits)))
- * in descending order, compared in 64 bits with logarithms that are whole multiples of 2^-34 (ties: lower beam; within a beam the larger logit, then the lower token).  A finished beam has one candidate, end_token
+ * in descending order, compared in 64 bits with logarithms that are whole multiples of 2^-34 (ties: lower beam; within a beam the larger logit, then the lower token).  Beams with
+ * the same logits at the same tokens have the same logarithm; the same logits at other tokens may make neighbouring multiples.  A finished beam has one candidate, end_token
  * with the beam's score unchanged; its logits are not read.  Candidates without a finite score are not picked (logits or beams at -inf, rows with a NaN or +inf).
  *   n_seq, n_beams, k   n_beams 1..64, k 1..64, n_seq * n_beams at most 2^20;  vocab 1..2^24
  *   logits         device [n_seq * n_beams, ld], FOCUS_F32 or FOCUS_BF16;  scores  device [n_seq, n_beams] fp32

@@ -219,3 +219,43 @@ def test_reserve_writes_what_lacks_over_the_lengths():
     got = pk.focus_kv_reserve(lens, 1, table, refs, 16, lacking=lens)
     assert got is lens and lens.tolist() == [0, 0, 2] and refs.tolist() == [1] * 5       # 50 + 1 tokens want four pages: two were left, and the row has three entries
     assert table.tolist() == [[1, 0, -1], [2, -1, -1], [3, 4, -1]]
+
+
+# -- beams that tie ----------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("vocab,pad", [(70, 1), (4097, 3), (20011, 5)])
+def test_beams_of_the_same_logits_tie(dtype, vocab, pad):
+    """The lower beam comes first wherever its row begins, and the same logits are taken from every beam before the next ones."""
+    pk, gen = _pk(), torch.Generator().manual_seed(vocab)
+    n, beams, k = 50, 3, 6
+    wide = torch.zeros(n * beams, vocab + pad, dtype=dtype, device=DEV)
+    for scale in (0.5, 3.0):
+        l = (torch.randn(n, vocab, generator=gen) * scale).to(dtype)
+        l[:, 17], l[:, 40] = 19.0, 18.0                    # the best two by far
+        wide[:, :vocab] = l.repeat_interleave(beams, 0).to(DEV)
+        scores = (-torch.rand(n, 1, generator=gen) * 7).repeat(1, beams).to(DEV)
+        rows, tokens, new = pk.focus_beam_select(wide[:, :vocab], scores, k)
+        assert torch.equal(rows.cpu(), i32([0, 1, 2, 0, 1, 2]) + beams * torch.arange(n, dtype=torch.int32).view(n, 1))
+        assert tokens.tolist() == [[17] * 3 + [40] * 3] * n
+        assert torch.equal(new[:, :1].expand(n, 3), new[:, :3]) and torch.equal(new[:, 3:4].expand(n, 3), new[:, 3:])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("vocab", [300, 4096, 9001])
+def test_beams_of_the_same_logits_at_other_tokens(dtype, vocab):
+    """Their log-sums are 4e-12 apart at most, so the multiples of 2^-34 = 5.8e-11 that they round to are the same or neighbours; the chance that they are neighbours is 7 % at most."""
+    pk, gen = _pk(), torch.Generator().manual_seed(vocab)
+    n = 256
+    l = torch.randn(n, vocab, generator=gen).to(dtype)
+    l[:, 5] = 12.0
+    order = torch.stack([torch.randperm(vocab, generator=gen) for _ in range(n)])
+    logits = torch.stack([l, torch.gather(l, 1, order)], 1).view(2 * n, vocab)
+    scores = torch.full((n, 2), -1.0)
+    rows, tokens, new = (t.cpu() for t in pk.focus_beam_select(logits.to(DEV), scores.to(DEV), 2))
+    place = torch.stack([torch.full((n,), 5), (order == 5).int().argmax(1)], 1)
+    first = rows[:, 0] - 2 * torch.arange(n)
+    assert torch.equal(rows.sort(1).values, torch.arange(2 * n, dtype=torch.int32).view(n, 2))
+    assert torch.equal(tokens.long(), torch.where(first.view(n, 1) == 0, place, place.flip(1)))
+    want = -1.0 + (12.0 - torch.logsumexp(l.double(), 1, keepdim=True))
+    assert bool(((new.double() - want).abs() <= want.abs() * 2.0 ** -24 * 1.001 + 2.0 ** -34).all())
+    assert int((first == 1).sum()) <= 40                    # of 256: 18 at that chance, and five times their spread
