@@ -72,7 +72,7 @@ void kv_append(hipStream_t s, const AppendArgs &a) {
 // Compaction.  A workgroup takes one (sequence, head, layer), or a slice of its columns where those are few, and moves tokens in ascending order, 64 at a time.
 // In place that is safe: place i is read from place keep[i] >= i, so nothing that was written is read later; and every column of K (16 bytes) and every row of
 // V^T belongs to one wavefront, which loads all of a batch before it stores any of it.  So wavefronts do not wait for each other's data, only for the list of
-// where the next 256 tokens move, which is looked up while the last ones do.  Batches begin at every 64th token of what is written: a store to V^T fills a line.
+// where the next 256 tokens move: `keep` of them is asked for ahead of the last ones' moves, their pages are looked up behind them.  Batches begin at every 64th token of what is written: a store to V^T fills a line.
 // Rows of V^T that a batch's tokens come from are read in whole 16-byte pieces into LDS and picked from there, 16 bytes of neighbouring tokens a store, as long as
 // they span at most 256 tokens: single values, 64 lanes from three or four lines, took 342 us for a third of 8 x 8000 tokens (4 layers), this takes 263.
 template <int ES, int D, int SLICES>

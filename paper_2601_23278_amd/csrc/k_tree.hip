@@ -390,7 +390,8 @@ __global__ __launch_bounds__(NW * 64, NW == 1 && D == 128 ? 1 : 2) void k_tree(T
     float m = -INFINITY, l = 0.f;
 
     // One K buffer and one V buffer, each filled again as soon as the product that reads it is done.  Loads complete in order, so "at most IPW outstanding" means
-    // that the older tile is there.
+    // that the older tile is there.  Where ONE is false the page number that look_up compares is the newest load: in every tile the wavefront waits there for all before it,
+    // the next tile's K too: loads of K overlap with nothing and those of V with the first product alone.
     for (int tile = now.tile0; tile < now.tile1; ++tile) {
       const bool more = tile + 1 < now.tile1, any = more || next.tiles > 0;
       const int tile_n = more ? tile + 1 : next.tile0;
