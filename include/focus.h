@@ -445,7 +445,7 @@ int focus_kv_append(const focus_kv *kv, void *hip_stream, int32_t layer, int32_t
 
 /* Attention of drafted tokens: query row r of sequence b, with i = r - cu_rows[b], attends to the cached tokens t < lens[b] and to those drafted tokens j (token
  * lens[b] + j of the cache, j < the sequence's number of rows) whose bit is set in the row's set:  out = sum_t p_t v_t,  p = softmax(scale * q . k_t), fp32.
- * Tokens that a row does not see add nothing, whatever their K and V hold; a row that sees nothing is zero.  A single row per sequence is the step of
+ * Tokens that a row does not see add nothing, whatever their K and V hold; a row that sees nothing, or scores of -inf alone, is zero.  A single row per sequence is the step of
  * ordinary decoding, many rows with seen == NULL a part of a prompt.
  *   seen           device [n_rows, seen_words] uint64, bit j % 64 of word j / 64: drafted token j; seen_words 1..16; drafted tokens beyond its bits are unseen.
  *                  NULL: row i sees the drafted tokens j <= i

@@ -114,6 +114,30 @@ def test_tree_attention_tells_infinities_and_nan_apart(dtype, P, D, far, room):
             assert all(bool(f(want[0]).any()) for f in (torch.isnan, torch.isposinf, torch.isneginf))
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("far", [5, 900])
+def test_tree_attention_of_scores_of_minus_infinity(dtype, far):
+    """Keys of -inf under queries above zero: such tokens add nothing beside others, and a row that sees no others is zero, in drafted and in cached tokens."""
+    pk, gen = _pk(), torch.Generator().manual_seed(far)
+    counts, lens, Hq, H, P, D = [3, 2], [far, far], 4, 2, 16, 64
+    pool, q, cu, lens, table = ragged_tree(gen, dtype, Hq, H, P, D, lens, counts)
+    q = q.abs() + 0.1
+    lost = [(0, t) for t in range(1, far + 1)] + [(1, t) for t in range(far + 1)]      # of the second sequence all but the last drafted one
+    for b, t in lost:
+        page, place = ref.place_of(pool, table[b], t)
+        pool[0, page, 0, :, place] = -math.inf
+    args = [q.to(DEV), cu.to(DEV), lens.to(DEV), table.to(DEV)]
+    got = pk.focus_tree_attention(pool.to(DEV), 0, *args).cpu()
+    assert bool((got[3] == 0.0).all())
+    rows = [0, 1, 2, 4]
+    want = ref.attention(pool, 0, q, cu, lens, table, None, D ** -0.5)
+    for b, t in lost:                                      # the bound is that of the scores that count
+        page, place = ref.place_of(pool, table[b], t)
+        pool[0, page, 0, :, place] = 0.0
+    spread = ref.attention(pool, 0, q, cu, lens, table, None, D ** -0.5)[2]
+    held_against(got[rows], want[0][rows], want[1][rows], spread[rows], want[3][rows], D)
+
+
 # -- compaction ----------------------------------------------------------------------------------------
 def forms(keep, start):
     """What the batches of a sequence's moves are: 'few' (one batch), or for each 64 places 'whole' or 'single' (its tokens lie further apart than what is held of a row)."""
@@ -259,3 +283,25 @@ def test_beams_of_the_same_logits_at_other_tokens(dtype, vocab):
     want = -1.0 + (12.0 - torch.logsumexp(l.double(), 1, keepdim=True))
     assert bool(((new.double() - want).abs() <= want.abs() * 2.0 ** -24 * 1.001 + 2.0 ** -34).all())
     assert int((first == 1).sum()) <= 40                    # of 256: 18 at that chance, and five times their spread
+
+
+def test_captured_selection_of_many_picks():
+    """As many beams and picks as there may be: a launch with more shared memory than it has by itself, captured, and replayed over other logits."""
+    pk, gen = _pk(), torch.Generator().manual_seed(71)
+    n, beams, vocab, k = 2, 64, 5000, 64
+    logits, scores = torch.zeros(n * beams, vocab, device=DEV), torch.zeros(n, beams, device=DEV)
+    out = [torch.zeros(n, k, dtype=t, device=DEV) for t in (torch.int32, torch.int32, torch.float32)]
+    sets = [(torch.randn(n * beams, vocab, generator=gen).to(DEV), (-torch.rand(n, beams, generator=gen)).to(DEV)) for _ in range(4)]
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        pk.focus_beam_select(logits, scores, k, rows=out[0], tokens=out[1], new_scores=out[2], stream=side)
+    for _ in range(3):
+        for l, s in sets:
+            logits.copy_(l)
+            scores.copy_(s)
+            torch.cuda.synchronize()
+            graph.replay()
+            want = pk.focus_beam_select(l, s, k)
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(out, want))
